@@ -415,6 +415,98 @@ f3dc_status f3dc_attention(const void *q, int32_t ldq, const void *k, const void
                            void *out, int32_t nq, int32_t nk, int32_t heads, int32_t dh,
                            void *stream);
 
+/* ---------------------------------------------------------------------- */
+/* 8-bit linear layers.                                                    */
+/* ---------------------------------------------------------------------- */
+
+/* The paper runs the transformer's projections in 16 bits; these calls are
+ * library services for programs that run them in 8-bit floating point, beside
+ * f3dc_gemm and with its epilogues.  An 8-bit matrix is held as
+ *   q:      e4m3 bytes [rows, cols], row stride ld bytes, and
+ *   scales: one byte per row and block of 128 columns (the last block of a row
+ *           may be shorter), row stride lds bytes; byte b stands for the power
+ *           of two 2^(b - 127), 255 for NaN.
+ * Element (r, c) is q[r, c] * 2^(scales[r, c / 128] - 127).  Row strides are
+ * in elements everywhere.  Bytes between a row's end and the next row are
+ * neither read as values nor written.
+ * The calls are asynchronous on `stream`, allocate nothing, keep nothing
+ * between calls and may run at once on several streams and in captured graphs.
+ * Inputs and outputs must not overlap but where a call says so.  What their
+ * kernels find wrong goes into the current device's status word
+ * (f3dc_gemm_status).  Failures are described by f3dc_last_error(NULL). */
+
+#define F3DC_TYPE_BF16 0
+#define F3DC_TYPE_F32 1
+
+/* Quantises x [rows, cols] (F3DC_TYPE_*): for each block the smallest power of
+ * two 2^e, -127 <= e, with max |x| <= 448 2^e over the block's finite elements;
+ * q = x 2^-e rounded to nearest even.  A NaN or an infinity becomes NaN (e4m3 has
+ * no infinity) and leaves the block's other elements as they are without it.
+ *   x: device [rows, cols], row stride ldx; q: device bytes, row stride ldq;
+ *   scales: device bytes, row stride lds >= ceil(cols / 128).
+ *   Any rows >= 0, cols >= 1, strides and element-aligned pointers; rows that
+ *   start 16 bytes aligned are faster. */
+f3dc_status f3dc_quantize_fp8(const void *x, int32_t x_type, int64_t ldx, void *q, int64_t ldq, void *scales,
+                              int64_t lds, int32_t rows, int32_t cols, void *stream);
+
+/* out[m, n] = epi(sum_k A[m, k] B[n, k]) for 8-bit A [M, K] and B [N, K] (the
+ * values they stand for), with f3dc_gemm's epilogues:
+ *   F3DC_EPI_BIAS, F3DC_EPI_GELU: out bf16 [M, N], or with out_scales given an
+ *     8-bit matrix, quantised as f3dc_quantize_fp8 does (N % 16 == 0);
+ *   F3DC_EPI_RESID: out fp32 [M, N] += gate * (acc + bias), gate nullable (1).
+ * The sum runs in fp32 on the tensor cores, which apply the scales; a NaN scale
+ * makes its products NaN.  A scale product or a sum outside fp32's range
+ * overflows or vanishes as fp32 does.
+ *   A, B: device bytes, 16-byte aligned, lda and ldb multiples of 16;
+ *   a_scales, b_scales: device bytes, 4-byte aligned, ldas and ldbs multiples of
+ *     4 (all ldas bytes of a row are read);
+ *   bias: device bf16 [N], nullable; gate: device fp32 [N], nullable;
+ *   out: 16-byte aligned, row stride ldo elements, a multiple of 16 bytes;
+ *   out_scales: device bytes, row stride ldos, nullable.
+ *   Any M >= 0, N a positive multiple of 8, any K >= 1. */
+f3dc_status f3dc_gemm_fp8(const void *A, int64_t lda, const void *a_scales, int64_t ldas, const void *B, int64_t ldb,
+                          const void *b_scales, int64_t ldbs, const void *bias, const float *gate, void *out,
+                          int64_t ldo, void *out_scales, int64_t ldos, int32_t M, int32_t N, int32_t K,
+                          int32_t epilogue, void *stream);
+
+#define F3DC_NORM_NONE 0
+#define F3DC_NORM_LAYER 1 /* (v - mean) / sqrt(var + eps) */
+#define F3DC_NORM_RMS 2   /* v / sqrt(mean(v^2) + eps) */
+#define F3DC_NORM_MAX_WIDTH 8192
+
+/* The constant part of a norm-residual call. */
+typedef struct f3dc_norm_layer {
+    int32_t width;          /* W: a multiple of 8, at most F3DC_NORM_MAX_WIDTH */
+    int32_t post, pre;      /* F3DC_NORM_* of the block's output / of the sum */
+    float eps;
+    float res_scale;        /* residual scale alpha */
+    const void *post_g, *post_b, *pre_g, *pre_b; /* device bf16 [W], nullable (1 and 0) */
+} f3dc_norm_layer;
+
+/* Between two blocks, in one pass over the rows: the norm of block output y, its
+ * gate, the scaled residual sum, and the norm and modulation of the next block's
+ * input (Supp. Sec. F's adaLN block with post NONE and pre LAYER; with a post norm
+ * the block of a sandwich-normalised transformer).  With g = group_of_row[r]:
+ *   n = post(y_r) post_g + post_b
+ *   x'_r = alpha x_r + gate_g n          (n without a gate; alpha x_r without y)
+ *   h_r = (pre(x'_r) pre_g + pre_b) (1 + scale_g) + shift_g
+ * in fp32; x' is stored in fp32, h in bf16 or, with h_scales given, in 8 bits
+ * (quantised as f3dc_quantize_fp8 does).
+ *   x: device fp32 [rows, W]; x_out: device fp32, may be x itself, nullable;
+ *   y: device bf16 [rows, W], nullable;
+ *   gate, scale, shift: device fp32 [groups, W], row stride ldmod, each nullable;
+ *   group_of_row: device int32 [rows], nullable (all rows of group 0).  Rows of a
+ *     negative group (pad rows of a packed batch) are left as they are; a group
+ *     >= groups leaves its row too and records F3DC_DEV_BAD_INDEX;
+ *   h: device bf16 or bytes, nullable if x_out is given; h_scales: device bytes,
+ *     row stride ldhs, nullable.
+ *   Pointers 16-byte aligned, ldx, ldxo and ldmod multiples of 4, ldy and ldh of
+ *   8.  Any rows >= 0. */
+f3dc_status f3dc_norm_residual(const f3dc_norm_layer *layer, const float *x, int64_t ldx, float *x_out, int64_t ldxo,
+                               const void *y, int64_t ldy, const float *gate, const float *scale, const float *shift,
+                               int64_t ldmod, const int32_t *group_of_row, int32_t groups, void *h, int64_t ldh,
+                               void *h_scales, int64_t ldhs, int32_t rows, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -344,4 +344,66 @@ uint32_t *gemm_status_word();
 bool make_tmap_bf16(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint64_t ld,
                     uint32_t box_rows, uint32_t box_cols);
 
+// 2-D tensor map over a row-major [rows, cols] matrix of any type, rows `row_bytes`
+// (a multiple of 16) apart, zero fill outside.  Returns false on failure.
+bool make_tmap_2d(CUtensorMap *map, CUtensorMapDataType type, const void *base, uint64_t rows, uint64_t cols,
+                  uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols, CUtensorMapSwizzle swizzle);
+
+// ------------------------------------------------------------ 8-bit linear layers
+constexpr int kScaleBlock = 128;  // elements of a row that share an E8M0 scale
+
+// q [rows, cols] e4m3 and scales [rows, ceil(cols / 128)] of x (bf16, or fp32 with f32)
+struct QuantArgs {
+    const void *x;
+    int64_t ldx;
+    uint8_t *q;
+    int64_t ldq;
+    uint8_t *scales;
+    int64_t lds;
+    int rows, cols;
+};
+cudaError_t launch_quantize(const QuantArgs &a, bool f32, int num_sms, cudaStream_t s);
+
+// out = epi(sum_k A B^T) of e4m3 operands with block scales
+struct Gemm8Params {
+    int M, N, K;
+    const uint8_t *sa, *sb;   // scale bytes [M, lda_s], [N, ldb_s]
+    int64_t lda_s, ldb_s;
+    const bf16 *bias;         // nullable
+    const float *gate;        // nullable (RESID)
+    uint8_t *out_scales;      // 8-bit output
+    int64_t ldo_s;
+    uint32_t *err;
+};
+// ta: A in boxes of 128 rows x 128 bytes; tb: B in boxes of 128, 64 and 32 rows; to: the
+// output in boxes of 128 rows x 64 bytes (64B swizzle), 128 bytes for 8-bit output
+// (128B swizzle).  epi as launch_gemm's.
+cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
+                              int epi, bool out8, cudaStream_t s);
+
+// norm of y, gate, residual, norm of the sum and modulation (f3dc_norm_residual)
+enum NormKind { kNormNone = 0, kNormLayer = 1, kNormRms = 2 };
+struct NormArgs {
+    int rows, width;
+    const float *x;
+    int64_t ldx;
+    float *x_out;                       // nullable
+    int64_t ldxo;
+    const bf16 *y;                      // nullable
+    int64_t ldy;
+    int post, pre;                      // NormKind
+    const bf16 *post_g, *post_b, *pre_g, *pre_b;  // nullable
+    const float *gate, *scale, *shift;  // nullable, [groups, ldmod]
+    int64_t ldmod;
+    const int32_t *group;               // nullable: every row is of group 0
+    int groups;
+    void *h;                            // nullable
+    int64_t ldh;
+    uint8_t *h_scales;                  // e4m3 output where given
+    int64_t ldhs;
+    float res_scale, eps;
+    uint32_t *err;
+};
+cudaError_t launch_norm_residual(const NormArgs &a, int num_sms, cudaStream_t s);
+
 }  // namespace f3dc

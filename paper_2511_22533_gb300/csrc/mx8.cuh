@@ -1,0 +1,121 @@
+// mx8.cuh -- device helpers of the 8-bit linear layers: tcgen05 MMAs with block
+// scales (kind::mxf8f6f4), the copy of scales into tensor memory, and conversion to
+// e4m3 under one power-of-two (E8M0) scale per block of 128 elements.
+#pragma once
+
+#include "common.cuh"
+
+namespace f3dc {
+
+// TMA load of a 2-D box into this CTA's shared memory whose completion is counted
+// on an mbarrier of either CTA of the pair (shared::cluster address)
+F3DC_DEV void tma_load_2d_pair(void *smem_dst, const CUtensorMap *map, int x, int y, uint32_t bar_cluster)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(smem_dst)),
+        "l"((uint64_t)map), "r"(x), "r"(y), "r"(bar_cluster)
+        : "memory");
+}
+
+// D (+)= A B^T over a CTA pair (mma_bf16_pair_128k says which rows lie where), e4m3
+// operands with one E8M0 scale per row and 128 K: the four MMAs of 128 K (32 K
+// further is 2 descriptor units).  The scales lie in tensor memory
+// (tmem_cp_scales_pair); each MMA takes the byte of a scale column that idesc names,
+// for all of its 32 K.
+F3DC_DEV void mma_mxf8_pair_128k(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t sfa_tmem,
+                                 uint32_t sfb_tmem, uint32_t idesc, uint32_t accumulate)
+{
+#define F3DC_MXF8 "@e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], "
+    asm volatile(
+        "{\n .reg .pred p, e, t;\n .reg .b64 a, b;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %6, 0;\n setp.eq.b32 t, 0, 0;\n"
+        " " F3DC_MXF8 "%1, %2, %5, [%3], [%4], p;\n"
+        " add.s64 a, %1, 2;\n add.s64 b, %2, 2;\n " F3DC_MXF8 "a, b, %5, [%3], [%4], t;\n"
+        " add.s64 a, a, 2;\n add.s64 b, b, 2;\n " F3DC_MXF8 "a, b, %5, [%3], [%4], t;\n"
+        " add.s64 a, a, 2;\n add.s64 b, b, 2;\n " F3DC_MXF8 "a, b, %5, [%3], [%4], t;\n"
+        "}\n" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(idesc), "r"(accumulate)
+        : "memory");
+#undef F3DC_MXF8
+}
+
+// Copies 32 rows of 16 bytes (512 consecutive bytes of shared memory, row r at 16 r)
+// of each CTA of the pair into 4 columns of its own tensor memory, the same 32 lanes
+// four times: the scale bytes of 128 matrix rows, of which row i is lane i % 32,
+// column i / 32.  Runs in issue order with the MMAs of the same thread.
+F3DC_DEV void tmem_cp_scales_pair(uint32_t taddr, uint64_t sdesc)
+{
+    asm volatile(
+        "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n"
+        " @e tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n}\n" ::"r"(taddr),
+        "l"(sdesc)
+        : "memory");
+}
+
+// Instruction descriptor, kind::mxf8f6f4 with block scales: e4m3 A and B (bits 7-9,
+// 10-12 = 0), both K-major, N >> 3 in bits 17-22, E8M0 scales (bit 23 = 1), M >> 4 in
+// bits 24-28; the byte of the scale columns to take, for B in bits 4-5, for A in 29-30.
+__host__ __device__ constexpr uint32_t make_idesc_mxf8(int M, int N, int scale_byte)
+{
+    return ((uint32_t)scale_byte << 4) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 4) << 24) |
+           ((uint32_t)scale_byte << 29);
+}
+
+// ---- e4m3 with one E8M0 (power-of-two) scale per block of 128.
+// Scale byte of a block whose largest finite magnitude is `top`: the smallest e with
+// top <= 448 2^e = 1.75 2^(8 + e), as e + 127, read off top's exponent and mantissa.
+// A normal top gives 0 <= byte <= 247; smaller ones clamp to 2^-127.
+F3DC_DEV uint32_t e8m0_byte(float top)
+{
+    const uint32_t u = __float_as_uint(top);
+    const int b = (int)(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return (uint32_t)max(b, 0);
+}
+// 2^-e of such a byte (at most 247): multiplying by it is exact but for results
+// below fp32's range, which e4m3 cannot hold either
+F3DC_DEV float e8m0_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// four floats (at most 448 in magnitude, or NaN) to e4m3, round to nearest even, `a` in the lowest byte
+F3DC_DEV uint32_t pack_e4m3x4(float a, float b, float c, float d)
+{
+    uint32_t r;
+    asm("{\n .reg .b16 lo, hi;\n cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n"
+        " mov.b32 %0, {lo, hi};\n}\n"
+        : "=r"(r)
+        : "f"(a), "f"(b), "f"(c), "f"(d));
+    return r;
+}
+
+// Quantises N consecutive values of a row, the share of this lane in a block that
+// `LANES` neighbouring lanes hold together: v becomes the quotients (at most 448 in
+// magnitude; NaN for NaN and for infinities, which e4m3 does not have), the scale
+// byte is returned.  Every lane of the warp calls it; absent values are zeros.
+// fmaxf passes over NaN, so the plain maximum is infinite only with an infinity among
+// the values: the rare block that has one takes the maximum of the finite ones.
+template <int N, int LANES>
+F3DC_DEV uint32_t quantize_block(float (&v)[N])
+{
+    const float inf = __int_as_float(0x7F800000);
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[j]));
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (__any_sync(0xffffffffu, top == inf)) {
+        top = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (fabsf(v[j]) == inf) v[j] = __int_as_float(0x7FC00000);
+            top = fmaxf(top, fabsf(v[j]));
+        }
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    }
+    const uint32_t byte = e8m0_byte(top);
+    const float inv = e8m0_inverse(byte);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] *= inv;
+    return byte;
+}
+
+}  // namespace f3dc

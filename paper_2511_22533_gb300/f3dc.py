@@ -21,6 +21,7 @@ STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "CUDA", 3: "OOM", 4: "UNSUPPORTED"
                 6: "NONFINITE", 7: "DEVICE"}
 REFRESH_PERIOD, REFRESH_LITERAL = 0, 1
 EPI_BIAS, EPI_GELU, EPI_RESID = 0, 1, 2
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
 HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "f3dc.h")
 
 
@@ -55,8 +56,22 @@ class FaultInjection(C.Structure):
                 ("attn_missing_kv", C.c_int32)]
 
 
+class NormLayer(C.Structure):
+    """The constant part of a norm_residual call; keeps its tensors (bf16
+    [width], or None) alive."""
+    _fields_ = [("width", C.c_int32), ("post", C.c_int32), ("pre", C.c_int32), ("eps", C.c_float),
+                ("res_scale", C.c_float), ("post_g", C.c_void_p), ("post_b", C.c_void_p), ("pre_g", C.c_void_p),
+                ("pre_b", C.c_void_p)]
+
+    def __init__(self, width, post=NORM_NONE, pre=NORM_LAYER, post_g=None, post_b=None, pre_g=None, pre_b=None,
+                 eps=1e-6, res_scale=1.0):
+        super().__init__(width, post, pre, eps, res_scale, _ptr(post_g), _ptr(post_b), _ptr(pre_g), _ptr(pre_b))
+        self._tensors = (post_g, post_b, pre_g, pre_b)
+
+
 _lock = threading.Lock()
 _lib = None
+_i64 = C.c_int64
 _vp, _i32p, _f32p, _f64p, _u32p = C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_float), C.POINTER(
     C.c_double), C.POINTER(C.c_uint32)
 
@@ -105,6 +120,10 @@ def lib():
                 "f3dc_set_fault_injection": ([C.POINTER(FaultInjection)], C.c_int),
                 "f3dc_attention": ([_vp, C.c_int32, _vp, _vp, C.c_int32, _vp, C.c_int32, C.c_int32, C.c_int32,
                                     C.c_int32, _vp], C.c_int),
+                "f3dc_quantize_fp8": ([_vp, C.c_int32, _i64, _vp, _i64, _vp, _i64, C.c_int32, C.c_int32, _vp], C.c_int),
+                "f3dc_gemm_fp8": ([_vp, _i64] * 4 + [_vp, _vp] + [_vp, _i64] * 2 + [C.c_int32] * 4 + [_vp], C.c_int),
+                "f3dc_norm_residual": ([C.POINTER(NormLayer), _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp,
+                                        C.c_int32, _vp, _i64, _vp, _i64, C.c_int32, _vp], C.c_int),
             }
             for name, (args, res) in sig.items():
                 fn = getattr(L, name)
@@ -321,3 +340,61 @@ def gemm_status() -> int:
 def attention(q, ldq, k, v, ldkv, out, nq, nk, heads, dh, stream=None):
     _check(lib().f3dc_attention(_ptr(q), ldq, _ptr(k), _ptr(v), ldkv, _ptr(out), nq, nk, heads, dh,
                                 _stream(stream)))
+
+
+# ---------------------------------------------------------------- 8-bit linear layers
+
+_get_device = None
+_quantize_types = None
+
+
+def _device_checks():
+    """(current device's getter, {dtype: F3DC_TYPE_*}), without importing torch before it is needed."""
+    global _get_device, _quantize_types
+    import torch
+    torch.cuda.init()
+    _quantize_types = {torch.bfloat16: 0, torch.int16: 0, torch.uint16: 0, torch.float32: 1}
+    _get_device = torch._C._cuda_getDevice
+    return _get_device
+
+
+def _ptrs(*tensors):
+    """Pointers of tensors that must lie on the current device (None: null)."""
+    dev = (_get_device or _device_checks())()
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+        elif t.get_device() != dev:
+            raise F3dcError(1, f"a tensor on {t.device}, the current device is cuda:{dev}")
+        else:
+            out.append(t.data_ptr())
+    return out
+
+
+def quantize_fp8(x, ldx, q, ldq, scales, lds, rows, cols, stream=None):
+    """x [rows, cols] (bf16 or fp32; 16-bit integers are bf16 bits) -> e4m3
+    bytes q and one power-of-two scale byte per row and block of 128 columns."""
+    px, pq, ps = _ptrs(x, q, scales)
+    x_type = _quantize_types.get(x.dtype) if x is not None else 0
+    if x_type is None:
+        raise F3dcError(1, f"x is {x.dtype}: need bf16 or fp32")
+    _check(lib().f3dc_quantize_fp8(px, x_type, ldx, pq, ldq, ps, lds, rows, cols, _stream(stream)))
+
+
+def gemm_fp8(A, lda, a_scales, ldas, Bw, ldb, b_scales, ldbs, bias, gate, out, ldo, out_scales, ldos, M, N, K, epilogue,
+             stream=None):
+    """Matrix product of two 8-bit matrices with f3dc_gemm's epilogues; with
+    out_scales the output is an 8-bit matrix too."""
+    pa, psa, pb, psb, pbias, pgate, po, pos = _ptrs(A, a_scales, Bw, b_scales, bias, gate, out, out_scales)
+    _check(lib().f3dc_gemm_fp8(pa, lda, psa, ldas, pb, ldb, psb, ldbs, pbias, pgate, po, ldo, pos, ldos, M, N, K, epilogue,
+                               _stream(stream)))
+
+
+def norm_residual(layer, x, ldx, x_out, ldxo, y, ldy, gate, scale, shift, ldmod, group_of_row, groups, h, ldh, h_scales,
+                  ldhs, rows, stream=None):
+    """x_out = alpha x + gate post(y), h = pre(x_out) (1 + scale) + shift in one
+    pass (`layer`: a NormLayer); with h_scales h is an 8-bit matrix."""
+    px, pxo, py, pg, psc, psh, pgr, ph, phs = _ptrs(x, x_out, y, gate, scale, shift, group_of_row, h, h_scales)
+    _check(lib().f3dc_norm_residual(C.byref(layer), px, ldx, pxo, ldxo, py, ldy, pg, psc, psh, ldmod, pgr, groups, ph, ldh,
+                                    phs, ldhs, rows, _stream(stream)))

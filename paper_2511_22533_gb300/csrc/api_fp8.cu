@@ -88,6 +88,8 @@ extern "C" f3dc_status f3dc_gemm_fp8(const void *A, int64_t lda, const void *a_s
     p.sb = (const uint8_t *)b_scales;
     p.lda_s = ldas;
     p.ldb_s = ldbs;
+    const uintptr_t align = (uintptr_t)a_scales | (uintptr_t)b_scales | (uintptr_t)ldas | (uintptr_t)ldbs;
+    p.scale_sets = align % 16 == 0 ? 4 : (align % 8 == 0 ? 2 : 1);
     p.bias = (const bf16 *)bias;
     p.gate = gate;
     p.out_scales = (uint8_t *)out_scales;
@@ -98,14 +100,10 @@ extern "C" f3dc_status f3dc_gemm_fp8(const void *A, int64_t lda, const void *a_s
     CUtensorMap ta, to;
     GemmPairB tb;
     const auto u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8;
-    bool ok = make_tmap_2d(&ta, u8, A, M, K, lda, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B);
-    for (int i = 0; i < 3; ++i)
-        ok = ok && make_tmap_2d(&tb.rows[i], u8, B, N, K, ldb, 128 >> i, 128, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (out8)
-        ok = ok && make_tmap_2d(&to, u8, out, M, N, ldo, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B);
-    else
-        ok = ok && make_tmap_2d(&to, esz == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, out, M,
-                                N, ldo * esz, 128, 64 / esz, CU_TENSOR_MAP_SWIZZLE_64B);
+    bool ok = make_tmap_rows(&ta, u8, A, M, K, lda, 128, 128);
+    for (int i = 0; i < 3; ++i) ok = ok && make_tmap_rows(&tb.rows[i], u8, B, N, K, ldb, 128 >> i, 128);
+    ok = ok && make_tmap_rows(&to, out8 ? u8 : (esz == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16),
+                              out, M, N, ldo * esz, 32, 128 / esz);
     if (!ok) return bad("cuTensorMapEncodeTiled rejected A, B or out");
     const int epi = epilogue == F3DC_EPI_BIAS ? kEpiBias : (epilogue == F3DC_EPI_GELU ? kEpiGelu : kEpiResid);
     const cudaError_t e = launch_gemm8_pair(&ta, &tb, &to, p, epi, out8, (cudaStream_t)stream);

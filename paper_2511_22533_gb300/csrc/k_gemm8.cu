@@ -12,12 +12,13 @@
 // Clusters of two CTAs (cta_group::2), persistent over tiles of 256 x 256 (narrower
 // ones in the last wave), 384 threads:
 //   warp 0      TMA producer: this CTA's 128 rows of A and half of the tile's rows of
-//               B, 128 K (one 128-byte swizzled line per row) per stage
+//               B, 128 K (a scale block, one 128-byte swizzled line per row) per stage
 //   warp 1      of the even CTA issues the copies of scales and the MMAs for both
 //   warp 2      reads scale bytes from global memory (plain rows) and lays them out
 //               for the tensor memory: 512 K of A's 128 and B's 256 rows at a time
 //   warp 3      allocates tensor memory
-//   warps 4-11  epilogue, two groups of four (one warp per TMEM lane quarter)
+//   warps 4-11  epilogue: each has 32 rows (its TMEM lanes) and half of the columns, stages
+//               its output and sends it by TMA; no warp waits for another
 // Tensor memory: 512 columns hold two accumulators of 256 only if nothing else is
 // there, but two sets of scales need 24.  So the second accumulator starts at column
 // 232: the tile after may begin as soon as the epilogue has read the 24 columns that
@@ -34,31 +35,51 @@ namespace f3dc {
 namespace {
 
 constexpr int kThreads8 = 384;
-constexpr int kBK8 = 128;                   // K of a stage: one scale block
+constexpr int kOperand8 = 128 * 128;        // a stage's 128 K of A, or of up to 128 rows of B, per CTA
 constexpr int kStages8 = 5;
-constexpr int kOperand8 = 128 * kBK8;       // 128 rows of A, or up to 128 of B, per CTA
-constexpr int kStageScales = 512 + 1024;    // A's 128 rows, B's 256, four scale bytes each
-constexpr int kOutBuf8 = 128 * 64;          // staged output: 128 rows of 64 bytes
-constexpr int kOutBytes8 = 2 * 2 * kOutBuf8;
+constexpr int kSetBytes = 512 + 1024;       // scales of A's 128 rows, B's 256, four bytes each (512 K)
+constexpr int kSets = 4;                    // such sets in shared memory
+constexpr int kVecBytes8 = 8 * 2 * 128 * 4; // an epilogue warp's biases and gates of a unit
+constexpr int kOutBytes8 = 8 * 32 * 128;    // an epilogue warp's 32 rows of 128 bytes on their way out
 constexpr uint32_t kTmemCols8 = 512;
 constexpr uint32_t kAcc1 = 232;             // first column of the second accumulator
 constexpr uint32_t kScaleCols = 488;        // two sets of 4 (A) + 8 (B) columns
-constexpr size_t kSmem8 = 1024 + (size_t)kStages8 * 2 * kOperand8 + kOutBytes8 + 2 * kStageScales + 256;
+constexpr size_t kSmem8 = 1024 + (size_t)kStages8 * 2 * kOperand8 + kSets * kSetBytes + kVecBytes8 + kOutBytes8 + 256;
+
+// n / d and n % d for n < 2^31 (d >= 1) by a multiplication (the round-up method).
+struct FastDiv {
+    uint32_t d, mul, shift;
+    void set(uint32_t v)
+    {
+        d = v;
+        shift = 0;
+        while ((1ull << shift) < v) ++shift;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - v)) / v + 1);
+    }
+    F3DC_DEV int div(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+};
 
 // Work units: full waves of 256 x 256 tiles, the tiles left for the last wave cut into
-// 2 or 4 pieces of 128 or 64 columns where there are clusters for all of them.  Units run
-// column-fastest.  A tile's columns behind N are not computed but for the rounding up
-// of its width to 64, 128 or 256.
+// 2 or 4 pieces of 128 or 64 columns where there are clusters for all of them.  Tiles
+// run in bands of kBand row pairs, row-fastest within a band's columns, so that what
+// the clusters work on at a time is about as many rows of A as of B.  A tile's columns
+// behind N are not computed but for the rounding up of its width to 64, 128 or 256.
+constexpr int kBand = 8;
 struct Units8 {
-    int line, full, sub, total, N, min_width;
-    F3DC_DEV Units8(int M, int N_, int clusters, int min_width_) : N(N_), min_width(min_width_)
+    int full, sub, total, N, min_width, last_band;
+    FastDiv band, last_high;  // tiles of a band, rows of the last band
+    void set(int M, int N_, int clusters, int min_width_)
     {
-        line = (N + 255) / 256;
-        const int tiles = ((M + 255) / 256) * line;
+        N = N_;
+        min_width = min_width_;
+        const int pairs = (M + 255) / 256, line = (N + 255) / 256, tiles = pairs * line;
         full = tiles / clusters * clusters;
         const int rest = tiles - full;
         sub = 4 * rest <= clusters && min_width <= 64 ? 4 : (2 * rest <= clusters ? 2 : 1);
         total = full + rest * sub;
+        band.set((uint32_t)kBand * line);
+        last_band = (pairs - 1) / kBand;
+        last_high.set(pairs - last_band * kBand);
     }
     // unit u: first row m0 of the pair, first column n0, width bn (0: nothing to do)
     F3DC_DEV void decode(int u, int &m0, int &n0, int &bn) const
@@ -71,11 +92,23 @@ struct Units8 {
             piece = v & (sub - 1);
             bn = 256 >> log_sub;
         }
-        const int m = tile / line;
-        m0 = m * 256;
-        n0 = (tile - m * line) * 256 + piece * bn;
+        const int b = band.div(tile), in = tile - b * (int)band.d;
+        const int high = b == last_band ? (int)last_high.d : kBand;
+        const int col = b == last_band ? last_high.div(in) : in / kBand;
+        m0 = (b * kBand + in - col * high) * 256;
+        n0 = col * 256 + piece * bn;
         const int left = N - n0;
         bn = left <= 0 ? 0 : min(bn, left <= min_width ? min_width : (left <= 128 ? 128 : 256));
+    }
+    // the unit after u of a cluster, ncl clusters in all; false: none
+    F3DC_DEV bool next(int &u, int ncl, int &m0, int &n0, int &bn) const
+    {
+        do {
+            u += ncl;
+            if (u >= total) return false;
+            decode(u, m0, n0, bn);
+        } while (bn == 0);
+        return true;
     }
 };
 
@@ -87,80 +120,102 @@ F3DC_DEV bool wait_ns8(uint64_t *bar, uint32_t parity, uint64_t ns)
     return true;
 }
 
-// Staged output of a group of four epilogue warps: boxes of 128 rows x 64 bytes, the
-// 16-byte piece c of row r at 64 r + 16 (c ^ ((r / 2) % 4)) (TMA 64B swizzle), in two
-// buffers; the issuer sends a box when all four warps have written it and waits
-// before the next is written until the store of the one before has been read.
+// 0.5 x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) of two values.  tanh.approx is within
+// 2^-11 of the value, half a step of the bf16 output where it counts most.
+F3DC_DEV f32x2 gelu2(f32x2 x)
+{
+    const float k0 = 0.7978845608028654f, k1 = 0.7978845608028654f * 0.044715f;
+    const f32x2 w = ffma2(fmul2(x, x), {k1, k1}, {k0, k0});
+    const f32x2 z = fmul2(x, w), h = fmul2(x, {0.5f, 0.5f});
+    return ffma2(h, {tanh_fast(z.x), tanh_fast(z.y)}, h);
+}
+
+// Waits for this thread's TMEM loads; r's values count from here on.
+F3DC_DEV void wait_chunk(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+                   "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                   "+r"(r[30]), "+r"(r[31])::"memory");
+}
+
+// acc + bias and the epilogue's function of 32 columns, in place (fp32 bits); biases
+// and gates from shared memory.
+template <int EPI>
+F3DC_DEV void apply(uint32_t (&r)[32], const float *bias, const float *gate)
+{
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+        const float4 b = *reinterpret_cast<const float4 *>(bias + j);
+        f32x2 x0 = fadd2({__uint_as_float(r[j]), __uint_as_float(r[j + 1])}, {b.x, b.y});
+        f32x2 x1 = fadd2({__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])}, {b.z, b.w});
+        if constexpr (EPI == kEpiGelu) {
+            x0 = gelu2(x0);
+            x1 = gelu2(x1);
+        }
+        if constexpr (EPI == kEpiResid) {
+            const float4 g = *reinterpret_cast<const float4 *>(gate + j);
+            x0 = fmul2(x0, {g.x, g.y});
+            x1 = fmul2(x1, {g.z, g.w});
+        }
+        r[j] = __float_as_uint(x0.x), r[j + 1] = __float_as_uint(x0.y);
+        r[j + 2] = __float_as_uint(x1.x), r[j + 3] = __float_as_uint(x1.y);
+    }
+}
+
+// Staged output of an epilogue warp: a box of its 32 rows x 128 bytes, the 16-byte piece c
+// of row r at 128 r + 16 (c ^ (r % 8)) (TMA 128B swizzle).  Lane 0 issues the stores and
+// waits before the box is written again until the last one has been read.  (Stores from
+// registers, or turned through shared memory into whole sectors, took 132 and 129 us
+// instead of 115 at 32768 x 4096 x 1024; a second box made no difference.)
 struct Stage8 {
     uint8_t *buf;
     const CUtensorMap *map;
-    int row, bar;
-    bool issuer;
-    int ck;
+    int row, lane;
+    F3DC_DEV void begin() const
+    {
+        if (lane == 0) bulk_wait_read<0>();
+        __syncwarp();
+    }
     F3DC_DEV void put16(int c, uint4 u) const
     {
-        *reinterpret_cast<uint4 *>(buf + (ck & 1) * kOutBuf8 + row * 64 + ((c ^ ((row >> 1) & 3)) << 4)) = u;
+        *reinterpret_cast<uint4 *>(buf + lane * 128 + ((c ^ (lane & 7)) << 4)) = u;
     }
     template <bool kReduce>
-    F3DC_DEV void emit(int x, int y)
+    F3DC_DEV void send(int x) const
     {
         fence_proxy_async_smem();
-        if (issuer) bulk_wait_read<0>();
-        asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory");
-        if (issuer) {
+        __syncwarp();
+        if (lane == 0) {
             if (kReduce)
-                tma_reduce_add_2d(map, buf + (ck & 1) * kOutBuf8, x, y);
+                tma_reduce_add_2d(map, buf, x, row);
             else
-                tma_store_2d(map, buf + (ck & 1) * kOutBuf8, x, y);
+                tma_store_2d(map, buf, x, row);
             bulk_commit();
         }
-        ++ck;
     }
 };
-
-// Adds the biases of 32 columns to v (N is a multiple of 8; columns from N on get none).
-F3DC_DEV void add_bias(const Gemm8Params &p, int col, float (&v)[32])
-{
-    if (!p.bias) return;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (col + 8 * q >= p.N) break;
-        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p.bias + col) + q);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[8 * q + 2 * j] += bf16_bits_to_f32(w[j] & 0xFFFFu);
-            v[8 * q + 2 * j + 1] += __uint_as_float(w[j] & 0xFFFF0000u);
-        }
-    }
-}
-
-F3DC_DEV void load_acc(uint32_t taddr, float (&v)[32])
-{
-    uint32_t r[32];
-    tmem_ld32(taddr, r);
-    tmem_wait_ld();
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
-}
 
 template <int EPI, bool OUT8>
 __global__ void __launch_bounds__(kThreads8, 1)
     k_gemm8_pair(const __grid_constant__ CUtensorMap tma, const __grid_constant__ GemmPairB tmb,
-                 const __grid_constant__ CUtensorMap tmo, const Gemm8Params p)
+                 const __grid_constant__ CUtensorMap tmo, const Units8 U, const Gemm8Params p)
 {
     constexpr int S = kStages8;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *sa = smem;
     uint8_t *sb = sa + S * kOperand8;
-    uint8_t *so = sb + S * kOperand8;
-    uint8_t *ss = so + kOutBytes8;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(ss + 2 * kStageScales);
-    uint64_t *full = bars, *empty = full + S;          // operands of a stage there (even CTA) / used (both)
-    uint64_t *sfull = empty + S, *sempty = sfull + 2;  // scales of a set there (even CTA) / used (both)
-    uint64_t *accf = sempty + 2, *acce = accf + 2;     // accumulator complete (both) / read (even CTA)
-    uint64_t *shared_read = acce + 2;                  // its columns that the next one needs are read (even CTA)
+    uint8_t *ss = sb + S * kOperand8;
+    float *sv = reinterpret_cast<float *>(ss + kSets * kSetBytes);
+    uint8_t *so = ss + kSets * kSetBytes + kVecBytes8;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(so + kOutBytes8);
+    uint64_t *full = bars, *empty = full + S;              // operands of a stage there (even CTA) / used (both)
+    uint64_t *sfull = empty + S, *sempty = sfull + kSets;  // scales of a set there (even CTA) / copied (both)
+    uint64_t *accf = sempty + kSets, *acce = accf + 2;     // accumulator complete (both) / read (even CTA)
+    uint64_t *shared_read = acce + 2;                      // its columns that the next one needs are read (even CTA)
     uint64_t *drain = shared_read + 1;
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(drain + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
@@ -179,13 +234,15 @@ __global__ void __launch_bounds__(kThreads8, 1)
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kSets; ++b) {
             mbar_init(&sfull[b], 2);   // one scale warp in each CTA
             mbar_init(&sempty[b], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
             mbar_init(&accf[b], 1);
             mbar_init(&acce[b], 16);   // eight epilogue warps in each CTA
         }
-        mbar_init(shared_read, 8);     // the group of four that holds the columns, in each CTA
+        mbar_init(shared_read, 8);     // the four warps that hold the columns, in each CTA
         mbar_init(drain, 1);
         *abort_flag = 0;
         fence_mbar_init();
@@ -194,13 +251,14 @@ __global__ void __launch_bounds__(kThreads8, 1)
         tmem_alloc_pair(tmem_holder, kTmemCols8);
         tmem_relinquish_pair();
     }
+    const int kb_n = (p.K + 127) / 128;  // scale blocks of a row
+    const int cl = blockIdx.x >> 1, ncl = gridDim.x >> 1;
+    int t = cl - ncl, m0 = 0, n0 = 0, bn = 0;
+    bool more = U.next(t, ncl, m0, n0, bn);  // this cluster's first unit
     tc_fence_before();
     cluster_sync();  // both CTAs' barriers are initialised before any remote signal
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
-    const int kb_n = (p.K + kBK8 - 1) / kBK8;
-    const int cl = blockIdx.x >> 1, ncl = gridDim.x >> 1;
-    const Units8 U(p.M, p.N, ncl, OUT8 ? 128 : 64);
     griddep_wait();
 
     if (warp == 0) {
@@ -208,30 +266,26 @@ __global__ void __launch_bounds__(kThreads8, 1)
             const uint32_t full_c = mapa_shared(smem_u32(full), 0);
             int s = 0;
             uint32_t ph = 0;
-            bool ok = true;
 #pragma unroll 1
-            for (int t = cl; t < U.total && ok; t += ncl) {
-                int m0, n0, bn;  // this CTA holds bn / 2 of the unit's B rows
-                U.decode(t, m0, n0, bn);
-                if (bn == 0) continue;
+            for (; more; more = U.next(t, ncl, m0, n0, bn)) {
+                // this CTA holds bn / 2 of the unit's B rows
                 const CUtensorMap *mb = &tmb.rows[bn == 256 ? 0 : (bn == 128 ? 1 : 2)];
-                const uint32_t bytes = 2u * (kOperand8 + (uint32_t)(bn / 2) * kBK8);  // both CTAs
+                const int row_a = m0 + (int)rank * 128, row_b = n0 + (int)rank * (bn / 2);
+                const uint32_t bytes = 2u * (kOperand8 + (uint32_t)(bn / 2) * 128);  // both CTAs
 #pragma unroll 1
                 for (int kb = 0; kb < kb_n; ++kb) {
-                    if (!mbar_wait(&empty[s], ph ^ 1, abort_flag, p.err)) {
-                        ok = false;
-                        break;
-                    }
+                    if (!mbar_wait(&empty[s], ph ^ 1, abort_flag, p.err)) goto produced;
                     if (rank == 0) mbar_arrive_expect_tx(&full[s], bytes);
                     const uint32_t fb = full_c + 8u * (uint32_t)s;
-                    tma_load_2d_pair(sa + s * kOperand8, &tma, kb * kBK8, m0 + (int)rank * 128, fb);
-                    tma_load_2d_pair(sb + s * kOperand8, mb, kb * kBK8, n0 + (int)rank * (bn / 2), fb);
+                    tma_load_2d_pair(sa + s * kOperand8, &tma, kb * 128, row_a, fb);
+                    tma_load_2d_pair(sb + s * kOperand8, mb, kb * 128, row_b, fb);
                     if (++s == S) {
                         s = 0;
                         ph ^= 1;
                     }
                 }
             }
+        produced:;
         }
     } else if (warp == 1) {
         if (rank == 0) {
@@ -239,224 +293,253 @@ __global__ void __launch_bounds__(kThreads8, 1)
             const uint64_t b_desc0 = make_sdesc(smem_u32(sb), 16, 1024, kSwizzle128);
             // 32 rows of 16 bytes: groups of 8 rows are 128 bytes apart
             const uint64_t s_desc0 = make_sdesc(smem_u32(ss), 16, 128, kSwizzleNone);
-            int s = 0, it = 0, set = 0;
-            uint32_t ph = 0, sph = 0;
-            bool ok = true;
+            int s = 0, it = 0, set = 0, copied = 0;
+            uint32_t ph = 0;
+            // Copies the next set of scales into tensor memory, its half that set
+            // copied - 2 had: that set's MMAs are over when its last stage is empty.
+            int over_s = 0;
+            uint32_t over_ph = 0;
+            auto copy_scales = [&] {
+                const int b = copied % kSets;
+                if (!warp_wait(&sfull[b], (copied / kSets) & 1, abort_flag, p.err)) return false;
+                if (copied >= 2 && !warp_wait(&empty[over_s], over_ph, abort_flag, p.err)) return false;
+                tc_fence_after();
+                const uint64_t sd = s_desc0 + (uint64_t)b * (kSetBytes >> 4);
+                const uint32_t col = tmem + kScaleCols + 12u * (uint32_t)(copied & 1);
+                tmem_cp_scales_pair(col, sd);
+                tmem_cp_scales_pair(col + 4, sd + (512 >> 4));
+                tmem_cp_scales_pair(col + 8, sd + (1024 >> 4));
+                mma_commit_pair_mc_elect(&sempty[b], 3);
+                ++copied;
+                return true;
+            };
+            bool ok = !more || copy_scales();
+            // a stage's barrier is read while the MMAs of the stage before are issued
+            bool ready = warp_all(mbar_test(&full[0], 0));
 #pragma unroll 1
-            for (int t = cl; t < U.total && ok; t += ncl) {
-                int m0, n0, bn;
-                U.decode(t, m0, n0, bn);
-                if (bn == 0) continue;
+            while (more && ok) {
                 const int buf = it & 1;
                 if (!warp_wait(&acce[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.err)) break;
                 if (it > 0 && !warp_wait(shared_read, (it - 1) & 1, abort_flag, p.err)) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (buf ? kAcc1 : 0u);
                 const uint32_t idesc0 = make_idesc_mxf8(256, 0, 0) | ((uint32_t)(bn >> 3) << 17);
+                const bool another = U.next(t, ncl, m0, n0, bn);
 #pragma unroll 1
                 for (int kb = 0; kb < kb_n; ++kb) {
-                    const uint32_t sfa = tmem + kScaleCols + 12u * (uint32_t)set, sfb = sfa + 4;
-                    if ((kb & 3) == 0) {
-                        // this set's last use is over: its scales were written after the wait for that
-                        if (!warp_wait(&sfull[set], sph, abort_flag, p.err)) {
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
-                        const uint64_t sd = s_desc0 + (uint64_t)set * (kStageScales >> 4);
-                        tmem_cp_scales_pair(sfa, sd);
-                        tmem_cp_scales_pair(sfb, sd + (512 >> 4));
-                        if (bn > 128) tmem_cp_scales_pair(sfb + 4, sd + (1024 >> 4));
-                    }
-                    if (!warp_wait(&full[s], ph, abort_flag, p.err)) {
+                    const uint32_t sfa = tmem + kScaleCols + 12u * (uint32_t)(set & 1);
+                    if (!ready && !warp_wait(&full[s], ph, abort_flag, p.err)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
+                    const int s_next = s + 1 == S ? 0 : s + 1;
+                    const uint32_t ph_next = s_next == 0 ? ph ^ 1 : ph;
+                    ready = warp_all(mbar_test(&full[s_next], ph_next));
                     const uint32_t byte = (uint32_t)(kb & 3);
                     mma_mxf8_pair_128k(d, a_desc0 + (uint64_t)s * (kOperand8 >> 4), b_desc0 + (uint64_t)s * (kOperand8 >> 4),
-                                       sfa, sfb, idesc0 | byte << 4 | byte << 29, kb != 0);
+                                       sfa, sfa + 4, idesc0 | byte << 4 | byte << 29, kb != 0);
                     mma_commit_pair_mc_elect(&empty[s], 3);
-                    if ((kb & 3) == 3 || kb + 1 == kb_n) {
-                        mma_commit_pair_mc_elect(&sempty[set], 3);
-                        set ^= 1;
-                        if (set == 0) sph ^= 1;
+                    // the next set's scales are copied behind this set's first MMAs, which
+                    // keep the tensor core busy until the copies run
+                    const bool last = byte == 3 || kb + 1 == kb_n;
+                    if ((byte == 1 || last) && copied == set + 1 && ((kb | 3) + 1 < kb_n || another) && !copy_scales()) {
+                        ok = false;
+                        break;
                     }
-                    if (++s == S) {
-                        s = 0;
-                        ph ^= 1;
+                    if (last) {
+                        ++set;
+                        over_s = s;
+                        over_ph = ph;
                     }
+                    s = s_next;
+                    ph = ph_next;
                 }
                 if (ok) mma_commit_pair_mc_elect(&accf[buf], 3);
                 ++it;
+                more = another;
             }
         }
     } else if (warp == 2) {
-        // lane l: rows l, l + 32, l + 64, l + 96 of each 128, four scale bytes (512 K) of each
-        const uint32_t sfull_c = mapa_shared(smem_u32(sfull), 0);
-        int set = 0;
-        uint32_t ph = 0;
-        bool ok = true;
-        auto four = [&](const uint8_t *sc, int64_t ld, int row0, int rows, int byte) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = row0 + 32 * j + lane;
-                w[j] = r < rows ? *reinterpret_cast<const uint32_t *>(sc + r * ld + byte) : 0x7F7F7F7Fu;
-            }
-            return make_uint4(w[0], w[1], w[2], w[3]);
+        // lane l: rows l, l + 32, l + 64, l + 96 of each 128, four scale bytes (512 K) of
+        // each per set.  A row's bytes are read for 1, 2 or 4 sets at once, as far as
+        // the rows' alignment allows: 4-byte loads of every set cost 10 % of the whole
+        // product at 8192 x 8192 x 8192.  A group's loads are in flight while the sets
+        // of the group before wait for their places.
+        struct Group {
+            uint4 a[4], b[8];
         };
+        const int per = p.scale_sets;
+        auto row_bytes = [&](const uint8_t *sc, int64_t ld, int r, int rows, int byte) {
+            uint4 w = make_uint4(0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+            if (r >= rows) return w;
+            const uint8_t *q = sc + r * ld + byte;
+            if (per == 4) return *reinterpret_cast<const uint4 *>(q);
+            if (per == 2) {
+                const uint2 h = *reinterpret_cast<const uint2 *>(q);
+                w.x = h.x, w.y = h.y;
+            } else {
+                w.x = *reinterpret_cast<const uint32_t *>(q);
+            }
+            return w;
+        };
+        auto load = [&](Group &x, int kb) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.a[j] = row_bytes(p.sa, p.lda_s, m0 + (int)rank * 128 + 32 * j + lane, p.M, kb);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (32 * j < bn) x.b[j] = row_bytes(p.sb, p.ldb_s, n0 + 32 * j + lane, p.N, kb);
+        };
+        const uint32_t sfull_c = mapa_shared(smem_u32(sfull), 0);
+        Group x, next;
+        if (more) load(x, 0);
+        int kb = 0, n = 0;
+        bool ok = true;
 #pragma unroll 1
-        for (int t = cl; t < U.total && ok; t += ncl) {
-            int m0, n0, bn;
-            U.decode(t, m0, n0, bn);
-            if (bn == 0) continue;
-#pragma unroll 1
-            for (int kb = 0; kb < kb_n; kb += 4) {
-                const uint4 wa = four(p.sa, p.lda_s, m0 + (int)rank * 128, p.M, kb);
-                const uint4 wb0 = four(p.sb, p.ldb_s, n0, p.N, kb);
-                uint4 wb1 = wb0;
-                if (bn > 128) wb1 = four(p.sb, p.ldb_s, n0 + 128, p.N, kb);
-                if (!warp_wait(&sempty[set], ph ^ 1, abort_flag, p.err)) {
-                    ok = false;
-                    break;
-                }
-                uint4 *dst = reinterpret_cast<uint4 *>(ss + set * kStageScales) + lane;
-                dst[0] = wa;
-                dst[32] = wb0;
-                dst[64] = wb1;
+        while (more && ok) {
+            const int sets = min(per, (kb_n - kb + 3) / 4);
+            kb += 4 * per;
+            if (kb >= kb_n) {
+                kb = 0;
+                more = U.next(t, ncl, m0, n0, bn);
+            }
+            if (more) load(next, kb);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i >= sets || !ok) break;
+                const int b = n % kSets;
+                ok = warp_wait(&sempty[b], (n / kSets & 1) ^ 1, abort_flag, p.err);
+                if (!ok) break;
+                auto word = [&](const uint4 &w) { return i == 0 ? w.x : (i == 1 ? w.y : (i == 2 ? w.z : w.w)); };
+                uint4 *dst = reinterpret_cast<uint4 *>(ss + b * kSetBytes) + lane;
+                dst[0] = make_uint4(word(x.a[0]), word(x.a[1]), word(x.a[2]), word(x.a[3]));
+                dst[32] = make_uint4(word(x.b[0]), word(x.b[1]), word(x.b[2]), word(x.b[3]));
+                dst[64] = make_uint4(word(x.b[4]), word(x.b[5]), word(x.b[6]), word(x.b[7]));
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(sfull_c + 8u * (uint32_t)set);
-                set ^= 1;
-                if (set == 0) ph ^= 1;
+                if (lane == 0) mbar_arrive_cluster(sfull_c + 8u * (uint32_t)b);
+                ++n;
             }
+            x = next;
         }
     } else if (warp >= 4) {
-        const int q = warp & 3, grp = (warp - 4) >> 2;
-        const int row = q * 32 + lane;
-        Stage8 o{so + grp * 2 * kOutBuf8, &tmo, row, 1 + grp, (int)threadIdx.x == 128 + 128 * grp, 0};
+        // warp w: rows 32 q .. 32 q + 31 of this CTA's 128 (its TMEM lanes), one half of
+        // the unit's columns (of 8-bit output a whole scale block)
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        float *bias = sv + (warp - 4) * 256, *gate = bias + 128;
+        Stage8 o{so + (warp - 4) * 4096, &tmo, 0, lane};
         const uint32_t acce_c = mapa_shared(smem_u32(acce), 0), shared_c = mapa_shared(smem_u32(shared_read), 0);
         auto arrive = [&](uint32_t bar) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(bar);
         };
-        int it = 0;
 #pragma unroll 1
-        for (int t = cl; t < U.total; t += ncl) {
-            int m0, n0, bn;
-            U.decode(t, m0, n0, bn);
-            if (bn == 0) continue;
-            m0 += (int)rank * 128;
-            const int buf = it & 1;
-            // the group's warps meet at barriers below: they take the wait's outcome together
-            const uint32_t got = mbar_wait(&accf[buf], (it >> 1) & 1, abort_flag, p.err) ? 1u : 0u;
-            uint32_t all;
-            asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.and.pred q, %2, 128, p;\n"
-                         " selp.u32 %0, 1, 0, q;\n}\n"
-                         : "=r"(all)
-                         : "r"(got), "r"(o.bar)
-                         : "memory");
-            if (!all) break;
-            tc_fence_after();
-            const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (buf ? kAcc1 : 0u);
-            // the group whose first chunk covers the 24 columns that the other
-            // accumulator shares: the last ones of a full first accumulator, the
-            // first ones of the second
+        for (int it = 0; more; ++it) {
+            // (a box of 128 bytes is the least that a warp stores)
+            const int buf = it & 1, width = OUT8 ? 128 : (EPI == kEpiResid ? bn / 2 : max(64, bn / 2)), c0 = half * width;
+            const int col0 = n0 + c0;
+            o.row = m0 + (int)rank * 128 + q * 32;
+            const bool mine = o.row < p.M && c0 < bn && col0 < p.N;
+            // the half that holds the 24 columns which the other accumulator shares, the
+            // last ones of a full first accumulator or the first of the second, reads
+            // them first
             const bool from_end = bn == 256 && buf == 0;
-            const bool shares = grp == (from_end ? 1 : 0);
-            const bool rows = m0 < p.M;  // the odd CTA's rows may lie behind M
-            if constexpr (OUT8) {
-                // group g has columns 128 g .. 128 g + 127: a scale block of each row
-                const int c0 = 128 * grp;
-                if (rows && c0 < bn) {
-                    float v[128];
+            const bool shares = half == (from_end ? 1 : 0);
+            const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (buf ? kAcc1 : 0u) + c0;
+            // this unit's biases and gates, loaded while its sums run
+            if (mine) {
+                __syncwarp();
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        float w[32];
-                        load_acc(acc + c0 + 32 * k, w);
-                        add_bias(p, n0 + c0 + 32 * k, w);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[32 * k + j] = EPI == kEpiGelu ? gelu_tanh(w[j]) : w[j];
-                    }
-                    if (shares) arrive(shared_c);
-                    arrive(acce_c + 8u * (uint32_t)buf);
-                    const int col = n0 + c0;
-                    const uint32_t byte = quantize_block<128, 1>(v);
-                    if (m0 + row < p.M && col < p.N)
-                        p.out_scales[(int64_t)(m0 + row) * p.ldo_s + col / kScaleBlock] = (uint8_t)byte;
-                    // one box of 128 rows x 128 bytes (128B swizzle) over both buffers
-                    if (o.issuer) bulk_wait_read<0>();
-                    asm volatile("bar.sync %0, 128;" ::"r"(o.bar) : "memory");
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint4 u;
-                        u.x = pack_e4m3x4(v[16 * c], v[16 * c + 1], v[16 * c + 2], v[16 * c + 3]);
-                        u.y = pack_e4m3x4(v[16 * c + 4], v[16 * c + 5], v[16 * c + 6], v[16 * c + 7]);
-                        u.z = pack_e4m3x4(v[16 * c + 8], v[16 * c + 9], v[16 * c + 10], v[16 * c + 11]);
-                        u.w = pack_e4m3x4(v[16 * c + 12], v[16 * c + 13], v[16 * c + 14], v[16 * c + 15]);
-                        *reinterpret_cast<uint4 *>(o.buf + row * 128 + ((c ^ (row & 7)) << 4)) = u;
-                    }
-                    fence_proxy_async_smem();
-                    asm volatile("bar.sync %0, 128;" ::"r"(o.bar) : "memory");
-                    if (o.issuer && col < p.N) {
-                        tma_store_2d(&tmo, o.buf, col, m0);
-                        bulk_commit();
-                    }
-                } else {
-                    if (shares) arrive(shared_c);
-                    arrive(acce_c + 8u * (uint32_t)buf);
+                for (int i = 0; i < 4; ++i) {
+                    const int c = 32 * i + lane;
+                    const bool in = c < width && col0 + c < p.N;
+                    bias[c] = in && p.bias ? __bfloat162float(p.bias[col0 + c]) : 0.f;
+                    if constexpr (EPI == kEpiResid) gate[c] = in && p.gate ? p.gate[col0 + c] : 1.f;
                 }
+                __syncwarp();
+            }
+            more = U.next(t, ncl, m0, n0, bn);
+            if (!warp_wait(&accf[buf], (it >> 1) & 1, abort_flag, p.err)) break;
+            tc_fence_after();
+            if (!mine) {
+                if (shares) arrive(shared_c);
+                arrive(acce_c + 8u * (uint32_t)buf);
+                continue;
+            }
+            if constexpr (OUT8) {
+                // the 128 columns are one scale block of this lane's row
+                float f[128];  // columns behind N: GELU of zero sums without a bias
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t r[32];
+                    tmem_ld32(acc + 32 * k, r);
+                    wait_chunk(r);
+                    apply<EPI>(r, bias + 32 * k, gate);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[32 * k + j] = __uint_as_float(r[j]);
+                }
+                if (shares) arrive(shared_c);
+                arrive(acce_c + 8u * (uint32_t)buf);
+                const uint32_t byte = quantize_block<128, 1>(f);
+                if (o.row + lane < p.M) p.out_scales[(int64_t)(o.row + lane) * p.ldo_s + col0 / kScaleBlock] = (uint8_t)byte;
+                o.begin();
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const float *x = f + 16 * c;
+                    o.put16(c, make_uint4(pack_e4m3x4(x[0], x[1], x[2], x[3]), pack_e4m3x4(x[4], x[5], x[6], x[7]),
+                                          pack_e4m3x4(x[8], x[9], x[10], x[11]), pack_e4m3x4(x[12], x[13], x[14], x[15])));
+                }
+                o.template send<false>(col0);
             } else {
-                const int chunks = rows ? bn / 32 : 0;
-#pragma unroll 1
-                for (int k = grp; k < chunks; k += 2) {
-                    const int c0 = 32 * (from_end ? chunks - 1 - (k ^ 1) : k);
-                    const int col = n0 + c0;
-                    float v[32];
-                    load_acc(acc + c0, v);
-                    if (k == grp && shares) arrive(shared_c);
-                    if (col >= p.N) continue;
-                    add_bias(p, col, v);
-                    if constexpr (EPI == kEpiGelu) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = gelu_tanh(v[j]);
-                    }
+                const int chunks = width / 32;
+                auto at = [&](int i) { return 32 * (from_end ? chunks - 1 - i : i); };
+                // 32 columns: a box of fp32, half a box of bf16
+                auto finish = [&](uint32_t (&r)[32], int c) {
+                    if (col0 + c >= p.N) return;
+                    apply<EPI>(r, bias + c, gate + c);
                     if constexpr (EPI == kEpiResid) {
-                        // x += gate y as an fp32 reduce-add of gate y, 16 columns per box
+                        // x += gate y as an fp32 reduce-add of gate y
+                        o.begin();
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int c = col + 16 * h + 4 * i;
-                                const float *w = v + 16 * h + 4 * i;
-                                const float4 g = p.gate && c < p.N ? __ldg(reinterpret_cast<const float4 *>(p.gate + c))
-                                                                   : make_float4(1.f, 1.f, 1.f, 1.f);
-                                o.put16(i, make_uint4(__float_as_uint(g.x * w[0]), __float_as_uint(g.y * w[1]),
-                                                      __float_as_uint(g.z * w[2]), __float_as_uint(g.w * w[3])));
-                            }
-                            if (col + 16 * h < p.N) o.template emit<true>(col + 16 * h, m0);
-                        }
+                        for (int i = 0; i < 8; ++i) o.put16(i, make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]));
+                        o.template send<true>(col0 + c);
                     } else {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            uint4 u;
-                            u.x = pack_bf16x2(v[8 * i + 0], v[8 * i + 1]);
-                            u.y = pack_bf16x2(v[8 * i + 2], v[8 * i + 3]);
-                            u.z = pack_bf16x2(v[8 * i + 4], v[8 * i + 5]);
-                            u.w = pack_bf16x2(v[8 * i + 6], v[8 * i + 7]);
-                            o.put16(i, u);
+                            const float *x = reinterpret_cast<const float *>(r + 8 * i);
+                            o.put16(((c >> 3) & 4) + i, make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                                                   pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])));
                         }
-                        o.template emit<false>(col, m0);
                     }
+                };
+                // the next chunk's load runs while a chunk is worked on
+                uint32_t a[32], b[32];
+                tmem_ld32(acc + at(0), a);
+                wait_chunk(a);
+                if (shares) arrive(shared_c);
+#pragma unroll 1
+                for (int i = 0; i < chunks; i += 2) {
+                    if (i + 1 < chunks)
+                        tmem_ld32(acc + at(i + 1), b);
+                    else
+                        arrive(acce_c + 8u * (uint32_t)buf);
+                    if constexpr (EPI != kEpiResid) o.begin();
+                    finish(a, at(i));
+                    if (i + 1 < chunks) {
+                        wait_chunk(b);
+                        if (i + 2 < chunks)
+                            tmem_ld32(acc + at(i + 2), a);
+                        else
+                            arrive(acce_c + 8u * (uint32_t)buf);
+                        finish(b, at(i + 1));
+                        if (i + 2 < chunks) wait_chunk(a);
+                    }
+                    if constexpr (EPI != kEpiResid) o.template send<false>(col0 + (at(i) & ~63));
                 }
-                if (chunks == 0 && shares) arrive(shared_c);
-                arrive(acce_c + 8u * (uint32_t)buf);
             }
-            ++it;
         }
-        if (o.issuer) bulk_wait_all();
+        if (lane == 0) bulk_wait_all();
     }
     __syncthreads();
     if (*abort_flag) {
@@ -477,8 +560,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
 }
 
 template <int EPI, bool OUT8>
-cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
-                        cudaStream_t s)
+cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p, cudaStream_t s)
 {
     // per device: the shared-memory attribute and the resident-cluster count are
     // taken on each device's first launch (0 = not yet known)
@@ -511,21 +593,23 @@ cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtens
         max_clusters_of[dev & 63].store(n, std::memory_order_release);
     }
     // units: 64 columns (128 with 8-bit output) are the smallest
-    const int64_t width = OUT8 ? 128 : 64;
-    const int64_t units = (((int64_t)p.M + 255) / 256) * ((p.N + width - 1) / width);
+    constexpr int width = OUT8 ? 128 : 64;
+    const int64_t units = (((int64_t)p.M + 255) / 256) * (((int64_t)p.N + width - 1) / width);
     const int clusters = units < max_clusters ? (int)units : max_clusters;
+    Units8 u;
+    u.set(p.M, p.N, clusters, width);
     cfg.gridDim = dim3(2 * clusters);
     cfg.stream = s;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, k_gemm8_pair<EPI, OUT8>, *ta, *tb, *to, p);
+    e = cudaLaunchKernelEx(&cfg, k_gemm8_pair<EPI, OUT8>, *ta, *tb, *to, u, p);
     if (e != cudaSuccess) return e;
     return cudaGetLastError();
 }
 
 }  // namespace
 
-bool make_tmap_2d(CUtensorMap *map, CUtensorMapDataType type, const void *base, uint64_t rows, uint64_t cols,
-                  uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols, CUtensorMapSwizzle swizzle)
+bool make_tmap_rows(CUtensorMap *map, CUtensorMapDataType type, const void *base, uint64_t rows, uint64_t cols,
+                    uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols)
 {
     static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> encoder{nullptr};
     PFN_cuTensorMapEncodeTiled_v12000 encode = encoder.load(std::memory_order_acquire);
@@ -539,17 +623,17 @@ bool make_tmap_2d(CUtensorMap *map, CUtensorMapDataType type, const void *base, 
         encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
         encoder.store(encode, std::memory_order_release);
     }
-    if (((uintptr_t)base & 15) != 0 || row_bytes % 16 != 0) return false;
     cuuint64_t dims[2] = {cols, rows};
     cuuint64_t strides[1] = {row_bytes};
     cuuint32_t box[2] = {box_cols, box_rows};
     cuuint32_t estr[2] = {1, 1};
-    return encode(map, type, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode(map, type, 2, const_cast<void *>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
-                              int epi, bool out8, cudaStream_t s)
+cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p, int epi, bool out8,
+                              cudaStream_t s)
 {
     switch (epi) {
     case kEpiBias: return out8 ? launch_one8<kEpiBias, true>(ta, tb, to, p, s) : launch_one8<kEpiBias, false>(ta, tb, to, p, s);

@@ -344,10 +344,11 @@ uint32_t *gemm_status_word();
 bool make_tmap_bf16(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint64_t ld,
                     uint32_t box_rows, uint32_t box_cols);
 
-// 2-D tensor map over a row-major [rows, cols] matrix of any type, rows `row_bytes`
-// (a multiple of 16) apart, zero fill outside.  Returns false on failure.
-bool make_tmap_2d(CUtensorMap *map, CUtensorMapDataType type, const void *base, uint64_t rows, uint64_t cols,
-                  uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols, CUtensorMapSwizzle swizzle);
+// Tensor map over a row-major matrix [rows, cols], rows `row_bytes` (a multiple of 16)
+// apart, base 16-byte aligned: boxes of box_rows rows x 128 bytes (box_cols elements),
+// 128B swizzle, zero fill outside.  Returns false on failure.
+bool make_tmap_rows(CUtensorMap *map, CUtensorMapDataType type, const void *base, uint64_t rows, uint64_t cols,
+                    uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols);
 
 // ------------------------------------------------------------ 8-bit linear layers
 constexpr int kScaleBlock = 128;  // elements of a row that share an E8M0 scale
@@ -369,15 +370,15 @@ struct Gemm8Params {
     int M, N, K;
     const uint8_t *sa, *sb;   // scale bytes [M, lda_s], [N, ldb_s]
     int64_t lda_s, ldb_s;
+    int scale_sets;           // scale bytes read at once from a row: 4, 8 or 16 (1, 2 or 4 sets)
     const bf16 *bias;         // nullable
     const float *gate;        // nullable (RESID)
     uint8_t *out_scales;      // 8-bit output
     int64_t ldo_s;
     uint32_t *err;
 };
-// ta: A in boxes of 128 rows x 128 bytes; tb: B in boxes of 128, 64 and 32 rows; to: the
-// output in boxes of 128 rows x 64 bytes (64B swizzle), 128 bytes for 8-bit output
-// (128B swizzle).  epi as launch_gemm's.
+// ta: A in boxes of 128 rows; tb: B in boxes of 128, 64 and 32 rows; to: the output in
+// boxes of 32 rows (make_tmap_rows).  epi as launch_gemm's.
 cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
                               int epi, bool out8, cudaStream_t s);
 

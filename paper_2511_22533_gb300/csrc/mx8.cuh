@@ -19,25 +19,28 @@ F3DC_DEV void tma_load_2d_pair(void *smem_dst, const CUtensorMap *map, int x, in
 }
 
 // D (+)= A B^T over a CTA pair (mma_bf16_pair_128k says which rows lie where), e4m3
-// operands with one E8M0 scale per row and 128 K: the four MMAs of 128 K (32 K
-// further is 2 descriptor units).  The scales lie in tensor memory
-// (tmem_cp_scales_pair); each MMA takes the byte of a scale column that idesc names,
-// for all of its 32 K.
+// operands with one E8M0 scale per row and 128 K.  The scales lie in tensor memory
+// (tmem_cp_scales_pair); each MMA takes the byte of a scale column that its instruction
+// descriptor names for all of its 32 K.  The four MMAs of 128 K (32 K further is 2
+// descriptor units) under one election.
+#define F3DC_MXF8(D, A, B, SA, SB, I, P) \
+    " @e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [" D "], " A ", " B ", " I ", [" SA "], [" SB "], " P ";\n"
+#define F3DC_MXF8_NEXT " add.s64 a, a, 2;\n add.s64 b, b, 2;\n"
 F3DC_DEV void mma_mxf8_pair_128k(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t sfa_tmem,
                                  uint32_t sfb_tmem, uint32_t idesc, uint32_t accumulate)
 {
-#define F3DC_MXF8 "@e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], "
     asm volatile(
         "{\n .reg .pred p, e, t;\n .reg .b64 a, b;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %6, 0;\n setp.eq.b32 t, 0, 0;\n"
-        " " F3DC_MXF8 "%1, %2, %5, [%3], [%4], p;\n"
-        " add.s64 a, %1, 2;\n add.s64 b, %2, 2;\n " F3DC_MXF8 "a, b, %5, [%3], [%4], t;\n"
-        " add.s64 a, a, 2;\n add.s64 b, b, 2;\n " F3DC_MXF8 "a, b, %5, [%3], [%4], t;\n"
-        " add.s64 a, a, 2;\n add.s64 b, b, 2;\n " F3DC_MXF8 "a, b, %5, [%3], [%4], t;\n"
+        F3DC_MXF8("%0", "%1", "%2", "%3", "%4", "%5", "p")
+        " add.s64 a, %1, 2;\n add.s64 b, %2, 2;\n" F3DC_MXF8("%0", "a", "b", "%3", "%4", "%5", "t")
+        F3DC_MXF8_NEXT F3DC_MXF8("%0", "a", "b", "%3", "%4", "%5", "t")
+        F3DC_MXF8_NEXT F3DC_MXF8("%0", "a", "b", "%3", "%4", "%5", "t")
         "}\n" ::"r"(d_tmem),
         "l"(a_desc), "l"(b_desc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(idesc), "r"(accumulate)
         : "memory");
-#undef F3DC_MXF8
 }
+#undef F3DC_MXF8
+#undef F3DC_MXF8_NEXT
 
 // Copies 32 rows of 16 bytes (512 consecutive bytes of shared memory, row r at 16 r)
 // of each CTA of the pair into 4 columns of its own tensor memory, the same 32 lanes

@@ -7,10 +7,12 @@
 // one power-of-two scale per block of 128.
 //
 // Bound by memory: x, y read and x', h written once (12 bytes per element, 11 with
-// 8-bit h).  A row stays in registers between its two norms: a warp holds a row of up
-// to 1024 values (8 consecutive ones per lane and step, so that 16 lanes hold a scale
-// block), four warps a wider one.  Means, then mean squared deviations from them, in
-// fp32.
+// 8-bit h).  A CTA has one thread per 8 columns, so that 16 threads hold a scale block,
+// and takes R rows at once: their loads are in flight together, their sums share the
+// shuffles and the barrier, and a gain or a modulation is read once for all of them
+// (from L1: with one row at a time these vectors, 20 bytes per element, are more than
+// the rows themselves).  The rows stay in registers between the two norms.  Means, then
+// mean squared deviations from them, in fp32.
 #include "kernels.h"
 #include "mx8.cuh"
 
@@ -18,208 +20,297 @@ namespace f3dc {
 
 namespace {
 
-constexpr int kNormThreads = 128;
+constexpr int kNormRows = 2;
+constexpr int kNormThreadsPerSm = 1024;
 
 struct V8 {
-    float v[8];
+    f32x2 v[4];
 };
 
-F3DC_DEV V8 load_f32x8(const float *p)
-{
-    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-    return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-}
+F3DC_DEV V8 zero8() { return V8{{{0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}}}; }
 
-F3DC_DEV V8 load_bf16x8(const bf16 *p)
+F3DC_DEV V8 from_bf16(uint4 u)
 {
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    V8 r;
+    return V8{{{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u)},
+               {__uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u)},
+               {__uint_as_float(u.z << 16), __uint_as_float(u.z & 0xFFFF0000u)},
+               {__uint_as_float(u.w << 16), __uint_as_float(u.w & 0xFFFF0000u)}}};
+}
+// gains, biases, modulations: read by every CTA, kept in L1
+F3DC_DEV V8 vec_bf16(const bf16 *p) { return from_bf16(*reinterpret_cast<const uint4 *>(p)); }
+F3DC_DEV V8 vec_f32(const float *p)
+{
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    return V8{{{a.x, a.y}, {a.z, a.w}, {b.x, b.y}, {b.z, b.w}}};
+}
+// rows: read once, past L1
+F3DC_DEV uint4 row_load16(const void *p)
+{
+    uint4 u;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    return u;
+}
+F3DC_DEV f32x2 both(float a) { return {a, a}; }
+
+// Sums of R values over the CTA's NW warps, in every thread.  Two values share a step that
+// halves what a lane holds; a warp's sums lie in sh[i][warp].
+template <int R, int NW>
+F3DC_DEV void row_sums(float (&s)[R], float (*sh)[NW])
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if constexpr (R == 1) {
+        const float v = warp_sum(s[0]);
+        if constexpr (NW == 1) {
+            s[0] = v;
+            return;
+        }
+        if (lane == 0) sh[0][warp] = v;
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        r.v[2 * j] = bf16_bits_to_f32(w[j] & 0xFFFFu);
-        r.v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        for (int i = 0; i < R; i += 2) {
+            const bool up = lane & 16;
+            float v = up ? s[i + 1] : s[i];
+            v += __shfl_xor_sync(0xffffffffu, up ? s[i] : s[i + 1], 16);
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (NW == 1) {
+                s[i] = __shfl_sync(0xffffffffu, v, 0);
+                s[i + 1] = __shfl_sync(0xffffffffu, v, 16);
+            } else if ((lane & 15) == 0) {
+                sh[i + (lane >> 4)][warp] = v;
+            }
+        }
     }
-    return r;
-}
-
-// Sum over the TPR threads of a row.
-template <int TPR>
-F3DC_DEV float row_sum(float v, float *sh)
-{
-    v = warp_sum(v);
-    if constexpr (TPR > 32) {
-        __syncthreads();  // the last sum has been read
-        if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+    if constexpr (NW > 1) {
         __syncthreads();
-        v = 0.f;
 #pragma unroll
-        for (int i = 0; i < TPR / 32; ++i) v += sh[i];
+        for (int i = 0; i < R; ++i) {
+            float v = 0.f;
+            if constexpr (NW == 2) {
+                const float2 u = *reinterpret_cast<const float2 *>(sh[i]);
+                v = u.x + u.y;
+            } else {
+#pragma unroll
+                for (int w = 0; w < NW; w += 4) {
+                    const float4 u = *reinterpret_cast<const float4 *>(sh[i] + w);
+                    v += (u.x + u.y) + (u.z + u.w);
+                }
+            }
+            s[i] = v;
+        }
     }
-    return v;
 }
 
-// v becomes its norm times g plus b; vectors from `nv` on are zeros and stay out of the sums.
-template <int NV, int TPR>
-F3DC_DEV void normalise(V8 (&v)[NV], int t, int W, int kind, const bf16 *g, const bf16 *b, float eps, float *sh)
+// v[i] becomes its norm times g plus b.  `in`: this thread has columns of the row (its
+// values are zeros otherwise, and stay out of the sums).
+template <int R, int NW>
+F3DC_DEV void normalise(V8 (&v)[R], bool in, float inv_w, int kind, const bf16 *g, const bf16 *b, float eps,
+                        float (*sh)[R][NW], int &turn)
 {
     if (kind != kNormNone) {
-        float mean = 0.f;
+        float s[R];
         if (kind == kNormLayer) {
-            float s = 0.f;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s += v[i].v[j];
-            mean = row_sum<TPR>(s, sh) / (float)W;
-        }
-        float ss = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if ((t + TPR * i) * 8 < W) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    v[i].v[j] -= mean;
-                    ss += v[i].v[j] * v[i].v[j];
-                }
+            for (int i = 0; i < R; ++i) {
+                const f32x2 t = fadd2(fadd2(v[i].v[0], v[i].v[1]), fadd2(v[i].v[2], v[i].v[3]));
+                s[i] = t.x + t.y;
             }
-        const float r = rsqrtf(row_sum<TPR>(ss, sh) / (float)W + eps);
+            row_sums<R, NW>(s, sh[turn]);
+            turn ^= 1;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < R; ++i) {
+                const f32x2 m = both(in ? -s[i] * inv_w : 0.f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i].v[j] *= r;
+                for (int j = 0; j < 4; ++j) v[i].v[j] = fadd2(v[i].v[j], m);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            f32x2 t = fmul2(v[i].v[0], v[i].v[0]);
+#pragma unroll
+            for (int j = 1; j < 4; ++j) t = ffma2(v[i].v[j], v[i].v[j], t);
+            s[i] = t.x + t.y;
+        }
+        row_sums<R, NW>(s, sh[turn]);
+        turn ^= 1;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const f32x2 r = both(rsqrtf(s[i] * inv_w + eps));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i].v[j] = fmul2(v[i].v[j], r);
+        }
     }
-    if (!g && !b) return;
+    if (g && in) {
+        const V8 u = vec_bf16(g);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int col = (t + TPR * i) * 8;
-        if (col >= W) continue;
-        if (g) {
-            const V8 u = load_bf16x8(g + col);
+        for (int i = 0; i < R; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i].v[j] *= u.v[j];
-        }
-        if (b) {
-            const V8 u = load_bf16x8(b + col);
+            for (int j = 0; j < 4; ++j) v[i].v[j] = fmul2(v[i].v[j], u.v[j]);
+    }
+    if (b && in) {
+        const V8 u = vec_bf16(b);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i].v[j] += u.v[j];
-        }
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i].v[j] = fadd2(v[i].v[j], u.v[j]);
     }
 }
 
-// NV vectors of 8 per thread, TPR threads per row (32: a warp; kNormThreads: the CTA).
-template <int NV, int TPR>
-__global__ void __launch_bounds__(kNormThreads) k_norm_residual(const NormArgs a)
+// R rows per CTA, at most NW warps (a power of two)
+template <int R, int NW>
+__global__ void __launch_bounds__(32 * NW, kNormThreadsPerSm / (32 * NW)) k_norm_residual(const NormArgs a)
 {
-    __shared__ float sh[kNormThreads / 32];
+    __shared__ __align__(16) float sh[2][R][NW];  // by turns: one barrier per sum
     griddep_launch();
+    // the sums of warps that the CTA does not have
+    if (NW > 2 && blockDim.x < 32 * NW && threadIdx.x < 2 * R * NW && threadIdx.x % NW >= blockDim.x / 32)
+        (&sh[0][0][0])[threadIdx.x] = 0.f;
     griddep_wait();
-    constexpr int kRows = kNormThreads / TPR;
-    const int t = threadIdx.x % TPR, W = a.width;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * kRows) {
-        const int g = a.group ? a.group[row] : 0;
-        if (g < 0) continue;
-        if (g >= a.groups) {
-            if (t == 0) raise_error(a.err, kDevBadIndex);
-            continue;
+    const int col = threadIdx.x * 8;
+    const bool in = col < a.width;
+    const float inv_w = 1.0f / (float)a.width;
+    const int64_t row0 = (int64_t)blockIdx.x * R;
+    int turn = 0;
+
+    int g[R];  // group of each row; -1: left as it is
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        g[i] = -1;
+        if (row0 + i < a.rows) g[i] = a.group ? a.group[row0 + i] : 0;
+        if (g[i] >= a.groups) {
+            if (threadIdx.x == 0) raise_error(a.err, kDevBadIndex);
+            g[i] = -1;
         }
-        V8 x[NV];
+        any |= g[i] >= 0;
+    }
+    if (!any) return;  // the same for every thread of the CTA
+
+    uint4 xr[R][2], yr[R];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int col = (t + TPR * i) * 8;
-            x[i] = V8{};
-            if (col < W) x[i] = load_f32x8(a.x + row * a.ldx + col);
+    for (int i = 0; i < R; ++i) {
+        xr[i][0] = xr[i][1] = yr[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (in && g[i] >= 0) {
+            const float *p = a.x + (row0 + i) * a.ldx + col;
+            xr[i][0] = row_load16(p);
+            xr[i][1] = row_load16(p + 4);
+            if (a.y) yr[i] = row_load16(a.y + (row0 + i) * a.ldy + col);
         }
-        if (a.y) {
-            V8 y[NV];
+    }
+    V8 x[R];
+    const f32x2 alpha = both(a.res_scale);
+    if (a.y) {
+        V8 y[R];
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int col = (t + TPR * i) * 8;
-                y[i] = V8{};
-                if (col < W) y[i] = load_bf16x8(a.y + row * a.ldy + col);
-            }
-            normalise<NV, TPR>(y, t, W, a.post, a.post_g, a.post_b, a.eps, sh);
+        for (int i = 0; i < R; ++i) y[i] = from_bf16(yr[i]);
+        normalise<R, NW>(y, in, inv_w, a.post, a.post_g ? a.post_g + col : nullptr, a.post_b ? a.post_b + col : nullptr,
+                         a.eps, sh, turn);
+        V8 gate;
+        int of = -1;  // the group whose vector `gate` is
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int col = (t + TPR * i) * 8;
-                if (col >= W) continue;
-                V8 gate;
-                if (a.gate) gate = load_f32x8(a.gate + g * a.ldmod + col);
+        for (int i = 0; i < R; ++i) {
+            const float *f = reinterpret_cast<const float *>(xr[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[i].v[j] = a.res_scale * x[i].v[j] + (a.gate ? gate.v[j] * y[i].v[j] : y[i].v[j]);
-            }
-        } else {
+            for (int j = 0; j < 4; ++j) x[i].v[j] = fmul2({f[2 * j], f[2 * j + 1]}, alpha);
+            if (a.gate && in && g[i] >= 0) {
+                if (g[i] != of) gate = vec_f32(a.gate + g[i] * a.ldmod + col);
+                of = g[i];
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+                for (int j = 0; j < 4; ++j) x[i].v[j] = ffma2(gate.v[j], y[i].v[j], x[i].v[j]);
+            } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[i].v[j] *= a.res_scale;
-        }
-        if (a.x_out) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int col = (t + TPR * i) * 8;
-                if (col >= W) continue;
-                float4 *p = reinterpret_cast<float4 *>(a.x_out + row * a.ldxo + col);
-                p[0] = make_float4(x[i].v[0], x[i].v[1], x[i].v[2], x[i].v[3]);
-                p[1] = make_float4(x[i].v[4], x[i].v[5], x[i].v[6], x[i].v[7]);
-            }
-        }
-        if (!a.h) continue;
-        normalise<NV, TPR>(x, t, W, a.pre, a.pre_g, a.pre_b, a.eps, sh);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int col = (t + TPR * i) * 8;
-            const bool in = col < W;
-            if (in && a.scale) {
-                const V8 u = load_f32x8(a.scale + g * a.ldmod + col);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[i].v[j] *= 1.0f + u.v[j];
-            }
-            if (in && a.shift) {
-                const V8 u = load_f32x8(a.shift + g * a.ldmod + col);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[i].v[j] += u.v[j];
-            }
-            const float(&v)[8] = x[i].v;
-            if (a.h_scales) {
-                float w[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-                const uint32_t byte = quantize_block<8, 16>(w);
-                if (in) {
-                    *reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(a.h) + row * a.ldh + col) =
-                        make_uint2(pack_e4m3x4(w[0], w[1], w[2], w[3]), pack_e4m3x4(w[4], w[5], w[6], w[7]));
-                    if (t % 16 == 0) a.h_scales[row * a.ldhs + col / kScaleBlock] = (uint8_t)byte;
-                }
-            } else if (in) {
-                uint4 u;
-                u.x = pack_bf16x2(v[0], v[1]);
-                u.y = pack_bf16x2(v[2], v[3]);
-                u.z = pack_bf16x2(v[4], v[5]);
-                u.w = pack_bf16x2(v[6], v[7]);
-                *reinterpret_cast<uint4 *>(reinterpret_cast<bf16 *>(a.h) + row * a.ldh + col) = u;
+                for (int j = 0; j < 4; ++j) x[i].v[j] = fadd2(y[i].v[j], x[i].v[j]);
             }
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float *f = reinterpret_cast<const float *>(xr[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i].v[j] = fmul2({f[2 * j], f[2 * j + 1]}, alpha);
+        }
+    }
+    if (a.x_out) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (in && g[i] >= 0) {
+                float4 *p = reinterpret_cast<float4 *>(a.x_out + (row0 + i) * a.ldxo + col);
+                p[0] = make_float4(x[i].v[0].x, x[i].v[0].y, x[i].v[1].x, x[i].v[1].y);
+                p[1] = make_float4(x[i].v[2].x, x[i].v[2].y, x[i].v[3].x, x[i].v[3].y);
+            }
+    }
+    if (!a.h) return;
+    normalise<R, NW>(x, in, inv_w, a.pre, a.pre_g ? a.pre_g + col : nullptr, a.pre_b ? a.pre_b + col : nullptr, a.eps, sh,
+                     turn);
+    if (a.scale || a.shift) {
+        V8 sc = zero8(), sf = zero8();
+        int of = -1;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (!in || g[i] < 0) continue;
+            if (g[i] != of) {
+                if (a.scale) sc = vec_f32(a.scale + g[i] * a.ldmod + col);
+                if (a.shift) sf = vec_f32(a.shift + g[i] * a.ldmod + col);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sc.v[j] = fadd2(sc.v[j], both(1.0f));
+            }
+            of = g[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i].v[j] = ffma2(x[i].v[j], sc.v[j], sf.v[j]);
+        }
+    }
+    if (a.h_scales) {
+        float f[R][8];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f[i][2 * j] = in ? x[i].v[j].x : 0.f;
+                f[i][2 * j + 1] = in ? x[i].v[j].y : 0.f;
+            }
+        uint32_t byte[R];
+        quantize_blocks<R, 8, 16>(f, byte);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (in && g[i] >= 0) {
+                *reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(a.h) + (row0 + i) * a.ldh + col) =
+                    make_uint2(pack_e4m3x4(f[i][0], f[i][1], f[i][2], f[i][3]), pack_e4m3x4(f[i][4], f[i][5], f[i][6], f[i][7]));
+                if (threadIdx.x % 16 == 0) a.h_scales[(row0 + i) * a.ldhs + col / kScaleBlock] = (uint8_t)byte[i];
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (in && g[i] >= 0)
+                *reinterpret_cast<uint4 *>(reinterpret_cast<bf16 *>(a.h) + (row0 + i) * a.ldh + col) =
+                    make_uint4(pack_bf16x2(x[i].v[0].x, x[i].v[0].y), pack_bf16x2(x[i].v[1].x, x[i].v[1].y),
+                               pack_bf16x2(x[i].v[2].x, x[i].v[2].y), pack_bf16x2(x[i].v[3].x, x[i].v[3].y));
     }
 }
 
-template <int NV, int TPR>
-cudaError_t launch_rows(const NormArgs &a, int num_sms, cudaStream_t s)
+template <int R, int NW>
+cudaError_t launch_rows(const NormArgs &a, cudaStream_t s)
 {
-    constexpr int kRows = kNormThreads / TPR;
-    const int64_t ctas = ((int64_t)a.rows + kRows - 1) / kRows, most = (int64_t)num_sms * 16;
-    return launch_k(k_norm_residual<NV, TPR>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kNormThreads), 0, s, a);
+    const unsigned threads = (unsigned)((a.width + 255) / 256 * 32);
+    const unsigned ctas = (unsigned)(((int64_t)a.rows + R - 1) / R);
+    return launch_k(k_norm_residual<R, NW>, dim3(ctas), dim3(threads), 0, s, a);
+}
+
+template <int R>
+cudaError_t launch_width(const NormArgs &a, cudaStream_t s)
+{
+    if (a.width <= 256) return launch_rows<R, 1>(a, s);
+    if (a.width <= 512) return launch_rows<R, 2>(a, s);
+    if (a.width <= 1024) return launch_rows<R, 4>(a, s);
+    if (a.width <= 2048) return launch_rows<R, 8>(a, s);
+    if (a.width <= 4096) return launch_rows<R, 16>(a, s);
+    return launch_rows<1, 32>(a, s);
 }
 
 }  // namespace
 
 cudaError_t launch_norm_residual(const NormArgs &a, int num_sms, cudaStream_t s)
 {
-    if (a.width <= 256) return launch_rows<1, 32>(a, num_sms, s);
-    if (a.width <= 512) return launch_rows<2, 32>(a, num_sms, s);
-    if (a.width <= 1024) return launch_rows<4, 32>(a, num_sms, s);
-    if (a.width <= 2048) return launch_rows<2, kNormThreads>(a, num_sms, s);
-    if (a.width <= 4096) return launch_rows<4, kNormThreads>(a, num_sms, s);
-    return launch_rows<8, kNormThreads>(a, num_sms, s);
+    return a.rows >= 8 * num_sms ? launch_width<kNormRows>(a, s) : launch_width<1>(a, s);
 }
 
 }  // namespace f3dc

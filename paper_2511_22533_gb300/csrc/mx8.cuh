@@ -89,36 +89,59 @@ F3DC_DEV uint32_t pack_e4m3x4(float a, float b, float c, float d)
     return r;
 }
 
-// Quantises N consecutive values of a row, the share of this lane in a block that
-// `LANES` neighbouring lanes hold together: v becomes the quotients (at most 448 in
-// magnitude; NaN for NaN and for infinities, which e4m3 does not have), the scale
-// byte is returned.  Every lane of the warp calls it; absent values are zeros.
-// fmaxf passes over NaN, so the plain maximum is infinite only with an infinity among
-// the values: the rare block that has one takes the maximum of the finite ones.
+// Quantises N consecutive values of each of R rows, the share of this lane in a block of
+// each that `LANES` neighbouring lanes hold together: v becomes the quotients (at most 448
+// in magnitude; NaN for NaN and for infinities, which e4m3 does not have), byte the scale
+// bytes.  Every lane of the warp calls it; absent values are zeros.  fmaxf passes over
+// NaN, so the plain maximum is infinite only with an infinity among the values: the rare
+// block that has one takes the maximum of the finite ones.
+template <int R, int N, int LANES>
+F3DC_DEV void quantize_blocks(float (&v)[R][N], uint32_t (&byte)[R])
+{
+    const float inf = __int_as_float(0x7F800000);
+    float top[R];
+    auto maxima = [&] {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            top[i] = 0.f;
+#pragma unroll
+            for (int j = 0; j + 1 < N; j += 2) top[i] = fmax3(top[i], fabsf(v[i][j]), fabsf(v[i][j + 1]));
+        }
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < R; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+    };
+    maxima();
+    bool some = false;
+#pragma unroll
+    for (int i = 0; i < R; ++i) some |= top[i] == inf;
+    if (__any_sync(0xffffffffu, some)) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (fabsf(v[i][j]) == inf) v[i][j] = __int_as_float(0x7FC00000);
+        maxima();
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        byte[i] = e8m0_byte(top[i]);
+        const float inv = e8m0_inverse(byte[i]);
+#pragma unroll
+        for (int j = 0; j + 1 < N; j += 2) {
+            const f32x2 q = fmul2({v[i][j], v[i][j + 1]}, {inv, inv});
+            v[i][j] = q.x, v[i][j + 1] = q.y;
+        }
+    }
+}
 template <int N, int LANES>
 F3DC_DEV uint32_t quantize_block(float (&v)[N])
 {
-    const float inf = __int_as_float(0x7F800000);
-    float top = 0.f;
-#pragma unroll
-    for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[j]));
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (__any_sync(0xffffffffu, top == inf)) {
-        top = 0.f;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            if (fabsf(v[j]) == inf) v[j] = __int_as_float(0x7FC00000);
-            top = fmaxf(top, fabsf(v[j]));
-        }
-#pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    }
-    const uint32_t byte = e8m0_byte(top);
-    const float inv = e8m0_inverse(byte);
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[j] *= inv;
-    return byte;
+    static_assert(N % 2 == 0, "pairs");
+    uint32_t byte[1];
+    quantize_blocks<1, N, LANES>(reinterpret_cast<float (&)[1][N]>(v), byte);
+    return byte[0];
 }
 
 }  // namespace f3dc

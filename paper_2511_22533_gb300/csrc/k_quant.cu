@@ -6,8 +6,10 @@
 // the conversion's and the result is the same bit for bit in whatever order.
 //
 // Bound by memory: x is read once, one byte and 1/128 written per element.  A block
-// is held by 8 lanes, 16 elements each (rows that start on 16 bytes), or by a whole
-// warp (any other row).
+// is held by 8 lanes, 16 elements each.  Where there is more than a wave of work a warp
+// takes two groups of four blocks at a time, so that enough loads are in flight (32768 x
+// 4096 bf16: 74 us with one, 68 with two); where there is not, one is less latency (955
+// rows: 2.7 and 4.2 us).
 #include "kernels.h"
 #include "mx8.cuh"
 
@@ -17,45 +19,84 @@ namespace {
 
 constexpr int kQuantThreads = 256;
 
-// 16 consecutive elements of a row from 16-byte aligned memory, zeros from n on
+// 16 elements as 32-bit words: 8 of bf16 pairs, 16 of fp32
 template <bool F32>
-F3DC_DEV void load16(const void *row, int col, int n, float (&v)[16])
+struct Words {
+    static constexpr int kN = F32 ? 16 : 8;
+    uint32_t w[kN];
+};
+
+F3DC_DEV uint4 load_stream(const void *p) { return __ldcs(reinterpret_cast<const uint4 *>(p)); }
+
+// Elements col .. col + 15 of a row, zeros from n on.  ALIGNED: the row starts on 16
+// bytes.  Otherwise the 16-byte pieces that hold the elements are read and shifted
+// into place; `edge` (the matrix's first and last elements, whose pieces may reach out
+// of it) and a row's last elements are read one by one.
+template <bool F32, bool ALIGNED>
+F3DC_DEV void load16(const uint8_t *row, int col, int n, bool edge, Words<F32> &x)
 {
-    if (n >= 16) {
-        if constexpr (F32) {
-            const float4 *p = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(row) + col);
+    constexpr int N = Words<F32>::kN;
+    const uint8_t *p = row + (int64_t)col * (F32 ? 4 : 2);
+    if (n < 16 || (!ALIGNED && edge)) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float4 u = __ldcs(p + q);
-                v[4 * q] = u.x, v[4 * q + 1] = u.y, v[4 * q + 2] = u.z, v[4 * q + 3] = u.w;
-            }
-        } else {
-            const uint4 *p = reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(row) + col);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const uint4 u = __ldcs(p + q);
-                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[8 * q + 2 * j] = bf16_bits_to_f32(w[j] & 0xFFFFu);
-                    v[8 * q + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-                }
+        for (int j = 0; j < N; ++j) {
+            if constexpr (F32) {
+                x.w[j] = j < n ? reinterpret_cast<const uint32_t *>(p)[j] : 0u;
+            } else {
+                const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+                x.w[j] = (2 * j < n ? (uint32_t)h[2 * j] : 0u) | (2 * j + 1 < n ? (uint32_t)h[2 * j + 1] << 16 : 0u);
             }
         }
         return;
     }
+    if constexpr (ALIGNED) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        v[j] = 0.f;
-        if (j < n)
-            v[j] = F32 ? reinterpret_cast<const float *>(row)[col + j]
-                       : bf16_bits_to_f32(reinterpret_cast<const uint16_t *>(row)[col + j]);
+        for (int c = 0; c < N / 4; ++c) {
+            const uint4 u = load_stream(p + 16 * c);
+            x.w[4 * c] = u.x, x.w[4 * c + 1] = u.y, x.w[4 * c + 2] = u.z, x.w[4 * c + 3] = u.w;
+        }
+    } else {
+        const uint32_t off = (uint32_t)(uintptr_t)p & 15u;
+        const uint8_t *a = p - off;
+        uint32_t w[N + 4];
+#pragma unroll
+        for (int c = 0; c < N / 4; ++c) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(a + 16 * c);
+            w[4 * c] = u.x, w[4 * c + 1] = u.y, w[4 * c + 2] = u.z, w[4 * c + 3] = u.w;
+        }
+        w[N] = w[N + 1] = w[N + 2] = w[N + 3] = 0u;
+        if (off) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(a + 4 * N);
+            w[N] = u.x, w[N + 1] = u.y, w[N + 2] = u.z, w[N + 3] = u.w;
+        }
+        if (off & 8u) {
+#pragma unroll
+            for (int j = 0; j < N + 2; ++j) w[j] = w[j + 2];
+        }
+        if (off & 4u) {
+#pragma unroll
+            for (int j = 0; j < N + 1; ++j) w[j] = w[j + 1];
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) x.w[j] = F32 ? w[j] : __funnelshift_r(w[j], w[j + 1], 8 * (off & 2u));
     }
 }
 
-// Rows that start on 16 bytes (x, q): a warp takes four blocks at a time.
 template <bool F32>
-__global__ void __launch_bounds__(kQuantThreads) k_quantize(const QuantArgs a)
+F3DC_DEV void unpack(const Words<F32> &x, float (&v)[16])
+{
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        v[j] = __uint_as_float(F32 ? x.w[j & (Words<F32>::kN - 1)] : (j & 1 ? x.w[j / 2] & 0xFFFF0000u : x.w[j / 2] << 16));
+}
+
+// Resident CTAs per SM: 40 registers for bf16, up to 80 for the 64 bytes per lane of fp32.
+constexpr int quant_ctas(bool f32) { return f32 ? 3 : 6; }
+
+// ALIGNED: rows of x start on 16 bytes.  WIDE: rows of q do; otherwise bytes are stored
+// one by one.  U groups of four blocks per warp and step.
+template <bool F32, bool ALIGNED, bool WIDE, int U>
+__global__ void __launch_bounds__(kQuantThreads, quant_ctas(F32)) k_quantize(const QuantArgs a)
 {
     griddep_launch();
     griddep_wait();
@@ -63,83 +104,59 @@ __global__ void __launch_bounds__(kQuantThreads) k_quantize(const QuantArgs a)
     const int chunks = (a.cols + 511) / 512;  // of four blocks
     const int64_t items = (int64_t)a.rows * chunks;
     const int64_t step = (int64_t)gridDim.x * (kQuantThreads / 32);
-    for (int64_t it = (int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5); it < items; it += step) {
-        const int64_t row = it / chunks;
-        const int col = (int)(it - row * chunks) * 512 + lane * 16;
-        const int n = a.cols - col;  // this lane's elements (more than 16, or none, too)
-        float v[16];
-        load16<F32>(reinterpret_cast<const uint8_t *>(a.x) + row * a.ldx * (F32 ? 4 : 2), col, n, v);
-        const uint32_t byte = quantize_block<16, 8>(v);
-        uint4 u;
-        u.x = pack_e4m3x4(v[0], v[1], v[2], v[3]);
-        u.y = pack_e4m3x4(v[4], v[5], v[6], v[7]);
-        u.z = pack_e4m3x4(v[8], v[9], v[10], v[11]);
-        u.w = pack_e4m3x4(v[12], v[13], v[14], v[15]);
-        uint8_t *q = a.q + row * a.ldq + col;
-        if (n >= 16) {
-            *reinterpret_cast<uint4 *>(q) = u;
-        } else {
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    for (int64_t it = (int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5); it < items; it += U * step) {
+        Words<F32> x[U];
+        int64_t row[U];
+        int col[U], n[U];
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (j < n) q[j] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = it + u * step;
+            row[u] = i / chunks;
+            col[u] = (int)(i - row[u] * chunks) * 512 + lane * 16;
+            n[u] = i < items ? a.cols - col[u] : 0;  // this lane's elements (more than 16, or none, too)
+            const bool edge = (row[u] == 0 && col[u] == 0) || (row[u] == a.rows - 1 && n[u] < 32);
+            load16<F32, ALIGNED>(reinterpret_cast<const uint8_t *>(a.x) + row[u] * a.ldx * (F32 ? 4 : 2), col[u], n[u], edge, x[u]);
         }
-        if (lane % 8 == 0 && n > 0) a.scales[row * a.lds + col / kScaleBlock] = (uint8_t)byte;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[16];
+            unpack<F32>(x[u], v);
+            const uint32_t byte = quantize_block<16, 8>(v);
+            const uint32_t w[4] = {pack_e4m3x4(v[0], v[1], v[2], v[3]), pack_e4m3x4(v[4], v[5], v[6], v[7]),
+                                   pack_e4m3x4(v[8], v[9], v[10], v[11]), pack_e4m3x4(v[12], v[13], v[14], v[15])};
+            uint8_t *q = a.q + row[u] * a.ldq + col[u];
+            if (WIDE && n[u] >= 16) {
+                __stcs(reinterpret_cast<uint4 *>(q), make_uint4(w[0], w[1], w[2], w[3]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (j < n[u]) q[j] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
+            }
+            if (lane % 8 == 0 && n[u] > 0) a.scales[row[u] * a.lds + col[u] / kScaleBlock] = (uint8_t)byte;
+        }
     }
 }
 
-// Any rows: a warp takes four blocks, element 32 i + lane of the 512 in lane `lane`, so
-// that single-element loads and stores are whole sectors.
 template <bool F32>
-__global__ void __launch_bounds__(kQuantThreads) k_quantize_any(const QuantArgs a)
+cudaError_t launch_type(const QuantArgs &a, int num_sms, cudaStream_t s)
 {
-    griddep_launch();
-    griddep_wait();
-    const int lane = threadIdx.x & 31;
-    const int chunks = (a.cols + 511) / 512;
-    const int64_t items = (int64_t)a.rows * chunks;
-    const int64_t step = (int64_t)gridDim.x * (kQuantThreads / 32);
-    for (int64_t it = (int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5); it < items; it += step) {
-        const int64_t row = it / chunks;
-        const int col0 = (int)(it - row * chunks) * 512;
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int col = col0 + 32 * i + lane;
-            v[i] = 0.f;
-            if (col < a.cols)
-                v[i] = F32 ? __ldcs(reinterpret_cast<const float *>(a.x) + row * a.ldx + col)
-                           : bf16_bits_to_f32(__ldcs(reinterpret_cast<const uint16_t *>(a.x) + row * a.ldx + col));
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            float w[4] = {v[4 * b], v[4 * b + 1], v[4 * b + 2], v[4 * b + 3]};
-            const uint32_t byte = quantize_block<4, 32>(w);
-            const uint32_t u = pack_e4m3x4(w[0], w[1], w[2], w[3]);
-            const int col = col0 + kScaleBlock * b + lane;
-            uint8_t *q = a.q + row * a.ldq;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (col + 32 * j < a.cols) q[col + 32 * j] = (uint8_t)(u >> (8 * j));
-            if (lane == 0 && col < a.cols) a.scales[row * a.lds + col / kScaleBlock] = (uint8_t)byte;
-        }
-    }
+    const int64_t items = (int64_t)a.rows * ((a.cols + 511) / 512), per = kQuantThreads / 32;
+    const int64_t ctas = (items + per - 1) / per, most = (int64_t)num_sms * quant_ctas(F32);
+    const dim3 g((unsigned)(ctas < most ? ctas : most)), b(kQuantThreads);
+    const bool two = ctas > 2 * most;
+    const bool aligned = ((uintptr_t)a.x & 15) == 0 && (a.ldx * (F32 ? 4 : 2)) % 16 == 0;
+    const bool wide = ((uintptr_t)a.q & 15) == 0 && a.ldq % 16 == 0;
+    if (!wide) return launch_k(k_quantize<F32, false, false, 1>, g, b, 0, s, a);
+    if (aligned)
+        return two ? launch_k(k_quantize<F32, true, true, 2>, g, b, 0, s, a) : launch_k(k_quantize<F32, true, true, 1>, g, b, 0, s, a);
+    return two ? launch_k(k_quantize<F32, false, true, 2>, g, b, 0, s, a) : launch_k(k_quantize<F32, false, true, 1>, g, b, 0, s, a);
 }
 
 }  // namespace
 
 cudaError_t launch_quantize(const QuantArgs &a, bool f32, int num_sms, cudaStream_t s)
 {
-    const int64_t items = (int64_t)a.rows * ((a.cols + 511) / 512), per = kQuantThreads / 32;
-    const int64_t most = (int64_t)num_sms * 8;  // resident CTAs
-    const int grid = (int)((items + per - 1) / per < most ? (items + per - 1) / per : most);
-    const bool aligned = ((uintptr_t)a.x & 15) == 0 && (a.ldx * (f32 ? 4 : 2)) % 16 == 0 &&
-                         ((uintptr_t)a.q & 15) == 0 && a.ldq % 16 == 0;
-    if (aligned)
-        return f32 ? launch_k(k_quantize<true>, dim3(grid), dim3(kQuantThreads), 0, s, a)
-                   : launch_k(k_quantize<false>, dim3(grid), dim3(kQuantThreads), 0, s, a);
-    return f32 ? launch_k(k_quantize_any<true>, dim3(grid), dim3(kQuantThreads), 0, s, a)
-               : launch_k(k_quantize_any<false>, dim3(grid), dim3(kQuantThreads), 0, s, a);
+    return f32 ? launch_type<true>(a, num_sms, s) : launch_type<false>(a, num_sms, s);
 }
 
 }  // namespace f3dc

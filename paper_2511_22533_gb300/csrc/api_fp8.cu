@@ -80,6 +80,16 @@ extern "C" f3dc_status f3dc_gemm_fp8(const void *A, int64_t lda, const void *a_s
     if (misaligned(A, 16) || misaligned(B, 16) || misaligned(out, 16) || misaligned(bias, 16) || misaligned(gate, 16))
         return bad("pointers must be 16-byte aligned");
     if (misaligned(a_scales, 4) || misaligned(b_scales, 4)) return bad("a_scales and b_scales must be 4-byte aligned");
+    const int epi = epilogue == F3DC_EPI_BIAS ? kEpiBias : (epilogue == F3DC_EPI_GELU ? kEpiGelu : kEpiResid);
+    if (gemm8_few_rows(M, N, K)) {
+        const FewArgs g{M, N, K, (const uint8_t *)A, lda, (const uint8_t *)a_scales, ldas, (const uint8_t *)B, ldb,
+                        (const uint8_t *)b_scales, ldbs, (const bf16 *)bias, gate, out, ldo, (uint8_t *)out_scales, ldos};
+        int sms = 0;
+        cudaError_t e = sm_count(&sms);
+        if (e != cudaSuccess) return fail(F3DC_ERR_CUDA, "device query", e);
+        e = launch_few8(g, epi, sms, (cudaStream_t)stream);
+        return e == cudaSuccess ? F3DC_OK : fail(F3DC_ERR_CUDA, "launch", e);
+    }
     Gemm8Params p;
     p.M = M;
     p.N = N;
@@ -105,7 +115,6 @@ extern "C" f3dc_status f3dc_gemm_fp8(const void *A, int64_t lda, const void *a_s
     ok = ok && make_tmap_rows(&to, out8 ? u8 : (esz == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16),
                               out, M, N, ldo * esz, 32, 128 / esz);
     if (!ok) return bad("cuTensorMapEncodeTiled rejected A, B or out");
-    const int epi = epilogue == F3DC_EPI_BIAS ? kEpiBias : (epilogue == F3DC_EPI_GELU ? kEpiGelu : kEpiResid);
     const cudaError_t e = launch_gemm8_pair(&ta, &tb, &to, p, epi, out8, (cudaStream_t)stream);
     return e == cudaSuccess ? F3DC_OK : fail(F3DC_ERR_CUDA, "launch", e);
 }

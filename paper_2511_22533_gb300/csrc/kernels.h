@@ -382,6 +382,35 @@ struct Gemm8Params {
 cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
                               int epi, bool out8, cudaStream_t s);
 
+// The same product for few rows, and f3dc_gemm_fp8's rule for it.  It reads the weights
+// once for every 16 rows, about 1.8 us + 0.42 us per 2^20 of them; CTA pairs take 5 us and
+// 0.22 per 128 K whatever the rows.  Few rows / pairs, us:
+//   M x N x K      1 x 4096 x 1024 2.7 / 8.4, 16 x 4096 x 4096 8.2 / 14, 16 x 8192 x 8192
+//   29 / 24, 32 x 4096 x 1024 5.8 / 7.7, 32 x 4096 x 4096 15 / 14, 48 x 4096 x 1024 8.2 /
+//   7.7, 64 x 1024 x 4096 7.7 / 13.4, 64 x 4096 x 1024 10.1 / 7.7.
+inline bool gemm8_few_rows(int M, int N, int K)
+{
+    return M <= 64 && (int64_t)K * ((int64_t)(M + 15) / 16 * N - 4096) < 7600000;
+}
+struct FewArgs {
+    int M, N, K;
+    const uint8_t *A;
+    int64_t lda;
+    const uint8_t *sa;
+    int64_t ldas;
+    const uint8_t *B;
+    int64_t ldb;
+    const uint8_t *sb;
+    int64_t ldbs;
+    const bf16 *bias;         // nullable
+    const float *gate;        // nullable (RESID)
+    void *out;
+    int64_t ldo;              // elements
+    uint8_t *out_scales;      // 8-bit output where given
+    int64_t ldos;
+};
+cudaError_t launch_few8(const FewArgs &a, int epi, int num_sms, cudaStream_t s);
+
 // norm of y, gate, residual, norm of the sum and modulation (f3dc_norm_residual)
 enum NormKind { kNormNone = 0, kNormLayer = 1, kNormRms = 2 };
 struct NormArgs {

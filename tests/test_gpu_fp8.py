@@ -124,7 +124,8 @@ def operands(M, N, K, seed):
 
 # below, at and above the sizes of a row pair, a column unit, a scale block and a set of
 # four; one row; ragged N; full waves with a rest (76 clusters: 80, 96 and 256 tiles)
-SHAPES = [(1, 8, 1), (1, 128, 128), (2, 64, 31), (5, 72, 129), (127, 256, 512), (128, 264, 513), (129, 200, 640),
+SHAPES = [(1, 8, 1), (1, 128, 128), (2, 64, 31), (5, 72, 129), (8, 1024, 4096), (9, 136, 1500), (17, 4096, 1024), (32, 264, 640),
+          (33, 264, 640), (127, 256, 512), (128, 264, 513), (129, 200, 640),
           (255, 1000, 1374), (256, 256, 128), (257, 512, 2048), (300, 1088, 700), (64, 4096, 1024), (1229, 4096, 384),
           (1300, 4096, 256), (4096, 4096, 128), (2600, 1960, 1100)]
 
@@ -151,7 +152,8 @@ def test_gemm_fp8(M, N, K, epi):
     assert f3dc.gemm_status() == 0
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 16, 16), (3, 128, 128), (129, 144, 300), (255, 1008, 1374), (300, 4096, 512),
+@pytest.mark.parametrize("M,N,K", [(1, 16, 16), (3, 128, 128), (1, 4096, 1024), (11, 1040, 1300), (32, 144, 4096),
+                                   (33, 144, 300), (129, 144, 300), (255, 1008, 1374), (300, 4096, 512),
                                    (955, 1152, 1024), (4000, 2048, 256)])
 @pytest.mark.parametrize("epi", [f3dc.EPI_BIAS, f3dc.EPI_GELU])
 def test_gemm_fp8_8bit_output(M, N, K, epi):
@@ -199,9 +201,10 @@ def test_gemm_fp8_scales_of_both_operands_apply_to_their_blocks():
     assert torch.equal(out.double(), y)
 
 
-def test_gemm_fp8_scale_range():
+@pytest.mark.parametrize("M", [3, 64])
+def test_gemm_fp8_scale_range(M):
     # scales far apart whose products are moderate, zero rows under the smallest scale
-    M, N, K = 64, 64, 256
+    N, K = 64, 256
     A, sa, B, sb = operands(M, N, K, 5)
     for da, db in ((100, -100), (-110, 110), (60, -20)):
         sa2, sb2 = (sa.int() + da).clamp(0, 254).to(torch.uint8), (sb.int() + db).clamp(0, 254).to(torch.uint8)
@@ -211,16 +214,17 @@ def test_gemm_fp8_scale_range():
         assert torch.all((out.double() - y).abs() <= 1.01 * err + R.U32 * y.abs())
 
 
-def test_gemm_fp8_nan_stays_in_its_row_and_column():
-    M, N, K = 200, 136, 512
+@pytest.mark.parametrize("M", [16, 200])
+def test_gemm_fp8_nan_stays_in_its_row_and_column(M):
+    N, K, last = 136, 512, M - 2
     A, sa, B, sb = operands(M, N, K, 6)
     A[3, 77] = 0x7F          # a NaN value
-    sa[150, 2] = 0xFF        # a NaN scale
+    sa[last, 2] = 0xFF       # a NaN scale
     B[70, 300] = 0xFF
     out = torch.zeros((M, N), dtype=torch.bfloat16, device=DEV)
     gemm8(A, sa, B, sb, K, f3dc.EPI_BIAS, None, None, out)
     want = torch.zeros((M, N), dtype=torch.bool, device=DEV)
-    want[3], want[150], want[:, 70] = True, True, True
+    want[3], want[last], want[:, 70] = True, True, True
     assert torch.equal(torch.isnan(out), want)
     # 8-bit output: NaN elements, and a scale from the finite ones
     q, s = R.storage(M, 144)

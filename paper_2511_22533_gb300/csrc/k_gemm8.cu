@@ -36,11 +36,12 @@ namespace {
 
 constexpr int kThreads8 = 384;
 constexpr int kOperand8 = 128 * 128;        // a stage's 128 K of A, or of up to 128 rows of B, per CTA
-constexpr int kStages8 = 5;
+constexpr int kStages8 = 4;
 constexpr int kSetBytes = 512 + 1024;       // scales of A's 128 rows, B's 256, four bytes each (512 K)
 constexpr int kSets = 4;                    // such sets in shared memory
 constexpr int kVecBytes8 = 8 * 2 * 128 * 4; // an epilogue warp's biases and gates of a unit
-constexpr int kOutBytes8 = 8 * 32 * 128;    // an epilogue warp's 32 rows of 128 bytes on their way out
+constexpr int kOutBox8 = 32 * 128;          // 32 rows of 128 bytes on their way out
+constexpr int kOutBytes8 = 8 * 2 * kOutBox8;  // two boxes for each epilogue warp
 constexpr uint32_t kTmemCols8 = 512;
 constexpr uint32_t kAcc1 = 232;             // first column of the second accumulator
 constexpr uint32_t kScaleCols = 488;        // two sets of 4 (A) + 8 (B) columns
@@ -166,35 +167,37 @@ F3DC_DEV void apply(uint32_t (&r)[32], const float *bias, const float *gate)
 }
 
 // Staged output of an epilogue warp: a box of its 32 rows x 128 bytes, the 16-byte piece c
-// of row r at 128 r + 16 (c ^ (r % 8)) (TMA 128B swizzle).  Lane 0 issues the stores and
-// waits before the box is written again until the last one has been read.  (Stores from
-// registers, or turned through shared memory into whole sectors, took 132 and 129 us
-// instead of 115 at 32768 x 4096 x 1024; a second box made no difference.)
+// of row r at 128 r + 16 (c ^ (r % 8)) (TMA 128B swizzle), in two boxes by turns.  Lane 0
+// issues the stores and waits before a box is written again until its last store has read
+// it.  (Stores from registers, or turned through shared memory into whole sectors, took
+// 132 and 129 us instead of 115 at 32768 x 4096 x 1024.  With one box a tile's second half
+// waits 2000 clocks for the first.)
 struct Stage8 {
     uint8_t *buf;
     const CUtensorMap *map;
-    int row, lane;
+    int row, lane, turn;
     F3DC_DEV void begin() const
     {
-        if (lane == 0) bulk_wait_read<0>();
+        if (lane == 0) bulk_wait_read<1>();
         __syncwarp();
     }
     F3DC_DEV void put16(int c, uint4 u) const
     {
-        *reinterpret_cast<uint4 *>(buf + lane * 128 + ((c ^ (lane & 7)) << 4)) = u;
+        *reinterpret_cast<uint4 *>(buf + turn * kOutBox8 + lane * 128 + ((c ^ (lane & 7)) << 4)) = u;
     }
     template <bool kReduce>
-    F3DC_DEV void send(int x) const
+    F3DC_DEV void send(int x)
     {
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
             if (kReduce)
-                tma_reduce_add_2d(map, buf, x, row);
+                tma_reduce_add_2d(map, buf + turn * kOutBox8, x, row);
             else
-                tma_store_2d(map, buf, x, row);
+                tma_store_2d(map, buf + turn * kOutBox8, x, row);
             bulk_commit();
         }
+        turn ^= 1;
     }
 };
 
@@ -251,17 +254,18 @@ __global__ void __launch_bounds__(kThreads8, 1)
         tmem_alloc_pair(tmem_holder, kTmemCols8);
         tmem_relinquish_pair();
     }
+    tc_fence_before();
+    // both CTAs' barriers are initialised (and tensor memory allocated) before any warp
+    // passes its cluster_wait(); what needs neither runs before that
+    cluster_arrive();
     const int kb_n = (p.K + 127) / 128;  // scale blocks of a row
     const int cl = blockIdx.x >> 1, ncl = gridDim.x >> 1;
     int t = cl - ncl, m0 = 0, n0 = 0, bn = 0;
     bool more = U.next(t, ncl, m0, n0, bn);  // this cluster's first unit
-    tc_fence_before();
-    cluster_sync();  // both CTAs' barriers are initialised before any remote signal
-    tc_fence_after();
-    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
     griddep_wait();
 
     if (warp == 0) {
+        cluster_wait();
         if (lane == 0) {
             const uint32_t full_c = mapa_shared(smem_u32(full), 0);
             int s = 0;
@@ -287,8 +291,12 @@ __global__ void __launch_bounds__(kThreads8, 1)
             }
         produced:;
         }
+        __syncwarp();
     } else if (warp == 1) {
+        cluster_wait();
+        tc_fence_after();
         if (rank == 0) {
+            const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
             const uint64_t a_desc0 = make_sdesc(smem_u32(sa), 16, 1024, kSwizzle128);
             const uint64_t b_desc0 = make_sdesc(smem_u32(sb), 16, 1024, kSwizzle128);
             // 32 rows of 16 bytes: groups of 8 rows are 128 bytes apart
@@ -301,8 +309,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
             uint32_t over_ph = 0;
             auto copy_scales = [&] {
                 const int b = copied % kSets;
-                if (!warp_wait(&sfull[b], (copied / kSets) & 1, abort_flag, p.err)) return false;
-                if (copied >= 2 && !warp_wait(&empty[over_s], over_ph, abort_flag, p.err)) return false;
+                if (!warp_wait_near(&sfull[b], (copied / kSets) & 1, abort_flag, p.err)) return false;
+                if (copied >= 2 && !warp_wait_near(&empty[over_s], over_ph, abort_flag, p.err)) return false;
                 tc_fence_after();
                 const uint64_t sd = s_desc0 + (uint64_t)b * (kSetBytes >> 4);
                 const uint32_t col = tmem + kScaleCols + 12u * (uint32_t)(copied & 1);
@@ -319,16 +327,16 @@ __global__ void __launch_bounds__(kThreads8, 1)
 #pragma unroll 1
             while (more && ok) {
                 const int buf = it & 1;
-                if (!warp_wait(&acce[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.err)) break;
-                if (it > 0 && !warp_wait(shared_read, (it - 1) & 1, abort_flag, p.err)) break;
+                if (!warp_wait_near(&acce[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.err)) break;
+                if (it > 0 && !warp_wait_near(shared_read, (it - 1) & 1, abort_flag, p.err)) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (buf ? kAcc1 : 0u);
                 const uint32_t idesc0 = make_idesc_mxf8(256, 0, 0) | ((uint32_t)(bn >> 3) << 17);
-                const bool another = U.next(t, ncl, m0, n0, bn);
+                bool another = false;
 #pragma unroll 1
                 for (int kb = 0; kb < kb_n; ++kb) {
                     const uint32_t sfa = tmem + kScaleCols + 12u * (uint32_t)(set & 1);
-                    if (!ready && !warp_wait(&full[s], ph, abort_flag, p.err)) {
+                    if (!ready && !warp_wait_near(&full[s], ph, abort_flag, p.err)) {
                         ok = false;
                         break;
                     }
@@ -340,6 +348,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     mma_mxf8_pair_128k(d, a_desc0 + (uint64_t)s * (kOperand8 >> 4), b_desc0 + (uint64_t)s * (kOperand8 >> 4),
                                        sfa, sfa + 4, idesc0 | byte << 4 | byte << 29, kb != 0);
                     mma_commit_pair_mc_elect(&empty[s], 3);
+                    if (kb == 0) another = U.next(t, ncl, m0, n0, bn);
                     // the next set's scales are copied behind this set's first MMAs, which
                     // keep the tensor core busy until the copies run
                     const bool last = byte == 3 || kb + 1 == kb_n;
@@ -359,6 +368,12 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 ++it;
                 more = another;
             }
+            if (*abort_flag) {
+                // wait (bounded) for the MMAs in flight, which their issuing lane commits
+                mma_commit_pair_elect(drain);
+                if (lane == 0) wait_ns8(drain, 0, 100000000ull);
+                __syncwarp();
+            }
         }
     } else if (warp == 2) {
         // lane l: rows l, l + 32, l + 64, l + 96 of each 128, four scale bytes (512 K) of
@@ -370,40 +385,39 @@ __global__ void __launch_bounds__(kThreads8, 1)
             uint4 a[4], b[8];
         };
         const int per = p.scale_sets;
-        auto row_bytes = [&](const uint8_t *sc, int64_t ld, int r, int rows, int byte) {
-            uint4 w = make_uint4(0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-            if (r >= rows) return w;
-            const uint8_t *q = sc + r * ld + byte;
-            if (per == 4) return *reinterpret_cast<const uint4 *>(q);
-            if (per == 2) {
-                const uint2 h = *reinterpret_cast<const uint2 *>(q);
-                w.x = h.x, w.y = h.y;
-            } else {
-                w.x = *reinterpret_cast<const uint32_t *>(q);
+        // the bytes of 32 COUNT rows from row0 on (rows from `rows` on read the last row's,
+        // which nothing uses)
+        auto row_bytes = [&](uint4 *w, int count, const uint8_t *sc, int64_t ld, int row0, int rows, int byte) {
+            const uint8_t *q = sc + byte;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j >= count) break;
+                const uint8_t *r = q + (int64_t)min(row0 + 32 * j + lane, rows - 1) * ld;
+                if (per == 4)
+                    w[j] = *reinterpret_cast<const uint4 *>(r);
+                else if (per == 2)
+                    *reinterpret_cast<uint2 *>(&w[j]) = *reinterpret_cast<const uint2 *>(r);
+                else
+                    w[j].x = *reinterpret_cast<const uint32_t *>(r);
             }
-            return w;
         };
         auto load = [&](Group &x, int kb) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x.a[j] = row_bytes(p.sa, p.lda_s, m0 + (int)rank * 128 + 32 * j + lane, p.M, kb);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (32 * j < bn) x.b[j] = row_bytes(p.sb, p.ldb_s, n0 + 32 * j + lane, p.N, kb);
+            row_bytes(x.a, 4, p.sa, p.lda_s, m0 + (int)rank * 128, p.M, kb);
+            if (bn > 128)
+                row_bytes(x.b, 8, p.sb, p.ldb_s, n0, p.N, kb);
+            else
+                row_bytes(x.b, 4, p.sb, p.ldb_s, n0, p.N, kb);
         };
         const uint32_t sfull_c = mapa_shared(smem_u32(sfull), 0);
         Group x, next;
         if (more) load(x, 0);
+        cluster_wait();
         int kb = 0, n = 0;
         bool ok = true;
 #pragma unroll 1
         while (more && ok) {
             const int sets = min(per, (kb_n - kb + 3) / 4);
             kb += 4 * per;
-            if (kb >= kb_n) {
-                kb = 0;
-                more = U.next(t, ncl, m0, n0, bn);
-            }
-            if (more) load(next, kb);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (i >= sets || !ok) break;
@@ -419,6 +433,14 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(sfull_c + 8u * (uint32_t)b);
                 ++n;
+                if (i == 0) {
+                    // behind the release, which would wait for loads in flight
+                    if (kb >= kb_n) {
+                        kb = 0;
+                        more = U.next(t, ncl, m0, n0, bn);
+                    }
+                    if (more) load(next, kb);
+                }
             }
             x = next;
         }
@@ -427,13 +449,15 @@ __global__ void __launch_bounds__(kThreads8, 1)
         // the unit's columns (of 8-bit output a whole scale block)
         const int q = warp & 3, half = (warp - 4) >> 2;
         float *bias = sv + (warp - 4) * 256, *gate = bias + 128;
-        Stage8 o{so + (warp - 4) * 4096, &tmo, 0, lane};
+        Stage8 o{so + (warp - 4) * 2 * kOutBox8, &tmo, 0, lane, 0};
         const uint32_t acce_c = mapa_shared(smem_u32(acce), 0), shared_c = mapa_shared(smem_u32(shared_read), 0);
         auto arrive = [&](uint32_t bar) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(bar);
+            if (lane == 0) mbar_arrive_relaxed(bar);
         };
+        uint32_t tmem = 0;
+        if (!more) cluster_wait();  // (every warp waits once)
 #pragma unroll 1
         for (int it = 0; more; ++it) {
             // (a box of 128 bytes is the least that a warp stores)
@@ -441,12 +465,6 @@ __global__ void __launch_bounds__(kThreads8, 1)
             const int col0 = n0 + c0;
             o.row = m0 + (int)rank * 128 + q * 32;
             const bool mine = o.row < p.M && c0 < bn && col0 < p.N;
-            // the half that holds the 24 columns which the other accumulator shares, the
-            // last ones of a full first accumulator or the first of the second, reads
-            // them first
-            const bool from_end = bn == 256 && buf == 0;
-            const bool shares = half == (from_end ? 1 : 0);
-            const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (buf ? kAcc1 : 0u) + c0;
             // this unit's biases and gates, loaded while its sums run
             if (mine) {
                 __syncwarp();
@@ -459,7 +477,18 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 }
                 __syncwarp();
             }
+            // the half that holds the 24 columns which the other accumulator shares, the
+            // last ones of a full first accumulator or the first of the second, reads
+            // them first
+            const bool from_end = bn == 256 && buf == 0;
+            const bool shares = half == (from_end ? 1 : 0);
             more = U.next(t, ncl, m0, n0, bn);
+            if (it == 0) {
+                cluster_wait();
+                tc_fence_after();
+                tmem = *tmem_holder + ((uint32_t)(q * 32) << 16);
+            }
+            const uint32_t acc = tmem + (buf ? kAcc1 : 0u) + c0;
             if (!warp_wait(&accf[buf], (it >> 1) & 1, abort_flag, p.err)) break;
             tc_fence_after();
             if (!mine) {
@@ -540,22 +569,18 @@ __global__ void __launch_bounds__(kThreads8, 1)
             }
         }
         if (lane == 0) bulk_wait_all();
-    }
-    __syncthreads();
-    if (*abort_flag) {
-        if (warp == 1 && rank == 0) {
-            mma_commit_pair_elect(drain);  // the MMAs' issuing lane
-            if (lane == 0) wait_ns8(drain, 0, 100000000ull);
-        }
-        if (threadIdx.x == 0) spin_ns(200000);
-        __syncthreads();
+        __syncwarp();
+    } else {
+        cluster_wait();
     }
     // neither CTA leaves while the other may still signal its barriers or
     // (the even CTA's MMAs) write its TMEM
-    cluster_sync();
+    cluster_arrive();
+    cluster_wait();
+    if (*abort_flag) spin_ns(200000);  // loads in flight land
     if (warp == 3) {
         tc_fence_after();
-        tmem_dealloc_pair(tmem, kTmemCols8);
+        tmem_dealloc_pair(*tmem_holder, kTmemCols8);
     }
 }
 

@@ -36,16 +36,34 @@ namespace {
 
 constexpr int kThreads8 = 384;
 constexpr int kOperand8 = 128 * 128;        // a stage's 128 K of A, or of up to 128 rows of B, per CTA
-constexpr int kStages8 = 4;
+constexpr int kMaxStages8 = 8;
 constexpr int kSetBytes = 512 + 1024;       // scales of A's 128 rows, B's 256, four bytes each (512 K)
 constexpr int kSets = 4;                    // such sets in shared memory
 constexpr int kVecBytes8 = 8 * 2 * 128 * 4; // an epilogue warp's biases and gates of a unit
 constexpr int kOutBox8 = 32 * 128;          // 32 rows of 128 bytes on their way out
-constexpr int kOutBytes8 = 8 * 2 * kOutBox8;  // two boxes for each epilogue warp
 constexpr uint32_t kTmemCols8 = 512;
 constexpr uint32_t kAcc1 = 232;             // first column of the second accumulator
 constexpr uint32_t kScaleCols = 488;        // two sets of 4 (A) + 8 (B) columns
-constexpr size_t kSmem8 = 1024 + (size_t)kStages8 * 2 * kOperand8 + kSets * kSetBytes + kVecBytes8 + kOutBytes8 + 256;
+// What shared memory holds beside the scales: stages of operands (b_bytes of B in each,
+// this CTA's half of the widest unit's rows) and output boxes per epilogue warp.
+struct Depth8 {
+    int stages, boxes, b_bytes;
+    size_t smem() const
+    {
+        return 1024 + (size_t)stages * (kOperand8 + b_bytes) + kSets * kSetBytes + kVecBytes8 + (size_t)boxes * 8 * kOutBox8 + 256;
+    }
+};
+constexpr size_t kMostSmem8 = 227 * 1024;
+// Short sums of full units: a unit's epilogue is as long as its sum, and the second box
+// saves it a wait; long ones: a fifth stage instead (8192 x 4096 x 4096 101 -> 98 us, 32768
+// x 1024 x 4096 residual 110 -> 103; 32768 x 4096 x 1024 121 instead of 113).  Narrow units
+// leave room for more stages: the loads' latency counts most where there is one unit.
+inline Depth8 depth8(int kb_n, int width)
+{
+    Depth8 d{1, kb_n >= 16 || width < 256 ? 1 : 2, width / 2 * 128};
+    while (d.stages < kMaxStages8 && Depth8{d.stages + 1, d.boxes, d.b_bytes}.smem() <= kMostSmem8) ++d.stages;
+    return d;
+}
 
 // n / d and n % d for n < 2^31 (d >= 1) by a multiplication (the round-up method).
 struct FastDiv {
@@ -167,7 +185,7 @@ F3DC_DEV void apply(uint32_t (&r)[32], const float *bias, const float *gate)
 }
 
 // Staged output of an epilogue warp: a box of its 32 rows x 128 bytes, the 16-byte piece c
-// of row r at 128 r + 16 (c ^ (r % 8)) (TMA 128B swizzle), in two boxes by turns.  Lane 0
+// of row r at 128 r + 16 (c ^ (r % 8)) (TMA 128B swizzle), in one box or two by turns.  Lane 0
 // issues the stores and waits before a box is written again until its last store has read
 // it.  (Stores from registers, or turned through shared memory into whole sectors, took
 // 132 and 129 us instead of 115 at 32768 x 4096 x 1024.  With one box a tile's second half
@@ -175,10 +193,15 @@ F3DC_DEV void apply(uint32_t (&r)[32], const float *bias, const float *gate)
 struct Stage8 {
     uint8_t *buf;
     const CUtensorMap *map;
-    int row, lane, turn;
+    int row, lane, turn, more;  // more: boxes beyond the first (0 or 1)
     F3DC_DEV void begin() const
     {
-        if (lane == 0) bulk_wait_read<1>();
+        if (lane == 0) {
+            if (more)
+                bulk_wait_read<1>();
+            else
+                bulk_wait_read<0>();
+        }
         __syncwarp();
     }
     F3DC_DEV void put16(int c, uint4 u) const
@@ -197,26 +220,26 @@ struct Stage8 {
                 tma_store_2d(map, buf + turn * kOutBox8, x, row);
             bulk_commit();
         }
-        turn ^= 1;
+        turn ^= more;
     }
 };
 
 template <int EPI, bool OUT8>
 __global__ void __launch_bounds__(kThreads8, 1)
     k_gemm8_pair(const __grid_constant__ CUtensorMap tma, const __grid_constant__ GemmPairB tmb,
-                 const __grid_constant__ CUtensorMap tmo, const Units8 U, const Gemm8Params p)
+                 const __grid_constant__ CUtensorMap tmo, const Units8 U, const Depth8 depth, const Gemm8Params p)
 {
-    constexpr int S = kStages8;
+    const int S = depth.stages;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *sa = smem;
     uint8_t *sb = sa + S * kOperand8;
-    uint8_t *ss = sb + S * kOperand8;
+    uint8_t *ss = sb + S * depth.b_bytes;
     float *sv = reinterpret_cast<float *>(ss + kSets * kSetBytes);
     uint8_t *so = ss + kSets * kSetBytes + kVecBytes8;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(so + kOutBytes8);
-    uint64_t *full = bars, *empty = full + S;              // operands of a stage there (even CTA) / used (both)
-    uint64_t *sfull = empty + S, *sempty = sfull + kSets;  // scales of a set there (even CTA) / copied (both)
+    uint64_t *bars = reinterpret_cast<uint64_t *>(so + depth.boxes * 8 * kOutBox8);
+    uint64_t *full = bars, *empty = full + kMaxStages8;    // operands of a stage there (even CTA) / used (both)
+    uint64_t *sfull = empty + kMaxStages8, *sempty = sfull + kSets;  // scales of a set there (even CTA) / copied (both)
     uint64_t *accf = sempty + kSets, *acce = accf + 2;     // accumulator complete (both) / read (even CTA)
     uint64_t *shared_read = acce + 2;                      // its columns that the next one needs are read (even CTA)
     uint64_t *drain = shared_read + 1;
@@ -282,7 +305,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     if (rank == 0) mbar_arrive_expect_tx(&full[s], bytes);
                     const uint32_t fb = full_c + 8u * (uint32_t)s;
                     tma_load_2d_pair(sa + s * kOperand8, &tma, kb * 128, row_a, fb);
-                    tma_load_2d_pair(sb + s * kOperand8, mb, kb * 128, row_b, fb);
+                    tma_load_2d_pair(sb + s * depth.b_bytes, mb, kb * 128, row_b, fb);
                     if (++s == S) {
                         s = 0;
                         ph ^= 1;
@@ -327,7 +350,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
 #pragma unroll 1
             while (more && ok) {
                 const int buf = it & 1;
-                if (!warp_wait_near(&acce[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.err)) break;
+                if (it > 1 && !warp_wait_near(&acce[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.err)) break;
                 if (it > 0 && !warp_wait_near(shared_read, (it - 1) & 1, abort_flag, p.err)) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (buf ? kAcc1 : 0u);
@@ -345,7 +368,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     const uint32_t ph_next = s_next == 0 ? ph ^ 1 : ph;
                     ready = warp_all(mbar_test(&full[s_next], ph_next));
                     const uint32_t byte = (uint32_t)(kb & 3);
-                    mma_mxf8_pair_128k(d, a_desc0 + (uint64_t)s * (kOperand8 >> 4), b_desc0 + (uint64_t)s * (kOperand8 >> 4),
+                    mma_mxf8_pair_128k(d, a_desc0 + (uint64_t)s * (kOperand8 >> 4), b_desc0 + (uint64_t)s * (uint32_t)(depth.b_bytes >> 4),
                                        sfa, sfa + 4, idesc0 | byte << 4 | byte << 29, kb != 0);
                     mma_commit_pair_mc_elect(&empty[s], 3);
                     if (kb == 0) another = U.next(t, ncl, m0, n0, bn);
@@ -431,7 +454,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 dst[64] = make_uint4(word(x.b[4]), word(x.b[5]), word(x.b[6]), word(x.b[7]));
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(sfull_c + 8u * (uint32_t)b);
+                if (lane == 0) mbar_arrive_own_smem(sfull_c + 8u * (uint32_t)b);
                 ++n;
                 if (i == 0) {
                     // behind the release, which would wait for loads in flight
@@ -449,7 +472,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
         // the unit's columns (of 8-bit output a whole scale block)
         const int q = warp & 3, half = (warp - 4) >> 2;
         float *bias = sv + (warp - 4) * 256, *gate = bias + 128;
-        Stage8 o{so + (warp - 4) * 2 * kOutBox8, &tmo, 0, lane, 0};
+        Stage8 o{so + (warp - 4) * depth.boxes * kOutBox8, &tmo, 0, lane, 0, depth.boxes - 1};
         const uint32_t acce_c = mapa_shared(smem_u32(acce), 0), shared_c = mapa_shared(smem_u32(shared_read), 0);
         auto arrive = [&](uint32_t bar) {
             tc_fence_before();
@@ -497,28 +520,33 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 continue;
             }
             if constexpr (OUT8) {
-                // the 128 columns are one scale block of this lane's row
+                // The 128 columns are one scale block of this lane's row.  The chunk with the
+                // shared columns comes first; f has the chunks in the order of their reading.
+                auto chunk = [&](int i) { return from_end ? (i + 3) & 3 : i; };
                 float f[128];  // columns behind N: GELU of zero sums without a bias
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int i = 0; i < 4; ++i) {
                     uint32_t r[32];
-                    tmem_ld32(acc + 32 * k, r);
+                    tmem_ld32(acc + 32 * chunk(i), r);
                     wait_chunk(r);
-                    apply<EPI>(r, bias + 32 * k, gate);
+                    if (i == 0 && shares) arrive(shared_c);
+                    if (i == 3) arrive(acce_c + 8u * (uint32_t)buf);
+                    apply<EPI>(r, bias + 32 * chunk(i), gate);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) f[32 * k + j] = __uint_as_float(r[j]);
+                    for (int j = 0; j < 32; ++j) f[32 * i + j] = __uint_as_float(r[j]);
                 }
-                if (shares) arrive(shared_c);
-                arrive(acce_c + 8u * (uint32_t)buf);
                 const uint32_t byte = quantize_block<128, 1>(f);
                 if (o.row + lane < p.M) p.out_scales[(int64_t)(o.row + lane) * p.ldo_s + col0 / kScaleBlock] = (uint8_t)byte;
                 o.begin();
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const float *x = f + 16 * c;
-                    o.put16(c, make_uint4(pack_e4m3x4(x[0], x[1], x[2], x[3]), pack_e4m3x4(x[4], x[5], x[6], x[7]),
-                                          pack_e4m3x4(x[8], x[9], x[10], x[11]), pack_e4m3x4(x[12], x[13], x[14], x[15])));
-                }
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float *x = f + 32 * i + 16 * h;
+                        o.put16(2 * chunk(i) + h,
+                                make_uint4(pack_e4m3x4(x[0], x[1], x[2], x[3]), pack_e4m3x4(x[4], x[5], x[6], x[7]),
+                                           pack_e4m3x4(x[8], x[9], x[10], x[11]), pack_e4m3x4(x[12], x[13], x[14], x[15])));
+                    }
                 o.template send<false>(col0);
             } else {
                 const int chunks = width / 32;
@@ -603,12 +631,12 @@ cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtens
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3(2);
     cfg.blockDim = dim3(kThreads8);
-    cfg.dynamicSmemBytes = kSmem8;
+    cfg.dynamicSmemBytes = kMostSmem8;
     cfg.attrs = at;
     cfg.numAttrs = 1;
     int max_clusters = max_clusters_of[dev & 63].load(std::memory_order_acquire);
     if (!max_clusters) {
-        e = cudaFuncSetAttribute(k_gemm8_pair<EPI, OUT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem8);
+        e = cudaFuncSetAttribute(k_gemm8_pair<EPI, OUT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem8);
         if (e != cudaSuccess) return e;
         int n = 0;
         e = cudaOccupancyMaxActiveClusters(&n, k_gemm8_pair<EPI, OUT8>, &cfg);
@@ -623,10 +651,12 @@ cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtens
     const int clusters = units < max_clusters ? (int)units : max_clusters;
     Units8 u;
     u.set(p.M, p.N, clusters, width);
+    const Depth8 depth = depth8((p.K + 127) / 128, u.full ? 256 : 256 / u.sub);
+    cfg.dynamicSmemBytes = depth.smem();
     cfg.gridDim = dim3(2 * clusters);
     cfg.stream = s;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, k_gemm8_pair<EPI, OUT8>, *ta, *tb, *to, u, p);
+    e = cudaLaunchKernelEx(&cfg, k_gemm8_pair<EPI, OUT8>, *ta, *tb, *to, u, depth, p);
     if (e != cudaSuccess) return e;
     return cudaGetLastError();
 }

@@ -26,6 +26,14 @@ F3DC_DEV void mbar_arrive_relaxed(uint32_t cluster_addr)
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
+// Arrival that publishes this CTA's shared memory, already made visible to the async proxy
+// (fence_proxy_async_smem), to the tensor core that reads it in this CTA: a release at CTA
+// scope, wherever the mbarrier lies.
+F3DC_DEV void mbar_arrive_own_smem(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
 // the two halves of cluster_sync(), for whole warps
 F3DC_DEV void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 F3DC_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }

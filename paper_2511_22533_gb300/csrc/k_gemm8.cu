@@ -332,8 +332,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
             uint32_t over_ph = 0;
             auto copy_scales = [&] {
                 const int b = copied % kSets;
-                if (!warp_wait_near(&sfull[b], (copied / kSets) & 1, abort_flag, p.err)) return false;
-                if (copied >= 2 && !warp_wait_near(&empty[over_s], over_ph, abort_flag, p.err)) return false;
+                if (!warp_wait(&sfull[b], (copied / kSets) & 1, abort_flag, p.err)) return false;
+                if (copied >= 2 && !warp_wait(&empty[over_s], over_ph, abort_flag, p.err)) return false;
                 tc_fence_after();
                 const uint64_t sd = s_desc0 + (uint64_t)b * (kSetBytes >> 4);
                 const uint32_t col = tmem + kScaleCols + 12u * (uint32_t)(copied & 1);
@@ -350,8 +350,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
 #pragma unroll 1
             while (more && ok) {
                 const int buf = it & 1;
-                if (it > 1 && !warp_wait_near(&acce[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.err)) break;
-                if (it > 0 && !warp_wait_near(shared_read, (it - 1) & 1, abort_flag, p.err)) break;
+                if (it > 1 && !warp_wait(&acce[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.err)) break;
+                if (it > 0 && !warp_wait(shared_read, (it - 1) & 1, abort_flag, p.err)) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (buf ? kAcc1 : 0u);
                 const uint32_t idesc0 = make_idesc_mxf8(256, 0, 0) | ((uint32_t)(bn >> 3) << 17);
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
 #pragma unroll 1
                 for (int kb = 0; kb < kb_n; ++kb) {
                     const uint32_t sfa = tmem + kScaleCols + 12u * (uint32_t)(set & 1);
-                    if (!ready && !warp_wait_near(&full[s], ph, abort_flag, p.err)) {
+                    if (!ready && !warp_wait(&full[s], ph, abort_flag, p.err)) {
                         ok = false;
                         break;
                     }

@@ -38,16 +38,6 @@ F3DC_DEV void mbar_arrive_own_smem(uint32_t cluster_addr)
 F3DC_DEV void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 F3DC_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// warp_wait that looks again without sleeping for a while: the phase is near, and a
-// sleeping warp takes its time to wake
-F3DC_DEV bool warp_wait_near(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t *err)
-{
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-        if (warp_all(mbar_test(bar, parity))) return true;
-    return warp_wait(bar, parity, abort, err);
-}
-
 // D (+)= A B^T over a CTA pair (mma_bf16_pair_128k says which rows lie where), e4m3
 // operands with one E8M0 scale per row and 128 K.  The scales lie in tensor memory
 // (tmem_cp_scales_pair); each MMA takes the byte of a scale column that its instruction

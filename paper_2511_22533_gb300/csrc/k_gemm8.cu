@@ -100,6 +100,16 @@ struct Units8 {
         last_band = (pairs - 1) / kBand;
         last_high.set(pairs - last_band * kBand);
     }
+    // split sums: one unit of `width` columns (256 or 128) per cluster
+    int set_single(int M, int N_, int width)
+    {
+        set(M, N_, 1, width);  // (every unit is that wide, also behind N)
+        const int tiles = ((M + 255) / 256) * ((N + 255) / 256);
+        full = width == 256 ? tiles : 0;
+        sub = width == 256 ? 1 : 2;
+        total = tiles * sub;
+        return total;
+    }
     // unit u: first row m0 of the pair, first column n0, width bn (0: nothing to do)
     F3DC_DEV void decode(int u, int &m0, int &n0, int &bn) const
     {
@@ -224,7 +234,12 @@ struct Stage8 {
     }
 };
 
-template <int EPI, bool OUT8>
+// SPLIT: a cluster is two pairs that share the K of one unit, the first taking p.split_kb
+// blocks (whole scale sets).  Each pair finishes one half of the columns: its partial sums
+// of the other half go to the other pair's CTA of the same rows, into operand stages that
+// are no longer used, and are added to that CTA's own (two addends: their order does not
+// matter).
+template <int EPI, bool OUT8, bool SPLIT>
 __global__ void __launch_bounds__(kThreads8, 1)
     k_gemm8_pair(const __grid_constant__ CUtensorMap tma, const __grid_constant__ GemmPairB tmb,
                  const __grid_constant__ CUtensorMap tmo, const Units8 U, const Depth8 depth, const Gemm8Params p)
@@ -243,11 +258,16 @@ __global__ void __launch_bounds__(kThreads8, 1)
     uint64_t *accf = sempty + kSets, *acce = accf + 2;     // accumulator complete (both) / read (even CTA)
     uint64_t *shared_read = acce + 2;                      // its columns that the next one needs are read (even CTA)
     uint64_t *drain = shared_read + 1;
+    // SPLIT has one unit and two barriers to spare: the other pair's stages are free, its
+    // partial sums are here
+    uint64_t *other_done = &acce[1], *parts = &accf[1];
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(drain + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const uint32_t rank = __shfl_sync(0xffffffffu, cluster_rank(), 0);
+    const uint32_t crank = __shfl_sync(0xffffffffu, cluster_rank(), 0);
+    const uint32_t rank = crank & 1, pair = SPLIT ? crank >> 1 : 0, even = SPLIT ? crank & ~1u : 0;
+    const uint16_t both = (uint16_t)(3u << (2 * pair));  // this pair's CTAs
     griddep_launch();
 
     if (threadIdx.x == 64) {
@@ -264,10 +284,10 @@ __global__ void __launch_bounds__(kThreads8, 1)
             mbar_init(&sfull[b], 2);   // one scale warp in each CTA
             mbar_init(&sempty[b], 1);
         }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(&accf[b], 1);
-            mbar_init(&acce[b], 16);   // eight epilogue warps in each CTA
-        }
+        mbar_init(&accf[0], 1);
+        mbar_init(&accf[1], SPLIT ? 8 : 1);
+        mbar_init(&acce[0], 16);       // eight epilogue warps in each CTA
+        mbar_init(&acce[1], SPLIT ? 1 : 16);
         mbar_init(shared_read, 8);     // the four warps that hold the columns, in each CTA
         mbar_init(drain, 1);
         *abort_flag = 0;
@@ -281,8 +301,10 @@ __global__ void __launch_bounds__(kThreads8, 1)
     // both CTAs' barriers are initialised (and tensor memory allocated) before any warp
     // passes its cluster_wait(); what needs neither runs before that
     cluster_arrive();
-    const int kb_n = (p.K + 127) / 128;  // scale blocks of a row
-    const int cl = blockIdx.x >> 1, ncl = gridDim.x >> 1;
+    // scale blocks of a row, and the ones that this pair sums (from a whole set on)
+    const int kb_all = (p.K + 127) / 128;
+    const int kb_0 = SPLIT ? (int)pair * p.split_kb : 0, kb_n = SPLIT ? min(kb_all, kb_0 + p.split_kb) : kb_all;
+    const int cl = blockIdx.x / (SPLIT ? 4 : 2), ncl = gridDim.x / (SPLIT ? 4 : 2);
     int t = cl - ncl, m0 = 0, n0 = 0, bn = 0;
     bool more = U.next(t, ncl, m0, n0, bn);  // this cluster's first unit
     griddep_wait();
@@ -290,7 +312,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
     if (warp == 0) {
         cluster_wait();
         if (lane == 0) {
-            const uint32_t full_c = mapa_shared(smem_u32(full), 0);
+            const uint32_t full_c = mapa_shared(smem_u32(full), even);
             int s = 0;
             uint32_t ph = 0;
 #pragma unroll 1
@@ -300,7 +322,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 const int row_a = m0 + (int)rank * 128, row_b = n0 + (int)rank * (bn / 2);
                 const uint32_t bytes = 2u * (kOperand8 + (uint32_t)(bn / 2) * 128);  // both CTAs
 #pragma unroll 1
-                for (int kb = 0; kb < kb_n; ++kb) {
+                for (int kb = kb_0; kb < kb_n; ++kb) {
                     if (!mbar_wait(&empty[s], ph ^ 1, abort_flag, p.err)) goto produced;
                     if (rank == 0) mbar_arrive_expect_tx(&full[s], bytes);
                     const uint32_t fb = full_c + 8u * (uint32_t)s;
@@ -340,7 +362,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 tmem_cp_scales_pair(col, sd);
                 tmem_cp_scales_pair(col + 4, sd + (512 >> 4));
                 tmem_cp_scales_pair(col + 8, sd + (1024 >> 4));
-                mma_commit_pair_mc_elect(&sempty[b], 3);
+                mma_commit_pair_mc_elect(&sempty[b], both);
                 ++copied;
                 return true;
             };
@@ -357,7 +379,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 const uint32_t idesc0 = make_idesc_mxf8(256, 0, 0) | ((uint32_t)(bn >> 3) << 17);
                 bool another = false;
 #pragma unroll 1
-                for (int kb = 0; kb < kb_n; ++kb) {
+                for (int kb = kb_0; kb < kb_n; ++kb) {
                     const uint32_t sfa = tmem + kScaleCols + 12u * (uint32_t)(set & 1);
                     if (!ready && !warp_wait(&full[s], ph, abort_flag, p.err)) {
                         ok = false;
@@ -369,9 +391,9 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     ready = warp_all(mbar_test(&full[s_next], ph_next));
                     const uint32_t byte = (uint32_t)(kb & 3);
                     mma_mxf8_pair_128k(d, a_desc0 + (uint64_t)s * (kOperand8 >> 4), b_desc0 + (uint64_t)s * (uint32_t)(depth.b_bytes >> 4),
-                                       sfa, sfa + 4, idesc0 | byte << 4 | byte << 29, kb != 0);
-                    mma_commit_pair_mc_elect(&empty[s], 3);
-                    if (kb == 0) another = U.next(t, ncl, m0, n0, bn);
+                                       sfa, sfa + 4, idesc0 | byte << 4 | byte << 29, kb != kb_0);
+                    mma_commit_pair_mc_elect(&empty[s], both);
+                    if (kb == kb_0) another = U.next(t, ncl, m0, n0, bn);
                     // the next set's scales are copied behind this set's first MMAs, which
                     // keep the tensor core busy until the copies run
                     const bool last = byte == 3 || kb + 1 == kb_n;
@@ -387,7 +409,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     s = s_next;
                     ph = ph_next;
                 }
-                if (ok) mma_commit_pair_mc_elect(&accf[buf], 3);
+                if (ok) mma_commit_pair_mc_elect(&accf[buf], both);
                 ++it;
                 more = another;
             }
@@ -431,11 +453,11 @@ __global__ void __launch_bounds__(kThreads8, 1)
             else
                 row_bytes(x.b, 4, p.sb, p.ldb_s, n0, p.N, kb);
         };
-        const uint32_t sfull_c = mapa_shared(smem_u32(sfull), 0);
+        const uint32_t sfull_c = mapa_shared(smem_u32(sfull), even);
         Group x, next;
-        if (more) load(x, 0);
+        if (more) load(x, kb_0);
         cluster_wait();
-        int kb = 0, n = 0;
+        int kb = kb_0, n = 0;
         bool ok = true;
 #pragma unroll 1
         while (more && ok) {
@@ -459,7 +481,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 if (i == 0) {
                     // behind the release, which would wait for loads in flight
                     if (kb >= kb_n) {
-                        kb = 0;
+                        kb = kb_0;
                         more = U.next(t, ncl, m0, n0, bn);
                     }
                     if (more) load(next, kb);
@@ -473,7 +495,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
         const int q = warp & 3, half = (warp - 4) >> 2;
         float *bias = sv + (warp - 4) * 256, *gate = bias + 128;
         Stage8 o{so + (warp - 4) * depth.boxes * kOutBox8, &tmo, 0, lane, 0, depth.boxes - 1};
-        const uint32_t acce_c = mapa_shared(smem_u32(acce), 0), shared_c = mapa_shared(smem_u32(shared_read), 0);
+        const uint32_t acce_c = mapa_shared(smem_u32(acce), even), shared_c = mapa_shared(smem_u32(shared_read), even);
         auto arrive = [&](uint32_t bar) {
             tc_fence_before();
             __syncwarp();
@@ -484,10 +506,11 @@ __global__ void __launch_bounds__(kThreads8, 1)
 #pragma unroll 1
         for (int it = 0; more; ++it) {
             // (a box of 128 bytes is the least that a warp stores)
-            const int buf = it & 1, width = OUT8 ? 128 : (EPI == kEpiResid ? bn / 2 : max(64, bn / 2)), c0 = half * width;
-            const int col0 = n0 + c0;
+            const int slice = SPLIT ? bn / 2 : bn;  // columns that this pair finishes
+            const int buf = it & 1, width = OUT8 ? 128 : (EPI == kEpiResid ? slice / 2 : max(64, slice / 2)), c0 = half * width;
+            const int col0 = n0 + (int)pair * slice + c0;
             o.row = m0 + (int)rank * 128 + q * 32;
-            const bool mine = o.row < p.M && c0 < bn && col0 < p.N;
+            const bool mine = o.row < p.M && c0 < slice && col0 < p.N;
             // this unit's biases and gates, loaded while its sums run
             if (mine) {
                 __syncwarp();
@@ -503,7 +526,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
             // the half that holds the 24 columns which the other accumulator shares, the
             // last ones of a full first accumulator or the first of the second, reads
             // them first
-            const bool from_end = bn == 256 && buf == 0;
+            const bool from_end = !SPLIT && bn == 256 && buf == 0;
             const bool shares = half == (from_end ? 1 : 0);
             more = U.next(t, ncl, m0, n0, bn);
             if (it == 0) {
@@ -511,12 +534,49 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 tc_fence_after();
                 tmem = *tmem_holder + ((uint32_t)(q * 32) << 16);
             }
-            const uint32_t acc = tmem + (buf ? kAcc1 : 0u) + c0;
+            const uint32_t acc = tmem + (buf ? kAcc1 : 0u) + (uint32_t)pair * slice + c0;
             if (!warp_wait(&accf[buf], (it >> 1) & 1, abort_flag, p.err)) break;
             tc_fence_after();
+            // partial sums of this lane's row and this warp's columns: 16 bytes (4 columns)
+            // every 128 rows
+            const uint32_t part = 16u * (uint32_t)(q * 32 + lane) + 512u * (uint32_t)c0;
+            if constexpr (SPLIT) {
+                const uint32_t other = crank ^ 2u;  // the other pair's CTA of these rows
+                if (warp == 4 && lane == 0) mbar_arrive_relaxed(mapa_shared(smem_u32(other_done), other));
+                __syncwarp();
+                if (!warp_wait(other_done, 0, abort_flag, p.err)) break;
+                if (c0 < slice) {
+                    const uint32_t from = tmem + (uint32_t)((pair ^ 1) * slice + c0), dst = mapa_shared(smem_u32(sa) + part, other);
+#pragma unroll 1
+                    for (int c = 0; c < width; c += 32) {
+                        uint32_t r[32];
+                        tmem_ld32(from + c, r);
+                        wait_chunk(r);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4)
+                            store_cluster16(dst + 512u * (uint32_t)(c + j), r[j], r[j + 1], r[j + 2], r[j + 3]);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(parts), other));
+                if (!warp_wait_cluster(parts, 0, abort_flag, p.err)) break;
+            }
+            // adds the other pair's sums of columns c .. c + 31
+            auto join = [&](uint32_t (&r)[32], int c) {
+                if constexpr (SPLIT) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 v = *reinterpret_cast<const float4 *>(sa + part + 512 * (c + j));
+                        const f32x2 x0 = fadd2({__uint_as_float(r[j]), __uint_as_float(r[j + 1])}, {v.x, v.y});
+                        const f32x2 x1 = fadd2({__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])}, {v.z, v.w});
+                        r[j] = __float_as_uint(x0.x), r[j + 1] = __float_as_uint(x0.y);
+                        r[j + 2] = __float_as_uint(x1.x), r[j + 3] = __float_as_uint(x1.y);
+                    }
+                }
+            };
             if (!mine) {
-                if (shares) arrive(shared_c);
-                arrive(acce_c + 8u * (uint32_t)buf);
+                if (!SPLIT && shares) arrive(shared_c);
+                if (!SPLIT) arrive(acce_c + 8u * (uint32_t)buf);
                 continue;
             }
             if constexpr (OUT8) {
@@ -529,8 +589,9 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     uint32_t r[32];
                     tmem_ld32(acc + 32 * chunk(i), r);
                     wait_chunk(r);
-                    if (i == 0 && shares) arrive(shared_c);
-                    if (i == 3) arrive(acce_c + 8u * (uint32_t)buf);
+                    if (!SPLIT && i == 0 && shares) arrive(shared_c);
+                    if (!SPLIT && i == 3) arrive(acce_c + 8u * (uint32_t)buf);
+                    join(r, 32 * chunk(i));
                     apply<EPI>(r, bias + 32 * chunk(i), gate);
 #pragma unroll
                     for (int j = 0; j < 32; ++j) f[32 * i + j] = __uint_as_float(r[j]);
@@ -554,6 +615,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 // 32 columns: a box of fp32, half a box of bf16
                 auto finish = [&](uint32_t (&r)[32], int c) {
                     if (col0 + c >= p.N) return;
+                    join(r, c);
                     apply<EPI>(r, bias + c, gate + c);
                     if constexpr (EPI == kEpiResid) {
                         // x += gate y as an fp32 reduce-add of gate y
@@ -574,12 +636,12 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 uint32_t a[32], b[32];
                 tmem_ld32(acc + at(0), a);
                 wait_chunk(a);
-                if (shares) arrive(shared_c);
+                if (!SPLIT && shares) arrive(shared_c);
 #pragma unroll 1
                 for (int i = 0; i < chunks; i += 2) {
                     if (i + 1 < chunks)
                         tmem_ld32(acc + at(i + 1), b);
-                    else
+                    else if (!SPLIT)
                         arrive(acce_c + 8u * (uint32_t)buf);
                     if constexpr (EPI != kEpiResid) o.begin();
                     finish(a, at(i));
@@ -587,7 +649,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                         wait_chunk(b);
                         if (i + 2 < chunks)
                             tmem_ld32(acc + at(i + 2), a);
-                        else
+                        else if (!SPLIT)
                             arrive(acce_c + 8u * (uint32_t)buf);
                         finish(b, at(i + 1));
                         if (i + 2 < chunks) wait_chunk(a);
@@ -601,8 +663,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
     } else {
         cluster_wait();
     }
-    // neither CTA leaves while the other may still signal its barriers or
-    // (the even CTA's MMAs) write its TMEM
+    // no CTA leaves while another may still signal its barriers, (an even CTA's MMAs)
+    // write its TMEM or (SPLIT) its shared memory
     cluster_arrive();
     cluster_wait();
     if (*abort_flag) spin_ns(200000);  // loads in flight land
@@ -612,53 +674,98 @@ __global__ void __launch_bounds__(kThreads8, 1)
     }
 }
 
-template <int EPI, bool OUT8>
-cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p, cudaStream_t s)
+// Resident clusters of 2 (SPLIT: 4) CTAs on the current device.  They are counted, and the
+// kernel's shared-memory attribute set, on each device's first launch (0 = not yet).
+template <int EPI, bool OUT8, bool SPLIT>
+cudaError_t resident8(int *clusters)
 {
-    // per device: the shared-memory attribute and the resident-cluster count are
-    // taken on each device's first launch (0 = not yet known)
     static std::atomic<int> max_clusters_of[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    *clusters = max_clusters_of[dev & 63].load(std::memory_order_acquire);
+    if (*clusters) return cudaSuccess;
+    e = cudaFuncSetAttribute(k_gemm8_pair<EPI, OUT8, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem8);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[2];
+    cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.x = SPLIT ? 4 : 2;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(2);
+    cfg.gridDim = dim3(SPLIT ? 4 : 2);
     cfg.blockDim = dim3(kThreads8);
     cfg.dynamicSmemBytes = kMostSmem8;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    int max_clusters = max_clusters_of[dev & 63].load(std::memory_order_acquire);
-    if (!max_clusters) {
-        e = cudaFuncSetAttribute(k_gemm8_pair<EPI, OUT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem8);
-        if (e != cudaSuccess) return e;
-        int n = 0;
-        e = cudaOccupancyMaxActiveClusters(&n, k_gemm8_pair<EPI, OUT8>, &cfg);
-        if (e != cudaSuccess) return e;
-        if (n < 1) return cudaErrorInvalidConfiguration;
-        max_clusters = n;
-        max_clusters_of[dev & 63].store(n, std::memory_order_release);
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, k_gemm8_pair<EPI, OUT8, SPLIT>, &cfg);
+    if (e != cudaSuccess) return e;
+    if (n < 1) return cudaErrorInvalidConfiguration;
+    max_clusters_of[dev & 63].store(n, std::memory_order_release);
+    *clusters = n;
+    return cudaSuccess;
+}
+
+template <int EPI, bool OUT8, bool SPLIT>
+cudaError_t launch_units8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
+                          const Units8 &u, int width, int clusters, cudaStream_t s)
+{
+    const Depth8 depth = depth8(SPLIT ? p.split_kb : (p.K + 127) / 128, width);
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = SPLIT ? 4 : 2;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((SPLIT ? 4u : 2u) * (unsigned)clusters);
+    cfg.blockDim = dim3(kThreads8);
+    cfg.dynamicSmemBytes = depth.smem();
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_gemm8_pair<EPI, OUT8, SPLIT>, *ta, *tb, *to, u, depth, p);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// Width of the units of a split sum, 0: the sum is not split.  Few tiles leave clusters
+// idle that may take half of the K: it costs 2 us with units of 128 columns, 3.5 with 256
+// (64 KB per CTA change places), and saves 0.14 us per 128 K.  Whole / split, us:
+//   300 x 1024 x 4096 (units of 128) 13.4 / 10.9, 300 x 1024 x 8192 21.5 / 15.2, 300 x 2048 x
+//   2048 8.8 / 9.0; 1229 x 1024 x 4096 (256) 14.4 / 13.8, 1229 x 1024 x 8192 22.1 / 17.9, 600
+//   x 1024 x 4096 with 8-bit output, which needs whole scale blocks, 14.0 / 14.7.
+int split_width8(int M, int N, int kb_n, bool out8, int max_clusters)
+{
+    const int64_t tiles = (((int64_t)M + 255) / 256) * (((int64_t)N + 255) / 256);
+    if (kb_n >= 24 && !out8 && 2 * tiles <= max_clusters) return 128;
+    return kb_n >= (out8 ? 48 : 32) && tiles <= max_clusters ? 256 : 0;
+}
+
+template <int EPI, bool OUT8>
+cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, Gemm8Params p, cudaStream_t s)
+{
+    Units8 u;
+    int max_clusters = 0;
+    const int kb_n = (p.K + 127) / 128;
+    cudaError_t e = resident8<EPI, OUT8, true>(&max_clusters);
+    if (e != cudaSuccess) return e;
+    if (const int width = split_width8(p.M, p.N, kb_n, OUT8, max_clusters)) {
+        p.split_kb = ((kb_n + 1) / 2 + 3) / 4 * 4;
+        // the second pair's scale bytes start there: they are read as far as that is aligned
+        while (p.split_kb % (4 * p.scale_sets) != 0) p.scale_sets /= 2;
+        const int n = u.set_single(p.M, p.N, width);
+        return launch_units8<EPI, OUT8, true>(ta, tb, to, p, u, width, n, s);
     }
+    e = resident8<EPI, OUT8, false>(&max_clusters);
+    if (e != cudaSuccess) return e;
     // units: 64 columns (128 with 8-bit output) are the smallest
     constexpr int width = OUT8 ? 128 : 64;
     const int64_t units = (((int64_t)p.M + 255) / 256) * (((int64_t)p.N + width - 1) / width);
     const int clusters = units < max_clusters ? (int)units : max_clusters;
-    Units8 u;
     u.set(p.M, p.N, clusters, width);
-    const Depth8 depth = depth8((p.K + 127) / 128, u.full ? 256 : 256 / u.sub);
-    cfg.dynamicSmemBytes = depth.smem();
-    cfg.gridDim = dim3(2 * clusters);
-    cfg.stream = s;
-    cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, k_gemm8_pair<EPI, OUT8>, *ta, *tb, *to, u, depth, p);
-    if (e != cudaSuccess) return e;
-    return cudaGetLastError();
+    return launch_units8<EPI, OUT8, false>(ta, tb, to, p, u, u.full ? 256 : 256 / u.sub, clusters, s);
 }
 
 }  // namespace

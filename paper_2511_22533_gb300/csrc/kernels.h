@@ -375,6 +375,7 @@ struct Gemm8Params {
     const float *gate;        // nullable (RESID)
     uint8_t *out_scales;      // 8-bit output
     int64_t ldo_s;
+    int split_kb;             // set by the launch: a split sum's first pair takes so many blocks
     uint32_t *err;
 };
 // ta: A in boxes of 128 rows; tb: B in boxes of 128, 64 and 32 rows; to: the output in
@@ -382,15 +383,18 @@ struct Gemm8Params {
 cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
                               int epi, bool out8, cudaStream_t s);
 
-// The same product for few rows, and f3dc_gemm_fp8's rule for it.  It reads the weights
-// once for every 16 rows, about 1.8 us + 0.42 us per 2^20 of them; CTA pairs take 5 us and
-// 0.22 per 128 K whatever the rows.  Few rows / pairs, us:
-//   M x N x K      1 x 4096 x 1024 2.7 / 8.4, 16 x 4096 x 4096 8.2 / 14, 16 x 8192 x 8192
-//   29 / 24, 32 x 4096 x 1024 5.8 / 7.7, 32 x 4096 x 4096 15 / 14, 48 x 4096 x 1024 8.2 /
-//   7.7, 64 x 1024 x 4096 7.7 / 13.4, 64 x 4096 x 1024 10.1 / 7.7.
+// The same product for few rows, and f3dc_gemm_fp8's rule for it: it reads the weights
+// once for every 16 rows, about 1.8 us + 0.4 us per 2^20 of them, where CTA pairs take 4.6
+// us + 0.15 to 0.26 per 128 K.  Few rows / pairs, us:
+//   M     1024 x 1024   4096 x 1024   1024 x 4096   4096 x 4096   8192 x 8192   (N x K)
+//   1     2.4 / 5.6     2.7 / 6.9     4.1 / 9.4     6.8 / 12.1    25.1 / 25.7
+//   16    2.9 / 5.7     3.4 / 6.3     5.0 / 9.5     8.2 / 10.9    29.4 / 19.4
+//   32    3.2 / 5.8     5.8 / 6.3     5.1 / 9.6     15.1 / 10.6   55.4 / 19.6
+//   64    3.3 / 5.9     10.2 / 6.6    7.8 / 9.9     26.7 / 10.7   97.5 / 19.9
+//   77    4.9 / 5.9     12.1 / 6.6    12.2 / 10.0   31.9 / 10.8   122 / 20.2
 inline bool gemm8_few_rows(int M, int N, int K)
 {
-    return M <= 64 && (int64_t)K * ((int64_t)(M + 15) / 16 * N - 4096) < 7600000;
+    return M <= 64 && (int64_t)K * ((int64_t)(M + 15) / 16 * N - 2700) < 6000000;
 }
 struct FewArgs {
     int M, N, K;

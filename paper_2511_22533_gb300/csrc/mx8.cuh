@@ -34,6 +34,22 @@ F3DC_DEV void mbar_arrive_own_smem(uint32_t cluster_addr)
     asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
+// 16 bytes into the shared memory of a CTA of the cluster
+F3DC_DEV void store_cluster16(uint32_t cluster_addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(a), "r"(b), "r"(c), "r"(d)
+                 : "memory");
+}
+
+// mbar_wait by a whole warp for what other CTAs of the cluster have written before their
+// arrivals (mbar_arrive_cluster)
+F3DC_DEV bool warp_wait_cluster(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t *err)
+{
+    const bool ok = warp_wait(bar, parity, abort, err);
+    asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    return ok;
+}
+
 // the two halves of cluster_sync(), for whole warps
 F3DC_DEV void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 F3DC_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }

@@ -123,10 +123,13 @@ def operands(M, N, K, seed):
 
 
 # below, at and above the sizes of a row pair, a column unit, a scale block and a set of
-# four; one row; ragged N; full waves with a rest (76 clusters: 80, 96 and 256 tiles)
+# four; one row; ragged N; full waves with a rest (76 clusters: 80, 96 and 256 tiles); long
+# sums of few tiles (units of 128 and of 256 columns shared by two pairs, a K that leaves
+# the second an uneven number of blocks)
 SHAPES = [(1, 8, 1), (1, 128, 128), (2, 64, 31), (5, 72, 129), (8, 1024, 4096), (9, 136, 1500), (17, 4096, 1024), (32, 264, 640),
           (33, 264, 640), (127, 256, 512), (128, 264, 513), (129, 200, 640),
-          (255, 1000, 1374), (256, 256, 128), (257, 512, 2048), (300, 1088, 700), (64, 4096, 1024), (1229, 4096, 384),
+          (255, 1000, 1374), (256, 256, 128), (257, 512, 2048), (300, 1088, 700), (64, 4096, 1024), (1229, 4096, 384), (300, 1000, 3200), (260, 2048, 4100),
+          (1229, 1024, 4096), (70, 2056, 8000),
           (1300, 4096, 256), (4096, 4096, 128), (2600, 1960, 1100)]
 
 
@@ -153,7 +156,7 @@ def test_gemm_fp8(M, N, K, epi):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 16, 16), (3, 128, 128), (1, 4096, 1024), (11, 1040, 1300), (32, 144, 4096),
-                                   (33, 144, 300), (129, 144, 300), (255, 1008, 1374), (300, 4096, 512),
+                                   (33, 144, 300), (129, 144, 300), (255, 1008, 1374), (300, 4096, 512), (300, 1040, 6200),
                                    (955, 1152, 1024), (4000, 2048, 256)])
 @pytest.mark.parametrize("epi", [f3dc.EPI_BIAS, f3dc.EPI_GELU])
 def test_gemm_fp8_8bit_output(M, N, K, epi):
@@ -241,13 +244,14 @@ def test_gemm_fp8_nan_stays_in_its_row_and_column(M):
 
 
 def test_gemm_fp8_is_deterministic_and_no_rows():
-    A, sa, B, sb = operands(777, 1024, 2000, 8)
-    outs = []
-    for _ in range(3):
-        out = torch.zeros((777, 1024), device=DEV)
-        gemm8(A, sa, B, sb, 2000, f3dc.EPI_RESID, None, None, out)
-        outs.append(out)
-    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    for M, K in ((10, 2000), (300, 5000), (777, 2000)):  # each kernel
+        A, sa, B, sb = operands(M, 1024, K, 8)
+        outs = []
+        for _ in range(3):
+            out = torch.zeros((M, 1024), device=DEV)
+            gemm8(A, sa, B, sb, K, f3dc.EPI_RESID, None, None, out)
+            outs.append(out)
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
     out = torch.full((1, 1024), 2.0, device=DEV)
     f3dc.gemm_fp8(A, A.stride(0), sa, sa.stride(0), B, B.stride(0), sb, sb.stride(0), None, None, out, 1024, None, 0, 0,
                   1024, 2000, f3dc.EPI_RESID)

@@ -736,10 +736,11 @@ cudaError_t launch_units8(const CUtensorMap *ta, const GemmPairB *tb, const CUte
 //   300 x 1024 x 4096 (units of 128) 13.4 / 10.9, 300 x 1024 x 8192 21.5 / 15.2, 300 x 2048 x
 //   2048 8.8 / 9.0; 1229 x 1024 x 4096 (256) 14.4 / 13.8, 1229 x 1024 x 8192 22.1 / 17.9, 600
 //   x 1024 x 4096 with 8-bit output, which needs whole scale blocks, 14.0 / 14.7.
+constexpr int kSplitBlocks = 24;  // no sum of fewer scale blocks is split
 int split_width8(int M, int N, int kb_n, bool out8, int max_clusters)
 {
     const int64_t tiles = (((int64_t)M + 255) / 256) * (((int64_t)N + 255) / 256);
-    if (kb_n >= 24 && !out8 && 2 * tiles <= max_clusters) return 128;
+    if (kb_n >= kSplitBlocks && !out8 && 2 * tiles <= max_clusters) return 128;
     return kb_n >= (out8 ? 48 : 32) && tiles <= max_clusters ? 256 : 0;
 }
 
@@ -749,14 +750,17 @@ cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtens
     Units8 u;
     int max_clusters = 0;
     const int kb_n = (p.K + 127) / 128;
-    cudaError_t e = resident8<EPI, OUT8, true>(&max_clusters);
-    if (e != cudaSuccess) return e;
-    if (const int width = split_width8(p.M, p.N, kb_n, OUT8, max_clusters)) {
-        p.split_kb = ((kb_n + 1) / 2 + 3) / 4 * 4;
-        // the second pair's scale bytes start there: they are read as far as that is aligned
-        while (p.split_kb % (4 * p.scale_sets) != 0) p.scale_sets /= 2;
-        const int n = u.set_single(p.M, p.N, width);
-        return launch_units8<EPI, OUT8, true>(ta, tb, to, p, u, width, n, s);
+    cudaError_t e;
+    if (kb_n >= kSplitBlocks) {
+        e = resident8<EPI, OUT8, true>(&max_clusters);
+        if (e != cudaSuccess) return e;
+        if (const int width = split_width8(p.M, p.N, kb_n, OUT8, max_clusters)) {
+            p.split_kb = ((kb_n + 1) / 2 + 3) / 4 * 4;
+            // the second pair's scale bytes start there: they are read as far as that is aligned
+            while (p.split_kb % (4 * p.scale_sets) != 0) p.scale_sets /= 2;
+            const int n = u.set_single(p.M, p.N, width);
+            return launch_units8<EPI, OUT8, true>(ta, tb, to, p, u, width, n, s);
+        }
     }
     e = resident8<EPI, OUT8, false>(&max_clusters);
     if (e != cudaSuccess) return e;

@@ -67,6 +67,7 @@ class NormLayer(C.Structure):
                  eps=1e-6, res_scale=1.0):
         super().__init__(width, post, pre, eps, res_scale, _ptr(post_g), _ptr(post_b), _ptr(pre_g), _ptr(pre_b))
         self._tensors = (post_g, post_b, pre_g, pre_b)
+        self._ref = C.pointer(self)
 
 
 _lock = threading.Lock()
@@ -344,57 +345,68 @@ def attention(q, ldq, k, v, ldkv, out, nq, nk, heads, dh, stream=None):
 
 # ---------------------------------------------------------------- 8-bit linear layers
 
-_get_device = None
-_quantize_types = None
+_fp8_state = None
 
 
-def _device_checks():
-    """(current device's getter, {dtype: F3DC_TYPE_*}), without importing torch before it is needed."""
-    global _get_device, _quantize_types
-    import torch
-    torch.cuda.init()
-    _quantize_types = {torch.bfloat16: 0, torch.int16: 0, torch.uint16: 0, torch.float32: 1}
-    _get_device = torch._C._cuda_getDevice
-    return _get_device
+def _fp8():
+    """(calls, {dtype: F3DC_TYPE_*}, current device's getter or None where there
+    is one device only), made on first use: a call is bound by its marshalling."""
+    global _fp8_state
+    if _fp8_state is None:
+        import torch
+        torch.cuda.init()
+        L = lib()
+        types = {torch.bfloat16: 0, torch.int16: 0, torch.uint16: 0, torch.float32: 1}
+        _fp8_state = ((L.f3dc_quantize_fp8, L.f3dc_gemm_fp8, L.f3dc_norm_residual), types,
+                      torch._C._cuda_getDevice if torch.cuda.device_count() > 1 else None)
+    return _fp8_state
 
 
-def _ptrs(*tensors):
-    """Pointers of tensors that must lie on the current device (None: null)."""
-    dev = (_get_device or _device_checks())()
+def _here(tensors, current):
+    """Pointers of tensors (None: null), which must lie on the current device."""
     out = []
     for t in tensors:
         if t is None:
             out.append(None)
-        elif t.get_device() != dev:
-            raise F3dcError(1, f"a tensor on {t.device}, the current device is cuda:{dev}")
-        else:
+        elif t.is_cuda and (current is None or t.get_device() == current()):
             out.append(t.data_ptr())
+        else:
+            raise F3dcError(1, f"a tensor on {t.device}, which is not the current device")
     return out
 
 
 def quantize_fp8(x, ldx, q, ldq, scales, lds, rows, cols, stream=None):
     """x [rows, cols] (bf16 or fp32; 16-bit integers are bf16 bits) -> e4m3
     bytes q and one power-of-two scale byte per row and block of 128 columns."""
-    px, pq, ps = _ptrs(x, q, scales)
-    x_type = _quantize_types.get(x.dtype) if x is not None else 0
+    calls, types, current = _fp8_state or _fp8()
+    px, pq, ps = _here((x, q, scales), current)
+    x_type = types.get(x.dtype) if x is not None else 0
     if x_type is None:
         raise F3dcError(1, f"x is {x.dtype}: need bf16 or fp32")
-    _check(lib().f3dc_quantize_fp8(px, x_type, ldx, pq, ldq, ps, lds, rows, cols, _stream(stream)))
+    st = calls[0](px, x_type, ldx, pq, ldq, ps, lds, rows, cols, _stream(stream))
+    if st:
+        _check(st)
 
 
 def gemm_fp8(A, lda, a_scales, ldas, Bw, ldb, b_scales, ldbs, bias, gate, out, ldo, out_scales, ldos, M, N, K, epilogue,
              stream=None):
     """Matrix product of two 8-bit matrices with f3dc_gemm's epilogues; with
     out_scales the output is an 8-bit matrix too."""
-    pa, psa, pb, psb, pbias, pgate, po, pos = _ptrs(A, a_scales, Bw, b_scales, bias, gate, out, out_scales)
-    _check(lib().f3dc_gemm_fp8(pa, lda, psa, ldas, pb, ldb, psb, ldbs, pbias, pgate, po, ldo, pos, ldos, M, N, K, epilogue,
-                               _stream(stream)))
+    calls, _, current = _fp8_state or _fp8()
+    pa, psa, pb, psb, pbias, pgate, po, pos = _here((A, a_scales, Bw, b_scales, bias, gate, out, out_scales), current)
+    st = calls[1](pa, lda, psa, ldas, pb, ldb, psb, ldbs, pbias, pgate, po, ldo, pos, ldos, M, N, K, epilogue,
+                  _stream(stream))
+    if st:
+        _check(st)
 
 
 def norm_residual(layer, x, ldx, x_out, ldxo, y, ldy, gate, scale, shift, ldmod, group_of_row, groups, h, ldh, h_scales,
                   ldhs, rows, stream=None):
     """x_out = alpha x + gate post(y), h = pre(x_out) (1 + scale) + shift in one
     pass (`layer`: a NormLayer); with h_scales h is an 8-bit matrix."""
-    px, pxo, py, pg, psc, psh, pgr, ph, phs = _ptrs(x, x_out, y, gate, scale, shift, group_of_row, h, h_scales)
-    _check(lib().f3dc_norm_residual(C.byref(layer), px, ldx, pxo, ldxo, py, ldy, pg, psc, psh, ldmod, pgr, groups, ph, ldh,
-                                    phs, ldhs, rows, _stream(stream)))
+    calls, _, current = _fp8_state or _fp8()
+    px, pxo, py, pg, psc, psh, pgr, ph, phs = _here((x, x_out, y, gate, scale, shift, group_of_row, h, h_scales), current)
+    st = calls[2](layer._ref, px, ldx, pxo, ldxo, py, ldy, pg, psc, psh, ldmod, pgr, groups, ph, ldh, phs, ldhs, rows,
+                  _stream(stream))
+    if st:
+        _check(st)

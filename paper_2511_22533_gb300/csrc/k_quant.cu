@@ -6,10 +6,9 @@
 // the conversion's and the result is the same bit for bit in whatever order.
 //
 // Bound by memory: x is read once, one byte and 1/128 written per element.  A block
-// is held by 8 lanes, 16 elements each.  Where there is more than a wave of work a warp
-// takes two groups of four blocks at a time, so that enough loads are in flight (32768 x
-// 4096 bf16: 74 us with one, 68 with two); where there is not, one is less latency (955
-// rows: 2.7 and 4.2 us).
+// is held by 8 lanes, 16 elements each; a warp takes four blocks at a time, wherever
+// rows end, and of fp32, with more than a wave of work, twice four (16384 x 4096: 56 us
+// with one group in flight, 50 with two; bf16, 32768 x 4096, 61 and 75).
 #include "kernels.h"
 #include "mx8.cuh"
 
@@ -101,19 +100,32 @@ __global__ void __launch_bounds__(kQuantThreads, quant_ctas(F32)) k_quantize(con
     griddep_launch();
     griddep_wait();
     const int lane = threadIdx.x & 31;
-    const int chunks = (a.cols + 511) / 512;  // of four blocks
-    const int64_t items = (int64_t)a.rows * chunks;
-    const int64_t step = (int64_t)gridDim.x * (kQuantThreads / 32);
-    for (int64_t it = (int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5); it < items; it += U * step) {
+    const int per_row = (a.cols + kScaleBlock - 1) / kScaleBlock;
+    const int64_t groups = ((int64_t)a.rows * per_row + 3) / 4;  // of four blocks
+    const int64_t warps = (int64_t)gridDim.x * (kQuantThreads / 32);
+    const int64_t first = (int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    // block i of the matrix is block i % per_row of row i / per_row; the one that is
+    // 4 `warps` further is found without a division (a 64-bit one is as long as the rest of
+    // the loop)
+    const int64_t step_rows = 4 * warps / per_row;
+    const int step_blocks = (int)(4 * warps - step_rows * per_row);
+    int64_t next_row = (4 * first + (lane >> 3)) / per_row;
+    int next_block = (int)(4 * first + (lane >> 3) - next_row * per_row);
+    for (int64_t group = first; group < groups; group += U * warps) {
         Words<F32> x[U];
         int64_t row[U];
         int col[U], n[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t i = it + u * step;
-            row[u] = i / chunks;
-            col[u] = (int)(i - row[u] * chunks) * 512 + lane * 16;
-            n[u] = i < items ? a.cols - col[u] : 0;  // this lane's elements (more than 16, or none, too)
+            row[u] = next_row;
+            col[u] = next_block * kScaleBlock + (lane & 7) * 16;
+            n[u] = next_row < a.rows ? a.cols - col[u] : 0;  // this lane's elements (more than 16, or none, too)
+            next_row += step_rows;
+            next_block += step_blocks;
+            if (next_block >= per_row) {
+                next_block -= per_row;
+                ++next_row;
+            }
             const bool edge = (row[u] == 0 && col[u] == 0) || (row[u] == a.rows - 1 && n[u] < 32);
             load16<F32, ALIGNED>(reinterpret_cast<const uint8_t *>(a.x) + row[u] * a.ldx * (F32 ? 4 : 2), col[u], n[u], edge, x[u]);
         }
@@ -140,16 +152,19 @@ __global__ void __launch_bounds__(kQuantThreads, quant_ctas(F32)) k_quantize(con
 template <bool F32>
 cudaError_t launch_type(const QuantArgs &a, int num_sms, cudaStream_t s)
 {
-    const int64_t items = (int64_t)a.rows * ((a.cols + 511) / 512), per = kQuantThreads / 32;
-    const int64_t ctas = (items + per - 1) / per, most = (int64_t)num_sms * quant_ctas(F32);
+    const int64_t groups = ((int64_t)a.rows * ((a.cols + kScaleBlock - 1) / kScaleBlock) + 3) / 4, per = kQuantThreads / 32;
+    const int64_t ctas = (groups + per - 1) / per, most = (int64_t)num_sms * quant_ctas(F32);
     const dim3 g((unsigned)(ctas < most ? ctas : most)), b(kQuantThreads);
-    const bool two = ctas > 2 * most;
     const bool aligned = ((uintptr_t)a.x & 15) == 0 && (a.ldx * (F32 ? 4 : 2)) % 16 == 0;
     const bool wide = ((uintptr_t)a.q & 15) == 0 && a.ldq % 16 == 0;
     if (!wide) return launch_k(k_quantize<F32, false, false, 1>, g, b, 0, s, a);
-    if (aligned)
-        return two ? launch_k(k_quantize<F32, true, true, 2>, g, b, 0, s, a) : launch_k(k_quantize<F32, true, true, 1>, g, b, 0, s, a);
-    return two ? launch_k(k_quantize<F32, false, true, 2>, g, b, 0, s, a) : launch_k(k_quantize<F32, false, true, 1>, g, b, 0, s, a);
+    if constexpr (F32) {
+        if (ctas > 2 * most)
+            return aligned ? launch_k(k_quantize<F32, true, true, 2>, g, b, 0, s, a)
+                           : launch_k(k_quantize<F32, false, true, 2>, g, b, 0, s, a);
+    }
+    return aligned ? launch_k(k_quantize<F32, true, true, 1>, g, b, 0, s, a)
+                   : launch_k(k_quantize<F32, false, true, 1>, g, b, 0, s, a);
 }
 
 }  // namespace

@@ -27,8 +27,6 @@ struct V8 {
     f32x2 v[4];
 };
 
-F3DC_DEV V8 zero8() { return V8{{{0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}}}; }
-
 F3DC_DEV V8 from_bf16(uint4 u)
 {
     return V8{{{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u)},
@@ -36,18 +34,28 @@ F3DC_DEV V8 from_bf16(uint4 u)
                {__uint_as_float(u.z << 16), __uint_as_float(u.z & 0xFFFF0000u)},
                {__uint_as_float(u.w << 16), __uint_as_float(u.w & 0xFFFF0000u)}}};
 }
-// gains, biases, modulations: read by every CTA, kept in L1
-F3DC_DEV V8 vec_bf16(const bf16 *p) { return from_bf16(*reinterpret_cast<const uint4 *>(p)); }
-F3DC_DEV V8 vec_f32(const float *p)
+// gains, biases, modulations: read by every CTA, kept in L1.  Issued where they stand, ahead
+// of the sums that run before their use (a null p: nothing is read).
+F3DC_DEV uint4 vec_load16(const void *p)
 {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    return V8{{{a.x, a.y}, {a.z, a.w}, {b.x, b.y}, {b.z, b.w}}};
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+    if (p) asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    return u;
 }
-// rows: read once, past L1
+struct Vec {  // 8 fp32
+    uint4 lo, hi;
+    F3DC_DEV f32x2 pair(int j) const
+    {
+        const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        return {__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1])};
+    }
+};
+F3DC_DEV Vec vec_f32(const float *p) { return Vec{vec_load16(p), vec_load16(p ? p + 4 : nullptr)}; }
+// rows: read once
 F3DC_DEV uint4 row_load16(const void *p)
 {
     uint4 u;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
     return u;
 }
 F3DC_DEV f32x2 both(float a) { return {a, a}; }
@@ -107,6 +115,7 @@ template <int R, int NW>
 F3DC_DEV void normalise(V8 (&v)[R], bool in, float inv_w, int kind, const bf16 *g, const bf16 *b, float eps,
                         float (*sh)[R][NW], int &turn)
 {
+    const uint4 gain = vec_load16(in ? g : nullptr), bias = vec_load16(in ? b : nullptr);
     if (kind != kNormNone) {
         float s[R];
         if (kind == kNormLayer) {
@@ -141,14 +150,14 @@ F3DC_DEV void normalise(V8 (&v)[R], bool in, float inv_w, int kind, const bf16 *
         }
     }
     if (g && in) {
-        const V8 u = vec_bf16(g);
+        const V8 u = from_bf16(gain);
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[i].v[j] = fmul2(v[i].v[j], u.v[j]);
     }
     if (b && in) {
-        const V8 u = vec_bf16(b);
+        const V8 u = from_bf16(bias);
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
@@ -200,13 +209,14 @@ __global__ void __launch_bounds__(32 * NW, kNormThreadsPerSm / (32 * NW)) k_norm
     V8 x[R];
     const f32x2 alpha = both(a.res_scale);
     if (a.y) {
+        // the gate of the first row's group (a batch's rows are rarely of two)
+        Vec gate = vec_f32(a.gate && in && g[0] >= 0 ? a.gate + g[0] * a.ldmod + col : nullptr);
+        int of = g[0];  // the group whose vector `gate` is
         V8 y[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) y[i] = from_bf16(yr[i]);
         normalise<R, NW>(y, in, inv_w, a.post, a.post_g ? a.post_g + col : nullptr, a.post_b ? a.post_b + col : nullptr,
                          a.eps, sh, turn);
-        V8 gate;
-        int of = -1;  // the group whose vector `gate` is
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const float *f = reinterpret_cast<const float *>(xr[i]);
@@ -216,7 +226,7 @@ __global__ void __launch_bounds__(32 * NW, kNormThreadsPerSm / (32 * NW)) k_norm
                 if (g[i] != of) gate = vec_f32(a.gate + g[i] * a.ldmod + col);
                 of = g[i];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[i].v[j] = ffma2(gate.v[j], y[i].v[j], x[i].v[j]);
+                for (int j = 0; j < 4; ++j) x[i].v[j] = ffma2(gate.pair(j), y[i].v[j], x[i].v[j]);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[i].v[j] = fadd2(y[i].v[j], x[i].v[j]);
@@ -240,23 +250,23 @@ __global__ void __launch_bounds__(32 * NW, kNormThreadsPerSm / (32 * NW)) k_norm
             }
     }
     if (!a.h) return;
+    const bool mod0 = in && g[0] >= 0;
+    Vec sc = vec_f32(a.scale && mod0 ? a.scale + g[0] * a.ldmod + col : nullptr);
+    Vec sf = vec_f32(a.shift && mod0 ? a.shift + g[0] * a.ldmod + col : nullptr);
     normalise<R, NW>(x, in, inv_w, a.pre, a.pre_g ? a.pre_g + col : nullptr, a.pre_b ? a.pre_b + col : nullptr, a.eps, sh,
                      turn);
     if (a.scale || a.shift) {
-        V8 sc = zero8(), sf = zero8();
-        int of = -1;
+        int of = g[0];  // the group whose vectors sc and sf are
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             if (!in || g[i] < 0) continue;
             if (g[i] != of) {
-                if (a.scale) sc = vec_f32(a.scale + g[i] * a.ldmod + col);
-                if (a.shift) sf = vec_f32(a.shift + g[i] * a.ldmod + col);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sc.v[j] = fadd2(sc.v[j], both(1.0f));
+                sc = vec_f32(a.scale ? a.scale + g[i] * a.ldmod + col : nullptr);
+                sf = vec_f32(a.shift ? a.shift + g[i] * a.ldmod + col : nullptr);
             }
             of = g[i];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[i].v[j] = ffma2(x[i].v[j], sc.v[j], sf.v[j]);
+            for (int j = 0; j < 4; ++j) x[i].v[j] = ffma2(x[i].v[j], fadd2(sc.pair(j), both(1.0f)), sf.pair(j));
         }
     }
     if (a.h_scales) {

@@ -463,7 +463,7 @@ f3dc_status f3dc_quantize_fp8(const void *x, int32_t x_type, int64_t ldx, void *
  *   bias: device bf16 [N], nullable; gate: device fp32 [N], nullable;
  *   out: 16-byte aligned, row stride ldo elements, a multiple of 16 bytes;
  *   out_scales: device bytes, row stride ldos, nullable.
- *   Any M >= 0, N a positive multiple of 8, any K >= 1. */
+ *   Any M >= 0, N a positive multiple of 8, 1 <= K <= 2^26. */
 f3dc_status f3dc_gemm_fp8(const void *A, int64_t lda, const void *a_scales, int64_t ldas, const void *B, int64_t ldb,
                           const void *b_scales, int64_t ldbs, const void *bias, const float *gate, void *out,
                           int64_t ldo, void *out_scales, int64_t ldos, int32_t M, int32_t N, int32_t K,

@@ -72,8 +72,9 @@ extern "C" f3dc_status f3dc_gemm_fp8(const void *A, int64_t lda, const void *a_s
     const int esz = out8 ? 1 : (epilogue == F3DC_EPI_RESID ? 4 : 2);
     if (ldo < N || ldo * esz % 16) return bad("ldo must be at least N, and rows of out a multiple of 16 bytes");
     if (out8 && (ldos < blocks(N))) return bad("ldos is smaller than ceil(N / 128)");
+    // (a tile of 2^26 K takes 0.15 s or so of the second that a wait for it may last)
     if (((int64_t)M + 255) / 256 * (((int64_t)N + 63) / 64) > (1 << 30) || M > INT32_MAX - 512 || N > INT32_MAX - 512 ||
-        K > INT32_MAX - 512)
+        K > 1 << 26)
         return bad("the problem is too large");
     if (M == 0) return F3DC_OK;
     if (!A || !B || !a_scales || !b_scales || !out) return bad("null pointer");

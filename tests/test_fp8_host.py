@@ -43,7 +43,8 @@ GEMM = dict(A=P, lda=1024, sa=P, ldas=8, B=P, ldb=1024, sb=P, ldbs=8, bias=P, ga
     (dict(epi=2, gate=P + 8), b"aligned"), (dict(bias=P + 2), b"aligned"), (dict(A=P + 8), b"aligned"),
     (dict(out=P + 4), b"aligned"), (dict(sb=P + 2), b"aligned"), (dict(epi=2, out_scales=P, ldos=4), b"8-bit"),
     (dict(out_scales=P, ldos=3), b"ldos"), (dict(out_scales=P, ldos=4, N=504, ldo=512), b"multiple of 16"),
-    (dict(out_scales=P, ldos=4, ldo=520), b"ldo"), (dict(M=2 ** 31 - 1), b"large")])
+    (dict(out_scales=P, ldos=4, ldo=520), b"ldo"), (dict(M=2 ** 31 - 1), b"large"),
+    (dict(N=2 ** 31 - 8, ldo=2 ** 31), b"large"), (dict(K=2 ** 26 + 1, lda=2 ** 27, ldb=2 ** 27, ldas=2 ** 20, ldbs=2 ** 20), b"large")])
 def test_gemm_refusals(L, kw, needle):
     a = dict(GEMM)
     a.update(kw)

@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kQuantThreads, quant_ctas(F32)) k_quantize(con
     griddep_launch();
     griddep_wait();
     const int lane = threadIdx.x & 31;
-    const int per_row = (a.cols + kScaleBlock - 1) / kScaleBlock;
+    const int per_row = (a.cols - 1) / kScaleBlock + 1;
     const int64_t groups = ((int64_t)a.rows * per_row + 3) / 4;  // of four blocks
     const int64_t warps = (int64_t)gridDim.x * (kQuantThreads / 32);
     const int64_t first = (int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kQuantThreads, quant_ctas(F32)) k_quantize(con
 template <bool F32>
 cudaError_t launch_type(const QuantArgs &a, int num_sms, cudaStream_t s)
 {
-    const int64_t groups = ((int64_t)a.rows * ((a.cols + kScaleBlock - 1) / kScaleBlock) + 3) / 4, per = kQuantThreads / 32;
+    const int64_t groups = ((int64_t)a.rows * ((a.cols - 1) / kScaleBlock + 1) + 3) / 4, per = kQuantThreads / 32;
     const int64_t ctas = (groups + per - 1) / per, most = (int64_t)num_sms * quant_ctas(F32);
     const dim3 g((unsigned)(ctas < most ? ctas : most)), b(kQuantThreads);
     const bool aligned = ((uintptr_t)a.x & 15) == 0 && (a.ldx * (F32 ? 4 : 2)) % 16 == 0;

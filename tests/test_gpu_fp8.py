@@ -107,6 +107,34 @@ def test_quantize_offsets_past_32_bits():
     assert torch.equal(q.contiguous(), rq) and torch.equal(s[:, :2], rs)
 
 
+def test_quantize_longest_row():
+    # the last block of a row of 2^31 - 1 elements, and the first
+    cols = 2 ** 31 - 1
+    x = torch.zeros((1, cols), dtype=torch.bfloat16, device=DEV)
+    x[0, :256], x[0, -300:] = randn(256, seed=6).bfloat16(), randn(300, seed=7).bfloat16()
+    q = torch.full((1, cols + 1), 0x55, dtype=torch.uint8, device=DEV)
+    s = torch.full((1, R.nblocks(cols) + 1), 0x33, dtype=torch.uint8, device=DEV)
+    quantize(x, q, s)
+    for lo in (0, cols - cols % 128 - 256):
+        rq, rs = R.quantized(x[:, lo:lo + 512].double())
+        assert torch.equal(q[:, lo:min(lo + 512, cols)], rq)
+        assert torch.equal(s[:, lo // 128:lo // 128 + rs.shape[1]], rs)
+    assert q[0, -1] == 0x55 and s[0, -1] == 0x33
+
+
+# more blocks than one step of the grid takes (fp32: two groups of four per warp), a whole
+# number of groups and not, aligned rows and not
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols,shift", [(6001, 1300, 0), (6000, 1280, 0), (6001, 1280, 1), (60001, 128, 0), (70000, 40, 0)])
+def test_quantize_more_than_a_wave(rows, cols, shift, dtype):
+    x = randn(rows, cols + 4, seed=rows + cols, dtype=dtype)[:, shift:shift + cols]
+    x.mul_(torch.exp2(torch.randint(-20, 20, (rows, 1), generator=gen(2), device=DEV).float()).to(dtype))
+    q, s = quantize(x)
+    rq, rs = R.quantized(x.double())
+    assert torch.equal(s[:, :R.nblocks(cols)], rs) and torch.equal(q[:, :cols], rq)
+    assert torch.all(q[:, cols:] == 0x55) and torch.all(s[:, R.nblocks(cols):] == 0x33)
+
+
 def test_quantize_no_rows():
     x, (q, s) = torch.zeros((0, 64), device=DEV), R.storage(1, 64)
     f3dc.quantize_fp8(x, 64, q, 64, s, 4, 0, 64)

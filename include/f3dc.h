@@ -492,7 +492,8 @@ typedef struct f3dc_norm_layer {
  *   h_r = (pre(x'_r) pre_g + pre_b) (1 + scale_g) + shift_g
  * in fp32; x' is stored in fp32, h in bf16 or, with h_scales given, in 8 bits
  * (quantised as f3dc_quantize_fp8 does).
- *   x: device fp32 [rows, W]; x_out: device fp32, may be x itself, nullable;
+ *   x: device fp32 [rows, W]; x_out: device fp32, may be x itself (ldxo = ldx),
+ *     nullable;
  *   y: device bf16 [rows, W], nullable;
  *   gate, scale, shift: device fp32 [groups, W], row stride ldmod, each nullable;
  *   group_of_row: device int32 [rows], nullable (all rows of group 0).  Rows of a

@@ -139,6 +139,7 @@ extern "C" f3dc_status f3dc_norm_residual(const f3dc_norm_layer *l, const float 
     if ((gate || scale || shift) && (ldmod < W || ldmod % 4)) return bad("ldmod must be a multiple of 4, at least the width");
     if (ldx < W || ldx % 4 || (x_out && (ldxo < W || ldxo % 4)) || (y && (ldy < W || ldy % 8)))
         return bad("rows of x, x_out and y must start 16 bytes aligned and hold the width");
+    if (x && x_out == x && ldxo != ldx) return bad("x_out in place of x needs ldxo = ldx");
     if (h && (ldh < W || ldh % 8)) return bad("ldh must be a multiple of 8, at least the width");
     if (h_scales && ldhs < blocks(W)) return bad("ldhs is smaller than ceil(width / 128)");
     if (rows == 0) return F3DC_OK;

@@ -61,7 +61,7 @@ NORM = dict(x=P, ldx=256, x_out=P, ldxo=256, y=P, ldy=256, gate=P, scale=P, shif
     (dict(y=None), b"gate"), (dict(rows=-1), b"rows"), (dict(groups=0), b"groups"), (dict(ldx=255), b"rows of x"),
     (dict(ldxo=250), b"rows of x"), (dict(ldy=260), b"rows of x"), (dict(ldh=252), b"ldh"), (dict(ldmod=128), b"ldmod"),
     (dict(ldmod=258), b"ldmod"), (dict(hs=P, ldhs=1), b"ldhs"), (dict(x=P + 4), b"aligned"), (dict(h=P + 8), b"aligned"),
-    (dict(scale=P + 4), b"aligned"), (dict(group=P + 2), b"group_of_row")])
+    (dict(x_out=P, ldxo=260), b"in place"), (dict(scale=P + 4), b"aligned"), (dict(group=P + 2), b"group_of_row")])
 def test_norm_refusals(L, kw, needle):
     a = dict(NORM)
     a.update(kw)

@@ -66,8 +66,11 @@ class NormLayer(C.Structure):
     def __init__(self, width, post=NORM_NONE, pre=NORM_LAYER, post_g=None, post_b=None, pre_g=None, pre_b=None,
                  eps=1e-6, res_scale=1.0):
         super().__init__(width, post, pre, eps, res_scale, _ptr(post_g), _ptr(post_b), _ptr(pre_g), _ptr(pre_b))
-        self._tensors = (post_g, post_b, pre_g, pre_b)
+        self._tensors = tuple(t for t in (post_g, post_b, pre_g, pre_b) if t is not None)
         self._ref = C.pointer(self)
+        for t in self._tensors:
+            if not t.is_cuda or t.element_size() != 2 or t.numel() < width or not t.is_contiguous():
+                raise F3dcError(1, f"gains and biases are bf16 [{width}] on a GPU: got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 _lock = threading.Lock()
@@ -406,6 +409,8 @@ def norm_residual(layer, x, ldx, x_out, ldxo, y, ldy, gate, scale, shift, ldmod,
     pass (`layer`: a NormLayer); with h_scales h is an 8-bit matrix."""
     calls, _, current = _fp8_state or _fp8()
     px, pxo, py, pg, psc, psh, pgr, ph, phs = _here((x, x_out, y, gate, scale, shift, group_of_row, h, h_scales), current)
+    if current is not None:
+        _here(layer._tensors, current)
     st = calls[2](layer._ref, px, ldx, pxo, ldxo, py, ldy, pg, psc, psh, ldmod, pgr, groups, ph, ldh, phs, ldhs, rows,
                   _stream(stream))
     if st:

@@ -297,6 +297,136 @@ def test_gemm_fp8_long_positive_sums(M, N, K):
     assert torch.all((out.double() - y).abs() <= err + R.U32 * y)
 
 
+# rows and scales more than 4 GiB apart from the first, in both kernels
+@pytest.mark.parametrize("M,N,K", [(3, 40, 200), (200, 264, 200), (300, 256, 4096)])
+@pytest.mark.parametrize("out8", [False, True])
+def test_gemm_fp8_offsets_past_32_bits(M, N, K, out8):
+    if out8:
+        N = N // 16 * 16
+    A, sa, B, sb = operands(M, N, K, 5)
+    bias = randn(N, seed=7, dtype=torch.bfloat16)
+    y, err = R.gemm(A, sa, B, sb, K, bias)
+
+    def wide(v, most=1 << 32):
+        ld = most // (v.shape[0] - 1) // 64 * 64 + 64
+        return torch.empty((v.shape[0], ld), dtype=v.dtype, device=DEV)[:, :v.shape[1]].copy_(v)
+    ops = [wide(t) for t in (A, sa, B, sb)]
+    if out8:
+        q, s = (wide(t) for t in R.storage(M, N))
+        gemm8(*ops, K, f3dc.EPI_BIAS, bias, None, q, s)
+        R.check_out8(q, s, y, err)
+    else:
+        out = wide(torch.full((M, N), 7.0, dtype=torch.bfloat16, device=DEV))
+        gemm8(*ops, K, f3dc.EPI_BIAS, bias, None, out)
+        assert torch.all((out.double() - y).abs() <= R.U_BF16 * y.abs() + 1.01 * err)
+    assert f3dc.gemm_status() == 0
+
+
+# scales whose rows start 4, 8 and 16 bytes aligned are read in pieces of as many
+@pytest.mark.parametrize("align", [4, 8, 16])
+@pytest.mark.parametrize("M,N,K", [(70, 264, 5000), (600, 1024, 4200), (300, 520, 4200)])
+def test_gemm_fp8_scale_alignment(M, N, K, align):
+    A, sa, B, sb = operands(M, N, K, 6)
+    y, err = R.gemm(A, sa, B, sb, K)
+
+    def at(v):
+        ld = -(-v.shape[1] // 16) * 16 + align
+        buf = torch.full((16 + v.shape[0] * ld,), 0xFF, dtype=torch.uint8, device=DEV)
+        return buf[align % 16:][:v.shape[0] * ld].view(-1, ld)[:, :v.shape[1]].copy_(v)
+    out = torch.zeros((M, N), dtype=torch.bfloat16, device=DEV)
+    gemm8(A, at(sa), B, at(sb), K, f3dc.EPI_BIAS, None, None, out)
+    assert torch.all((out.double() - y).abs() <= R.U_BF16 * y.abs() + 1.01 * err)
+    assert f3dc.gemm_status() == 0
+
+
+# the few rows' kernel, whole and split sums: at once on two streams and in two graphs
+# replayed at once, and captured by a process's very first call
+@pytest.mark.parametrize("M,N,K,epi", [(1, 1024, 4096, 0), (16, 512, 1024, 1), (300, 1024, 4096, 0), (600, 1024, 6400, 1), (2000, 1024, 640, 0)])
+@pytest.mark.parametrize("out8", [False, True])
+def test_gemm_fp8_streams_and_graphs(M, N, K, epi, out8):
+    jobs = []
+    for i in range(2):
+        A, sa, B, sb = operands(M, N, K, 40 + i)
+        o = R.storage(M, N) if out8 else (torch.zeros((M, N), dtype=torch.bfloat16, device=DEV), None)
+        gemm8(A, sa, B, sb, K, epi, None, None, *o)
+        jobs.append(((A, sa, B, sb), o, o[0].clone(), o[1].clone() if out8 else None))
+    streams = [torch.cuda.Stream() for _ in jobs]
+
+    def check():
+        torch.cuda.synchronize()
+        for _, o, q, s in jobs:
+            assert torch.equal(o[0], q) and (s is None or torch.equal(o[1], s))
+            for t in o:
+                if t is not None:
+                    t.zero_()
+        torch.cuda.synchronize()
+    check()
+    for _ in range(4):
+        for (ops, o, _, _), st in zip(jobs, streams):
+            gemm8(*ops, K, epi, None, None, *o, stream=st.cuda_stream)
+    torch.cuda.synchronize()
+    if out8:
+        pad = [(o[0][:, N:].clone(), q[:, N:], o[1][:, R.nblocks(N):], s[:, R.nblocks(N):]) for _, o, q, s in jobs]
+        assert all(torch.all(a == 0) and torch.all(b == 0x55) and torch.all(c == 0) and torch.all(d == 0x33) for a, b, c, d in pad)
+        for _, o, q, s in jobs:
+            o[0][:, N:], o[1][:, R.nblocks(N):] = 0x55, 0x33
+    check()
+    graphs = []
+    for ops, o, _, _ in jobs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            gemm8(*ops, K, epi, None, None, *o)
+    for _ in range(3):
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+    torch.cuda.synchronize()
+    if out8:
+        for _, o, _, _ in jobs:
+            o[0][:, N:], o[1][:, R.nblocks(N):] = 0x55, 0x33
+    check()
+    assert f3dc.gemm_status() == 0
+
+
+FIRST_CALL_CAPTURED = """
+import sys
+sys.path[:0] = [%r, %r]
+import torch
+import fp8_ref as R
+from test_gpu_fp8 import *
+f3dc.lib()
+A = torch.full((%d, 4096), 0x38, dtype=torch.uint8, device=DEV)
+B = torch.full((256, 4096), 0x38, dtype=torch.uint8, device=DEV)
+sa, sb = (torch.full((t.shape[0], 32), 127, dtype=torch.uint8, device=DEV) for t in (A, B))
+out = torch.zeros((A.shape[0], 256), dtype=torch.bfloat16, device=DEV)
+x, (q, s) = torch.ones((4, 256), device=DEV), R.storage(4, 256)
+h = torch.zeros((4, 256), dtype=torch.bfloat16, device=DEV)
+layer = f3dc.NormLayer(256, pre=f3dc.NORM_RMS, eps=0.0)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    gemm8(A, sa, B, sb, 4096, f3dc.EPI_BIAS, None, None, out)
+    quantize(x, q, s)
+    f3dc.norm_residual(layer, x, 256, None, 0, None, 0, None, None, None, 0, None, 1, h, 256, None, 0, 4)
+g.replay()
+torch.cuda.synchronize()
+assert torch.all(out == 4096.0) and f3dc.gemm_status() == 0
+assert torch.all(h == 1.0) and torch.all(s[:, :2] == 119) and torch.all(q == 0x78)
+print("captured")
+"""
+
+
+@pytest.mark.parametrize("M", [4, 300])
+def test_first_call_of_a_process_in_a_capture(M):
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = FIRST_CALL_CAPTURED % (here, os.path.dirname(here), M)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
 # ------------------------------------------------------------------ norms
 
 def norm_case(rows, W, post, pre, affine, mod, groups, out8, y=True, x_out=True, h=True, seed=0, alpha=0.875, eps=1e-6,
@@ -359,6 +489,52 @@ def norm_case(rows, W, post, pre, affine, mod, groups, out8, y=True, x_out=True,
 @pytest.mark.parametrize("out8", [False, True])
 def test_norm_widths(rows, W, out8):
     norm_case(rows, W, f3dc.NORM_RMS, f3dc.NORM_LAYER, True, True, 2, out8, seed=W)
+
+
+# rows in pairs, an odd number of them, of different groups and pads within a pair
+@pytest.mark.parametrize("W", [8, 128, 264, 512, 520, 1024, 1032, 2056, 4096, 4104])
+@pytest.mark.parametrize("out8", [False, True])
+def test_norm_many_rows(W, out8):
+    norm_case(1301, W, f3dc.NORM_LAYER, f3dc.NORM_RMS, True, True, 3, out8, seed=W + 1, pad_cols=0 if out8 else 1)
+
+
+def test_norm_bad_groups_in_many_rows():
+    W, rows = 136, 2001
+    x, y = randn(rows, W, seed=1), randn(rows, W, seed=2, dtype=torch.bfloat16)
+    group = torch.randint(-2, 5, (rows,), generator=gen(3), device=DEV).to(torch.int32)  # 3 and 4 are behind the last
+    m = randn(3, 3, W, seed=4)
+    xo = torch.full((rows, W), 9.0, device=DEV)
+    q, s = R.storage(rows, W)
+    layer = f3dc.NormLayer(W, f3dc.NORM_RMS, f3dc.NORM_NONE)
+    f3dc.norm_residual(layer, x, W, xo, W, y, W, m[:, 0], m[:, 1], m[:, 2], 3 * W, group, 3, q, q.stride(0), s, s.stride(0), rows)
+    assert f3dc.gemm_status() == 2
+    left = (group < 0) | (group > 2)
+    assert torch.all(xo[left] == 9.0) and torch.all(q[left] == 0x55) and torch.all(s[left] == 0x33)
+    g = group.clamp(0, 2).long()
+    n, ne = R.norm(y.double(), torch.zeros_like(y.double()), 2, None, None, 1e-6)
+    ref = x.double() + m[g, 0].double() * n
+    bound = 1.01 * (ne * m[g, 0].double().abs() + R.U32 * ((m[g, 0].double() * n).abs() + ref.abs()))
+    assert torch.all(((xo.double() - ref).abs() <= bound)[~left])
+
+
+@pytest.mark.parametrize("rows", [3, 1300])
+def test_norm_offsets_past_32_bits(rows):
+    W = 256
+    ld = (1 << 31) // (rows - 1) // 8 * 8 + 64  # the last row lies behind 8, 4 and 2 GiB
+    def wide(v):
+        t = torch.empty((rows - 1) * ld + W, dtype=v.dtype, device=DEV).as_strided((rows, W), (ld, 1))
+        return t.copy_(v)
+    x, y = randn(rows, W, seed=1), randn(rows, W, seed=2, dtype=torch.bfloat16)
+    m = randn(2, W, seed=3)
+    mw = torch.empty((1 << 31) + W, device=DEV).as_strided((2, W), (1 << 31, 1)).copy_(m)
+    group = torch.randint(0, 2, (rows,), generator=gen(4), device=DEV).to(torch.int32)
+    layer = f3dc.NormLayer(W, f3dc.NORM_LAYER, f3dc.NORM_RMS)
+    h, xo = torch.zeros((rows, W), dtype=torch.bfloat16, device=DEV), torch.zeros((rows, W), device=DEV)
+    f3dc.norm_residual(layer, x, W, xo, W, y, W, m, None, m, W, group, 2, h, W, None, 0, rows)
+    hw, xow = wide(torch.zeros_like(h)), wide(torch.zeros_like(xo))
+    f3dc.norm_residual(layer, wide(x), ld, xow, ld, wide(y), ld, mw, None, mw, 1 << 31, group, 2, hw, ld, None, 0, rows)
+    assert torch.equal(hw, h) and torch.equal(xow, xo)
+    assert f3dc.gemm_status() == 0
 
 
 @pytest.mark.parametrize("post", [0, 1, 2])
@@ -524,3 +700,7 @@ def test_tensors_of_another_device_are_refused():
     with pytest.raises(f3dc.F3dcError) as e:
         f3dc.quantize_fp8(x.to(DEV).half(), 64, q, 64, s, 4, 4, 64)
     assert e.value.status == 1
+    for vec in (torch.ones(64, dtype=torch.bfloat16), torch.ones(64, device=DEV), torch.ones(32, dtype=torch.bfloat16, device=DEV)):
+        with pytest.raises(f3dc.F3dcError) as e:
+            f3dc.NormLayer(64, pre_g=vec)
+        assert e.value.status == 1

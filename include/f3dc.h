@@ -366,9 +366,10 @@ f3dc_status f3dc_gemm_noalloc(const void *A, const void *B, const void *bias, co
                               int32_t M, int32_t N, int32_t K, int32_t epilogue, void *stream);
 
 /* Reads and clears the current device's status word of the standalone
- * kernel calls (f3dc_gemm, f3dc_gemm_noalloc, f3dc_attention): F3DC_DEV_*
- * bits recorded by their kernels since the last read, e.g. F3DC_DEV_TIMEOUT
- * when a bounded wait ran out and part of the output was left unwritten.
+ * kernel calls (f3dc_gemm, f3dc_gemm_noalloc, f3dc_attention, f3dc_gemm_fp8,
+ * f3dc_norm_residual): F3DC_DEV_* bits recorded by their kernels since the last
+ * read, e.g. F3DC_DEV_TIMEOUT when a bounded wait ran out and part of the output
+ * was left unwritten.
  * Synchronizes the device first.
  * The word is a static device variable of the library: this call allocates
  * nothing.  Failures are described by f3dc_last_error(NULL). */

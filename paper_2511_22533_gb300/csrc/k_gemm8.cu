@@ -23,6 +23,12 @@
 // there, but two sets of scales need 24.  So the second accumulator starts at column
 // 232: the tile after may begin as soon as the epilogue has read the 24 columns that
 // the two share, which it reads first.
+//
+// 32768 x 4096 x 1024 with GELU takes 108 us (2.55 PFLOP/s), 8192 x 8192 x
+// 8192 360 (3.05), where the board's power is the bound.  With K = 1024 the tensor cores are
+// busy in 57 % of the cycles: a tile's sum is as short as its epilogue.  A few tiles take
+// 4.6 us (launch, tensor memory, first loads, epilogue) and 0.15 to 0.26 per 128 K, what an
+// SM takes in of 20 to 32 KB operands.
 #include <atomic>
 
 #include <cudaTypedefs.h>

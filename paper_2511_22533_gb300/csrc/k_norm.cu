@@ -12,7 +12,10 @@
 // shuffles and the barrier, and a gain or a modulation is read once for all of them
 // (from L1: with one row at a time these vectors, 20 bytes per element, are more than
 // the rows themselves).  The rows stay in registers between the two norms.  Means, then
-// mean squared deviations from them, in fp32.
+// mean squared deviations from them, in fp32.  32768 x 1024 with a gate, modulations and
+// 8-bit h take 69 us: 5.35 TB/s, 79 % of a plain copy's rate (one row per CTA 82 us, four
+// 81); instructions issue in 64 % of the cycles, and the rows' loads do not overlap their
+// CTA's sums.  One row of 128 takes 1.9 us.
 #include "kernels.h"
 #include "mx8.cuh"
 
@@ -318,6 +321,9 @@ cudaError_t launch_width(const NormArgs &a, cudaStream_t s)
 
 }  // namespace
 
+// One row per CTA while all of them run at once: with one / two, us, of width 1024: 600 rows
+// 4.2 / 4.3, 1000 4.4 / 5.1, 1400 5.6 / 5.5, 2400 7.4 / 6.0; of width 256: 600 rows 2.2 / 2.4,
+// 1400 3.5 / 2.7.
 cudaError_t launch_norm_residual(const NormArgs &a, int num_sms, cudaStream_t s)
 {
     return a.rows >= 8 * num_sms ? launch_width<kNormRows>(a, s) : launch_width<1>(a, s);

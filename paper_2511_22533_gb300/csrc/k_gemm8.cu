@@ -13,10 +13,11 @@
 // ones in the last wave), 384 threads:
 //   warp 0      TMA producer: this CTA's 128 rows of A and half of the tile's rows of
 //               B, 128 K (a scale block, one 128-byte swizzled line per row) per stage
-//   warp 1      of the even CTA issues the copies of scales and the MMAs for both
+//   warp 1      of the even CTA issues the MMAs for both
 //   warp 2      reads scale bytes from global memory (plain rows) and lays them out
 //               for the tensor memory: 512 K of A's 128 and B's 256 rows at a time
-//   warp 3      allocates tensor memory
+//   warp 3      allocates tensor memory; of the even CTA issues the copies of scales into it, so
+//               that the MMAs' issuer, whose 128 K take some 300 clocks, has less to do
 //   warps 4-11  epilogue: each has 32 rows (its TMEM lanes) and half of the columns, stages
 //               its output and sends it by TMA; no warp waits for another
 // Tensor memory: 512 columns hold two accumulators of 256 only if nothing else is
@@ -47,6 +48,7 @@ constexpr int kSetBytes = 512 + 1024;       // scales of A's 128 rows, B's 256, 
 constexpr int kSets = 4;                    // such sets in shared memory
 constexpr int kVecBytes8 = 8 * 2 * 128 * 4; // an epilogue warp's biases and gates of a unit
 constexpr int kOutBox8 = 32 * 128;          // 32 rows of 128 bytes on their way out
+constexpr int kBarBytes8 = 320;             // mbarriers and two words
 constexpr uint32_t kTmemCols8 = 512;
 constexpr uint32_t kAcc1 = 232;             // first column of the second accumulator
 constexpr uint32_t kScaleCols = 488;        // two sets of 4 (A) + 8 (B) columns
@@ -56,7 +58,7 @@ struct Depth8 {
     int stages, boxes, b_bytes;
     size_t smem() const
     {
-        return 1024 + (size_t)stages * (kOperand8 + b_bytes) + kSets * kSetBytes + kVecBytes8 + (size_t)boxes * 8 * kOutBox8 + 256;
+        return 1024 + (size_t)stages * (kOperand8 + b_bytes) + kSets * kSetBytes + kVecBytes8 + (size_t)boxes * 8 * kOutBox8 + kBarBytes8;
     }
 };
 constexpr size_t kMostSmem8 = 227 * 1024;
@@ -261,13 +263,17 @@ __global__ void __launch_bounds__(kThreads8, 1)
     uint64_t *bars = reinterpret_cast<uint64_t *>(so + depth.boxes * 8 * kOutBox8);
     uint64_t *full = bars, *empty = full + kMaxStages8;    // operands of a stage there (even CTA) / used (both)
     uint64_t *sfull = empty + kMaxStages8, *sempty = sfull + kSets;  // scales of a set there (even CTA) / copied (both)
-    uint64_t *accf = sempty + kSets, *acce = accf + 2;     // accumulator complete (both) / read (even CTA)
+    uint64_t *tfull = sempty + kSets, *tempty = tfull + 2; // scales of a set in tensor memory / used (even CTA)
+    uint64_t *accf = tempty + 2, *acce = accf + 2;         // accumulator complete (both) / read (even CTA)
     uint64_t *shared_read = acce + 2;                      // its columns that the next one needs are read (even CTA)
-    uint64_t *drain = shared_read + 1;
+    uint64_t *drain = shared_read + 1;                     // of the MMAs, of the copies
+    uint64_t *tmem_there = drain + 2;                      // tensor memory of both CTAs (even CTA)
+    constexpr int kBars = 2 * kMaxStages8 + 2 * kSets + 4 + 4 + 1 + 2 + 1;
+    static_assert(kBars * 8 + 8 <= kBarBytes8, "barriers");
     // SPLIT has one unit and two barriers to spare: the other pair's stages are free, its
     // partial sums are here
     uint64_t *other_done = &acce[1], *parts = &accf[1];
-    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(drain + 1);
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bars + kBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -281,32 +287,29 @@ __global__ void __launch_bounds__(kThreads8, 1)
         for (int i = 0; i < 3; ++i) tma_prefetch(&tmb.rows[i]);
         tma_prefetch(&tmo);
     }
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < S; ++s) {
-            mbar_init(&full[s], 1);
-            mbar_init(&empty[s], 1);
+    if (warp == 0) {
+        for (int i = lane; i < kBars; i += 32) {
+            uint64_t *const b = bars + i;
+            uint32_t count = 1;
+            if (b >= sfull && b < sempty) count = 2;         // one scale warp in each CTA
+            if (b == tmem_there) count = 2;                  // warp 3 of each CTA
+            if (b == &accf[1] && SPLIT) count = 8;
+            if (b == &acce[0] || (b == &acce[1] && !SPLIT)) count = 16;  // eight epilogue warps in each CTA
+            if (b == shared_read) count = 8;                 // the four warps that hold the columns, in each CTA
+            mbar_init(b, count);
         }
-        for (int b = 0; b < kSets; ++b) {
-            mbar_init(&sfull[b], 2);   // one scale warp in each CTA
-            mbar_init(&sempty[b], 1);
-        }
-        mbar_init(&accf[0], 1);
-        mbar_init(&accf[1], SPLIT ? 8 : 1);
-        mbar_init(&acce[0], 16);       // eight epilogue warps in each CTA
-        mbar_init(&acce[1], SPLIT ? 1 : 16);
-        mbar_init(shared_read, 8);     // the four warps that hold the columns, in each CTA
-        mbar_init(drain, 1);
-        *abort_flag = 0;
+        if (lane == 0) *abort_flag = 0;
         fence_mbar_init();
+        __syncwarp();
     }
+    // both CTAs' barriers are initialised before any warp passes its cluster_wait(); what
+    // does not need them runs before that
+    cluster_arrive();
     if (warp == 3) {
         tmem_alloc_pair(tmem_holder, kTmemCols8);
         tmem_relinquish_pair();
+        tc_fence_before();
     }
-    tc_fence_before();
-    // both CTAs' barriers are initialised (and tensor memory allocated) before any warp
-    // passes its cluster_wait(); what needs neither runs before that
-    cluster_arrive();
     // scale blocks of a row, and the ones that this pair sums (from a whole set on)
     const int kb_all = (p.K + 127) / 128;
     const int kb_0 = SPLIT ? (int)pair * p.split_kb : 0, kb_n = SPLIT ? min(kb_all, kb_0 + p.split_kb) : kb_all;
@@ -317,64 +320,52 @@ __global__ void __launch_bounds__(kThreads8, 1)
 
     if (warp == 0) {
         cluster_wait();
-        if (lane == 0) {
-            const uint32_t full_c = mapa_shared(smem_u32(full), even);
-            int s = 0;
-            uint32_t ph = 0;
+        const uint32_t full_u = smem_u32(full), full_c = mapa_shared(full_u, even), empty_u = smem_u32(empty);
+        const uint32_t sa_u = smem_u32(sa), sb_u = smem_u32(sb), b_bytes = (uint32_t)depth.b_bytes;
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = true, ready = true;
 #pragma unroll 1
-            for (; more; more = U.next(t, ncl, m0, n0, bn)) {
-                // this CTA holds bn / 2 of the unit's B rows
-                const CUtensorMap *mb = &tmb.rows[bn == 256 ? 0 : (bn == 128 ? 1 : 2)];
-                const int row_a = m0 + (int)rank * 128, row_b = n0 + (int)rank * (bn / 2);
-                const uint32_t bytes = 2u * (kOperand8 + (uint32_t)(bn / 2) * 128);  // both CTAs
+        for (; more && ok; more = U.next(t, ncl, m0, n0, bn)) {
+            // this CTA holds bn / 2 of the unit's B rows
+            const CUtensorMap *mb = &tmb.rows[bn == 256 ? 0 : (bn == 128 ? 1 : 2)];
+            const int row_a = m0 + (int)rank * 128, row_b = n0 + (int)rank * (bn / 2);
+            const uint32_t bytes = rank == 0 ? 2u * (kOperand8 + (uint32_t)(bn / 2) * 128) : 0u;  // both CTAs
 #pragma unroll 1
-                for (int kb = kb_0; kb < kb_n; ++kb) {
-                    if (!mbar_wait(&empty[s], ph ^ 1, abort_flag, p.err)) goto produced;
-                    if (rank == 0) mbar_arrive_expect_tx(&full[s], bytes);
-                    const uint32_t fb = full_c + 8u * (uint32_t)s;
-                    tma_load_2d_pair(sa + s * kOperand8, &tma, kb * 128, row_a, fb);
-                    tma_load_2d_pair(sb + s * depth.b_bytes, mb, kb * 128, row_b, fb);
-                    if (++s == S) {
-                        s = 0;
-                        ph ^= 1;
-                    }
+            for (int kb = kb_0; kb < kb_n; ++kb) {
+                if (!warp_all(ready) && !warp_wait(&empty[s], ph ^ 1, abort_flag, p.err)) {
+                    ok = false;
+                    break;
                 }
+                const int s_next = s + 1 == S ? 0 : s + 1;
+                const uint32_t ph_next = s_next == 0 ? ph ^ 1 : ph;
+                ready = tma_load_stage_pair(sa_u + (uint32_t)s * kOperand8, &tma, row_a, sb_u + (uint32_t)s * b_bytes, mb, row_b,
+                                            kb * 128, full_u + 8u * (uint32_t)s, full_c + 8u * (uint32_t)s, bytes,
+                                            empty_u + 8u * (uint32_t)s_next, ph_next ^ 1);
+                s = s_next;
+                ph = ph_next;
             }
-        produced:;
         }
-        __syncwarp();
+        // (every arrival at this CTA's barriers is awaited before it leaves)
+        for (int i = 0; i < S && ok; ++i) {
+            ok = warp_wait(&empty[s], ph ^ 1, abort_flag, p.err);
+            if (++s == S) {
+                s = 0;
+                ph ^= 1;
+            }
+        }
     } else if (warp == 1) {
         cluster_wait();
-        tc_fence_after();
-        if (rank == 0) {
+        if (rank == 0 && warp_wait(tmem_there, 0, abort_flag, p.err)) {
+            tc_fence_after();
             const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
             const uint64_t a_desc0 = make_sdesc(smem_u32(sa), 16, 1024, kSwizzle128);
             const uint64_t b_desc0 = make_sdesc(smem_u32(sb), 16, 1024, kSwizzle128);
-            // 32 rows of 16 bytes: groups of 8 rows are 128 bytes apart
-            const uint64_t s_desc0 = make_sdesc(smem_u32(ss), 16, 128, kSwizzleNone);
-            int s = 0, it = 0, set = 0, copied = 0;
+            int s = 0, it = 0, set = 0;
             uint32_t ph = 0;
-            // Copies the next set of scales into tensor memory, its half that set
-            // copied - 2 had: that set's MMAs are over when its last stage is empty.
-            int over_s = 0;
-            uint32_t over_ph = 0;
-            auto copy_scales = [&] {
-                const int b = copied % kSets;
-                if (!warp_wait(&sfull[b], (copied / kSets) & 1, abort_flag, p.err)) return false;
-                if (copied >= 2 && !warp_wait(&empty[over_s], over_ph, abort_flag, p.err)) return false;
-                tc_fence_after();
-                const uint64_t sd = s_desc0 + (uint64_t)b * (kSetBytes >> 4);
-                const uint32_t col = tmem + kScaleCols + 12u * (uint32_t)(copied & 1);
-                tmem_cp_scales_pair(col, sd);
-                tmem_cp_scales_pair(col + 4, sd + (512 >> 4));
-                tmem_cp_scales_pair(col + 8, sd + (1024 >> 4));
-                mma_commit_pair_mc_elect(&sempty[b], both);
-                ++copied;
-                return true;
-            };
-            bool ok = !more || copy_scales();
-            // a stage's barrier is read while the MMAs of the stage before are issued
-            bool ready = warp_all(mbar_test(&full[0], 0));
+            bool ok = true;
+            // a stage's barrier (and a set's) is read while the MMAs of the stage before are issued
+            bool ready = mbar_test(&full[0], 0) && mbar_test(&tfull[0], 0);
 #pragma unroll 1
             while (more && ok) {
                 const int buf = it & 1;
@@ -385,39 +376,40 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 const uint32_t idesc0 = make_idesc_mxf8(256, 0, 0) | ((uint32_t)(bn >> 3) << 17);
                 bool another = false;
 #pragma unroll 1
-                for (int kb = kb_0; kb < kb_n; ++kb) {
+                for (int kb0 = kb_0; kb0 < kb_n && ok; kb0 += 4) {
                     const uint32_t sfa = tmem + kScaleCols + 12u * (uint32_t)(set & 1);
-                    if (!ready && !warp_wait(&full[s], ph, abort_flag, p.err)) {
-                        ok = false;
-                        break;
+                    const uint32_t setp = (set >> 1) & 1, setp_next = ((set + 1) >> 1) & 1;
+                    uint64_t *const tf = &tfull[set & 1], *const tf_next = &tfull[(set + 1) & 1];
+#pragma unroll
+                    for (uint32_t byte = 0; byte < 4; ++byte) {
+                        const int kb = kb0 + (int)byte;
+                        if (byte != 0 && kb >= kb_n) break;
+                        if (!warp_all(ready) && !((byte != 0 || warp_wait(tf, setp, abort_flag, p.err)) &&
+                                                  warp_wait(&full[s], ph, abort_flag, p.err))) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const int s_next = s + 1 == S ? 0 : s + 1;
+                        const uint32_t ph_next = s_next == 0 ? ph ^ 1 : ph;
+                        const bool last = byte == 3 || kb + 1 == kb_n;
+                        ready = mma_mxf8_pair_128k(d, a_desc0 + (uint64_t)s * (kOperand8 >> 4), b_desc0 + (uint64_t)s * (uint32_t)(depth.b_bytes >> 4),
+                                           sfa, sfa + 4, idesc0 | byte << 4 | byte << 29, byte != 0 || kb0 != kb_0, &empty[s], both,
+                                           &full[s_next], ph_next, last ? tf_next : tf, last ? setp_next : setp);
+                        s = s_next;
+                        ph = ph_next;
                     }
-                    tc_fence_after();
-                    const int s_next = s + 1 == S ? 0 : s + 1;
-                    const uint32_t ph_next = s_next == 0 ? ph ^ 1 : ph;
-                    ready = warp_all(mbar_test(&full[s_next], ph_next));
-                    const uint32_t byte = (uint32_t)(kb & 3);
-                    mma_mxf8_pair_128k(d, a_desc0 + (uint64_t)s * (kOperand8 >> 4), b_desc0 + (uint64_t)s * (uint32_t)(depth.b_bytes >> 4),
-                                       sfa, sfa + 4, idesc0 | byte << 4 | byte << 29, kb != kb_0);
-                    mma_commit_pair_mc_elect(&empty[s], both);
-                    if (kb == kb_0) another = U.next(t, ncl, m0, n0, bn);
-                    // the next set's scales are copied behind this set's first MMAs, which
-                    // keep the tensor core busy until the copies run
-                    const bool last = byte == 3 || kb + 1 == kb_n;
-                    if ((byte == 1 || last) && copied == set + 1 && ((kb | 3) + 1 < kb_n || another) && !copy_scales()) {
-                        ok = false;
-                        break;
-                    }
-                    if (last) {
-                        ++set;
-                        over_s = s;
-                        over_ph = ph;
-                    }
-                    s = s_next;
-                    ph = ph_next;
+                    mma_commit_pair_elect(tf == &tfull[0] ? &tempty[0] : &tempty[1]);
+                    ++set;
+                    if (kb0 == kb_0) another = U.next(t, ncl, m0, n0, bn);
                 }
                 if (ok) mma_commit_pair_mc_elect(&accf[buf], both);
                 ++it;
                 more = another;
+            }
+            if (!SPLIT && ok && it > 0) {
+                warp_wait(shared_read, (it - 1) & 1, abort_flag, p.err);
+                for (int i = it > 1 ? it : 2; i < it + 2; ++i) warp_wait(&acce[i & 1], ((i >> 1) & 1) ^ 1, abort_flag, p.err);
             }
             if (*abort_flag) {
                 // wait (bounded) for the MMAs in flight, which their issuing lane commits
@@ -495,6 +487,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
             }
             x = next;
         }
+        for (int i = 0; i < kSets && ok; ++i, ++n) ok = warp_wait(&sempty[n % kSets], (n / kSets & 1) ^ 1, abort_flag, p.err);
     } else if (warp >= 4) {
         // warp w: rows 32 q .. 32 q + 31 of this CTA's 128 (its TMEM lanes), one half of
         // the unit's columns (of 8-bit output a whole scale block)
@@ -535,14 +528,11 @@ __global__ void __launch_bounds__(kThreads8, 1)
             const bool from_end = !SPLIT && bn == 256 && buf == 0;
             const bool shares = half == (from_end ? 1 : 0);
             more = U.next(t, ncl, m0, n0, bn);
-            if (it == 0) {
-                cluster_wait();
-                tc_fence_after();
-                tmem = *tmem_holder + ((uint32_t)(q * 32) << 16);
-            }
-            const uint32_t acc = tmem + (buf ? kAcc1 : 0u) + (uint32_t)pair * slice + c0;
+            if (it == 0) cluster_wait();
             if (!warp_wait(&accf[buf], (it >> 1) & 1, abort_flag, p.err)) break;
             tc_fence_after();
+            if (it == 0) tmem = *tmem_holder + ((uint32_t)(q * 32) << 16);
+            const uint32_t acc = tmem + (buf ? kAcc1 : 0u) + (uint32_t)pair * slice + c0;
             // partial sums of this lane's row and this warp's columns: 16 bytes (4 columns)
             // every 128 rows
             const uint32_t part = 16u * (uint32_t)(q * 32 + lane) + 512u * (uint32_t)c0;
@@ -667,11 +657,48 @@ __global__ void __launch_bounds__(kThreads8, 1)
         if (lane == 0) bulk_wait_all();
         __syncwarp();
     } else {
+        // copies the even CTA's and its peer's sets of scales into tensor memory, by turns into
+        // the half that the set before the last had, when its MMAs are over
         cluster_wait();
+        if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(tmem_there), even));
+        __syncwarp();
+        if (rank == 0 && warp_wait(tmem_there, 0, abort_flag, p.err)) {
+            tc_fence_after();
+            // 32 rows of 16 bytes: groups of 8 rows are 128 bytes apart
+            const uint64_t s_desc0 = make_sdesc(smem_u32(ss), 16, 128, kSwizzleNone);
+            const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
+            int n = 0;
+            bool ok = true;
+#pragma unroll 1
+            for (; more && ok; more = U.next(t, ncl, m0, n0, bn)) {
+#pragma unroll 1
+                for (int kb = kb_0; kb < kb_n; kb += 4, ++n) {
+                    const int b = n % kSets, h = n & 1;
+                    ok = warp_wait(&sfull[b], (n / kSets) & 1, abort_flag, p.err) &&
+                         (n < 2 || warp_wait(&tempty[h], ((n >> 1) & 1) ^ 1, abort_flag, p.err));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t sd = s_desc0 + (uint64_t)b * (kSetBytes >> 4);
+                    const uint32_t col = tmem + kScaleCols + 12u * (uint32_t)h;
+                    tmem_cp_scales_pair(col, sd);
+                    tmem_cp_scales_pair(col + 4, sd + (512 >> 4));
+                    tmem_cp_scales_pair(col + 8, sd + (1024 >> 4));
+                    mma_commit_pair_elect(&tfull[h]);
+                    mma_commit_pair_mc_elect(&sempty[b], both);
+                }
+            }
+            if (*abort_flag) {
+                mma_commit_pair_elect(&drain[1]);
+                if (lane == 0) wait_ns8(&drain[1], 0, 100000000ull);
+                __syncwarp();
+            }
+        }
     }
-    // no CTA leaves while another may still signal its barriers, (an even CTA's MMAs)
-    // write its TMEM or (SPLIT) its shared memory
-    cluster_arrive();
+    // No CTA leaves while another may still signal its barriers, (an even CTA's MMAs) write
+    // its TMEM or (SPLIT) its shared memory.  All of that has been awaited above, and nothing
+    // is published here: a release, which waits for the warp's stores, took 1000 clocks.
+    tc_fence_before();
+    cluster_arrive_relaxed();
     cluster_wait();
     if (*abort_flag) spin_ns(200000);  // loads in flight land
     if (warp == 3) {

@@ -7,15 +7,32 @@
 
 namespace f3dc {
 
-// TMA load of a 2-D box into this CTA's shared memory whose completion is counted
-// on an mbarrier of either CTA of the pair (shared::cluster address)
-F3DC_DEV void tma_load_2d_pair(void *smem_dst, const CUtensorMap *map, int x, int y, uint32_t bar_cluster)
+// A stage of operands of a CTA pair, under one election of a converged warp: TMA loads of a
+// 2-D box of A and of B into this CTA's shared memory, whose bytes an mbarrier of the even
+// CTA counts (full_cluster, a shared::cluster address).  expect != 0: that CTA, which first
+// arrives there, announcing both CTAs' bytes.  Returns whether the phase `parity` of `next`
+// is complete, read ahead of the loads so that nothing waits for the answer.  (Address
+// arithmetic in a loop run by one lane, two loads and a wait took some 490 clocks a stage.)
+F3DC_DEV bool tma_load_stage_pair(uint32_t dst_a, const CUtensorMap *map_a, int row_a, uint32_t dst_b,
+                                  const CUtensorMap *map_b, int row_b, int x, uint32_t full, uint32_t full_cluster,
+                                  uint32_t expect, uint32_t next, uint32_t parity)
 {
+    uint32_t ok;
     asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
-        " [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(smem_dst)),
-        "l"((uint64_t)map), "r"(x), "r"(y), "r"(bar_cluster)
+        "{\n .reg .pred e, q, r;\n"
+        " mbarrier.test_wait.parity.shared::cta.b64 r, [%11], %12;\n"
+        " elect.sync _|e, 0xffffffff;\n setp.ne.b32 q, %10, 0;\n and.pred q, q, e;\n"
+        " @q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%8], %10;\n"
+        " @e cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%1], [%2, {%7, %3}], [%9];\n"
+        " @e cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%4], [%5, {%7, %6}], [%9];\n"
+        " selp.u32 %0, 1, 0, r;\n}\n"
+        : "=r"(ok)
+        : "r"(dst_a), "l"((uint64_t)map_a), "r"(row_a), "r"(dst_b), "l"((uint64_t)map_b), "r"(row_b), "r"(x), "r"(full),
+          "r"(full_cluster), "r"(expect), "r"(next), "r"(parity)
         : "memory");
+    return ok != 0;
 }
 
 // Arrival on an mbarrier of either CTA that publishes no memory: what it orders are TMEM
@@ -52,6 +69,7 @@ F3DC_DEV bool warp_wait_cluster(uint64_t *bar, uint32_t parity, volatile int *ab
 
 // the two halves of cluster_sync(), for whole warps
 F3DC_DEV void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+F3DC_DEV void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 F3DC_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // D (+)= A B^T over a CTA pair (mma_bf16_pair_128k says which rows lie where), e4m3
@@ -62,18 +80,27 @@ F3DC_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligne
 #define F3DC_MXF8(D, A, B, SA, SB, I, P) \
     " @e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [" D "], " A ", " B ", " I ", [" SA "], [" SB "], " P ";\n"
 #define F3DC_MXF8_NEXT " add.s64 a, a, 2;\n add.s64 b, b, 2;\n"
-F3DC_DEV void mma_mxf8_pair_128k(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t sfa_tmem,
-                                 uint32_t sfb_tmem, uint32_t idesc, uint32_t accumulate)
+F3DC_DEV bool mma_mxf8_pair_128k(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t sfa_tmem,
+                                 uint32_t sfb_tmem, uint32_t idesc, uint32_t accumulate, uint64_t *bar, uint16_t mask,
+                                 uint64_t *next0, uint32_t parity0, uint64_t *next1, uint32_t parity1)
 {
+    uint32_t ok;
     asm volatile(
-        "{\n .reg .pred p, e, t;\n .reg .b64 a, b;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %6, 0;\n setp.eq.b32 t, 0, 0;\n"
-        F3DC_MXF8("%0", "%1", "%2", "%3", "%4", "%5", "p")
-        " add.s64 a, %1, 2;\n add.s64 b, %2, 2;\n" F3DC_MXF8("%0", "a", "b", "%3", "%4", "%5", "t")
-        F3DC_MXF8_NEXT F3DC_MXF8("%0", "a", "b", "%3", "%4", "%5", "t")
-        F3DC_MXF8_NEXT F3DC_MXF8("%0", "a", "b", "%3", "%4", "%5", "t")
-        "}\n" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(idesc), "r"(accumulate)
+        "{\n .reg .pred p, e, t, r0, r1;\n .reg .b64 a, b;\n"
+        " mbarrier.test_wait.parity.shared::cta.b64 r0, [%10], %11;\n"
+        " mbarrier.test_wait.parity.shared::cta.b64 r1, [%12], %13;\n"
+        " elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %7, 0;\n setp.eq.b32 t, 0, 0;\n"
+        F3DC_MXF8("%1", "%2", "%3", "%4", "%5", "%6", "p")
+        " add.s64 a, %2, 2;\n add.s64 b, %3, 2;\n" F3DC_MXF8("%1", "a", "b", "%4", "%5", "%6", "t")
+        F3DC_MXF8_NEXT F3DC_MXF8("%1", "a", "b", "%4", "%5", "%6", "t")
+        F3DC_MXF8_NEXT F3DC_MXF8("%1", "a", "b", "%4", "%5", "%6", "t")
+        " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%8], %9;\n"
+        " and.pred r0, r0, r1;\n selp.u32 %0, 1, 0, r0;\n"
+        "}\n" : "=r"(ok) : "r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(idesc), "r"(accumulate), "r"(smem_u32(bar)), "h"(mask),
+        "r"(smem_u32(next0)), "r"(parity0), "r"(smem_u32(next1)), "r"(parity1)
         : "memory");
+    return ok != 0;
 }
 #undef F3DC_MXF8
 #undef F3DC_MXF8_NEXT

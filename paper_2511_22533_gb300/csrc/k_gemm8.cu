@@ -267,8 +267,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
     uint64_t *accf = tempty + 2, *acce = accf + 2;         // accumulator complete (both) / read (even CTA)
     uint64_t *shared_read = acce + 2;                      // its columns that the next one needs are read (even CTA)
     uint64_t *drain = shared_read + 1;                     // of the MMAs, of the copies
-    uint64_t *tmem_there = drain + 2;                      // tensor memory of both CTAs (even CTA)
-    constexpr int kBars = 2 * kMaxStages8 + 2 * kSets + 4 + 4 + 1 + 2 + 1;
+    uint64_t *tmem_there = drain + 2, *tmem_here = tmem_there + 1;  // tensor memory of both CTAs (even CTA), of this one
+    constexpr int kBars = 2 * kMaxStages8 + 2 * kSets + 4 + 4 + 1 + 2 + 2;
     static_assert(kBars * 8 + 8 <= kBarBytes8, "barriers");
     // SPLIT has one unit and two barriers to spare: the other pair's stages are free, its
     // partial sums are here
@@ -529,6 +529,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
             const bool shares = half == (from_end ? 1 : 0);
             more = U.next(t, ncl, m0, n0, bn);
             if (it == 0) cluster_wait();
+            if (it == 0 && !warp_wait(tmem_here, 0, abort_flag, p.err)) break;
             if (!warp_wait(&accf[buf], (it >> 1) & 1, abort_flag, p.err)) break;
             tc_fence_after();
             if (it == 0) tmem = *tmem_holder + ((uint32_t)(q * 32) << 16);
@@ -660,7 +661,10 @@ __global__ void __launch_bounds__(kThreads8, 1)
         // copies the even CTA's and its peer's sets of scales into tensor memory, by turns into
         // the half that the set before the last had, when its MMAs are over
         cluster_wait();
-        if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(tmem_there), even));
+        if (lane == 0) {
+            mbar_arrive_own_smem(mapa_shared(smem_u32(tmem_there), even));
+            mbar_arrive(tmem_here);
+        }
         __syncwarp();
         if (rank == 0 && warp_wait(tmem_there, 0, abort_flag, p.err)) {
             tc_fence_after();
@@ -764,17 +768,17 @@ cudaError_t launch_units8(const CUtensorMap *ta, const GemmPairB *tb, const CUte
 }
 
 // Width of the units of a split sum, 0: the sum is not split.  Few tiles leave clusters
-// idle that may take half of the K: it costs 2 us with units of 128 columns, 3.5 with 256
-// (64 KB per CTA change places), and saves 0.14 us per 128 K.  Whole / split, us:
-//   300 x 1024 x 4096 (units of 128) 13.4 / 10.9, 300 x 1024 x 8192 21.5 / 15.2, 300 x 2048 x
-//   2048 8.8 / 9.0; 1229 x 1024 x 4096 (256) 14.4 / 13.8, 1229 x 1024 x 8192 22.1 / 17.9, 600
-//   x 1024 x 4096 with 8-bit output, which needs whole scale blocks, 14.0 / 14.7.
+// idle that may take half of the K: it costs 2 us with units of 128 columns, 4.5 with 256
+// (64 KB per CTA change places), and saves 0.09 us per 128 K.  Whole / split, us:
+//   300 x 1024 (units of 128) x 3200 8.9 / 8.9, x 4096 10.2 / 9.0, x 8192 15.8 / 12.0; 1229 x
+//   1024 (256) x 4096 11.8 / 13.5, x 8192 17.8 / 18.1, x 16384 30.7 / 27.3; 600 x 1024 with
+//   8-bit output, which needs whole scale blocks, x 8192 16.2 / 15.7, x 16384 29.1 / 25.2.
 constexpr int kSplitBlocks = 24;  // no sum of fewer scale blocks is split
 int split_width8(int M, int N, int kb_n, bool out8, int max_clusters)
 {
     const int64_t tiles = (((int64_t)M + 255) / 256) * (((int64_t)N + 255) / 256);
     if (kb_n >= kSplitBlocks && !out8 && 2 * tiles <= max_clusters) return 128;
-    return kb_n >= (out8 ? 48 : 32) && tiles <= max_clusters ? 256 : 0;
+    return kb_n >= (out8 ? 56 : 80) && tiles <= max_clusters ? 256 : 0;
 }
 
 template <int EPI, bool OUT8>

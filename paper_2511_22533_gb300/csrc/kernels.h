@@ -384,14 +384,14 @@ cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const 
                               int epi, bool out8, cudaStream_t s);
 
 // The same product for few rows, and f3dc_gemm_fp8's rule for it: it reads the weights
-// once for every 16 rows, about 1.8 us + 0.4 us per 2^20 of them, where CTA pairs take 4.6
-// us + 0.15 to 0.26 per 128 K.  Few rows / pairs, us:
+// once for every 16 rows, about 1.8 us + 0.4 us per 2^20 of them, where CTA pairs take 4 us +
+// 0.12 to 0.26 per 128 K.  Few rows / pairs, us:
 //   M     1024 x 1024   4096 x 1024   1024 x 4096   4096 x 4096   8192 x 8192   (N x K)
-//   1     2.4 / 5.6     2.7 / 6.9     4.1 / 9.4     6.8 / 12.1    25.1 / 25.7
-//   16    2.9 / 5.7     3.4 / 6.3     5.0 / 9.5     8.2 / 10.9    29.4 / 19.4
-//   32    3.2 / 5.8     5.8 / 6.3     5.1 / 9.6     15.1 / 10.6   55.4 / 19.6
-//   64    3.3 / 5.9     10.2 / 6.6    7.8 / 9.9     26.7 / 10.7   97.5 / 19.9
-//   77    4.9 / 5.9     12.1 / 6.6    12.2 / 10.0   31.9 / 10.8   122 / 20.2
+//   1     2.5 / 5.0     2.7 / 7.2     4.1 / 8.1     6.8 / 12.5    25.0 / 34
+//   16    2.9 / 5.0     3.4 / 6.3     4.9 / 8.1     8.0 / 10.5    30.0 / 18.6
+//   32    3.2 / 5.0     5.9 / 6.3     4.9 / 8.1     14.7 / 9.5    53.4 / 18.8
+//   64    3.3 / 5.1     10.1 / 6.4    7.6 / 8.2     26.3 / 9.6    91 / 19.1
+//   77    4.9 / 5.2     12.1 / 6.9    12.0 / 8.4    31.5 / 9.7    122 / 19.2
 inline bool gemm8_few_rows(int M, int N, int K)
 {
     return M <= 64 && (int64_t)K * ((int64_t)(M + 15) / 16 * N - 2700) < 6000000;

@@ -183,6 +183,32 @@ def test_gemm_fp8(M, N, K, epi):
     assert f3dc.gemm_status() == 0
 
 
+# sums so long that two pairs share tiles of 256 columns too
+@pytest.mark.parametrize("M,N,K", [(300, 1040, 7400), (1229, 1024, 10500), (260, 2000, 16384)])
+@pytest.mark.parametrize("epi", [f3dc.EPI_GELU, f3dc.EPI_RESID, "out8"])
+def test_gemm_fp8_very_long_sums(M, N, K, epi):
+    A, sa, B, sb = operands(M, N, K, M + N + K)
+    bias = randn(N, seed=7, dtype=torch.bfloat16)
+    y, err = R.gemm(A, sa, B, sb, K, bias)
+    if epi == f3dc.EPI_RESID:
+        x0 = randn(M, N, seed=9)
+        out = x0.clone()
+        gemm8(A, sa, B, sb, K, epi, bias, None, out)
+        ref = x0.double() + y
+        assert torch.all((out.double() - ref).abs() <= 1.01 * (err + R.U32 * (y.abs() + ref.abs())))
+    elif epi == "out8":
+        q, s = R.storage(M, N, pad=1)
+        gemm8(A, sa, B, sb, K, f3dc.EPI_BIAS, bias, None, q, s)
+        R.check_out8(q, s, y, err)
+        assert torch.all(q[:, N:] == 0x55) and torch.all(s[:, R.nblocks(N):] == 0x33)
+    else:
+        out = torch.full((M, N), 7.0, dtype=torch.bfloat16, device=DEV)
+        gemm8(A, sa, B, sb, K, epi, bias, None, out)
+        y, err = R.gelu(y), R.gelu_bound(y, err)
+        assert torch.all((out.double() - y).abs() <= R.U_BF16 * y.abs() + 1.01 * err)
+    assert f3dc.gemm_status() == 0
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 16, 16), (3, 128, 128), (1, 4096, 1024), (11, 1040, 1300), (32, 144, 4096),
                                    (33, 144, 300), (129, 144, 300), (255, 1008, 1374), (300, 4096, 512), (300, 1040, 6200),
                                    (955, 1152, 1024), (4000, 2048, 256)])

@@ -524,8 +524,17 @@ def test_norm_many_rows(W, out8):
     norm_case(1301, W, f3dc.NORM_LAYER, f3dc.NORM_RMS, True, True, 3, out8, seed=W + 1, pad_cols=0 if out8 else 1)
 
 
-def test_norm_bad_groups_in_many_rows():
-    W, rows = 136, 2001
+# and so many that pairs of rows are taken at every width
+@pytest.mark.parametrize("rows,W", [(16001, 136), (9000, 264), (4201, 520), (2101, 1024), (2100, 1032), (600, 4096), (70001, 32)])
+@pytest.mark.parametrize("out8", [False, True])
+def test_norm_pairs_of_rows(rows, W, out8):
+    norm_case(rows, W, f3dc.NORM_LAYER, f3dc.NORM_LAYER, True, True, 5, out8, seed=W + 2)
+    norm_case(rows, W, f3dc.NORM_RMS, f3dc.NORM_NONE, False, False, 1, out8, seed=W + 3, alpha=1.0, pads=False)
+
+
+@pytest.mark.parametrize("rows", [2001, 16001])
+def test_norm_bad_groups_in_many_rows(rows):
+    W = 136
     x, y = randn(rows, W, seed=1), randn(rows, W, seed=2, dtype=torch.bfloat16)
     group = torch.randint(-2, 5, (rows,), generator=gen(3), device=DEV).to(torch.int32)  # 3 and 4 are behind the last
     m = randn(3, 3, W, seed=4)
@@ -543,7 +552,7 @@ def test_norm_bad_groups_in_many_rows():
     assert torch.all(((xo.double() - ref).abs() <= bound)[~left])
 
 
-@pytest.mark.parametrize("rows", [3, 1300])
+@pytest.mark.parametrize("rows", [3, 1300, 9001])
 def test_norm_offsets_past_32_bits(rows):
     W = 256
     ld = (1 << 31) // (rows - 1) // 8 * 8 + 64  # the last row lies behind 8, 4 and 2 GiB

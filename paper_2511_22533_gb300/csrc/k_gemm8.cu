@@ -62,13 +62,14 @@ struct Depth8 {
     }
 };
 constexpr size_t kMostSmem8 = 227 * 1024;
-// Short sums of full units: a unit's epilogue is as long as its sum, and the second box
-// saves it a wait; long ones: a fifth stage instead (8192 x 4096 x 4096 101 -> 98 us, 32768
-// x 1024 x 4096 residual 110 -> 103; 32768 x 4096 x 1024 121 instead of 113).  Narrow units
-// leave room for more stages: the loads' latency counts most where there is one unit.
-inline Depth8 depth8(int kb_n, int width)
+// With 8-bit output a short full unit's epilogue is longer than its sum, and the second box
+// saves it a wait (32768 x 4096 x 1024 121 us, with a fifth stage instead 125); else the fifth
+// stage counts for more (the same with 16-bit output 98 us instead of 102, 8192 x 4096 x 4096
+// 83 instead of 91).  Narrow units leave room for more stages: the loads' latency counts most
+// where there is one unit.
+inline Depth8 depth8(int kb_n, int width, bool out8)
 {
-    Depth8 d{1, kb_n >= 16 || width < 256 ? 1 : 2, width / 2 * 128};
+    Depth8 d{1, out8 && kb_n < 16 && width == 256 ? 2 : 1, width / 2 * 128};
     while (d.stages < kMaxStages8 && Depth8{d.stages + 1, d.boxes, d.b_bytes}.smem() <= kMostSmem8) ++d.stages;
     return d;
 }
@@ -500,34 +501,68 @@ __global__ void __launch_bounds__(kThreads8, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive_relaxed(bar);
         };
-        uint32_t tmem = 0;
-        if (!more) cluster_wait();  // (every warp waits once)
-#pragma unroll 1
-        for (int it = 0; more; ++it) {
-            // (a box of 128 bytes is the least that a warp stores)
-            const int slice = SPLIT ? bn / 2 : bn;  // columns that this pair finishes
-            const int buf = it & 1, width = OUT8 ? 128 : (EPI == kEpiResid ? slice / 2 : max(64, slice / 2)), c0 = half * width;
-            const int col0 = n0 + (int)pair * slice + c0;
-            o.row = m0 + (int)rank * 128 + q * 32;
-            const bool mine = o.row < p.M && c0 < slice && col0 < p.N;
-            // this unit's biases and gates, loaded while its sums run
-            if (mine) {
-                __syncwarp();
+        // columns of a unit that this pair finishes, and this warp's of them (a box of 128
+        // bytes is the least that a warp stores)
+        auto unit_slice = [&] { return SPLIT ? bn / 2 : bn; };
+        auto unit_width = [&] { return OUT8 ? 128 : (EPI == kEpiResid ? unit_slice() / 2 : max(64, unit_slice() / 2)); };
+        // A unit's biases and gates of this warp's columns are on their way a unit ahead (they
+        // took 1000 clocks of each unit): in registers, columns 32 i + lane, or with 8-bit output,
+        // which needs its registers, as they are in the place of the gates.
+        float vb[4], vg[4];
+        auto load_vectors = [&] {
+            const int width = unit_width(), col0 = n0 + (int)pair * unit_slice() + half * width;
+            if constexpr (OUT8) {
+                if (lane < 16) {
+                    if (p.bias && col0 + 8 * lane < p.N)
+                        cp_async16(smem_u32(gate) + 16u * (uint32_t)lane, p.bias + col0 + 8 * lane);
+                    else
+                        *reinterpret_cast<uint4 *>(gate + 4 * lane) = make_uint4(0u, 0u, 0u, 0u);
+                }
+            } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int c = 32 * i + lane;
                     const bool in = c < width && col0 + c < p.N;
-                    bias[c] = in && p.bias ? __bfloat162float(p.bias[col0 + c]) : 0.f;
-                    if constexpr (EPI == kEpiResid) gate[c] = in && p.gate ? p.gate[col0 + c] : 1.f;
+                    vb[i] = in && p.bias ? __bfloat162float(p.bias[col0 + c]) : 0.f;
+                    if constexpr (EPI == kEpiResid) vg[i] = in && p.gate ? p.gate[col0 + c] : 1.f;
                 }
-                __syncwarp();
             }
+        };
+        auto place_vectors = [&] {
+            if constexpr (OUT8) {
+                cp_async_wait_all();
+                __syncwarp();
+                const uint2 u = *reinterpret_cast<const uint2 *>(gate + 2 * lane);
+                *reinterpret_cast<float4 *>(bias + 4 * lane) =
+                    make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
+                                __uint_as_float(u.y & 0xFFFF0000u));
+            } else {
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    bias[32 * i + lane] = vb[i];
+                    if constexpr (EPI == kEpiResid) gate[32 * i + lane] = vg[i];
+                }
+            }
+            __syncwarp();
+        };
+        if (more) load_vectors();
+        uint32_t tmem = 0;
+        if (!more) cluster_wait();  // (every warp waits once)
+#pragma unroll 1
+        for (int it = 0; more; ++it) {
+            const int slice = unit_slice(), width = unit_width(), c0 = half * width;
+            const int buf = it & 1, col0 = n0 + (int)pair * slice + c0;
+            o.row = m0 + (int)rank * 128 + q * 32;
+            const bool mine = o.row < p.M && c0 < slice && col0 < p.N;
+            place_vectors();
             // the half that holds the 24 columns which the other accumulator shares, the
             // last ones of a full first accumulator or the first of the second, reads
             // them first
             const bool from_end = !SPLIT && bn == 256 && buf == 0;
             const bool shares = half == (from_end ? 1 : 0);
             more = U.next(t, ncl, m0, n0, bn);
+            if (more) load_vectors();
             if (it == 0) cluster_wait();
             if (it == 0 && !warp_wait(tmem_here, 0, abort_flag, p.err)) break;
             if (!warp_wait(&accf[buf], (it >> 1) & 1, abort_flag, p.err)) break;
@@ -748,7 +783,7 @@ template <int EPI, bool OUT8, bool SPLIT>
 cudaError_t launch_units8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
                           const Units8 &u, int width, int clusters, cudaStream_t s)
 {
-    const Depth8 depth = depth8(SPLIT ? p.split_kb : (p.K + 127) / 128, width);
+    const Depth8 depth = depth8(SPLIT ? p.split_kb : (p.K + 127) / 128, width, OUT8);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;

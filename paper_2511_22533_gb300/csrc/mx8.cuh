@@ -67,6 +67,13 @@ F3DC_DEV bool warp_wait_cluster(uint64_t *bar, uint32_t parity, volatile int *ab
     return ok;
 }
 
+// 16 bytes of global memory into shared memory, and the wait for this thread's
+F3DC_DEV void cp_async16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+F3DC_DEV void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // the two halves of cluster_sync(), for whole warps
 F3DC_DEV void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 F3DC_DEV void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }

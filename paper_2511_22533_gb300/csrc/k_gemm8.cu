@@ -301,11 +301,11 @@ __global__ void __launch_bounds__(kThreads8, 1)
         }
         if (lane == 0) *abort_flag = 0;
         fence_mbar_init();
-        __syncwarp();
     }
+    __syncthreads();
     // both CTAs' barriers are initialised before any warp passes its cluster_wait(); what
     // does not need them runs before that
-    cluster_arrive();
+    cluster_arrive_relaxed();
     if (warp == 3) {
         tmem_alloc_pair(tmem_holder, kTmemCols8);
         tmem_relinquish_pair();
@@ -317,12 +317,12 @@ __global__ void __launch_bounds__(kThreads8, 1)
     const int cl = blockIdx.x / (SPLIT ? 4 : 2), ncl = gridDim.x / (SPLIT ? 4 : 2);
     int t = cl - ncl, m0 = 0, n0 = 0, bn = 0;
     bool more = U.next(t, ncl, m0, n0, bn);  // this cluster's first unit
-    griddep_wait();
 
     if (warp == 0) {
-        cluster_wait();
         const uint32_t full_u = smem_u32(full), full_c = mapa_shared(full_u, even), empty_u = smem_u32(empty);
         const uint32_t sa_u = smem_u32(sa), sb_u = smem_u32(sb), b_bytes = (uint32_t)depth.b_bytes;
+        cluster_wait();
+        griddep_wait();
         int s = 0;
         uint32_t ph = 0;
         bool ok = true, ready = true;
@@ -357,6 +357,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
         }
     } else if (warp == 1) {
         cluster_wait();
+        griddep_wait();
         if (rank == 0 && warp_wait(tmem_there, 0, abort_flag, p.err)) {
             tc_fence_after();
             const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
@@ -429,31 +430,35 @@ __global__ void __launch_bounds__(kThreads8, 1)
             uint4 a[4], b[8];
         };
         const int per = p.scale_sets;
-        // the bytes of 32 COUNT rows from row0 on (rows from `rows` on read the last row's,
-        // which nothing uses)
-        auto row_bytes = [&](uint4 *w, int count, const uint8_t *sc, int64_t ld, int row0, int rows, int byte) {
-            const uint8_t *q = sc + byte;
+        const uint8_t *ra[4], *rb[8];  // this lane's rows (rows from M, N on: the last one, which nothing uses)
+        auto set_rows = [&] {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (j >= count) break;
-                const uint8_t *r = q + (int64_t)min(row0 + 32 * j + lane, rows - 1) * ld;
-                if (per == 4)
-                    w[j] = *reinterpret_cast<const uint4 *>(r);
-                else if (per == 2)
-                    *reinterpret_cast<uint2 *>(&w[j]) = *reinterpret_cast<const uint2 *>(r);
-                else
-                    w[j].x = *reinterpret_cast<const uint32_t *>(r);
+            for (int j = 0; j < 4; ++j) ra[j] = p.sa + (int64_t)min(m0 + (int)rank * 128 + 32 * j + lane, p.M - 1) * p.lda_s;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) rb[j] = p.sb + (int64_t)min(n0 + 32 * j + lane, p.N - 1) * p.ldb_s;
+        };
+        auto load_rows = [&](Group &x, int kb, auto get) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) get(x.a[j], ra[j] + kb);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) get(x.b[j], rb[j] + kb);
+            if (bn > 128) {
+#pragma unroll
+                for (int j = 4; j < 8; ++j) get(x.b[j], rb[j] + kb);
             }
         };
         auto load = [&](Group &x, int kb) {
-            row_bytes(x.a, 4, p.sa, p.lda_s, m0 + (int)rank * 128, p.M, kb);
-            if (bn > 128)
-                row_bytes(x.b, 8, p.sb, p.ldb_s, n0, p.N, kb);
+            if (per == 4)
+                load_rows(x, kb, [](uint4 &w, const uint8_t *r) { w = *reinterpret_cast<const uint4 *>(r); });
+            else if (per == 2)
+                load_rows(x, kb, [](uint4 &w, const uint8_t *r) { *reinterpret_cast<uint2 *>(&w) = *reinterpret_cast<const uint2 *>(r); });
             else
-                row_bytes(x.b, 4, p.sb, p.ldb_s, n0, p.N, kb);
+                load_rows(x, kb, [](uint4 &w, const uint8_t *r) { w.x = *reinterpret_cast<const uint32_t *>(r); });
         };
         const uint32_t sfull_c = mapa_shared(smem_u32(sfull), even);
         Group x, next;
+        if (more) set_rows();
+        griddep_wait();
         if (more) load(x, kb_0);
         cluster_wait();
         int kb = kb_0, n = 0;
@@ -482,6 +487,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     if (kb >= kb_n) {
                         kb = kb_0;
                         more = U.next(t, ncl, m0, n0, bn);
+                        if (more) set_rows();
                     }
                     if (more) load(next, kb);
                 }
@@ -546,6 +552,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
             }
             __syncwarp();
         };
+        griddep_wait();
         if (more) load_vectors();
         uint32_t tmem = 0;
         if (!more) cluster_wait();  // (every warp waits once)
@@ -696,6 +703,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
         // copies the even CTA's and its peer's sets of scales into tensor memory, by turns into
         // the half that the set before the last had, when its MMAs are over
         cluster_wait();
+        griddep_wait();
         if (lane == 0) {
             mbar_arrive_own_smem(mapa_shared(smem_u32(tmem_there), even));
             mbar_arrive(tmem_here);

@@ -4,7 +4,7 @@
 //   out[m, n] = epilogue( sum_k A[m, k] 2^ea[m, k / 128] B[n, k] 2^eb[n, k / 128] ),  M small
 //
 // Bound by the weights' bytes and, for one layer, by latency: a 256-row tensor-memory
-// tile would be nearly empty and its pipeline takes 5 us to fill and drain.  So a warp
+// tile would be nearly empty and its pipeline takes 4 us to fill and drain.  So a warp
 // takes 16 weight rows and one scale block at a time, straight from global memory into
 // registers, converts e4m3 to fp16 (exactly) and multiplies with mma.m16n8k16 (products
 // exact, fp32 sums): the weights are the 16 rows, the tokens the 8 columns.  K may be

@@ -17,7 +17,7 @@
 //   warp 2      reads scale bytes from global memory (plain rows) and lays them out
 //               for the tensor memory: 512 K of A's 128 and B's 256 rows at a time
 //   warp 3      allocates tensor memory; of the even CTA issues the copies of scales into it, so
-//               that the MMAs' issuer, whose 128 K take some 300 clocks, has less to do
+//               that the MMAs' issuer, which is what bounds narrow units, has less to do
 //   warps 4-11  epilogue: each has 32 rows (its TMEM lanes) and half of the columns, stages
 //               its output and sends it by TMA; no warp waits for another
 // Tensor memory: 512 columns hold two accumulators of 256 only if nothing else is
@@ -25,11 +25,11 @@
 // 232: the tile after may begin as soon as the epilogue has read the 24 columns that
 // the two share, which it reads first.
 //
-// 32768 x 4096 x 1024 with GELU takes 108 us (2.55 PFLOP/s), 8192 x 8192 x
-// 8192 360 (3.05), where the board's power is the bound.  With K = 1024 the tensor cores are
-// busy in 57 % of the cycles: a tile's sum is as short as its epilogue.  A few tiles take
-// 4.6 us (launch, tensor memory, first loads, epilogue) and 0.15 to 0.26 per 128 K, what an
-// SM takes in of 20 to 32 KB operands.
+// 32768 x 4096 x 1024 takes 97 us (2.83 PFLOP/s), 104 with GELU, whose epilogue is then longer
+// than a tile's sum (tensor cores busy in 63 % of the cycles); 8192 x 8192 x 8192 348 (3.16),
+// where the board's power is the bound.  A few tiles take 3.6 us (launch, first fetches, scales,
+// epilogue, exit) and per 128 K 0.18 of narrow units, what issuing their loads and MMAs takes
+// one warp each, to 0.3 of full ones, whose MMAs alone are 512 clocks.
 #include <atomic>
 
 #include <cudaTypedefs.h>

@@ -384,8 +384,8 @@ cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const 
                               int epi, bool out8, cudaStream_t s);
 
 // The same product for few rows, and f3dc_gemm_fp8's rule for it: it reads the weights
-// once for every 16 rows, about 1.8 us + 0.4 us per 2^20 of them, where CTA pairs take 4 us +
-// 0.12 to 0.26 per 128 K.  Few rows / pairs, us:
+// once for every 16 rows, about 1.8 us + 0.4 us per 2^20 of them, where CTA pairs take 3.6 us +
+// 0.18 to 0.3 per 128 K.  Few rows / pairs, us:
 //   M     1024 x 1024   4096 x 1024   1024 x 4096   4096 x 4096   8192 x 8192   (N x K)
 //   1     2.5 / 5.0     2.7 / 7.2     4.1 / 8.1     6.8 / 12.5    25.0 / 34
 //   16    2.9 / 5.0     3.4 / 6.3     4.9 / 8.1     8.0 / 10.5    30.0 / 18.6

@@ -11,9 +11,11 @@
 // permuted within an MMA as long as both operands are: a lane's 16 consecutive bytes of a
 // row serve four MMAs, so nothing is rearranged.  The sums of a block are scaled in fp32
 // and added up; the warps of a CTA share the K of their 16 weight rows and their sums are
-// added in order.  1 x 4096 x 1024 takes 2.7 us (1.5 TB/s; it would be 0.6 at a plain copy's
-// rate), 1 x 16384 x 1024 9.0 (1.9 TB/s): each warp's first loads, its sums' way through shared
-// memory and the launch cost about 1.8 us.
+// added in order.  The next two blocks of a warp are on their way (of up to 8 tokens; one
+// ahead 8192 x 8192 took 24.9 us).  1 x 4096 x 1024 takes 2.7 us (1.6 TB/s), of which the
+// launch, the first loads and the sums' way through shared memory are 1.8; 1 x 8192 x 8192
+// 18.5 (3.6 TB/s), 1 x 32768 x 8192 59 (4.5), 67 % of a plain copy's rate, where the 16 warps
+// that an SM has registers for wait for their loads (conversions removed, it was no faster).
 #include "kernels.h"
 #include "mx8.cuh"
 
@@ -134,10 +136,15 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few8(const FewArgs a)
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[t][i] = 0.f;
-    Block<NT> cur, next;
+    // blocks ahead, as far as there are registers for them
+    constexpr int kAhead = NT == 1 ? 2 : 1;
+    Block<NT> cur, next[kAhead];
     if (warp < blocks) load(cur, warp);
+#pragma unroll
+    for (int i = 0; i < kAhead - 1; ++i)
+        if (warp + (i + 1) * ks < blocks) load(next[i], warp + (i + 1) * ks);
     for (int block = warp; block < blocks; block += ks) {
-        if (block + ks < blocks) load(next, block + ks);
+        if (block + kAhead * ks < blocks) load(next[kAhead - 1], block + kAhead * ks);
         float c[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -168,7 +175,9 @@ __global__ void __launch_bounds__(32 * kFewWarps) k_few8(const FewArgs a)
                 acc[t][i] = plain ? fmaf(c[t][i], __uint_as_float(ea << 23) * __uint_as_float(eb << 23), acc[t][i])
                                   : acc[t][i] + scaled(c[t][i], ea, eb);
             }
-        cur = next;
+        cur = next[0];
+#pragma unroll
+        for (int i = 0; i < kAhead - 1; ++i) next[i] = next[i + 1];
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -238,9 +247,12 @@ cudaError_t launch_one(const FewArgs &a, int num_sms, cudaStream_t s)
     const int blocks = (a.K + kScaleBlock - 1) / kScaleBlock;
     const unsigned groups = (unsigned)((a.M + 8 * NT - 1) / (8 * NT));
     unsigned ctas = (unsigned)((a.N + kFewCols - 1) / kFewCols);
-    // Half of the warps where several CTAs share an SM: with 16 / 8 warps 1 x 1024 x 4096 (64
-    // CTAs) takes 4.1 / 5.3 us, 1 x 4096 x 4096 (256) 7.7 / 6.7
-    const int most = (int64_t)ctas * groups <= num_sms ? kFewWarps : kFewWarps / 2;
+    // Half of the warps where several CTAs share an SM, and fewer yet where there are many, so
+    // that each warp has blocks to load ahead: with 16 / 8 warps 1 x 1024 x 4096 (64 CTAs) takes
+    // 4.1 / 5.3 us, 1 x 4096 x 4096 (256) 8.1 / 5.6; with 8 / 4 1 x 16384 x 4096 (1024) 21.3 / 17.7;
+    // with 8 / 2 1 x 65536 x 1024 (4096) 31.8 / 19.9
+    const int64_t all = (int64_t)ctas * groups, share = (24 * (int64_t)num_sms - 1) / all + 1;
+    const int most = all <= num_sms ? kFewWarps : (int)(share < 2 ? 2 : (share < kFewWarps / 2 ? share : kFewWarps / 2));
     if (OUT8) ctas = (ctas + 7) / 8 * 8;  // whole clusters
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas, groups);

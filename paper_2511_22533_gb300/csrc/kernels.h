@@ -384,17 +384,19 @@ cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const 
                               int epi, bool out8, cudaStream_t s);
 
 // The same product for few rows, and f3dc_gemm_fp8's rule for it: it reads the weights
-// once for every 16 rows, about 1.8 us + 0.4 us per 2^20 of them, where CTA pairs take 3.6 us +
-// 0.18 to 0.3 per 128 K.  Few rows / pairs, us:
+// once for every 16 rows, about 1.8 us + 0.3 us per 2^20 of them (0.4 of 9 rows and more),
+// where CTA pairs take 3.6 us + 0.18 to 0.3 per 128 K.  Few rows / pairs, us:
 //   M     1024 x 1024   4096 x 1024   1024 x 4096   4096 x 4096   8192 x 8192   (N x K)
-//   1     2.5 / 5.0     2.7 / 7.2     4.1 / 8.1     6.8 / 12.5    25.0 / 34
-//   16    2.9 / 5.0     3.4 / 6.3     4.9 / 8.1     8.0 / 10.5    30.0 / 18.6
-//   32    3.2 / 5.0     5.9 / 6.3     4.9 / 8.1     14.7 / 9.5    53.4 / 18.8
-//   64    3.3 / 5.1     10.1 / 6.4    7.6 / 8.2     26.3 / 9.6    91 / 19.1
-//   77    4.9 / 5.2     12.1 / 6.9    12.0 / 8.4    31.5 / 9.7    122 / 19.2
+//   1     2.5 / 4.6     2.6 / 6.7     3.8 / 8.0     5.6 / 12.4    18.5 / 33
+//   8     2.6 / 4.6     3.0 / 6.3     3.9 / 7.8     5.7 / 10.3    19.5 / 30
+//   16    2.9 / 4.6     3.3 / 6.0     4.8 / 7.8     8.0 / 9.6     30.1 / 17.6
+//   32    3.2 / 4.7     5.8 / 5.9     4.9 / 7.9     14.7 / 9.4    52 / 17.7
+//   64    3.3 / 4.7     8.6 / 6.0     7.6 / 7.9     25.7 / 9.5    99 / 17.9
+//   77    4.8 / 4.8     10.4 / 6.0    12.0 / 8.0    32.9 / 9.5    137 / 18.0
+// and 8 x 65536 x 1024 20.7 / 20.2, 1 x 16384 x 4096 18.1 / 25, 8 x 4096 x 16384 18.7 / 19.6.
 inline bool gemm8_few_rows(int M, int N, int K)
 {
-    return M <= 64 && (int64_t)K * ((int64_t)(M + 15) / 16 * N - 2700) < 6000000;
+    return M <= 8 || (M <= 64 && (int64_t)K * ((int64_t)(M + 15) / 16 * N - 2700) < 6000000);
 }
 struct FewArgs {
     int M, N, K;

@@ -157,7 +157,7 @@ def operands(M, N, K, seed):
 SHAPES = [(1, 8, 1), (1, 128, 128), (2, 64, 31), (5, 72, 129), (8, 1024, 4096), (9, 136, 1500), (17, 4096, 1024), (32, 264, 640),
           (33, 264, 640), (127, 256, 512), (128, 264, 513), (129, 200, 640),
           (255, 1000, 1374), (256, 256, 128), (257, 512, 2048), (300, 1088, 700), (64, 4096, 1024), (1229, 4096, 384), (300, 1000, 3200), (260, 2048, 4100),
-          (1229, 1024, 4096), (70, 2056, 8000),
+          (1229, 1024, 4096), (70, 2056, 8000), (5, 8200, 4096), (8, 40000, 1100), (1, 16384, 2900), (12, 16400, 300), (7, 512, 8100),
           (1300, 4096, 256), (4096, 4096, 128), (2600, 1960, 1100)]
 
 
@@ -210,7 +210,7 @@ def test_gemm_fp8_very_long_sums(M, N, K, epi):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 16, 16), (3, 128, 128), (1, 4096, 1024), (11, 1040, 1300), (32, 144, 4096),
-                                   (33, 144, 300), (129, 144, 300), (255, 1008, 1374), (300, 4096, 512), (300, 1040, 6200),
+                                   (33, 144, 300), (129, 144, 300), (255, 1008, 1374), (300, 4096, 512), (300, 1040, 6200), (7, 8208, 4000), (2, 40000, 700),
                                    (955, 1152, 1024), (4000, 2048, 256)])
 @pytest.mark.parametrize("epi", [f3dc.EPI_BIAS, f3dc.EPI_GELU])
 def test_gemm_fp8_8bit_output(M, N, K, epi):

@@ -74,8 +74,7 @@ F3DC_DEV void cp_async16(uint32_t dst, const void *src)
 }
 F3DC_DEV void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// the two halves of cluster_sync(), for whole warps
-F3DC_DEV void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+// the two halves of a cluster barrier that publishes nothing, for whole warps
 F3DC_DEV void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 F3DC_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
@@ -83,7 +82,9 @@ F3DC_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligne
 // operands with one E8M0 scale per row and 128 K.  The scales lie in tensor memory
 // (tmem_cp_scales_pair); each MMA takes the byte of a scale column that its instruction
 // descriptor names for all of its 32 K.  The four MMAs of 128 K (32 K further is 2
-// descriptor units) under one election.
+// descriptor units) and their commit to `bar` (of the CTAs in `mask`) under one election.
+// Returns whether the phases of next0 and next1 are complete, read ahead of the MMAs so that
+// nothing waits for the answer.
 #define F3DC_MXF8(D, A, B, SA, SB, I, P) \
     " @e tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [" D "], " A ", " B ", " I ", [" SA "], [" SB "], " P ";\n"
 #define F3DC_MXF8_NEXT " add.s64 a, a, 2;\n add.s64 b, b, 2;\n"
@@ -115,7 +116,7 @@ F3DC_DEV bool mma_mxf8_pair_128k(uint32_t d_tmem, uint64_t a_desc, uint64_t b_de
 // Copies 32 rows of 16 bytes (512 consecutive bytes of shared memory, row r at 16 r)
 // of each CTA of the pair into 4 columns of its own tensor memory, the same 32 lanes
 // four times: the scale bytes of 128 matrix rows, of which row i is lane i % 32,
-// column i / 32.  Runs in issue order with the MMAs of the same thread.
+// column i / 32.
 F3DC_DEV void tmem_cp_scales_pair(uint32_t taddr, uint64_t sdesc)
 {
     asm volatile(

@@ -734,6 +734,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     mma_commit_pair_mc_elect(&sempty[b], both);
                 }
             }
+            // the last commits to tempty, which no further set waits for
+            for (int i = n > 2 ? n : 2; i < n + 2 && ok; ++i) ok = warp_wait(&tempty[i & 1], ((i >> 1) & 1) ^ 1, abort_flag, p.err);
             if (*abort_flag) {
                 mma_commit_pair_elect(&drain[1]);
                 if (lane == 0) wait_ns8(&drain[1], 0, 100000000ull);

@@ -414,6 +414,33 @@ def test_gemm_fp8_streams_and_graphs(M, N, K, epi, out8):
     assert f3dc.gemm_status() == 0
 
 
+# A CTA's barriers are awaited to their last arrival before it leaves: one, two, three and more
+# sets of scales (512 K each), whole and shared sums, launch upon launch with other kernels in
+# between whose CTAs take over the same shared memory
+def test_gemm_fp8_back_to_back_with_other_kernels():
+    N = 512
+    jobs = []
+    for i, (M, K) in enumerate([(300, 300), (70, 900), (300, 1400), (300, 4096), (1300, 2100)]):
+        ops = operands(M, N, K, 60 + i)
+        out = torch.zeros((M, N), dtype=torch.bfloat16, device=DEV)
+        gemm8(*ops, K, f3dc.EPI_BIAS, None, None, out)
+        y, err = R.gemm(*ops, K)
+        assert torch.all((out.double() - y).abs() <= R.U_BF16 * y.abs() + 1.01 * err)
+        jobs.append((ops, K, out, out.clone()))
+    a, b = randn(256, 512, seed=70, dtype=torch.bfloat16), randn(N, 512, seed=71, dtype=torch.bfloat16)
+    plain = torch.zeros((256, N), dtype=torch.bfloat16, device=DEV)
+    f3dc.gemm(a, b, None, None, plain, 256, N, 512, f3dc.EPI_BIAS)
+    want = plain.clone()
+    for _ in range(100):
+        for ops, K, out, _ in jobs:
+            gemm8(*ops, K, f3dc.EPI_BIAS, None, None, out)
+            f3dc.gemm(a, b, None, None, plain, 256, N, 512, f3dc.EPI_BIAS)
+    assert f3dc.gemm_status() == 0
+    assert torch.equal(plain, want)
+    for _, _, out, first in jobs:
+        assert torch.equal(out, first)
+
+
 FIRST_CALL_CAPTURED = """
 import sys
 sys.path[:0] = [%r, %r]

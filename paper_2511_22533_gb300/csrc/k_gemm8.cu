@@ -581,9 +581,10 @@ __global__ void __launch_bounds__(kThreads8, 1)
             const uint32_t part = 16u * (uint32_t)(q * 32 + lane) + 512u * (uint32_t)c0;
             if constexpr (SPLIT) {
                 const uint32_t other = crank ^ 2u;  // the other pair's CTA of these rows
-                if (warp == 4 && lane == 0) mbar_arrive_relaxed(mapa_shared(smem_u32(other_done), other));
+                // this CTA's stages, which the MMAs have read, may be written by the other one
+                if (warp == 4 && lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(other_done), other));
                 __syncwarp();
-                if (!warp_wait(other_done, 0, abort_flag, p.err)) break;
+                if (!warp_wait_cluster(other_done, 0, abort_flag, p.err)) break;
                 if (c0 < slice) {
                     const uint32_t from = tmem + (uint32_t)((pair ^ 1) * slice + c0), dst = mapa_shared(smem_u32(sa) + part, other);
 #pragma unroll 1

@@ -58,12 +58,16 @@ F3DC_DEV void store_cluster16(uint32_t cluster_addr, uint32_t a, uint32_t b, uin
                  : "memory");
 }
 
-// mbar_wait by a whole warp for what other CTAs of the cluster have written before their
-// arrivals (mbar_arrive_cluster)
+// mbar_wait by a whole warp for what other CTAs of the cluster have read or written before
+// their arrivals (mbar_arrive_cluster): a last look at the phase, which is over, acquires at
+// cluster scope.
 F3DC_DEV bool warp_wait_cluster(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t *err)
 {
     const bool ok = warp_wait(bar, parity, abort, err);
-    asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n}\n" ::"r"(
+                     smem_u32(bar)),
+                 "r"(parity)
+                 : "memory");
     return ok;
 }
 

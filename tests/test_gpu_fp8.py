@@ -441,6 +441,25 @@ def test_gemm_fp8_back_to_back_with_other_kernels():
         assert torch.equal(out, first)
 
 
+# Two pairs share a sum: each writes its partial sums where the other's operands were.  Many
+# launches in a row, the operands of one being another's (a stage written too early, or sums
+# read too early, would show)
+@pytest.mark.parametrize("M,N,K,epi", [(300, 1024, 4096, 0), (600, 1024, 10500, 0), (300, 1040, 7400, 2)])
+def test_gemm_fp8_shared_sums_in_a_row(M, N, K, epi):
+    ops = [operands(M, N, K, 80 + i) for i in range(3)]
+    dtype = torch.float32 if epi == 2 else torch.bfloat16
+    outs = [torch.zeros((M, N), dtype=dtype, device=DEV) for _ in range(60)]
+    for i, out in enumerate(outs):
+        gemm8(*ops[i % 3], K, epi, None, None, out)
+    for i in range(3):
+        y, err = R.gemm(*ops[i], K)
+        bound = 1.01 * err + (R.U32 if epi == 2 else R.U_BF16) * y.abs()
+        assert torch.all((outs[i].double() - y).abs() <= bound)
+    for i, out in enumerate(outs):
+        assert torch.equal(out, outs[i % 3])
+    assert f3dc.gemm_status() == 0
+
+
 FIRST_CALL_CAPTURED = """
 import sys
 sys.path[:0] = [%r, %r]

@@ -36,16 +36,15 @@ F3DC_DEV bool tma_load_stage_pair(uint32_t dst_a, const CUtensorMap *map_a, int 
 }
 
 // Arrival on an mbarrier of either CTA that publishes no memory: what it orders are TMEM
-// reads, which tcgen05.fence::before_thread_sync covers.  (A release at cluster scope takes
-// about 1000 clocks here.)
+// reads (waited for) or an allocation of TMEM, which tcgen05.fence::before_thread_sync
+// covers.  (A release at cluster scope takes about 1000 clocks behind global stores.)
 F3DC_DEV void mbar_arrive_relaxed(uint32_t cluster_addr)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
 // Arrival that publishes this CTA's shared memory, already made visible to the async proxy
-// (fence_proxy_async_smem), to the tensor core that reads it in this CTA: a release at CTA
-// scope, wherever the mbarrier lies.
+// (fence_proxy_async_smem), on an mbarrier of the same CTA: a release at CTA scope.
 F3DC_DEV void mbar_arrive_own_smem(uint32_t cluster_addr)
 {
     asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");

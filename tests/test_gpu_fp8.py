@@ -460,6 +460,23 @@ def test_gemm_fp8_shared_sums_in_a_row(M, N, K, epi):
     assert f3dc.gemm_status() == 0
 
 
+# The even CTA's tensor core reads scales that the odd one has written: launches in a row whose
+# scales are all different, in whole numbers that any stale scale would change
+@pytest.mark.parametrize("M,N,K", [(256, 128, 512), (512, 256, 1664), (2048, 1024, 2560)])
+def test_gemm_fp8_scales_of_launches_in_a_row(M, N, K):
+    A, B = (torch.full((r, K), 0x38, dtype=torch.uint8, device=DEV) for r in (M, N))  # 1.0
+    blocks = R.nblocks(K)
+    scales = [[torch.randint(124, 131, (r, -(-blocks // 4) * 4), generator=gen(90 + 2 * i + j), device=DEV).to(torch.uint8)
+               for j, r in enumerate((M, N))] for i in range(40)]
+    outs = [torch.zeros((M, N), device=DEV) for _ in scales]
+    for (sa, sb), out in zip(scales, outs):
+        gemm8(A, sa, B, sb, K, f3dc.EPI_RESID, None, None, out)
+    assert f3dc.gemm_status() == 0
+    for (sa, sb), out in zip(scales, outs):
+        # every sum is 128 times a multiple of 2^-6 and at most 128 * 20 * 2^6: exact in 24 bits
+        assert torch.equal(out.double(), 128.0 * (R.pow2(sa[:, :blocks]) @ R.pow2(sb[:, :blocks]).T))
+
+
 FIRST_CALL_CAPTURED = """
 import sys
 sys.path[:0] = [%r, %r]

@@ -8,6 +8,7 @@ built, loading raises -- there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import re
 import threading
@@ -58,19 +59,19 @@ class FaultInjection(C.Structure):
 
 class NormLayer(C.Structure):
     """The constant part of a norm_residual call; keeps its tensors (bf16
-    [width], or None) alive."""
+    [width], as everywhere also as 16-bit integers, or None) alive."""
     _fields_ = [("width", C.c_int32), ("post", C.c_int32), ("pre", C.c_int32), ("eps", C.c_float),
                 ("res_scale", C.c_float), ("post_g", C.c_void_p), ("post_b", C.c_void_p), ("pre_g", C.c_void_p),
                 ("pre_b", C.c_void_p)]
 
     def __init__(self, width, post=NORM_NONE, pre=NORM_LAYER, post_g=None, post_b=None, pre_g=None, pre_b=None,
                  eps=1e-6, res_scale=1.0):
-        super().__init__(width, post, pre, eps, res_scale, _ptr(post_g), _ptr(post_b), _ptr(pre_g), _ptr(pre_b))
         self._tensors = tuple(t for t in (post_g, post_b, pre_g, pre_b) if t is not None)
-        self._ref = C.pointer(self)
         for t in self._tensors:
-            if not t.is_cuda or t.element_size() != 2 or t.numel() < width or not t.is_contiguous():
+            if not t.is_cuda or t.dtype not in _fp8_types()["bf16"] or t.numel() < width or not t.is_contiguous():
                 raise F3dcError(1, f"gains and biases are bf16 [{width}] on a GPU: got {t.dtype} {tuple(t.shape)} on {t.device}")
+        super().__init__(width, post, pre, eps, res_scale, _ptr(post_g), _ptr(post_b), _ptr(pre_g), _ptr(pre_b))
+        self._ref = C.pointer(self)
 
 
 _lock = threading.Lock()
@@ -169,7 +170,8 @@ def _stream(stream):
         import torch
         torch.cuda.init()
         get_stream, get_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-        _current_raw_stream = lambda: get_stream(get_device())  # noqa: E731
+        # (of the only device there is without asking which one is current)
+        _current_raw_stream = functools.partial(get_stream, 0) if torch.cuda.device_count() == 1 else lambda: get_stream(get_device())
     return _current_raw_stream()
 
 
@@ -349,43 +351,74 @@ def attention(q, ldq, k, v, ldkv, out, nq, nk, heads, dh, stream=None):
 # ---------------------------------------------------------------- 8-bit linear layers
 
 _fp8_state = None
+_fp8_kinds = None
+
+
+def _fp8_types():
+    """What element types a tensor may have where the library reads or writes one
+    kind of element.  Integers of the same size hold an element's bits."""
+    global _fp8_kinds
+    if _fp8_kinds is None:
+        import torch as t
+        _fp8_kinds = {"bf16": frozenset((t.bfloat16, t.int16, t.uint16)), "fp32": frozenset((t.float32,)),
+                      "int32": frozenset((t.int32,)), "e4m3": frozenset((t.uint8, t.int8, t.float8_e4m3fn)),
+                      "scale": frozenset((t.uint8, t.int8, t.float8_e8m0fnu))}
+    return _fp8_kinds
+
+
+class _Args:
+    """The tensor arguments of a call and the kind of element of each."""
+
+    def __init__(self, **kinds):
+        self.names, self.kinds = tuple(kinds), tuple(kinds.values())
+        self.types = tuple(frozenset().union(*(_fp8_types()[k] for k in v.split(" or "))) for v in self.kinds)
+
+    def pointers(self, tensors, current):
+        """Pointers of the tensors (None: null), which must be of their types and lie on the current device."""
+        if current is None:
+            return [None if t is None else t.data_ptr() if t.dtype in types and t.is_cuda else self._refuse(tensors)
+                    for t, types in zip(tensors, self.types)]
+        here = current()
+        return [None if t is None else t.data_ptr() if t.dtype in types and t.get_device() == here and t.is_cuda else
+                self._refuse(tensors, here) for t, types in zip(tensors, self.types)]
+
+    def _refuse(self, tensors, here=0):
+        for t, types, name, kind in zip(tensors, self.types, self.names, self.kinds):
+            if t is not None and t.dtype not in types:
+                raise F3dcError(1, f"{name} is {t.dtype}: need {kind}")
+            if t is not None and not (t.is_cuda and t.get_device() == here):
+                raise F3dcError(1, f"{name} is a tensor on {t.device}, which is not the current device")
+
+
+def _fp8_args():
+    """The arguments of quantize_fp8, of gemm_fp8 by its output (16 bits, fp32, 8 bits) and of
+    norm_residual with h in 16 and in 8 bits."""
+    ops = dict(A="e4m3", a_scales="scale", Bw="e4m3", b_scales="scale", bias="bf16", gate="fp32")
+    rows = dict(x="fp32", x_out="fp32", y="bf16", gate="fp32", scale="fp32", shift="fp32", group_of_row="int32")
+    return (_Args(x="bf16 or fp32", q="e4m3", scales="scale"),
+            *(_Args(**ops, out=k, out_scales="scale") for k in ("bf16", "fp32", "e4m3")),
+            *(_Args(**rows, h=k, h_scales="scale") for k in ("bf16", "e4m3")))
 
 
 def _fp8():
-    """(calls, {dtype: F3DC_TYPE_*}, current device's getter or None where there
-    is one device only), made on first use: a call is bound by its marshalling."""
+    """(calls, their arguments, current device's getter or None where there is one
+    device only), made on first use: a call is bound by its marshalling."""
     global _fp8_state
     if _fp8_state is None:
         import torch
         torch.cuda.init()
         L = lib()
-        types = {torch.bfloat16: 0, torch.int16: 0, torch.uint16: 0, torch.float32: 1}
-        _fp8_state = ((L.f3dc_quantize_fp8, L.f3dc_gemm_fp8, L.f3dc_norm_residual), types,
+        _fp8_state = ((L.f3dc_quantize_fp8, L.f3dc_gemm_fp8, L.f3dc_norm_residual), _fp8_args(),
                       torch._C._cuda_getDevice if torch.cuda.device_count() > 1 else None)
     return _fp8_state
-
-
-def _here(tensors, current):
-    """Pointers of tensors (None: null), which must lie on the current device."""
-    out = []
-    for t in tensors:
-        if t is None:
-            out.append(None)
-        elif t.is_cuda and (current is None or t.get_device() == current()):
-            out.append(t.data_ptr())
-        else:
-            raise F3dcError(1, f"a tensor on {t.device}, which is not the current device")
-    return out
 
 
 def quantize_fp8(x, ldx, q, ldq, scales, lds, rows, cols, stream=None):
     """x [rows, cols] (bf16 or fp32; 16-bit integers are bf16 bits) -> e4m3
     bytes q and one power-of-two scale byte per row and block of 128 columns."""
-    calls, types, current = _fp8_state or _fp8()
-    px, pq, ps = _here((x, q, scales), current)
-    x_type = types.get(x.dtype) if x is not None else 0
-    if x_type is None:
-        raise F3dcError(1, f"x is {x.dtype}: need bf16 or fp32")
+    calls, args, current = _fp8_state or _fp8()
+    px, pq, ps = args[0].pointers((x, q, scales), current)
+    x_type = 1 if x is not None and x.dtype in _fp8_kinds["fp32"] else 0
     st = calls[0](px, x_type, ldx, pq, ldq, ps, lds, rows, cols, _stream(stream))
     if st:
         _check(st)
@@ -395,8 +428,9 @@ def gemm_fp8(A, lda, a_scales, ldas, Bw, ldb, b_scales, ldbs, bias, gate, out, l
              stream=None):
     """Matrix product of two 8-bit matrices with f3dc_gemm's epilogues; with
     out_scales the output is an 8-bit matrix too."""
-    calls, _, current = _fp8_state or _fp8()
-    pa, psa, pb, psb, pbias, pgate, po, pos = _here((A, a_scales, Bw, b_scales, bias, gate, out, out_scales), current)
+    calls, args, current = _fp8_state or _fp8()
+    pa, psa, pb, psb, pbias, pgate, po, pos = args[3 if out_scales is not None else 2 if epilogue == EPI_RESID else 1].pointers(
+        (A, a_scales, Bw, b_scales, bias, gate, out, out_scales), current)
     st = calls[1](pa, lda, psa, ldas, pb, ldb, psb, ldbs, pbias, pgate, po, ldo, pos, ldos, M, N, K, epilogue,
                   _stream(stream))
     if st:
@@ -407,10 +441,11 @@ def norm_residual(layer, x, ldx, x_out, ldxo, y, ldy, gate, scale, shift, ldmod,
                   ldhs, rows, stream=None):
     """x_out = alpha x + gate post(y), h = pre(x_out) (1 + scale) + shift in one
     pass (`layer`: a NormLayer); with h_scales h is an 8-bit matrix."""
-    calls, _, current = _fp8_state or _fp8()
-    px, pxo, py, pg, psc, psh, pgr, ph, phs = _here((x, x_out, y, gate, scale, shift, group_of_row, h, h_scales), current)
-    if current is not None:
-        _here(layer._tensors, current)
+    calls, args, current = _fp8_state or _fp8()
+    px, pxo, py, pg, psc, psh, pgr, ph, phs = args[4 if h_scales is None else 5].pointers(
+        (x, x_out, y, gate, scale, shift, group_of_row, h, h_scales), current)
+    if current is not None and any(t.get_device() != current() for t in layer._tensors):
+        raise F3dcError(1, "a gain or bias is on another device than the current one")
     st = calls[2](layer._ref, px, ldx, pxo, ldxo, py, ldy, pg, psc, psh, ldmod, pgr, groups, ph, ldh, phs, ldhs, rows,
                   _stream(stream))
     if st:

@@ -4,6 +4,7 @@ binding declares."""
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2511_22533_gb300 import f3dc
 
@@ -94,3 +95,101 @@ def test_no_rows_is_no_work(L):
 def test_norm_layer_layout():
     assert [getattr(f3dc.NormLayer, n).offset for n, _ in f3dc.NormLayer._fields_] == [0, 4, 8, 12, 16, 24, 32, 40, 48]
     assert C.sizeof(f3dc.NormLayer) == 56
+
+
+# Element types: the calls take pointers, so a tensor of another type would be read as what it
+# is not, and an output of narrower elements written past its end.  Tensors that say they are on
+# a GPU and calls that only record stand in for both.
+
+class Tensor:
+    def __init__(self, dtype, is_cuda=True, width=256):
+        self.dtype, self.is_cuda, self.shape, self.device = dtype, is_cuda, (width,), "cuda:0" if is_cuda else "cpu"
+
+    def data_ptr(self):
+        return P
+
+    def get_device(self):
+        return 0
+
+    def numel(self):
+        return self.shape[0]
+
+    def is_contiguous(self):
+        return True
+
+
+@pytest.fixture
+def made(monkeypatch):
+    """The calls that reach the library."""
+    made = []
+    calls = tuple(lambda *a, n=n: made.append((n, a)) or 0 for n in ("quantize", "gemm", "norm"))
+    monkeypatch.setattr(f3dc, "_fp8_state", (calls, f3dc._fp8_args(), None))
+    return made
+
+
+BF16, F16, F32, F64 = torch.bfloat16, torch.float16, torch.float32, torch.float64
+U8, E4M3, E8M0, E5M2, I32, I64 = torch.uint8, torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float8_e5m2, torch.int32, torch.int64
+
+
+def py_quantize(x=BF16, q=U8, scales=U8):
+    f3dc.quantize_fp8(Tensor(x), 256, Tensor(q), 256, Tensor(scales), 4, 3, 200, stream=0)
+
+
+def py_gemm(A=U8, sa=U8, B=U8, sb=U8, bias=BF16, gate=None, out=BF16, out_scales=None, epi=0):
+    t = [None if d is None else Tensor(d) for d in (A, sa, B, sb, bias, gate, out, out_scales)]
+    f3dc.gemm_fp8(t[0], 1024, t[1], 8, t[2], 1024, t[3], 8, t[4], t[5], t[6], 512, t[7], 4, 5, 512, 1000, epi, stream=0)
+
+
+def py_norm(x=F32, x_out=F32, y=BF16, gate=F32, scale=F32, shift=F32, group=I32, h=BF16, hs=None):
+    t = [None if d is None else Tensor(d) for d in (x, x_out, y, gate, scale, shift, group, h, hs)]
+    f3dc.norm_residual(f3dc.NormLayer(256), t[0], 256, t[1], 256, t[2], 256, t[3], t[4], t[5], 256, t[6], 1, t[7], 256, t[8], 4, 3,
+                       stream=0)
+
+
+def each(call, base, wrong):
+    return [(call, dict(base, **{k: d})) for k, ds in wrong.items() for d in ds]
+
+
+RESID, OUT8 = dict(epi=2, gate=F32, out=F32), dict(out=U8, out_scales=U8)
+
+
+@pytest.mark.parametrize("call,kw", [
+    *each(py_quantize, {}, dict(x=[F16, F64, U8, I32], q=[BF16, F32, E5M2], scales=[F32, BF16, E4M3])),
+    *each(py_gemm, {}, dict(A=[BF16, E5M2, F32], sa=[F32, I32], B=[F16, E5M2], sb=[F32, BF16], bias=[F32, F16], out=[F32, F16, U8])),
+    *each(py_gemm, dict(epi=1), dict(bias=[F32], out=[F32, F16])),
+    *each(py_gemm, RESID, dict(gate=[BF16, F16, F64], out=[BF16, F16, F64], bias=[F32])),
+    *each(py_gemm, OUT8, dict(out=[BF16, F32, E5M2], out_scales=[F32, BF16])),
+    *each(py_norm, {}, dict(x=[BF16, F16, F64], x_out=[BF16, F16, F64], y=[F32, F16], gate=[BF16, F16], scale=[BF16, F64], shift=[BF16],
+                            group=[I64, F32], h=[F32, F16, U8])),
+    *each(py_norm, dict(h=U8, hs=U8), dict(h=[BF16, E5M2], hs=[F32, I32]))])
+def test_types_are_refused(made, call, kw):
+    with pytest.raises(f3dc.F3dcError) as e:
+        call(**kw)
+    assert e.value.status == 1 and "need" in str(e.value) and not made
+
+
+@pytest.mark.parametrize("call,kw", [
+    (py_quantize, {}), (py_quantize, dict(x=F32, q=E4M3, scales=E8M0)), (py_quantize, dict(x=torch.int16)), (py_quantize, dict(x=torch.uint16)),
+    (py_gemm, {}), (py_gemm, dict(A=E4M3, sa=E8M0, B=torch.int8, sb=torch.int8, bias=None, out=torch.int16)), (py_gemm, RESID),
+    (py_gemm, OUT8), (py_gemm, dict(out=E4M3, out_scales=E8M0, epi=1)), (py_norm, {}), (py_norm, dict(h=E4M3, hs=E8M0, group=None)),
+    (py_norm, dict(x_out=None, y=None, gate=None, scale=None, shift=None))])
+def test_types_that_fit_reach_the_library(made, call, kw):
+    call(**kw)
+    assert len(made) == 1
+    if call is py_quantize:
+        assert made[0][1][1] == (1 if kw.get("x") is F32 else 0)
+
+
+@pytest.mark.parametrize("dtype", [F16, F32, U8, torch.uint32])
+def test_norm_layer_refuses_vectors_of_other_types(dtype):
+    for name in ("post_g", "post_b", "pre_g", "pre_b"):
+        with pytest.raises(f3dc.F3dcError) as e:
+            f3dc.NormLayer(256, **{name: Tensor(dtype)})
+        assert e.value.status == 1
+    f3dc.NormLayer(256, post_g=Tensor(BF16), pre_b=Tensor(torch.int16))
+
+
+def test_tensors_off_the_gpu_are_refused(made):
+    with pytest.raises(f3dc.F3dcError) as e:
+        f3dc.quantize_fp8(Tensor(BF16, is_cuda=False), 256, Tensor(U8), 256, Tensor(U8), 4, 3, 200, stream=0)
+    assert e.value.status == 1 and "device" in str(e.value) and not made

@@ -458,6 +458,8 @@ f3dc_status f3dc_quantize_fp8(const void *x, int32_t x_type, int64_t ldx, void *
  * The sum runs in fp32 on the tensor cores, which apply the scales; a NaN scale
  * makes its products NaN.  A scale product or a sum outside fp32's range
  * overflows or vanishes as fp32 does.
+ * GELU is within 2^-14 of its value, negative sums included, before the
+ * output's rounding; results below 2^-120 may be zeros.
  *   A, B: device bytes, 16-byte aligned, lda and ldb multiples of 16;
  *   a_scales, b_scales: device bytes, 4-byte aligned, ldas and ldbs multiples of
  *     4 (all ldas bytes of a row are read);

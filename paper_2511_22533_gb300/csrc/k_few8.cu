@@ -68,13 +68,6 @@ F3DC_DEV float scaled(float s, uint32_t ea, uint32_t eb)
     return s * power(e1) * power(e2);
 }
 
-F3DC_DEV float gelu1(float x)
-{
-    const float k0 = 0.7978845608028654f, k1 = 0.7978845608028654f * 0.044715f;
-    const float h = 0.5f * x;
-    return fmaf(h, tanh_fast(x * fmaf(x * x, k1, k0)), h);
-}
-
 F3DC_DEV void store_cluster(float *p, uint32_t rank, float v)
 {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_shared(smem_u32(p), rank)), "f"(v) : "memory");

@@ -159,16 +159,6 @@ F3DC_DEV bool wait_ns8(uint64_t *bar, uint32_t parity, uint64_t ns)
     return true;
 }
 
-// 0.5 x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) of two values.  tanh.approx is within
-// 2^-11 of the value, half a step of the bf16 output where it counts most.
-F3DC_DEV f32x2 gelu2(f32x2 x)
-{
-    const float k0 = 0.7978845608028654f, k1 = 0.7978845608028654f * 0.044715f;
-    const f32x2 w = ffma2(fmul2(x, x), {k1, k1}, {k0, k0});
-    const f32x2 z = fmul2(x, w), h = fmul2(x, {0.5f, 0.5f});
-    return ffma2(h, {tanh_fast(z.x), tanh_fast(z.y)}, h);
-}
-
 // Waits for this thread's TMEM loads; r's values count from here on.
 F3DC_DEV void wait_chunk(uint32_t (&r)[32])
 {

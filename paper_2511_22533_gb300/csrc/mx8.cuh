@@ -138,6 +138,26 @@ __host__ __device__ constexpr uint32_t make_idesc_mxf8(int M, int N, int scale_b
            ((uint32_t)scale_byte << 29);
 }
 
+// ---- GELU, 0.5 x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))), as x / (1 + 2^-z) with z = 2
+// sqrt(2 / pi) log2(e) (x + 0.044715 x^3): with tanh the sum cancels for negative x, and below -4
+// little that is right is left.  The quotient is within 2^-15 of the value (the rounding of
+// z, at most 128 where it counts, and both approximations); results below 2^-120 may
+// become zeros.  2^-z is infinite for very negative x, whose quotient is then zero.
+constexpr float kGelu1 = -2.302208198f, kGelu3 = kGelu1 * 0.044715f;  // -z of x and of x^3
+F3DC_DEV float rcp_fast(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+F3DC_DEV f32x2 gelu2(f32x2 x)
+{
+    const f32x2 z = fmul2(x, ffma2(fmul2(x, x), {kGelu3, kGelu3}, {kGelu1, kGelu1}));
+    const f32x2 d = fadd2({exp2_fast(z.x), exp2_fast(z.y)}, {1.f, 1.f});
+    return fmul2(x, {rcp_fast(d.x), rcp_fast(d.y)});
+}
+F3DC_DEV float gelu1(float x) { return x * rcp_fast(1.f + exp2_fast(x * fmaf(x * x, kGelu3, kGelu1))); }
+
 // ---- e4m3 with one E8M0 (power-of-two) scale per block of 128.
 // Scale byte of a block whose largest finite magnitude is `top`: the smallest e with
 // top <= 448 2^e = 1.75 2^(8 + e), as e + 127, read off top's exponent and mantissa.

@@ -226,6 +226,50 @@ def test_gemm_fp8_8bit_output(M, N, K, epi):
     assert f3dc.gemm_status() == 0
 
 
+def gelu_exact(x):
+    # without the cancellation of 1 + tanh
+    return x * torch.sigmoid(2 * (2 / np.pi) ** 0.5 * (x + 0.044715 * x ** 3))
+
+
+# GELU keeps its relative accuracy where it is small: sums around a bias far below zero, each
+# kernel, bf16 and 8-bit output (where every value of a block may be small).  The bound: what the
+# error of the sum moves the result (it is monotonic below -0.76; above, its slope is at most 1.13),
+# 2^-14 relative for the evaluation (twice what the roundings of the exponent, at most 128 * 3 *
+# 2^-24 * ln 2, and two approximations within 2^-21 can give), the output's rounding.
+@pytest.mark.parametrize("centre", [1.5, 0.0, -0.5, -1.6, -3.0, -4.0, -5.0, -6.5, -8.0, -9.0])
+@pytest.mark.parametrize("M,N,K", [(4, 256, 512), (33, 144, 640), (300, 512, 512), (300, 1024, 7400)])
+@pytest.mark.parametrize("out8", [False, True])
+def test_gemm_fp8_gelu_of_negative_sums(M, N, K, centre, out8):
+    A, sa = quantize(randn(M, K, seed=1))
+    B, sb = quantize(randn(N, K, seed=2, scale=0.1 * K ** -0.5))
+    bias = (centre + randn(N, seed=3, scale=0.05)).to(torch.bfloat16)
+    y, err = R.gemm(A, sa, B, sb, K, bias)
+    g = gelu_exact(y)
+    moved = torch.where(y < -1.0, torch.maximum((gelu_exact(y + err) - g).abs(), (gelu_exact(y - err) - g).abs()), 1.13 * err)
+    bound = moved + 2.0 ** -14 * g.abs()
+    if out8:
+        q, s = R.storage(M, N)
+        gemm8(A, sa, B, sb, K, f3dc.EPI_GELU, bias, None, q, s)
+        R.check_out8(q, s, g, bound)
+    else:
+        out = torch.zeros((M, N), dtype=torch.bfloat16, device=DEV)
+        gemm8(A, sa, B, sb, K, f3dc.EPI_GELU, bias, None, out)
+        assert torch.all((out.double() - g).abs() <= (1 + 2.0 ** -7) * bound + R.U_BF16 * g.abs())
+
+
+@pytest.mark.parametrize("M", [4, 300])
+def test_gemm_fp8_gelu_of_extremes(M):
+    N, K = 128, 128
+    A, sa, B, sb = operands(M, N, K, 9)
+    bias = torch.zeros(N, dtype=torch.bfloat16, device=DEV)
+    bias[:6] = torch.tensor([float("inf"), float("nan"), 3e38, -3e38, 1e10, -1e10])
+    out = torch.full((M, N), 7.0, dtype=torch.bfloat16, device=DEV)
+    gemm8(A, sa, B, sb, K, f3dc.EPI_GELU, bias, None, out)
+    assert torch.all(torch.isposinf(out[:, 0])) and torch.all(torch.isnan(out[:, 1]))
+    assert torch.all(out[:, 2] == bias[2]) and torch.all(out[:, 4] == bias[4])
+    assert torch.all(out[:, 3] == 0) and torch.all(out[:, 5] == 0) and torch.all(torch.isfinite(out[:, 6:].float()))
+
+
 def test_gemm_fp8_without_bias_and_gate_and_strided():
     M, N, K = 333, 520, 900
     A, sa, B, sb = operands(M, N, K, 3)

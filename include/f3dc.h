@@ -455,7 +455,9 @@ f3dc_status f3dc_quantize_fp8(const void *x, int32_t x_type, int64_t ldx, void *
  *   F3DC_EPI_BIAS, F3DC_EPI_GELU: out bf16 [M, N], or with out_scales given an
  *     8-bit matrix, quantised as f3dc_quantize_fp8 does (N % 16 == 0);
  *   F3DC_EPI_RESID: out fp32 [M, N] += gate * (acc + bias), gate nullable (1).
- * The sum runs in fp32 on the tensor cores, which apply the scales; a NaN scale
+ * The sum runs in fp32 on the tensor cores, which apply the scales and drop up to
+ * 2^-23 of it at every 32 K: it is within 2^-14 (fp32 out) or 2^-12 of the sum of
+ * |A B|, for K of any length (longer ones are summed in pieces).  A NaN scale
  * makes its products NaN.  A scale product or a sum outside fp32's range
  * overflows or vanishes as fp32 does.
  * GELU is within 2^-14 of its value, negative sums included, before the

@@ -5,9 +5,10 @@
 // A [M, K] and B [N, K] e4m3 with one power-of-two scale per row and block of 128 K.
 //
 // The scales go into the tensor cores: kind::mxf8f6f4 with block scales multiplies
-// every 32 K of a row by a scale byte held in tensor memory, so the whole K is one
-// fp32 sum in one accumulator and nothing is rescaled in registers.  A block of 128
-// is four MMAs that take the same byte; one 32-bit column of scales serves 512 K.
+// every 32 K of a row by a scale byte held in tensor memory, so K up to 16384 or 65536
+// (piece_most) is one fp32 sum in one accumulator, longer ones are pieces of that, and nothing
+// is rescaled in registers.  A block of 128 is four MMAs that take the same byte; one 32-bit
+// column of scales serves 512 K.
 //
 // Clusters of two CTAs (cta_group::2), persistent over tiles of 256 x 256 (narrower
 // ones in the last wave), 384 threads:
@@ -24,7 +25,8 @@
 // Tensor memory: 512 columns hold two accumulators of 256 only if nothing else is
 // there, but two sets of scales need 24.  So the second accumulator starts at column
 // 232: the tile after may begin as soon as the epilogue has read the 24 columns that
-// the two share, which it reads first.
+// the two share, which it reads first.  Sums in pieces have units of 128 columns, whose
+// accumulators take turns, and the sum of the pieces so far in 128 columns more.
 //
 // 32768 x 4096 x 1024 takes 97 us (2.83 PFLOP/s), 104 with GELU, whose epilogue is then longer
 // than a tile's sum (tensor cores busy in 63 % of the cycles); 8192 x 8192 x 8192 348 (3.16),
@@ -53,6 +55,7 @@ constexpr int kBarBytes8 = 320;             // mbarriers and two words
 constexpr uint32_t kTmemCols8 = 512;
 constexpr uint32_t kAcc1 = 232;             // first column of the second accumulator
 constexpr uint32_t kScaleCols = 488;        // two sets of 4 (A) + 8 (B) columns
+constexpr uint32_t kSumCols = 360;          // sums in pieces: the 128 columns behind the second accumulator's
 // What shared memory holds beside the scales: stages of operands (b_bytes of B in each,
 // this CTA's half of the widest unit's rows) and output boxes per epilogue warp.
 struct Depth8 {
@@ -110,7 +113,7 @@ struct Units8 {
         last_band = (pairs - 1) / kBand;
         last_high.set(pairs - last_band * kBand);
     }
-    // split sums: one unit of `width` columns (256 or 128) per cluster
+    // split sums and sums in pieces: units of `width` columns (256 or 128); returns their number
     int set_single(int M, int N_, int width)
     {
         set(M, N_, 1, width);  // (every unit is that wide, also behind N)
@@ -168,6 +171,22 @@ F3DC_DEV void wait_chunk(uint32_t (&r)[32])
                    "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
                    "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
                    "+r"(r[30]), "+r"(r[31])::"memory");
+}
+
+// r += 32 columns of tensor memory (fp32)
+F3DC_DEV void add_sum(uint32_t (&r)[32], uint32_t taddr)
+{
+#pragma unroll
+    for (int h = 0; h < 32; h += 16) {
+        uint32_t v[16];
+        tmem_ld16(taddr + h, v);
+        asm volatile("tcgen05.wait::ld.sync.aligned;"
+                     : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                       "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]),
+                       "+r"(v[15])::"memory");
+#pragma unroll
+        for (int j = 0; j < 16; ++j) r[h + j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(r[h + j]));
+    }
 }
 
 // acc + bias and the epilogue's function of 32 columns, in place (fp32 bits); biases
@@ -239,7 +258,10 @@ struct Stage8 {
 // of the other half go to the other pair's CTA of the same rows, into operand stages that
 // are no longer used, and are added to that CTA's own (two addends: their order does not
 // matter).
-template <int EPI, bool OUT8, bool SPLIT>
+// LONG: what a pair sums is longer than piece_most and summed in pieces of p.piece_kb blocks
+// (whole scale sets), each in an accumulator as if it were a unit; the epilogue adds them up in
+// order, in tensor memory, and finishes the unit with the last.
+template <int EPI, bool OUT8, bool SPLIT, bool LONG>
 __global__ void __launch_bounds__(kThreads8, 1)
     k_gemm8_pair(const __grid_constant__ CUtensorMap tma, const __grid_constant__ GemmPairB tmb,
                  const __grid_constant__ CUtensorMap tmo, const Units8 U, const Depth8 depth, const Gemm8Params p)
@@ -260,11 +282,12 @@ __global__ void __launch_bounds__(kThreads8, 1)
     uint64_t *shared_read = acce + 2;                      // its columns that the next one needs are read (even CTA)
     uint64_t *drain = shared_read + 1;                     // of the MMAs, of the copies
     uint64_t *tmem_there = drain + 2, *tmem_here = tmem_there + 1;  // tensor memory of both CTAs (even CTA), of this one
-    constexpr int kBars = 2 * kMaxStages8 + 2 * kSets + 4 + 4 + 1 + 2 + 2;
+    uint64_t *other_done = tmem_here + 1, *parts = other_done + 1;  // SPLIT: the other pair's stages are free, its sums are here
+    constexpr int kBars = 2 * kMaxStages8 + 2 * kSets + 4 + 4 + 1 + 2 + 2 + 2;
     static_assert(kBars * 8 + 8 <= kBarBytes8, "barriers");
-    // SPLIT has one unit and two barriers to spare: the other pair's stages are free, its
-    // partial sums are here
-    uint64_t *other_done = &acce[1], *parts = &accf[1];
+    static_assert(!(OUT8 && SPLIT && LONG), "a unit of 128 columns is one scale block");
+    constexpr bool kReuse = !SPLIT || LONG;    // accumulators are used again: their readers say so,
+    constexpr bool kShared = !SPLIT && !LONG;  // and that they have read the columns that both have
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bars + kBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
 
@@ -285,8 +308,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
             uint32_t count = 1;
             if (b >= sfull && b < sempty) count = 2 - rank;  // even: this CTA's scale warp, the odd CTA's warp 3
             if (b == tmem_there) count = 2;                  // warp 3 of each CTA
-            if (b == &accf[1] && SPLIT) count = 8;
-            if (b == &acce[0] || (b == &acce[1] && !SPLIT)) count = 16;  // eight epilogue warps in each CTA
+            if (b == parts) count = 8;                       // the eight epilogue warps of the other CTA
+            if (b == &acce[0] || b == &acce[1]) count = 16;  // eight epilogue warps in each CTA
             if (b == shared_read) count = 8;                 // the four warps that hold the columns, in each CTA
             mbar_init(b, count);
         }
@@ -361,47 +384,57 @@ __global__ void __launch_bounds__(kThreads8, 1)
             bool ready = mbar_test(&full[0], 0) && mbar_test(&tfull[0], 0);
 #pragma unroll 1
             while (more && ok) {
-                const int buf = it & 1;
-                if (it > 1 && !warp_wait(&acce[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.err)) break;
-                if (it > 0 && !warp_wait(shared_read, (it - 1) & 1, abort_flag, p.err)) break;
-                tc_fence_after();
-                const uint32_t d = tmem + (buf ? kAcc1 : 0u);
-                const uint32_t idesc0 = make_idesc_mxf8(256, 0, 0) | ((uint32_t)(bn >> 3) << 17);
                 bool another = false;
+                int kb0 = kb_0;
 #pragma unroll 1
-                for (int kb0 = kb_0; kb0 < kb_n && ok; kb0 += 4) {
-                    const uint32_t sfa = tmem + kScaleCols + 12u * (uint32_t)(set & 1);
-                    const uint32_t setp = (set >> 1) & 1, setp_next = ((set + 1) >> 1) & 1;
-                    uint64_t *const tf = &tfull[set & 1], *const tf_next = &tfull[(set + 1) & 1];
-#pragma unroll
-                    for (uint32_t byte = 0; byte < 4; ++byte) {
-                        const int kb = kb0 + (int)byte;
-                        if (byte != 0 && kb >= kb_n) break;
-                        if (!warp_all(ready) && !((byte != 0 || warp_wait(tf, setp, abort_flag, p.err)) &&
-                                                  warp_wait(&full[s], ph, abort_flag, p.err))) {
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
-                        const int s_next = s + 1 == S ? 0 : s + 1;
-                        const uint32_t ph_next = s_next == 0 ? ph ^ 1 : ph;
-                        const bool last = byte == 3 || kb + 1 == kb_n;
-                        ready = mma_mxf8_pair_128k(d, a_desc0 + (uint64_t)s * (kOperand8 >> 4), b_desc0 + (uint64_t)s * (uint32_t)(depth.b_bytes >> 4),
-                                           sfa, sfa + 4, idesc0 | byte << 4 | byte << 29, byte != 0 || kb0 != kb_0, &empty[s], both,
-                                           &full[s_next], ph_next, last ? tf_next : tf, last ? setp_next : setp);
-                        s = s_next;
-                        ph = ph_next;
+                do {  // LONG: a piece of the unit
+                    const int buf = it & 1;
+                    if ((it > 1 && !warp_wait(&acce[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.err)) ||
+                        (kShared && it > 0 && !warp_wait(shared_read, (it - 1) & 1, abort_flag, p.err))) {
+                        ok = false;
+                        break;
                     }
-                    mma_commit_pair_elect(tf == &tfull[0] ? &tempty[0] : &tempty[1]);
-                    ++set;
-                    if (kb0 == kb_0) another = U.next(t, ncl, m0, n0, bn);
-                }
-                if (ok) mma_commit_pair_mc_elect(&accf[buf], both);
-                ++it;
+                    tc_fence_after();
+                    const uint32_t d = tmem + (buf ? kAcc1 : 0u);
+                    const uint32_t idesc0 = make_idesc_mxf8(256, 0, 0) | ((uint32_t)(bn >> 3) << 17);
+                    const int first = kb0, end = LONG ? min(kb_n, kb0 + p.piece_kb) : kb_n;
+#pragma unroll 1
+                    for (; kb0 < end && ok; kb0 += 4) {
+                        const uint32_t sfa = tmem + kScaleCols + 12u * (uint32_t)(set & 1);
+                        const uint32_t setp = (set >> 1) & 1, setp_next = ((set + 1) >> 1) & 1;
+                        uint64_t *const tf = &tfull[set & 1], *const tf_next = &tfull[(set + 1) & 1];
+#pragma unroll
+                        for (uint32_t byte = 0; byte < 4; ++byte) {
+                            const int kb = kb0 + (int)byte;
+                            if (byte != 0 && kb >= kb_n) break;
+                            if (!warp_all(ready) && !((byte != 0 || warp_wait(tf, setp, abort_flag, p.err)) &&
+                                                      warp_wait(&full[s], ph, abort_flag, p.err))) {
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                            const int s_next = s + 1 == S ? 0 : s + 1;
+                            const uint32_t ph_next = s_next == 0 ? ph ^ 1 : ph;
+                            const bool last = byte == 3 || kb + 1 == kb_n;
+                            ready = mma_mxf8_pair_128k(d, a_desc0 + (uint64_t)s * (kOperand8 >> 4),
+                                                       b_desc0 + (uint64_t)s * (uint32_t)(depth.b_bytes >> 4), sfa, sfa + 4,
+                                                       idesc0 | byte << 4 | byte << 29, byte != 0 || kb0 != first, &empty[s], both,
+                                                       &full[s_next], ph_next, last ? tf_next : tf, last ? setp_next : setp);
+                            s = s_next;
+                            ph = ph_next;
+                        }
+                        mma_commit_pair_elect(tf == &tfull[0] ? &tempty[0] : &tempty[1]);
+                        ++set;
+                        // (bn is this unit's until its last piece has begun)
+                        if (kb0 == first && end == kb_n) another = U.next(t, ncl, m0, n0, bn);
+                    }
+                    if (ok) mma_commit_pair_mc_elect(&accf[buf], both);
+                    ++it;
+                } while (LONG && ok && kb0 < kb_n);
                 more = another;
             }
-            if (!SPLIT && ok && it > 0) {
-                warp_wait(shared_read, (it - 1) & 1, abort_flag, p.err);
+            if (kReuse && ok && it > 0) {
+                if (kShared) warp_wait(shared_read, (it - 1) & 1, abort_flag, p.err);
                 for (int i = it > 1 ? it : 2; i < it + 2; ++i) warp_wait(&acce[i & 1], ((i >> 1) & 1) ^ 1, abort_flag, p.err);
             }
             if (*abort_flag) {
@@ -549,23 +582,51 @@ __global__ void __launch_bounds__(kThreads8, 1)
 #pragma unroll 1
         for (int it = 0; more; ++it) {
             const int slice = unit_slice(), width = unit_width(), c0 = half * width;
-            const int buf = it & 1, col0 = n0 + (int)pair * slice + c0;
+            const int col0 = n0 + (int)pair * slice + c0;
             o.row = m0 + (int)rank * 128 + q * 32;
             const bool mine = o.row < p.M && c0 < slice && col0 < p.N;
             place_vectors();
             // the half that holds the 24 columns which the other accumulator shares, the
             // last ones of a full first accumulator or the first of the second, reads
             // them first
-            const bool from_end = !SPLIT && bn == 256 && buf == 0;
+            const bool from_end = !SPLIT && !LONG && bn == 256 && (it & 1) == 0;
             const bool shares = half == (from_end ? 1 : 0);
             more = U.next(t, ncl, m0, n0, bn);
             if (more) load_vectors();
             if (it == 0) cluster_wait();
             if (it == 0 && !warp_wait(tmem_here, 0, abort_flag, p.err)) break;
+            if constexpr (LONG) {
+                // All pieces but the last: this warp's columns of both slices are added up.
+                if (it == 0) tmem = *tmem_holder + ((uint32_t)(q * 32) << 16);
+                bool ok = true;
+                const int last = it + (kb_n - kb_0 - 1) / p.piece_kb;
+#pragma unroll 1
+                for (const int first = it; it < last; ++it) {
+                    ok = warp_wait(&accf[it & 1], (it >> 1) & 1, abort_flag, p.err);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = c0; c < c0 + width && c0 < slice; c += 32)
+#pragma unroll 1
+                        for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+                            const uint32_t x = tmem + (uint32_t)(h * slice + c);
+                            uint32_t r[32];
+                            tmem_ld32(x + (it & 1 ? kAcc1 : 0u), r);
+                            wait_chunk(r);
+                            if (it != first) add_sum(r, x + kSumCols);
+                            tmem_st32(x + kSumCols, r);
+                        }
+                    tmem_wait_st();
+                    arrive(acce_c + 8u * (uint32_t)(it & 1));
+                }
+                if (!ok) break;
+            }
+            const int buf = it & 1;
             if (!warp_wait(&accf[buf], (it >> 1) & 1, abort_flag, p.err)) break;
             tc_fence_after();
-            if (it == 0) tmem = *tmem_holder + ((uint32_t)(q * 32) << 16);
+            if (!LONG && it == 0) tmem = *tmem_holder + ((uint32_t)(q * 32) << 16);
             const uint32_t acc = tmem + (buf ? kAcc1 : 0u) + (uint32_t)pair * slice + c0;
+            const uint32_t sum = tmem + kSumCols + (uint32_t)pair * slice + c0;  // LONG
             // partial sums of this lane's row and this warp's columns: 16 bytes (4 columns)
             // every 128 rows
             const uint32_t part = 16u * (uint32_t)(q * 32 + lane) + 512u * (uint32_t)c0;
@@ -576,12 +637,13 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 __syncwarp();
                 if (!warp_wait_cluster(other_done, 0, abort_flag, p.err)) break;
                 if (c0 < slice) {
-                    const uint32_t from = tmem + (uint32_t)((pair ^ 1) * slice + c0), dst = mapa_shared(smem_u32(sa) + part, other);
+                    const uint32_t from = (uint32_t)((pair ^ 1) * slice + c0), dst = mapa_shared(smem_u32(sa) + part, other);
 #pragma unroll 1
                     for (int c = 0; c < width; c += 32) {
                         uint32_t r[32];
-                        tmem_ld32(from + c, r);
+                        tmem_ld32(tmem + (buf ? kAcc1 : 0u) + from + c, r);
                         wait_chunk(r);
+                        if constexpr (LONG) add_sum(r, tmem + kSumCols + from + c);
 #pragma unroll
                         for (int j = 0; j < 32; j += 4)
                             store_cluster16(dst + 512u * (uint32_t)(c + j), r[j], r[j + 1], r[j + 2], r[j + 3]);
@@ -591,8 +653,9 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(parts), other));
                 if (!warp_wait_cluster(parts, 0, abort_flag, p.err)) break;
             }
-            // adds the other pair's sums of columns c .. c + 31
+            // adds the earlier pieces' and the other pair's sums of columns c .. c + 31
             auto join = [&](uint32_t (&r)[32], int c) {
+                if constexpr (LONG) add_sum(r, sum + c);
                 if constexpr (SPLIT) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
@@ -605,8 +668,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 }
             };
             if (!mine) {
-                if (!SPLIT && shares) arrive(shared_c);
-                if (!SPLIT) arrive(acce_c + 8u * (uint32_t)buf);
+                if (kShared && shares) arrive(shared_c);
+                if (kReuse) arrive(acce_c + 8u * (uint32_t)buf);
                 continue;
             }
             if constexpr (OUT8) {
@@ -619,8 +682,8 @@ __global__ void __launch_bounds__(kThreads8, 1)
                     uint32_t r[32];
                     tmem_ld32(acc + 32 * chunk(i), r);
                     wait_chunk(r);
-                    if (!SPLIT && i == 0 && shares) arrive(shared_c);
-                    if (!SPLIT && i == 3) arrive(acce_c + 8u * (uint32_t)buf);
+                    if (kShared && i == 0 && shares) arrive(shared_c);
+                    if (kReuse && i == 3) arrive(acce_c + 8u * (uint32_t)buf);
                     join(r, 32 * chunk(i));
                     apply<EPI>(r, bias + 32 * chunk(i), gate);
 #pragma unroll
@@ -666,12 +729,12 @@ __global__ void __launch_bounds__(kThreads8, 1)
                 uint32_t a[32], b[32];
                 tmem_ld32(acc + at(0), a);
                 wait_chunk(a);
-                if (!SPLIT && shares) arrive(shared_c);
+                if (kShared && shares) arrive(shared_c);
 #pragma unroll 1
                 for (int i = 0; i < chunks; i += 2) {
                     if (i + 1 < chunks)
                         tmem_ld32(acc + at(i + 1), b);
-                    else if (!SPLIT)
+                    else if (kReuse)
                         arrive(acce_c + 8u * (uint32_t)buf);
                     if constexpr (EPI != kEpiResid) o.begin();
                     finish(a, at(i));
@@ -679,7 +742,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
                         wait_chunk(b);
                         if (i + 2 < chunks)
                             tmem_ld32(acc + at(i + 2), a);
-                        else if (!SPLIT)
+                        else if (kReuse)
                             arrive(acce_c + 8u * (uint32_t)buf);
                         finish(b, at(i + 1));
                         if (i + 2 < chunks) wait_chunk(a);
@@ -771,7 +834,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
 
 // Resident clusters of 2 (SPLIT: 4) CTAs on the current device.  They are counted, and the
 // kernel's shared-memory attribute set, on each device's first launch (0 = not yet).
-template <int EPI, bool OUT8, bool SPLIT>
+template <int EPI, bool OUT8, bool SPLIT, bool LONG>
 cudaError_t resident8(int *clusters)
 {
     static std::atomic<int> max_clusters_of[64];
@@ -780,7 +843,7 @@ cudaError_t resident8(int *clusters)
     if (e != cudaSuccess) return e;
     *clusters = max_clusters_of[dev & 63].load(std::memory_order_acquire);
     if (*clusters) return cudaSuccess;
-    e = cudaFuncSetAttribute(k_gemm8_pair<EPI, OUT8, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem8);
+    e = cudaFuncSetAttribute(k_gemm8_pair<EPI, OUT8, SPLIT, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem8);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
@@ -794,7 +857,7 @@ cudaError_t resident8(int *clusters)
     cfg.attrs = at;
     cfg.numAttrs = 1;
     int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, k_gemm8_pair<EPI, OUT8, SPLIT>, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&n, k_gemm8_pair<EPI, OUT8, SPLIT, LONG>, &cfg);
     if (e != cudaSuccess) return e;
     if (n < 1) return cudaErrorInvalidConfiguration;
     max_clusters_of[dev & 63].store(n, std::memory_order_release);
@@ -802,7 +865,7 @@ cudaError_t resident8(int *clusters)
     return cudaSuccess;
 }
 
-template <int EPI, bool OUT8, bool SPLIT>
+template <int EPI, bool OUT8, bool SPLIT, bool LONG>
 cudaError_t launch_units8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
                           const Units8 &u, int width, int clusters, cudaStream_t s)
 {
@@ -821,7 +884,7 @@ cudaError_t launch_units8(const CUtensorMap *ta, const GemmPairB *tb, const CUte
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_gemm8_pair<EPI, OUT8, SPLIT>, *ta, *tb, *to, u, depth, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_gemm8_pair<EPI, OUT8, SPLIT, LONG>, *ta, *tb, *to, u, depth, p);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -839,32 +902,69 @@ int split_width8(int M, int N, int kb_n, bool out8, int max_clusters)
     return kb_n >= (out8 ? 56 : 80) && tiles <= max_clusters ? 256 : 0;
 }
 
+// A pair's sum of kb blocks, more than piece_most, is taken in pieces of that length or a little
+// less.  Every MMA adds 32 K to the accumulator and drops what is below its last bit, downwards
+// in magnitude (at most 2^-23), so the error of a sum of one sign grows with its length, and
+// faster than that: 0.9e-6 at 4096 K, 4.8e-6 at 16384, 2.6e-5 at 65536, 1.6e-4 at 262144.
+// Outputs of 16 and 8 bits, whose own rounding is 4e-3 and more, take 65536 K at once, fp32
+// ones 16384: pieces have units of 128 columns only (4096 x 4096 x 32768 470 us instead of 366; of
+// few tiles, narrow anyway, as long as before: 300 x 1024 x 65536 69 us).
+template <int EPI>
+constexpr int piece_most = EPI == kEpiResid ? 128 : 512;
+inline int piece_blocks(int kb, int most)
+{
+    const int pieces = (kb - 1) / most + 1;
+    return ((kb - 1) / pieces / 4 + 1) * 4;  // whole scale sets
+}
+
+template <int EPI, bool OUT8, bool SPLIT, bool LONG>
+cudaError_t launch_sum8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, Gemm8Params p, int width, cudaStream_t s)
+{
+    int max_clusters = 0;
+    const cudaError_t e = resident8<EPI, OUT8, SPLIT, LONG>(&max_clusters);
+    if (e != cudaSuccess) return e;
+    Units8 u;
+    const int n = u.set_single(p.M, p.N, width);
+    // (a cluster of two pairs takes one unit)
+    return launch_units8<EPI, OUT8, SPLIT, LONG>(ta, tb, to, p, u, width, SPLIT || n < max_clusters ? n : max_clusters, s);
+}
+
 template <int EPI, bool OUT8>
 cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, Gemm8Params p, cudaStream_t s)
 {
-    Units8 u;
     int max_clusters = 0;
     const int kb_n = (p.K + 127) / 128;
     cudaError_t e;
     if (kb_n >= kSplitBlocks) {
-        e = resident8<EPI, OUT8, true>(&max_clusters);
+        e = resident8<EPI, OUT8, true, false>(&max_clusters);
         if (e != cudaSuccess) return e;
-        if (const int width = split_width8(p.M, p.N, kb_n, OUT8, max_clusters)) {
-            p.split_kb = ((kb_n + 1) / 2 + 3) / 4 * 4;
+        const int width = split_width8(p.M, p.N, kb_n, OUT8, max_clusters);
+        const int half = ((kb_n + 1) / 2 + 3) / 4 * 4;
+        const bool pieces = half > piece_most<EPI>;
+        if (width && !(pieces && width == 256)) {  // (pieces of 256 columns have no place in tensor memory)
+            p.split_kb = half;
             // the second pair's scale bytes start there: they are read as far as that is aligned
             while (p.split_kb % (4 * p.scale_sets) != 0) p.scale_sets /= 2;
-            const int n = u.set_single(p.M, p.N, width);
-            return launch_units8<EPI, OUT8, true>(ta, tb, to, p, u, width, n, s);
+            if (!pieces) return launch_sum8<EPI, OUT8, true, false>(ta, tb, to, p, width, s);
+            if constexpr (!OUT8) {
+                p.piece_kb = piece_blocks(half, piece_most<EPI>);
+                return launch_sum8<EPI, OUT8, true, true>(ta, tb, to, p, width, s);
+            }
         }
     }
-    e = resident8<EPI, OUT8, false>(&max_clusters);
+    if (kb_n > piece_most<EPI>) {
+        p.piece_kb = piece_blocks(kb_n, piece_most<EPI>);
+        return launch_sum8<EPI, OUT8, false, true>(ta, tb, to, p, 128, s);
+    }
+    e = resident8<EPI, OUT8, false, false>(&max_clusters);
     if (e != cudaSuccess) return e;
     // units: 64 columns (128 with 8-bit output) are the smallest
     constexpr int width = OUT8 ? 128 : 64;
     const int64_t units = (((int64_t)p.M + 255) / 256) * (((int64_t)p.N + width - 1) / width);
     const int clusters = units < max_clusters ? (int)units : max_clusters;
+    Units8 u;
     u.set(p.M, p.N, clusters, width);
-    return launch_units8<EPI, OUT8, false>(ta, tb, to, p, u, u.full ? 256 : 256 / u.sub, clusters, s);
+    return launch_units8<EPI, OUT8, false, false>(ta, tb, to, p, u, u.full ? 256 : 256 / u.sub, clusters, s);
 }
 
 }  // namespace

@@ -376,6 +376,7 @@ struct Gemm8Params {
     uint8_t *out_scales;      // 8-bit output
     int64_t ldo_s;
     int split_kb;             // set by the launch: a split sum's first pair takes so many blocks
+    int piece_kb;             // set by the launch: a long sum is taken in pieces of so many
     uint32_t *err;
 };
 // ta: A in boxes of 128 rows; tb: B in boxes of 128, 64 and 32 rows; to: the output in

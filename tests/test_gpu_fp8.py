@@ -367,6 +367,87 @@ def test_gemm_fp8_long_positive_sums(M, N, K):
     assert torch.all((out.double() - y).abs() <= err + R.U32 * y)
 
 
+# Sums of one sign, however long, stay within 2^-14 with fp32 output and 2^-12 with others: the
+# tensor core may drop 2^-23 of the sum at each 32 K, no accumulator takes more than 16384 or 65536
+# K, and the pieces add one rounding each, fewer than 2^5 of them here (the few rows' kernel adds
+# rounded blocks: with 16 warps fewer than 2^8).  Few tiles (shared by two pairs), many, few rows; just
+# above the longest single sums; an uneven last piece.
+def piece_error(fp32):
+    return (2.0 ** -14 if fp32 else 2.0 ** -12) + 2.0 ** 8 * R.U32
+
+
+@pytest.mark.parametrize("M,N,K", [(4, 64, 1 << 18), (70, 136, 1 << 18), (300, 520, 1 << 17), (1300, 2048, 40000), (2600, 2056, 16400),
+                                   (2600, 2048, 32768), (300, 1024, 32896), (300, 1024, 40000), (1300, 2048, 65664)])
+@pytest.mark.parametrize("out8", [False, True])
+def test_gemm_fp8_sums_of_one_sign_however_long(M, N, K, out8):
+    N = N // 16 * 16 if out8 else N
+    A, sa = quantize(randn(M, K, seed=1).abs())
+    B, sb = quantize(randn(N, K, seed=2).abs())
+    y, _ = R.gemm(A, sa, B, sb, K)
+    err = piece_error(not out8) * y
+    if out8:
+        q, s = R.storage(M, N, pad=1)
+        gemm8(A, sa, B, sb, K, f3dc.EPI_BIAS, None, None, q, s)
+        R.check_out8(q, s, y, err)
+        assert torch.all(q[:, N:] == 0x55) and torch.all(s[:, R.nblocks(N):] == 0x33)
+    else:
+        out = torch.zeros((M, N), device=DEV)
+        gemm8(A, sa, B, sb, K, f3dc.EPI_RESID, None, None, out)
+        assert torch.all((out.double() - y).abs() <= err + R.U32 * y)
+    assert f3dc.gemm_status() == 0
+
+
+# sums in pieces with each epilogue, of either sign, with bias and gate, and again
+@pytest.mark.parametrize("M,N,K", [(70, 264, 66000), (300, 1040, 140000), (1229, 3000, 16500), (1229, 2056, 66100), (9, 8200, 16640),
+                                   (300, 1040, 70000)])
+@pytest.mark.parametrize("epi", [f3dc.EPI_BIAS, f3dc.EPI_GELU, f3dc.EPI_RESID, "out8"])
+def test_gemm_fp8_sums_in_pieces(M, N, K, epi):
+    N = N // 16 * 16 if epi == "out8" else N
+    A, sa, B, sb = operands(M, N, K, M + N + K)
+    bias, gate, x0 = randn(N, seed=7, dtype=torch.bfloat16), randn(N, seed=8), randn(M, N, seed=9)
+    y, _ = R.gemm(A, sa, B, sb, K, bias)
+    mag = R.values(A, sa, K).abs() @ R.values(B, sb, K).abs().T
+    err = piece_error(epi == f3dc.EPI_RESID) * mag + R.U32 * (mag + bias.double().abs())
+    outs = []
+    for _ in range(2):
+        if epi == "out8":
+            q, s = R.storage(M, N, pad=1)
+            gemm8(A, sa, B, sb, K, f3dc.EPI_GELU, bias, None, q, s)
+            outs.append(torch.cat([q.flatten(), s.flatten()]))
+        else:
+            out = x0.clone() if epi == f3dc.EPI_RESID else torch.zeros((M, N), dtype=torch.bfloat16, device=DEV)
+            gemm8(A, sa, B, sb, K, epi, bias, gate if epi == f3dc.EPI_RESID else None, out)
+            outs.append(out)
+    assert torch.equal(outs[0], outs[1])
+    g = gelu_exact(y)
+    moved = 1.13 * err + 2.0 ** -14 * g.abs()
+    if epi == "out8":
+        step = R.pow2(s[:, :R.nblocks(N)]).repeat_interleave(R.BLOCK, 1)[:, :N]
+        bound = R.U_E4M3 * g.abs() + 0.5 * R.E4M3_MIN * step + (1 + R.U_E4M3) * moved
+        assert torch.all((R.values(q, s, N) - g).abs() <= bound)
+        assert torch.all(q[:, N:] == 0x55) and torch.all(s[:, R.nblocks(N):] == 0x33)
+    elif epi == f3dc.EPI_GELU:
+        assert torch.all((out.double() - g).abs() <= (1 + 2.0 ** -7) * moved + R.U_BF16 * g.abs())
+    elif epi == f3dc.EPI_BIAS:
+        assert torch.all((out.double() - y).abs() <= (1 + 2.0 ** -7) * err + R.U_BF16 * y.abs())
+    else:
+        ref = x0.double() + gate.double() * y
+        bound = gate.double().abs() * err + R.U32 * ((gate.double() * y).abs() + ref.abs())
+        assert torch.all((out.double() - ref).abs() <= 1.01 * bound)
+    assert f3dc.gemm_status() == 0
+
+
+def test_gemm_fp8_longest_sum():
+    # ones: every partial sum is a whole number, the last one 2^26
+    M, N, K = 65, 8, 1 << 26
+    A, B = (torch.full((r, K), 0x38, dtype=torch.uint8, device=DEV) for r in (M, N))
+    sa, sb = (torch.full((r, K // 128), 127, dtype=torch.uint8, device=DEV) for r in (M, N))
+    out = torch.zeros((M, N), device=DEV)
+    gemm8(A, sa, B, sb, K, f3dc.EPI_RESID, None, None, out)
+    assert torch.all(out == float(K))
+    assert f3dc.gemm_status() == 0
+
+
 # rows and scales more than 4 GiB apart from the first, in both kernels
 @pytest.mark.parametrize("M,N,K", [(3, 40, 200), (200, 264, 200), (300, 256, 4096)])
 @pytest.mark.parametrize("out8", [False, True])

@@ -332,19 +332,18 @@ __global__ void __launch_bounds__(32 * NW, kNormRunThreadsPerSm / (32 * NW)) k_n
         int g;
     };
     const float *px = a.x + row0 * a.ldx + col;
-    const bf16 *py = a.y + row0 * a.ldy + col;
-    const int32_t *pg = a.group + row0;
+    const bf16 *py = a.y ? a.y + row0 * a.ldy + col : nullptr;
+    const int32_t *pg = a.group ? a.group + row0 : nullptr;
     auto load = [&](Row &r) {
         r.x[0] = r.x[1] = r.y = make_uint4(0u, 0u, 0u, 0u);
-        r.g = a.group ? *pg : 0;
+        r.g = a.group ? *pg++ : 0;
         if (in) {
             r.x[0] = row_load16(px);
             r.x[1] = row_load16(px + 4);
             if (a.y) r.y = row_load16(py);
         }
+        if (a.y) py += a.ldy;
         px += a.ldx;
-        py += a.ldy;
-        ++pg;
     };
     Row cur, next;
     if (row0 < end) load(cur);

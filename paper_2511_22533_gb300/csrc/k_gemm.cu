@@ -1045,7 +1045,8 @@ cudaError_t launch_bn(const CUtensorMap *ta, const CUtensorMap *tb, const CUtens
 
 PFN_cuTensorMapEncodeTiled_v12000 tmap_encoder()
 {
-    static PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
+    static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> encoder{nullptr};
+    PFN_cuTensorMapEncodeTiled_v12000 encode = encoder.load(std::memory_order_acquire);
     if (!encode) {
         cudaDriverEntryPointQueryResult q;
         void *fn = nullptr;
@@ -1054,6 +1055,7 @@ PFN_cuTensorMapEncodeTiled_v12000 tmap_encoder()
             q != cudaDriverEntryPointSuccess || !fn)
             return nullptr;
         encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+        encoder.store(encode, std::memory_order_release);
     }
     return encode;
 }
@@ -1152,6 +1154,20 @@ bool make_tmap_pair_b(GemmPairB *maps, const void *base, uint64_t rows, uint64_t
 {
     return make_tmap_pair(&maps->rows[0], base, rows, K, 128) && make_tmap_pair(&maps->rows[1], base, rows, K, 64) &&
            make_tmap_pair(&maps->rows[2], base, rows, K, 32);
+}
+
+bool make_tmap_rows(CUtensorMap *map, CUtensorMapDataType type, const void *base, uint64_t rows, uint64_t cols,
+                    uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 encode = tmap_encoder();
+    if (!encode) return false;
+    cuuint64_t dims[2] = {cols, rows};
+    cuuint64_t strides[1] = {row_bytes};
+    cuuint32_t box[2] = {box_cols, box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    return encode(map, type, 2, const_cast<void *>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool make_tmap_bf16(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint64_t ld,

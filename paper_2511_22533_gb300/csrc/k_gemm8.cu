@@ -35,8 +35,6 @@
 // one warp each, to 0.3 of full ones, whose MMAs alone are 512 clocks.
 #include <atomic>
 
-#include <cudaTypedefs.h>
-
 #include "kernels.h"
 #include "mx8.cuh"
 
@@ -968,30 +966,6 @@ cudaError_t launch_one8(const CUtensorMap *ta, const GemmPairB *tb, const CUtens
 }
 
 }  // namespace
-
-bool make_tmap_rows(CUtensorMap *map, CUtensorMapDataType type, const void *base, uint64_t rows, uint64_t cols,
-                    uint64_t row_bytes, uint32_t box_rows, uint32_t box_cols)
-{
-    static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> encoder{nullptr};
-    PFN_cuTensorMapEncodeTiled_v12000 encode = encoder.load(std::memory_order_acquire);
-    if (!encode) {
-        cudaDriverEntryPointQueryResult q;
-        void *fn = nullptr;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) !=
-                cudaSuccess ||
-            q != cudaDriverEntryPointSuccess || !fn)
-            return false;
-        encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
-        encoder.store(encode, std::memory_order_release);
-    }
-    cuuint64_t dims[2] = {cols, rows};
-    cuuint64_t strides[1] = {row_bytes};
-    cuuint32_t box[2] = {box_cols, box_rows};
-    cuuint32_t estr[2] = {1, 1};
-    return encode(map, type, 2, const_cast<void *>(base), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 
 cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p, int epi, bool out8,
                               cudaStream_t s)

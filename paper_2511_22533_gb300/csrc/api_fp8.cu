@@ -27,6 +27,8 @@ bool misaligned(const void *p, int n) { return ((uintptr_t)p & (n - 1)) != 0; }
 
 int blocks(int cols) { return (cols - 1) / kScaleBlock + 1; }
 
+static_assert(noexcept(gemm_status_word()), "nothing may throw through these calls");
+
 cudaError_t sm_count(int *sms)
 {
     int dev = 0;

@@ -336,7 +336,7 @@ FaultInjection &fault_injection();
 // (f3dc_gemm, f3dc_gemm_noalloc, f3dc_attention; read by f3dc_gemm_status), or null if
 // it cannot be resolved.  The word is a static device variable, not an
 // allocation.
-uint32_t *gemm_status_word();
+uint32_t *gemm_status_word() noexcept;
 
 // 2-D bf16 tensor map over a row-major [rows, cols] matrix with leading
 // dimension ld (elements), box [box_rows, box_cols], 128B (box_cols = 64) or

@@ -85,10 +85,14 @@ cudaError_t device_syms(DeviceSyms *out)
 
 }  // namespace
 
-uint32_t *f3dc::gemm_status_word()
+uint32_t *f3dc::gemm_status_word() noexcept
 {
-    DeviceSyms s;
-    return device_syms(&s) == cudaSuccess ? s.status : nullptr;
+    try {
+        DeviceSyms s;
+        return device_syms(&s) == cudaSuccess ? s.status : nullptr;
+    } catch (...) {  // no host memory for a device's first entry
+        return nullptr;
+    }
 }
 
 extern "C" f3dc_status f3dc_gemm_noalloc(const void *A, const void *B, const void *bias, const float *gate, void *out,

@@ -54,25 +54,25 @@ constexpr uint32_t kTmemCols8 = 512;
 constexpr uint32_t kAcc1 = 232;             // first column of the second accumulator
 constexpr uint32_t kScaleCols = 488;        // two sets of 4 (A) + 8 (B) columns
 constexpr uint32_t kSumCols = 360;          // sums in pieces: the 128 columns behind the second accumulator's
-// What shared memory holds beside the scales: stages of operands (b_bytes of B in each,
-// this CTA's half of the widest unit's rows) and output boxes per epilogue warp.
+// What shared memory holds beside the scales and an output box per epilogue warp: stages of
+// operands (b_bytes of B in each, this CTA's half of the widest unit's rows).
 struct Depth8 {
-    int stages, boxes, b_bytes;
+    int stages, b_bytes;
     size_t smem() const
     {
-        return 1024 + (size_t)stages * (kOperand8 + b_bytes) + kSets * kSetBytes + kVecBytes8 + (size_t)boxes * 8 * kOutBox8 + kBarBytes8;
+        return 1024 + (size_t)stages * (kOperand8 + b_bytes) + kSets * kSetBytes + kVecBytes8 + 8 * kOutBox8 + kBarBytes8;
     }
 };
 constexpr size_t kMostSmem8 = 227 * 1024;
-// With 8-bit output a short full unit's epilogue is longer than its sum, and the second box
-// saves it a wait (32768 x 4096 x 1024 121 us, with a fifth stage instead 125); else the fifth
-// stage counts for more (the same with 16-bit output 98 us instead of 102, 8192 x 4096 x 4096
-// 83 instead of 91).  Narrow units leave room for more stages: the loads' latency counts most
-// where there is one unit.
-inline Depth8 depth8(int kb_n, int width, bool out8)
+// As many stages as there is room for, five of full units.  (A second output box per warp instead
+// of the fifth: 32768 x 4096 x 1024 107 us instead of 103, with 8-bit output 104 and 102, with
+// GELU 133.4 and 132.6, 4096 x 4096 x 1024 with 8-bit output 17.4 and 16.9; 32768 x 4096 x 256
+// with 8-bit output and GELU 115.0 and 115.4.)  Narrow units leave room for more: the loads'
+// latency counts most where there is one unit.
+inline Depth8 depth8(int width)
 {
-    Depth8 d{1, out8 && kb_n < 16 && width == 256 ? 2 : 1, width / 2 * 128};
-    while (d.stages < kMaxStages8 && Depth8{d.stages + 1, d.boxes, d.b_bytes}.smem() <= kMostSmem8) ++d.stages;
+    Depth8 d{1, width / 2 * 128};
+    while (d.stages < kMaxStages8 && Depth8{d.stages + 1, d.b_bytes}.smem() <= kMostSmem8) ++d.stages;
     return d;
 }
 
@@ -212,42 +212,35 @@ F3DC_DEV void apply(uint32_t (&r)[32], const float *bias, const float *gate)
 }
 
 // Staged output of an epilogue warp: a box of its 32 rows x 128 bytes, the 16-byte piece c
-// of row r at 128 r + 16 (c ^ (r % 8)) (TMA 128B swizzle), in one box or two by turns.  Lane 0
-// issues the stores and waits before a box is written again until its last store has read
-// it.  (Stores from registers, or turned through shared memory into whole sectors, took
-// 132 and 129 us instead of 115 at 32768 x 4096 x 1024.  With one box a tile's second half
-// waits 2000 clocks for the first.)
+// of row r at 128 r + 16 (c ^ (r % 8)) (TMA 128B swizzle).  Lane 0 issues the stores and waits
+// before the box is written again until its last store has read it.  (Stores from registers, or
+// turned through shared memory into whole sectors, took 132 and 129 us instead of 115 at
+// 32768 x 4096 x 1024.)
 struct Stage8 {
     uint8_t *buf;
     const CUtensorMap *map;
-    int row, lane, turn, more;  // more: boxes beyond the first (0 or 1)
+    int row, lane;
     F3DC_DEV void begin() const
     {
-        if (lane == 0) {
-            if (more)
-                bulk_wait_read<1>();
-            else
-                bulk_wait_read<0>();
-        }
+        if (lane == 0) bulk_wait_read<0>();
         __syncwarp();
     }
     F3DC_DEV void put16(int c, uint4 u) const
     {
-        *reinterpret_cast<uint4 *>(buf + turn * kOutBox8 + lane * 128 + ((c ^ (lane & 7)) << 4)) = u;
+        *reinterpret_cast<uint4 *>(buf + lane * 128 + ((c ^ (lane & 7)) << 4)) = u;
     }
     template <bool kReduce>
-    F3DC_DEV void send(int x)
+    F3DC_DEV void send(int x) const
     {
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
             if (kReduce)
-                tma_reduce_add_2d(map, buf + turn * kOutBox8, x, row);
+                tma_reduce_add_2d(map, buf, x, row);
             else
-                tma_store_2d(map, buf + turn * kOutBox8, x, row);
+                tma_store_2d(map, buf, x, row);
             bulk_commit();
         }
-        turn ^= more;
     }
 };
 
@@ -272,7 +265,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
     uint8_t *ss = sb + S * depth.b_bytes;
     float *sv = reinterpret_cast<float *>(ss + kSets * kSetBytes);
     uint8_t *so = ss + kSets * kSetBytes + kVecBytes8;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(so + depth.boxes * 8 * kOutBox8);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(so + 8 * kOutBox8);
     uint64_t *full = bars, *empty = full + kMaxStages8;    // operands of a stage there (even CTA) / used (both)
     uint64_t *sfull = empty + kMaxStages8, *sempty = sfull + kSets;  // scales of a set there (even CTA) / copied (both)
     uint64_t *tfull = sempty + kSets, *tempty = tfull + 2; // scales of a set in tensor memory / used (even CTA)
@@ -521,7 +514,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
         // the unit's columns (of 8-bit output a whole scale block)
         const int q = warp & 3, half = (warp - 4) >> 2;
         float *bias = sv + (warp - 4) * 256, *gate = bias + 128;
-        Stage8 o{so + (warp - 4) * depth.boxes * kOutBox8, &tmo, 0, lane, 0, depth.boxes - 1};
+        Stage8 o{so + (warp - 4) * kOutBox8, &tmo, 0, lane};
         const uint32_t acce_c = mapa_shared(smem_u32(acce), even), shared_c = mapa_shared(smem_u32(shared_read), even);
         auto arrive = [&](uint32_t bar) {
             tc_fence_before();
@@ -867,7 +860,7 @@ template <int EPI, bool OUT8, bool SPLIT, bool LONG>
 cudaError_t launch_units8(const CUtensorMap *ta, const GemmPairB *tb, const CUtensorMap *to, const Gemm8Params &p,
                           const Units8 &u, int width, int clusters, cudaStream_t s)
 {
-    const Depth8 depth = depth8(SPLIT ? p.split_kb : (p.K + 127) / 128, width, OUT8);
+    const Depth8 depth = depth8(width);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;

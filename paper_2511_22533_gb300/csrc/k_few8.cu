@@ -14,8 +14,10 @@
 // added in order.  The next two blocks of a warp are on their way (of up to 8 tokens; one
 // ahead 8192 x 8192 took 24.9 us).  1 x 4096 x 1024 takes 2.7 us (1.6 TB/s), of which the
 // launch, the first loads and the sums' way through shared memory are 1.8; 1 x 8192 x 8192
-// 18.5 (3.6 TB/s), 1 x 32768 x 8192 59 (4.5), 67 % of a plain copy's rate, where the 16 warps
-// that an SM has registers for wait for their loads (conversions removed, it was no faster).
+// 18.5 (3.6 TB/s), 1 x 32768 x 8192 59 (4.5), 67 % of a plain copy's rate.  There 128 registers
+// leave room for 16 warps on an SM (13 on average: 512 CTAs are 1.7 waves), and instructions
+// issue in 46 % of the cycles; which of these bounds it has not been shown (without the
+// conversions it was no faster).
 #include "kernels.h"
 #include "mx8.cuh"
 

@@ -28,11 +28,14 @@
 // the two share, which it reads first.  Sums in pieces have units of 128 columns, whose
 // accumulators take turns, and the sum of the pieces so far in 128 columns more.
 //
-// 32768 x 4096 x 1024 takes 97 us (2.83 PFLOP/s), 104 with GELU, whose epilogue is then longer
-// than a tile's sum (tensor cores busy in 63 % of the cycles); 8192 x 8192 x 8192 348 (3.16),
-// where the board's power is the bound.  A few tiles take 3.6 us (launch, first fetches, scales,
-// epilogue, exit) and per 128 K 0.18 of narrow units, what issuing their loads and MMAs takes
-// one warp each, to 0.3 of full ones, whose MMAs alone are 512 clocks.
+// 32768 x 4096 x 1024 takes 96 us (2.86 PFLOP/s), 110 to 117 with GELU, back to back from Python
+// 129: a tile's epilogue is then longer than its sum, though neither issue (38 % of the cycles)
+// nor the special functions (28 %) nor the tensor cores (56 %) are near their limit: two epilogue
+// warps per scheduler do not hide one another's latencies.  8192 x 8192 x 8192 348 (3.16 PFLOP/s),
+// where the board's power is the bound.  A few tiles take 4.3 us (launch, first fetches, scales
+// and their way from the odd CTA to the even one, epilogue, exit) and per 128 K 0.18 of narrow
+// units, what issuing their loads and MMAs takes one warp each, to 0.3 of full ones, whose MMAs
+// alone are 512 clocks.
 #include <atomic>
 
 #include "kernels.h"
@@ -882,9 +885,9 @@ cudaError_t launch_units8(const CUtensorMap *ta, const GemmPairB *tb, const CUte
 // Width of the units of a split sum, 0: the sum is not split.  Few tiles leave clusters
 // idle that may take half of the K: it costs 2 us with units of 128 columns, 4.5 with 256
 // (64 KB per CTA change places), and saves 0.09 us per 128 K.  Whole / split, us:
-//   300 x 1024 (units of 128) x 3200 8.9 / 8.9, x 4096 10.2 / 9.0, x 8192 15.8 / 12.0; 1229 x
-//   1024 (256) x 4096 11.8 / 13.5, x 8192 17.8 / 18.1, x 16384 30.7 / 27.3; 600 x 1024 with
-//   8-bit output, which needs whole scale blocks, x 8192 16.2 / 15.7, x 16384 29.1 / 25.2.
+//   300 x 1024 (units of 128) x 3200 9.2 / 9.6, x 4096 10.5 / 9.5, x 8192 16.7 / 12.7; 1229 x
+//   1024 (256) x 4096 11.2 / 12.8, x 8192 17.8 to 19.2 / 17.4 to 18.1, x 16384 35.2 / 26.8; 600 x
+//   1024 with 8-bit output, which needs whole scale blocks, x 8192 17.2 / 16.4, x 16384 34.7 / 26.0.
 constexpr int kSplitBlocks = 24;  // no sum of fewer scale blocks is split
 int split_width8(int M, int N, int kb_n, bool out8, int max_clusters)
 {

@@ -14,12 +14,12 @@
 //     sums share the shuffles and the barrier, and for which a gain or a modulation is read
 //     once (from L1: with one row at a time these vectors, 20 bytes per element, are more
 //     than the rows themselves).  32768 x 1024 with a gate, modulations and 8-bit h take 69
-//     us: 5.35 TB/s, 79 % of a plain copy's rate (one row per CTA 82 us, four 81, runs of
+//     us: 5.4 TB/s, 80 % of a plain copy's rate (one row per CTA 82 us, four 81, runs of
 //     rows with the next one's loads in flight 79); the chain of four sums per row is as
-//     long as its loads, and instructions issue in 64 % of the cycles.
+//     long as its loads, and instructions issue in 61 % of the cycles.
 //   k_norm_runs, for few: a CTA takes a run of consecutive rows, mostly one, with everything
-//     loaded at once at the start and the next row ahead.  955 x 1024 take 4.1 us, one row of
-//     128 1.8.
+//     loaded at once at the start and the next row ahead.  955 x 1024 take 4.1 us (4.6 with all
+//     norms, gains and modulations and 8-bit h), one row of 128 1.8.
 #include "kernels.h"
 #include "mx8.cuh"
 

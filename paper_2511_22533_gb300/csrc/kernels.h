@@ -385,16 +385,16 @@ cudaError_t launch_gemm8_pair(const CUtensorMap *ta, const GemmPairB *tb, const 
                               int epi, bool out8, cudaStream_t s);
 
 // The same product for few rows, and f3dc_gemm_fp8's rule for it: it reads the weights
-// once for every 16 rows, about 1.8 us + 0.3 us per 2^20 of them (0.4 of 9 rows and more),
-// where CTA pairs take 3.6 us + 0.18 to 0.3 per 128 K.  Few rows / pairs, us:
+// once for every 16 rows, CTA pairs once, but start and finish later.  Few rows / pairs, us:
 //   M     1024 x 1024   4096 x 1024   1024 x 4096   4096 x 4096   8192 x 8192   (N x K)
-//   1     2.5 / 4.6     2.6 / 6.7     3.8 / 8.0     5.6 / 12.4    18.5 / 33
-//   8     2.6 / 4.6     3.0 / 6.3     3.9 / 7.8     5.7 / 10.3    19.5 / 30
-//   16    2.9 / 4.6     3.3 / 6.0     4.8 / 7.8     8.0 / 9.6     30.1 / 17.6
-//   32    3.2 / 4.7     5.8 / 5.9     4.9 / 7.9     14.7 / 9.4    52 / 17.7
-//   64    3.3 / 4.7     8.6 / 6.0     7.6 / 7.9     25.7 / 9.5    99 / 17.9
-//   77    4.8 / 4.8     10.4 / 6.0    12.0 / 8.0    32.9 / 9.5    137 / 18.0
-// and 8 x 65536 x 1024 20.7 / 20.2, 1 x 16384 x 4096 18.1 / 25, 8 x 4096 x 16384 18.7 / 19.6.
+//   1     2.5 / 6.0     2.7 / 8.5     3.8 / 9.1     5.6 / 13.3    18.5 / 41
+//   8     2.6 / 6.1     2.8 / 7.3     3.9 / 8.9     5.8 / 11.6    18.8 / 40
+//   16    2.9 / 5.3     3.4 / 7.2     4.9 / 8.8     8.2 / 11.4    29.3 / 21.2
+//   32    3.2 / 5.4     5.7 / 7.2     4.9 / 8.9     15.0 / 10.0   52 / 21.4
+//   64    3.3 / 5.5     8.5 / 7.2     7.6 / 8.9     25.8 / 10.1   98 / 21.6
+//   77    4.8 / 5.7     10.4 / 7.3    11.9 / 9.1    32.8 / 10.2   136 / 21.8
+// and 8 x 65536 x 1024 20.6 / 23.6, 1 x 16384 x 4096 18.2 / 24.4, 8 x 4096 x 16384 18.6 / 23.2.
+// (Why pairs take longer for up to 8 rows than for 16 has not been found.)
 inline bool gemm8_few_rows(int M, int N, int K)
 {
     return M <= 8 || (M <= 64 && (int64_t)K * ((int64_t)(M + 15) / 16 * N - 2700) < 6000000);

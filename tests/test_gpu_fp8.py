@@ -437,6 +437,30 @@ def test_gemm_fp8_sums_in_pieces(M, N, K, epi):
     assert f3dc.gemm_status() == 0
 
 
+# in two captured graphs replayed at once on two streams (the first launches of these kernels may
+# be the captured ones)
+@pytest.mark.parametrize("M,N,K", [(300, 512, 40000), (1300, 2048, 16640)])
+def test_gemm_fp8_sums_in_pieces_in_graphs(M, N, K):
+    jobs = [(operands(M, N, K, 50 + i), torch.zeros((M, N), device=DEV), torch.cuda.CUDAGraph(), torch.cuda.Stream()) for i in range(2)]
+    torch.cuda.synchronize()
+    for ops, out, g, _ in jobs:
+        with torch.cuda.graph(g):
+            gemm8(*ops, K, f3dc.EPI_RESID, None, None, out)
+    torch.cuda.synchronize()
+    for _, out, g, st in jobs:
+        with torch.cuda.stream(st):
+            g.replay()
+    torch.cuda.synchronize()
+    for ops, out, _, _ in jobs:
+        again = torch.zeros_like(out)
+        gemm8(*ops, K, f3dc.EPI_RESID, None, None, again)
+        y, _ = R.gemm(*ops, K)
+        mag = R.values(ops[0], ops[1], K).abs() @ R.values(ops[2], ops[3], K).abs().T
+        assert torch.all((out.double() - y).abs() <= piece_error(True) * mag + R.U32 * y.abs())
+        assert torch.equal(out, again)
+    assert f3dc.gemm_status() == 0
+
+
 def test_gemm_fp8_longest_sum():
     # ones: every partial sum is a whole number, the last one 2^26
     M, N, K = 65, 8, 1 << 26

@@ -513,6 +513,111 @@ f3dc_status f3dc_norm_residual(const f3dc_norm_layer *layer, const float *x, int
                                int64_t ldmod, const int32_t *group_of_row, int32_t groups, void *h, int64_t ldh,
                                void *h_scales, int64_t ldhs, int32_t rows, void *stream);
 
+/* ---------------------------------------------------------------------- */
+/* Attention over a paged 8-bit cache.                                     */
+/* ---------------------------------------------------------------------- */
+
+/* The paper's transformer attends to 16-bit keys and values of the same step;
+ * these calls are library services, beside f3dc_attention and the 8-bit linear
+ * layers, for programs that keep keys and values between calls.  A cache is a
+ * pool of pages; a page holds page_tokens consecutive tokens of one sequence for
+ * all key heads.  Token t of sequence b lies in page page_table[b, t /
+ * page_tokens] at place t % page_tokens, and its value there is
+ *   k[page, head, place, :] * 2^(k_scales[page, head] - 127)   (e4m3; 255: NaN)
+ * so a block of tokens that shares a scale is a page's tokens of one head.
+ * The calls are asynchronous on `stream`, allocate nothing, keep nothing between
+ * calls but what they write, and may run at once on several streams and in
+ * captured graphs as far as one call's outputs (the workspace among them) are
+ * no other's inputs or outputs.  Rows, lengths and the page table are read on the
+ * device: a captured call follows them.  What kernels find wrong there goes into
+ * the current device's status word (f3dc_gemm_status) as F3DC_DEV_BAD_INDEX: a
+ * sequence whose rows or length are outside the bounds of its f3dc_kv_batch is left out
+ * (its outputs stay as they were); a page outside the pool is written by nothing and
+ * read as zeros.  Failures are described by f3dc_last_error(NULL). */
+
+typedef struct f3dc_kv_cache {
+    int32_t pages;        /* of the pool, >= 1 */
+    int32_t page_tokens;  /* 16, 32, 64 or 128 */
+    int32_t kv_heads;     /* key heads Hk, 1 to 1024 */
+    int32_t dh;           /* head width: 32, 64 or 128 */
+    void *k, *v;          /* device e4m3 bytes [pages, Hk, page_tokens, dh], 16-byte aligned */
+    uint8_t *k_scales, *v_scales; /* device bytes [pages, Hk] */
+    int64_t page_stride;  /* bytes from a page to the next in k and in v: a multiple of 16,
+                           * at least Hk page_tokens dh */
+    int64_t scale_stride; /* bytes from a page to the next in k_scales and v_scales: at least Hk */
+} f3dc_kv_cache;
+
+/* The sequences of a call.  Sequence b's rows (new tokens, queries) are rows
+ * row_start[b] <= r < row_start[b + 1] of the packed matrices; rows of no
+ * sequence are neither read nor written.  Its length counts the tokens that
+ * its pages hold once the call's rows are appended. */
+typedef struct f3dc_kv_batch {
+    const int32_t *row_start;  /* device [batch + 1] */
+    const int32_t *lengths;    /* device [batch] */
+    const int32_t *page_table; /* device [batch, table_stride] */
+    int64_t table_stride;      /* pages of a row of page_table */
+    int32_t batch;             /* sequences, >= 0 */
+    int32_t rows;              /* packed rows, >= 0: row_start[batch] <= rows */
+    int32_t max_rows;          /* no sequence has more rows */
+    int32_t max_length;        /* nor is longer */
+} f3dc_kv_batch;
+
+/* Rotation of queries and keys by their positions.  Pair j < dims / 2 of a head is
+ * elements (j, j + dims / 2), or (2 j, 2 j + 1) with interleaved; it turns by
+ * 2 pi position turns[j] / 2^64.  Angles are taken modulo a whole turn in 64-bit integers, so
+ * far positions lose nothing.  With axes > 1 a position has that many coordinates (places in a
+ * grid): pairs are shared out in order, dims / 2 / axes to each, and those left over do not turn. */
+typedef struct f3dc_rotary {
+    int32_t dims;          /* leading elements of a head that turn: a multiple of 16 */
+    int32_t interleaved;   /* 0 or 1 */
+    int32_t axes;          /* 1 to 3 */
+    const uint64_t *turns; /* device [dims / 2], see f3dc_rotary_turns */
+} f3dc_rotary;
+
+/* turns_out[j] = inv_freq[j] / (2 pi) in units of 2^-64 turns, modulo a turn (radians per
+ * unit of position in; host arrays).  Host only. */
+f3dc_status f3dc_rotary_turns(const double *inv_freq, int32_t n, uint64_t *turns_out);
+
+/* Appends keys and values to their sequences' pages: row i of sequence b, of n_b,
+ * becomes token lengths[b] - n_b + i.  Keys are rotated first (rotary nullable), and so
+ * are the queries of the same rows if q is given.  Positions are the tokens' own, or
+ * positions[r, axis].
+ * A page's scale is the smallest power of two 2^e, -127 <= e, with max |x| <= 448 2^e over
+ * the finite elements that the call writes there, rotated in fp32; values are rounded to nearest even,
+ * NaN and infinities become NaN.  A page that already holds tokens of the sequence keeps its
+ * scale, or if the new tokens need a larger one the old ones are rounded to it.  A page whose first place is
+ * written starts anew, whatever it held.
+ *   k, v: device bf16 [rows, Hk dh], row strides ldk, ldv;
+ *   q: device bf16 [rows, heads dh], row stride ldq, nullable; q_out: the same, row
+ *     stride ldqo, may be q itself (ldqo = ldq);
+ *   positions: device int32 [rows, axes], nullable (one axis: the token; refused with more).
+ *   Pointers 16-byte aligned, row strides multiples of 8.  A page that is written belongs
+ *   to one sequence of the call. */
+f3dc_status f3dc_kv_append_fp8(const f3dc_kv_cache *cache, const f3dc_kv_batch *batch, const f3dc_rotary *rotary,
+                               const void *k, int64_t ldk, const void *v, int64_t ldv, const void *q, int64_t ldq,
+                               void *q_out, int64_t ldqo, int32_t heads, const int32_t *positions, void *stream);
+
+/* Bytes of workspace with which f3dc_kv_attention_fp8 shares long sequences out over
+ * the SMs for a batch within these bounds (0: it needs none, or invalid arguments).  Reads the current device's SM count. */
+size_t f3dc_kv_attention_workspace(const f3dc_kv_cache *cache, const f3dc_kv_batch *batch, int32_t heads);
+
+/* Attention of packed query rows over their sequences' cached tokens, head h reading
+ * key head h / (heads / Hk):
+ *   out[r, h] = sum_t p_t v_t,  p = softmax(scale q[r, h] . k_t)
+ * over the sequence's tokens t < lengths[b], with `causal` t <= lengths[b] - n_b + i for its
+ * row i.  A row that sees no token gets zeros (lse -infinity).  What lies behind a sequence's length or is
+ * masked counts for nothing, NaN included.  Sums and statistics are fp32;
+ * softmax weights are rounded to fp16 relative to a row's largest weight times value scale.
+ *   q: device bf16 [rows, heads dh], row stride ldq; out: the same, row stride ldo;
+ *   lse: device fp32 [rows, heads] contiguous, nullable: ln sum exp(scale q . k_t);
+ *   heads: a multiple of Hk; scale > 0;
+ *   workspace: device bytes, 16-byte aligned, nullable: with fewer than
+ *     f3dc_kv_attention_workspace() bytes (none at all) a long sequence is shared by fewer SMs.
+ *   Pointers 16-byte aligned, row strides multiples of 8. */
+f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f3dc_kv_batch *batch, const void *q, int64_t ldq,
+                                  void *out, int64_t ldo, float *lse, int32_t heads, float scale, int32_t causal,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,511 @@
+// k_kv_few.cu -- f3dc_kv_attention_fp8 for few query rows to a key head (single tokens, a
+// few at once, groups of heads): attention over a paged 8-bit cache, and the sum of the
+// parts where several CTAs share a sequence's keys.
+//
+//   S = Q K^T, x = S scale 2^(ek) + ev, w = 2^(x - m + shift), O += w V, l += w 2^-ev
+//
+// Bound by the cache's bytes.  A warp takes 32 tokens at a time: their keys and values come by cp.async into a ring
+// of its own (no other warp is waited for), are converted to fp16 (exactly) and multiplied
+// with mma.m16n8k16, query rows as the 16 rows (up to 32 of them).  K may be permuted within an MMA as long as both
+// operands are: a lane's 16 consecutive bytes of a key serve four MMAs; and the tokens behind the columns of S are
+// chosen so that its accumulators are the weights' operand of the second product as they stand, while four lanes
+// read four neighbouring tokens' values.  Each warp keeps sums and references of its own, which are joined at the end.
+#include "kv.cuh"
+
+namespace f3dc {
+
+namespace {
+
+constexpr int kWarps = 4, kChunk = 32;
+constexpr float kInf = __builtin_huge_valf();
+
+template <int DH>
+struct FewCfg {
+    static constexpr int kHalf = kChunk * DH, kStage = 2 * kHalf;  // bytes: keys, then values
+    static constexpr int kStages = DH == 128 ? 3 : 4;
+    static constexpr int kSmem = kWarps * kStages * kStage;
+};
+
+F3DC_DEV void cp_async16_or_zeros(uint32_t dst, const void *src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+F3DC_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+F3DC_DEV void cp_async_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+F3DC_DEV void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Places of a token's 16-byte pieces in a stage, chosen so that the reads below meet no bank twice.
+// Keys: row g of each eight holds the token behind column g of S.
+template <int DH>
+F3DC_DEV int key_place(int token, int piece)
+{
+    const int row = (token & ~7) | ((token & 3) << 1) | ((token >> 2) & 1);
+    if (DH == 128) piece ^= (row & 1) << 2;
+    return row * DH + 16 * piece;
+}
+template <int DH>
+F3DC_DEV int value_place(int token, int piece)
+{
+    if (DH == 128) piece ^= (token & 3) << 1;
+    if (DH == 64) piece ^= token & 2;
+    return token * DH + 16 * piece;
+}
+
+F3DC_DEV uint32_t half2_times(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// all ones in the halves that are no NaN
+F3DC_DEV uint32_t half2_numbers(uint32_t a)
+{
+    return __heq2_mask(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&a));
+}
+
+// MT: tiles of 16 packed rows
+template <int DH, int MT>
+__global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
+{
+    using Cfg = FewCfg<DH>;
+    constexpr int kSteps = DH / 16, kTiles = DH / 8, kVec = DH / 64 > 0 ? DH / 64 : 1;
+    constexpr int kStages = Cfg::kStages;
+    extern __shared__ uint4 smem4[];
+    uint8_t *const smem = reinterpret_cast<uint8_t *>(smem4);
+    __shared__ float sm_m[kWarps][16 * MT], sm_l[kWarps][16 * MT];
+    griddep_launch();
+    griddep_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+
+    int64_t item = blockIdx.x;
+    const int split = (int)(item % a.splits);
+    item /= a.splits;
+    const int rb = (int)(item % a.row_blocks);
+    item /= a.row_blocks;
+    const int hk = (int)(item % a.cache.heads), b = (int)(item / a.cache.heads);
+    const KvSeq s = kv_seq(a.batch, a.cache, b, a.err);
+    const int r0 = rb * 16 * MT;
+    const int64_t rows = (int64_t)s.n * a.group;  // packed
+    if (s.n <= 0 || r0 >= rows) return;
+    const int row_end = (int)min(rows, (int64_t)r0 + 16 * MT);
+
+    // tokens that the last and the first of the rows see
+    const int behind = s.length - s.n + 1;
+    const int most = a.causal ? max(0, behind + (row_end - 1) / a.group) : s.length;
+    const int least = a.causal ? behind + r0 / a.group : s.length;
+    const int chunks = (most + kChunk - 1) / kChunk;
+    const int c_begin = (int)((int64_t)chunks * split / a.splits), c_end = (int)((int64_t)chunks * (split + 1) / a.splits);
+
+    // ---- this warp's ring
+    uint8_t *const ring = smem + warp * kStages * Cfg::kStage;
+    const int page = a.cache.page, page_log2 = 31 - __clz(page);
+    int page0 = 0, page1 = 0;  // pages of the next chunk to come
+    auto look_up = [&](int c) {
+        const int t = c * kChunk;
+        if (c >= c_end) return;
+        page0 = kv_page(a.batch, a.cache, b, t >> page_log2, a.err);
+        page1 = t + 16 < s.length ? kv_page(a.batch, a.cache, b, (t + 16) >> page_log2, a.err) : page0;
+    };
+    // loads of chunk c; returns its scale byte of lane's kind: keys / values, first / second page
+    auto load = [&](int c, int slot) {
+        uint32_t scale = 127u;
+        if (c < c_end) {
+            const uint32_t dst = smem_u32(ring + slot * Cfg::kStage);
+            const int t0 = c * kChunk;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int p = lane + 32 * i, token = p / kSteps, piece = p % kSteps;
+                const int pg = token < 16 ? page0 : page1;
+                const bool real = t0 + token < s.length && pg >= 0;
+                const int64_t at = real ? (int64_t)pg * a.cache.page_stride +
+                                              ((int64_t)hk * page + ((t0 + token) & (page - 1))) * DH + 16 * piece
+                                        : 0;
+                cp_async16_or_zeros(dst + key_place<DH>(token, piece), a.cache.k + at, real);
+                cp_async16_or_zeros(dst + Cfg::kHalf + value_place<DH>(token, piece), a.cache.v + at, real);
+            }
+            const int pg = lane & 2 ? page1 : page0;
+            if (pg >= 0) scale = (lane & 1 ? a.cache.vs : a.cache.ks)[(int64_t)pg * a.cache.scale_stride + hk];
+        }
+        cp_async_commit();
+        return scale;
+    };
+    const int c0 = c_begin + warp;
+    uint32_t scales[kStages - 1];
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) {
+        look_up(c0 + i * kWarps);
+        scales[i] = load(c0 + i * kWarps, i);
+    }
+    look_up(c0 + (kStages - 1) * kWarps);
+
+    // ---- queries: fp16 times a power of two for each row; the k of step j are elements 16 q + 4 j .. + 3 of each 64
+    uint32_t qa[MT][kSteps][4];
+    float factor[MT][2];  // of S, in log2
+    int sees[MT][2];      // tokens
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = r0 + 16 * m + g + 8 * i, at = min(r, row_end - 1);
+            const int token = at / a.group, head = hk * a.group + at % a.group;
+            sees[m][i] = a.causal ? behind + token : s.length;
+            const bf16 *x = a.q + (int64_t)(s.row0 + token) * a.ldq + (int64_t)head * DH;
+            uint32_t w[DH / 8];
+            constexpr int kRun = DH >= 64 ? 16 : 8;  // consecutive elements of a lane
+#pragma unroll
+            for (int j = 0; j < DH / 32; ++j) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(x + (j * 8 / kRun) * 64 + kRun * q + j * 8 % kRun);
+                w[4 * j] = u.x, w[4 * j + 1] = u.y, w[4 * j + 2] = u.z, w[4 * j + 3] = u.w;
+            }
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < DH / 8; ++j)
+                top = fmax3(top, fabsf(__uint_as_float(w[j] << 16)), fabsf(__uint_as_float(w[j] & 0xFFFF0000u)));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = query_exponent(top);
+            const float up = pow2(e);
+            factor[m][i] = a.scale_log2 * pow2(-e);
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) {
+                qa[m][j][i] = pack_half2(__uint_as_float(w[2 * j] << 16) * up, __uint_as_float(w[2 * j] & 0xFFFF0000u) * up);
+                qa[m][j][2 + i] =
+                    pack_half2(__uint_as_float(w[2 * j + 1] << 16) * up, __uint_as_float(w[2 * j + 1] & 0xFFFF0000u) * up);
+            }
+        }
+
+    float acc[MT][kTiles][4];
+    float ref[MT][2], sum[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[m][j][e] = 0.f;
+        ref[m][0] = ref[m][1] = -kInf;
+        sum[m][0] = sum[m][1] = 0.f;
+    }
+
+    int slot = 0;
+#pragma unroll 1
+    for (int c = c0; c < c_end; c += kWarps) {
+        cp_async_wait<kStages - 2>();
+        __syncwarp();
+        const uint32_t scale = scales[0];
+#pragma unroll
+        for (int i = 0; i < kStages - 2; ++i) scales[i] = scales[i + 1];
+        const int next = c + (kStages - 1) * kWarps, next_slot = slot == 0 ? kStages - 1 : slot - 1;
+        scales[kStages - 2] = load(next, next_slot);
+        look_up(next + kWarps);
+
+        const uint8_t *const keys = ring + slot * Cfg::kStage, *const values = keys + Cfg::kHalf;
+        slot = slot + 1 == kStages ? 0 : slot + 1;
+        const int t0 = c * kChunk;
+
+        float x[MT][4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // eight tokens
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[m][i][e] = 0.f;
+            const int row = 8 * i + g;
+#pragma unroll
+            for (int h = 0; h < kVec; ++h) {
+                uint32_t w[4];
+                if constexpr (DH >= 64) {
+                    const int piece = (4 * h + q) ^ (DH == 128 ? (row & 1) << 2 : 0);
+                    const uint4 u = *reinterpret_cast<const uint4 *>(keys + row * DH + 16 * piece);
+                    w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+                } else {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(keys + row * DH + 8 * q);
+                    w[0] = u.x, w[1] = u.y;
+                }
+#pragma unroll
+                for (int j = 0; j < (DH >= 64 ? 4 : 2); ++j) {
+                    uint32_t b0, b1;
+                    e4m3x4_to_half2(w[j], b0, b1);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) mma16816(x[m][i], qa[m][4 * h + j], b0, b1);
+                }
+            }
+        }
+
+        // scales of the chunk's two halves, scores in log2 with their value scales
+        float ks[2];
+        ValueScale vs[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            ks[h] = key_scale(__shfl_sync(0xffffffffu, scale, 2 * h));
+            vs[h] = value_scale(__shfl_sync(0xffffffffu, scale, 2 * h + 1));
+        }
+        const bool partly = t0 + kChunk > least;
+        bool raise = false;
+        float top[MT][2];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float f[2] = {factor[m][r] * ks[0], factor[m][r] * ks[1]};
+                float t = -kInf;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float &y = x[m][i][2 * r + e];
+                        y = fmaf(y, f[i >> 1], vs[i >> 1].log2);
+                        // column 2 q + e of tile i is token 8 i + 4 e + q
+                        if (partly && t0 + 8 * i + 4 * e + q >= sees[m][r]) y = -kInf;
+                        t = fmaxf(t, y);
+                    }
+                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
+                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+                top[m][r] = t;
+                raise |= t > ref[m][r] + kLazy;
+            }
+        if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float to = fmaxf(ref[m][r], top[m][r]);
+                    const float by = ref[m][r] == -kInf ? 0.f : exp2_fast(ref[m][r] - to);
+                    ref[m][r] = to;
+                    sum[m][r] *= by;
+#pragma unroll
+                    for (int j = 0; j < kTiles; ++j) {
+                        acc[m][j][2 * r] *= by;
+                        acc[m][j][2 * r + 1] *= by;
+                    }
+                }
+        }
+        uint32_t w[MT][2][4];  // weights as operands of the two halves
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float base = kWeightShift - (ref[m][r] == -kInf ? 0.f : ref[m][r]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float p[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] = exp2_fast(x[m][2 * h + (e >> 1)][2 * r + (e & 1)] + base);
+                    sum[m][r] = fmaf((p[0] + p[1]) + (p[2] + p[3]), vs[h].inverse, sum[m][r]);
+                    w[m][h][r] = pack_half2(p[0], p[1]);
+                    w[m][h][2 + r] = pack_half2(p[2], p[3]);
+                }
+            }
+        const bool odd = partly || vs[0].times != kHalfOnes || vs[1].times != kHalfOnes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // sixteen tokens
+            uint32_t v[4][DH / 32];  // lane's columns g DH / 8 .. of tokens 4 i + q
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int token = 16 * h + 4 * i + q;
+                if constexpr (DH == 128) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(values + value_place<DH>(token, g));
+                    v[i][0] = u.x, v[i][1] = u.y, v[i][2] = u.z, v[i][3] = u.w;
+                } else if constexpr (DH == 64) {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(values + value_place<DH>(token, g >> 1) + 8 * (g & 1));
+                    v[i][0] = u.x, v[i][1] = u.y;
+                } else {
+                    v[i][0] = *reinterpret_cast<const uint32_t *>(values + token * DH + 4 * g);
+                }
+            }
+            auto operands = [&](int k, uint32_t (&b0)[4], uint32_t (&b1)[4]) {  // tiles 4 k .. 4 k + 3
+                e4m3x4_to_half2(__byte_perm(v[0][k], v[1][k], 0x5140), b0[0], b0[1]);
+                e4m3x4_to_half2(__byte_perm(v[0][k], v[1][k], 0x7362), b0[2], b0[3]);
+                e4m3x4_to_half2(__byte_perm(v[2][k], v[3][k], 0x5140), b1[0], b1[1]);
+                e4m3x4_to_half2(__byte_perm(v[2][k], v[3][k], 0x7362), b1[2], b1[3]);
+            };
+            if (!odd) {
+#pragma unroll
+                for (int k = 0; k < DH / 32; ++k) {
+                    uint32_t b0[4], b1[4];
+                    operands(k, b0, b1);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) mma16816(acc[m][4 * k + j], w[m][h], b0[j], b1[j]);
+                }
+            } else {
+                // A NaN that a row does not see must not meet its weight of zero: NaN count as zeros in the product,
+                // and where there are any, a second one counts for each row those that it sees.
+                const uint32_t times = vs[h].times;
+                uint32_t sight[MT][4];  // 1 for a token that the row sees
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int t = t0 + 16 * h + 8 * (e >> 1) + q;
+                        sight[m][e] = (t < sees[m][e & 1] ? 0x3C00u : 0u) | (t + 4 < sees[m][e & 1] ? 0x3C000000u : 0u);
+                    }
+#pragma unroll
+                for (int k = 0; k < DH / 32; ++k) {
+                    uint32_t b0[4], b1[4];
+                    operands(k, b0, b1);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        b0[j] = half2_times(b0[j], times), b1[j] = half2_times(b1[j], times);
+                        const uint32_t n0 = half2_numbers(b0[j]), n1 = half2_numbers(b1[j]);
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) mma16816(acc[m][4 * k + j], w[m][h], b0[j] & n0, b1[j] & n1);
+                        if (__any_sync(0xffffffffu, (n0 & n1) != 0xffffffffu)) {
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) {
+                                float count[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma16816(count, sight[m], ~n0 & kHalfOnes, ~n1 & kHalfOnes);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if (count[e] > 0.f) acc[m][4 * k + j][e] = __int_as_float(0x7FC00000);
+                            }
+                        }
+                    }
+                }
+            }
+        }
+    }
+
+    // ---- the warps' sums joined
+    cp_async_wait<0>();
+    __syncthreads();
+    float *const sums = reinterpret_cast<float *>(smem);  // [warps][16 MT][DH]
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float l = sum[m][r];
+            l += __shfl_xor_sync(0xffffffffu, l, 1);
+            l += __shfl_xor_sync(0xffffffffu, l, 2);
+            const int row = 16 * m + g + 8 * r;
+            if (q == 0) {
+                sm_m[warp][row] = ref[m][r];
+                sm_l[warp][row] = l;
+            }
+            float *o = sums + (warp * 16 * MT + row) * DH + q * (DH / 4);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int j = 0; j < kTiles; j += 4)
+                    *reinterpret_cast<float4 *>(o + e * kTiles + j) =
+                        make_float4(acc[m][j][2 * r + e], acc[m][j + 1][2 * r + e], acc[m][j + 2][2 * r + e],
+                                    acc[m][j + 3][2 * r + e]);
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < (row_end - r0) * (DH / 8); i += 32 * kWarps) {
+        const int row = i / (DH / 8), col = i % (DH / 8) * 8;
+        float m = sm_m[0][row];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm_m[w][row]);
+        float l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float by = sm_m[w][row] == -kInf ? 0.f : exp2_fast(sm_m[w][row] - m);
+            // (a NaN sum has no reference of its own)
+            l += sm_l[w][row] == 0.f ? 0.f : sm_l[w][row] * by;
+            const float *x = sums + (w * 16 * MT + row) * DH + col;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(x[e], by, o[e]);
+        }
+        const int token = (r0 + row) / a.group, head = hk * a.group + (r0 + row) % a.group;
+        const int64_t at = (int64_t)(s.row0 + token) * a.heads + head;
+        if (a.splits == 1) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            uint4 u;
+            u.x = pack_bf16x2(o[0] * inv, o[1] * inv);
+            u.y = pack_bf16x2(o[2] * inv, o[3] * inv);
+            u.z = pack_bf16x2(o[4] * inv, o[5] * inv);
+            u.w = pack_bf16x2(o[6] * inv, o[7] * inv);
+            *reinterpret_cast<uint4 *>(a.out + (int64_t)(s.row0 + token) * a.ldo + (int64_t)head * DH + col) = u;
+            if (a.lse && col == 0) a.lse[at] = log_sum(m, l);
+        } else {
+            const int64_t part = (int64_t)split * a.batch.rows * a.heads + at;
+            float *dst = a.part + part * DH + col;
+            *reinterpret_cast<float4 *>(dst) = make_float4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<float4 *>(dst + 4) = make_float4(o[4], o[5], o[6], o[7]);
+            if (col == 0) {
+                float2 *ml = reinterpret_cast<float2 *>(a.part + (int64_t)a.splits * a.batch.rows * a.heads * DH);
+                ml[part] = make_float2(m, l);
+            }
+        }
+    }
+}
+
+// Parts of a row and head added up: a warp for each.
+template <int DH>
+__global__ void __launch_bounds__(256) k_kv_join(const KvAttnArgs a)
+{
+    griddep_launch();
+    griddep_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), per = (int64_t)a.batch.rows * a.heads;
+    if (at >= per) return;
+    const int row = (int)(at / a.heads), head = (int)(at % a.heads);
+    // the row's sequence: the last that starts at or before it
+    int lo = 0, hi = a.batch.batch;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        (a.batch.row_start[mid] <= row ? lo : hi) = mid;
+    }
+    const KvSeq s = kv_seq(a.batch, a.cache, lo, nullptr);
+    if (s.n <= 0 || row < s.row0 || row >= s.row0 + s.n) return;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part + a.splits * per * DH) + at;
+    float m = -kInf;
+    for (int i = lane; i < a.splits; i += 32) m = fmaxf(m, ml[i * per].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float l = 0.f, o[DH / 32] = {};
+    for (int i = 0; i < a.splits; ++i) {
+        const float2 p = ml[i * per];
+        const float by = p.x == -kInf ? 0.f : exp2_fast(p.x - m);
+        l += p.y == 0.f ? 0.f : p.y * by;
+#pragma unroll
+        for (int e = 0; e < DH / 32; ++e) o[e] = fmaf(a.part[(i * per + at) * DH + lane + 32 * e], by, o[e]);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int e = 0; e < DH / 32; ++e)
+        a.out[(int64_t)row * a.ldo + (int64_t)head * DH + lane + 32 * e] = __float2bfloat16_rn(o[e] * inv);
+    if (a.lse && lane == 0) a.lse[at] = log_sum(m, l);
+}
+
+template <int DH, int MT>
+cudaError_t launch_few(const KvAttnArgs &args, cudaStream_t s)
+{
+    KvAttnArgs a = args;
+    a.row_blocks = (int)(((int64_t)a.batch.max_rows * a.group + 16 * MT - 1) / (16 * MT));
+    const int64_t ctas = (int64_t)a.splits * a.row_blocks * a.cache.heads * a.batch.batch;
+    if (ctas > INT32_MAX) return cudaErrorInvalidValue;
+    static std::atomic<uint64_t> devices{0};
+    cudaError_t e = ask_smem(k_kv_few<DH, MT>, FewCfg<DH>::kSmem, devices);
+    if (e != cudaSuccess) return e;
+    e = launch_k(k_kv_few<DH, MT>, dim3((unsigned)ctas), dim3(32 * kWarps), FewCfg<DH>::kSmem, s, a);
+    if (e != cudaSuccess || a.splits == 1) return e;
+    const int64_t rows = (int64_t)a.batch.rows * a.heads;
+    return launch_k(k_kv_join<DH>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_few(const KvAttnArgs &a, cudaStream_t s)
+{
+    const bool two = (int64_t)a.batch.max_rows * a.group > 16;
+    switch (a.cache.dh) {
+    case 32: return two ? launch_few<32, 2>(a, s) : launch_few<32, 1>(a, s);
+    case 64: return two ? launch_few<64, 2>(a, s) : launch_few<64, 1>(a, s);
+    case 128: return launch_few<128, 1>(a, s);
+    default: return cudaErrorInvalidValue;
+    }
+}
+
+}  // namespace f3dc

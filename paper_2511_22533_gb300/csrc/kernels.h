@@ -443,4 +443,63 @@ struct NormArgs {
 };
 cudaError_t launch_norm_residual(const NormArgs &a, int num_sms, cudaStream_t s);
 
+// ------------------------------------------------------------ paged 8-bit key / value cache
+struct KvCache {
+    uint8_t *k, *v, *ks, *vs;           // e4m3 [pages, heads, page, dh], scale bytes [pages, heads]
+    int64_t page_stride, scale_stride;  // bytes
+    int pages, page, heads, dh;         // page: tokens, a power of two
+};
+struct KvBatch {
+    const int32_t *row_start, *lengths, *table;
+    int64_t table_stride;
+    int batch, rows, max_rows, max_length;
+};
+
+struct KvAppendArgs {
+    KvCache cache;
+    KvBatch batch;
+    int dims, interleaved, axes;  // dims 0: no rotation
+    const uint64_t *turns;
+    const int32_t *positions;     // nullable, [rows, axes]
+    const bf16 *k, *v, *q;        // q nullable
+    int64_t ldk, ldv, ldq;
+    bf16 *q_out;
+    int64_t ldqo;
+    int heads;
+    int slots;                    // set by the launch: pages that a sequence's rows can touch
+    uint32_t *err;
+};
+cudaError_t launch_kv_append(const KvAppendArgs &a, int num_sms, cudaStream_t s);
+
+// Attention over the cache.  Rows of a key head are packed (row of the sequence, head of
+// the group) -> row * group + head, so those that share keys share tiles.
+struct KvAttnArgs {
+    KvCache cache;
+    KvBatch batch;
+    const bf16 *q;
+    int64_t ldq;
+    bf16 *out;
+    int64_t ldo;
+    float *lse;                   // nullable, [rows, heads]
+    int heads, group, causal;
+    float scale_log2;             // scale log2(e)
+    // keys of an item are shared by so many CTAs, whose partial sums go to part: [splits][rows][heads][dh]
+    // unnormalised sums, then [splits][rows][heads] pairs (reference, sum of weights)
+    int splits;
+    float *part;
+    int row_blocks;               // set by the launch: blocks of packed rows of a sequence
+    uint32_t *err;
+};
+cudaError_t launch_kv_few(const KvAttnArgs &a, cudaStream_t s);
+
+// CTAs that share a sequence's keys: as many as fill the SMs twice, each with at least
+// 512 tokens.
+inline int kv_splits(int batch, int max_rows, int max_length, int heads, int kv_heads, int dh, int sms)
+{
+    const int64_t rows = (int64_t)max_rows * (heads / kv_heads), blocks = (rows + 15) / 16 * kv_heads * batch;
+    int64_t n = 2 * (int64_t)sms / blocks;
+    if (n > max_length / 512) n = max_length / 512;
+    return n < 1 ? 1 : (int)n;
+}
+
 }  // namespace f3dc

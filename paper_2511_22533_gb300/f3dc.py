@@ -74,6 +74,84 @@ class NormLayer(C.Structure):
         self._ref = C.pointer(self)
 
 
+class Rotary(C.Structure):
+    """Rotation by positions: `inv_freq` are the dims / 2 pairs' angles per unit of
+    position (or base ** (-j / pairs of an axis) for each axis).  Keeps their turns
+    on the given (or current) GPU."""
+    _fields_ = [("dims", C.c_int32), ("interleaved", C.c_int32), ("axes", C.c_int32), ("turns", C.c_void_p)]
+
+    def __init__(self, dims, inv_freq=None, base=10000.0, interleaved=False, axes=1, device="cuda"):
+        import torch
+        n = dims // 2
+        if inv_freq is None:
+            of_axis = max(1, n // max(1, axes))
+            inv_freq = [base ** (-(j % of_axis) / of_axis) for j in range(n)]
+        if len(inv_freq) != n:
+            raise F3dcError(1, f"{dims} rotating elements have {n} frequencies: got {len(inv_freq)}")
+        self.host = rotary_turns(inv_freq)
+        self._turns = torch.from_numpy(self.host.view(np.int64)).to(device)
+        super().__init__(dims, int(interleaved), axes, self._turns.data_ptr())
+        self._ref = C.pointer(self)
+
+
+def _same_device(what, tensors):
+    for t in tensors:
+        if not t.is_cuda or t.get_device() != tensors[0].get_device():
+            raise F3dcError(1, f"{what}: tensors on one GPU are needed, got one on {t.device}")
+
+
+class KVCache(C.Structure):
+    """A pool of pages of 8-bit keys and values, as four tensors (kept alive): k and v
+    e4m3 [pages, kv_heads, page_tokens, dh] (bytes; pages may lie apart), their scales
+    bytes [pages, kv_heads]."""
+    _fields_ = [("pages", C.c_int32), ("page_tokens", C.c_int32), ("kv_heads", C.c_int32), ("dh", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("page_stride", C.c_int64), ("scale_stride", C.c_int64)]
+
+    def __init__(self, k, v, k_scales, v_scales):
+        self._tensors = (k, v, k_scales, v_scales)
+        kinds = _fp8_types()
+        for t, n, kind in zip(self._tensors, (4, 4, 2, 2), ("e4m3", "e4m3", "scale", "scale")):
+            if t.dtype not in kinds[kind] or t.dim() != n:
+                raise F3dcError(1, f"a cache holds {kind} bytes in {n} dimensions: got {t.dtype} {tuple(t.shape)}")
+        pages, heads, tokens, dh = k.shape
+        if v.shape != k.shape or tuple(k_scales.shape) != (pages, heads) or k_scales.shape != v_scales.shape:
+            raise F3dcError(1, "k and v need one shape [pages, kv_heads, page_tokens, dh], their scales [pages, kv_heads]")
+        for t in (k, v):
+            if t.stride()[1:] != (tokens * dh, dh, 1) or t.stride(0) != k.stride(0):
+                raise F3dcError(1, "a page's bytes must lie together, pages of k and v equally far apart")
+        for t in (k_scales, v_scales):
+            if t.stride(1) != 1 or t.stride(0) != k_scales.stride(0):
+                raise F3dcError(1, "a page's scales must lie together, pages of k_scales and v_scales equally far apart")
+        _same_device("cache", self._tensors)
+        super().__init__(pages, tokens, heads, dh, *(t.data_ptr() for t in self._tensors), k.stride(0), k_scales.stride(0))
+        self._ref = C.pointer(self)
+
+
+class KVBatch(C.Structure):
+    """The sequences of a call: row_start int32 [batch + 1], lengths int32 [batch] (with the
+    call's rows) and page_table int32 [batch, pages] on the GPU, kept alive; `rows` packed rows, and
+    bounds on a sequence's rows and length."""
+    _fields_ = [("row_start", C.c_void_p), ("lengths", C.c_void_p), ("page_table", C.c_void_p), ("table_stride", C.c_int64),
+                ("batch", C.c_int32), ("rows", C.c_int32), ("max_rows", C.c_int32), ("max_length", C.c_int32)]
+
+    def __init__(self, row_start, lengths, page_table, rows, max_rows, max_length):
+        self._tensors = (row_start, lengths, page_table)
+        for t, n in zip(self._tensors, (1, 1, 2)):
+            if t.dtype not in _fp8_types()["int32"] or t.dim() != n or (t.numel() and t.stride(n - 1) != 1):
+                raise F3dcError(1, f"row_start, lengths and page_table are int32 with neighbouring entries: got {t.dtype} {tuple(t.shape)}")
+        batch = lengths.shape[0]
+        if row_start.shape[0] != batch + 1 or page_table.shape[0] != batch:
+            raise F3dcError(1, "row_start needs batch + 1 entries, page_table a row for each sequence")
+        if batch > 1 and page_table.stride(0) < page_table.shape[1]:
+            raise F3dcError(1, "rows of page_table overlap")
+        _same_device("batch", self._tensors)
+        # (a single row's stride may be anything)
+        stride = page_table.shape[1] if batch <= 1 else page_table.stride(0)
+        super().__init__(row_start.data_ptr(), lengths.data_ptr(), page_table.data_ptr(), stride, batch, rows, max_rows, max_length)
+        self._ref = C.pointer(self)
+
+
 _lock = threading.Lock()
 _lib = None
 _i64 = C.c_int64
@@ -129,6 +207,12 @@ def lib():
                 "f3dc_gemm_fp8": ([_vp, _i64] * 4 + [_vp, _vp] + [_vp, _i64] * 2 + [C.c_int32] * 4 + [_vp], C.c_int),
                 "f3dc_norm_residual": ([C.POINTER(NormLayer), _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp,
                                         C.c_int32, _vp, _i64, _vp, _i64, C.c_int32, _vp], C.c_int),
+                "f3dc_rotary_turns": ([_f64p, C.c_int32, C.POINTER(C.c_uint64)], C.c_int),
+                "f3dc_kv_append_fp8": ([C.POINTER(KVCache), C.POINTER(KVBatch), C.POINTER(Rotary)] + [_vp, _i64] * 4 +
+                                       [C.c_int32, _vp, _vp], C.c_int),
+                "f3dc_kv_attention_workspace": ([C.POINTER(KVCache), C.POINTER(KVBatch), C.c_int32], C.c_size_t),
+                "f3dc_kv_attention_fp8": ([C.POINTER(KVCache), C.POINTER(KVBatch)] + [_vp, _i64] * 2 +
+                                          [_vp, C.c_int32, C.c_float, C.c_int32, _vp, C.c_size_t, _vp], C.c_int),
             }
             for name, (args, res) in sig.items():
                 fn = getattr(L, name)
@@ -448,5 +532,76 @@ def norm_residual(layer, x, ldx, x_out, ldxo, y, ldy, gate, scale, shift, ldmod,
         raise F3dcError(1, "a gain or bias is on another device than the current one")
     st = calls[2](layer._ref, px, ldx, pxo, ldxo, py, ldy, pg, psc, psh, ldmod, pgr, groups, ph, ldh, phs, ldhs, rows,
                   _stream(stream))
+    if st:
+        _check(st)
+
+
+# ---------------------------------------------------------------- attention over a paged 8-bit cache
+
+_kv_state = None
+
+
+def rotary_turns(inv_freq) -> np.ndarray:
+    """Angles per unit of position (radians) as 64-bit fractions of a turn."""
+    f = np.ascontiguousarray(inv_freq, np.float64)
+    out = np.empty(f.shape, np.uint64)
+    _check(lib().f3dc_rotary_turns(f.ctypes.data_as(_f64p), f.size, out.ctypes.data_as(C.POINTER(C.c_uint64))))
+    return out
+
+
+def _kv_args():
+    """The tensor arguments of kv_append_fp8 and of kv_attention_fp8."""
+    return (_Args(k="bf16", v="bf16", q="bf16", q_out="bf16", positions="int32"),
+            _Args(q="bf16", out="bf16", lse="fp32", workspace="e4m3"))
+
+
+def _kv():
+    """(calls, their arguments, current device's getter or None), made on first use."""
+    global _kv_state
+    if _kv_state is None:
+        current = _fp8()[2]
+        L = lib()
+        _kv_state = ((L.f3dc_kv_append_fp8, L.f3dc_kv_attention_fp8), _kv_args(), current)
+    return _kv_state
+
+
+def _kv_here(current, *structs):
+    for s in structs:
+        if s is not None and (s._turns if isinstance(s, Rotary) else s._tensors[0]).get_device() != current():
+            raise F3dcError(1, f"a {type(s).__name__} is on another device than the current one")
+
+
+def kv_append_fp8(cache, batch, k, ldk, v, ldv, q=None, ldq=0, q_out=None, ldqo=0, heads=0, rotary=None, positions=None,
+                  stream=None):
+    """Keys and values (bf16 rows) of the batch's new tokens into the pages of their
+    sequences, rotated by `rotary` (a Rotary) on the way; with q the rows' queries are rotated into q_out too."""
+    calls, args, current = _kv_state or _kv()
+    pk, pv, pq, pqo, pp = args[0].pointers((k, v, q, q_out, positions), current)
+    if current is not None:
+        _kv_here(current, cache, batch, rotary)
+    if positions is not None and (not positions.is_contiguous() or positions.numel() < batch.rows * (rotary.axes if rotary else 1)):
+        raise F3dcError(1, "positions are contiguous int32 [rows, axes]")
+    st = calls[0](cache._ref, batch._ref, rotary._ref if rotary is not None else None, pk, ldk, pv, ldv, pq, ldq, pqo, ldqo, heads,
+                  pp, _stream(stream))
+    if st:
+        _check(st)
+
+
+def kv_attention_workspace(cache, batch, heads) -> int:
+    """Bytes of workspace for kv_attention_fp8 (0: none is needed)."""
+    return int(lib().f3dc_kv_attention_workspace(cache._ref, batch._ref, heads))
+
+
+def kv_attention_fp8(cache, batch, q, ldq, out, ldo, heads, scale, causal=False, lse=None, workspace=None, stream=None):
+    """Attention of packed bf16 query rows over their sequences' cached tokens; lse
+    fp32 [rows, heads]; `workspace` a byte tensor of kv_attention_workspace() bytes."""
+    calls, args, current = _kv_state or _kv()
+    pq, po, pl, pw = args[1].pointers((q, out, lse, workspace), current)
+    if current is not None:
+        _kv_here(current, cache, batch)
+    if lse is not None and (not lse.is_contiguous() or lse.numel() < batch.rows * heads):
+        raise F3dcError(1, "lse is contiguous fp32 [rows, heads]")
+    st = calls[1](cache._ref, batch._ref, pq, ldq, po, ldo, pl, heads, scale, 1 if causal else 0, pw,
+                  workspace.numel() if workspace is not None else 0, _stream(stream))
     if st:
         _check(st)

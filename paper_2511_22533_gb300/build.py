@@ -20,7 +20,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "k_select.cu", "k_rows.cu", "k_gemm.cu", "k_attn.cu", "k_attn_one.cu", "k_decode.cu", "noalloc.cu",
            "k_quant.cu", "k_gemm8.cu", "k_few8.cu", "k_norm.cu", "api_fp8.cu",
-           "k_kv_append.cu", "k_kv_few.cu", "api_kv.cu"]
+           "k_kv_append.cu", "k_kv_few.cu", "k_kv_attn.cu", "api_kv.cu"]
 
 
 def _nvcc() -> str:

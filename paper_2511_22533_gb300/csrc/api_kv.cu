@@ -98,7 +98,7 @@ int64_t part_bytes(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads
 int splits(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads, int sms)
 {
     if (empty(t)) return 1;
-    return kv_splits(t->batch, t->max_rows, t->max_length, heads, c->kv_heads, c->dh, sms);
+    return kv_splits(t->batch, t->max_rows, t->max_length, heads, c->kv_heads, sms);
 }
 
 }  // namespace
@@ -247,6 +247,7 @@ extern "C" f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f
     // rows, lengths or pages out of range are recorded here (read by f3dc_gemm_status)
     a.err = gemm_status_word();
     if (!a.err) return fail(F3DC_ERR_CUDA, "cannot resolve the status word");
-    e = launch_kv_few(a, (cudaStream_t)stream);
+    e = kv_many_rows(batch->max_rows, heads, cache->kv_heads) ? launch_kv_attn(a, (cudaStream_t)stream)
+                                                              : launch_kv_few(a, (cudaStream_t)stream);
     return e == cudaSuccess ? F3DC_OK : fail(F3DC_ERR_CUDA, "launch", e);
 }

@@ -490,12 +490,20 @@ cudaError_t launch_few(const KvAttnArgs &args, cudaStream_t s)
     cudaError_t e = ask_smem(k_kv_few<DH, MT>, FewCfg<DH>::kSmem, devices);
     if (e != cudaSuccess) return e;
     e = launch_k(k_kv_few<DH, MT>, dim3((unsigned)ctas), dim3(32 * kWarps), FewCfg<DH>::kSmem, s, a);
-    if (e != cudaSuccess || a.splits == 1) return e;
-    const int64_t rows = (int64_t)a.batch.rows * a.heads;
-    return launch_k(k_kv_join<DH>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, a);
+    return e != cudaSuccess || a.splits == 1 ? e : launch_kv_join(a, s);
 }
 
 }  // namespace
+
+cudaError_t launch_kv_join(const KvAttnArgs &a, cudaStream_t s)
+{
+    const dim3 grid((unsigned)(((int64_t)a.batch.rows * a.heads + 7) / 8)), block(256);
+    switch (a.cache.dh) {
+    case 32: return launch_k(k_kv_join<32>, grid, block, 0, s, a);
+    case 64: return launch_k(k_kv_join<64>, grid, block, 0, s, a);
+    default: return launch_k(k_kv_join<128>, grid, block, 0, s, a);
+    }
+}
 
 cudaError_t launch_kv_few(const KvAttnArgs &a, cudaStream_t s)
 {

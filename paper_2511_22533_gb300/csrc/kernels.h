@@ -490,14 +490,21 @@ struct KvAttnArgs {
     int row_blocks;               // set by the launch: blocks of packed rows of a sequence
     uint32_t *err;
 };
-cudaError_t launch_kv_few(const KvAttnArgs &a, cudaStream_t s);
+cudaError_t launch_kv_few(const KvAttnArgs &a, cudaStream_t s);   // few packed rows to a key head
+cudaError_t launch_kv_attn(const KvAttnArgs &a, cudaStream_t s);  // many
+cudaError_t launch_kv_join(const KvAttnArgs &a, cudaStream_t s);  // adds the parts up (called by both)
 
-// CTAs that share a sequence's keys: as many as fill the SMs twice, each with at least
+// Packed rows from which tensor-memory tiles are taken.
+inline bool kv_many_rows(int max_rows, int heads, int kv_heads) { return (int64_t)max_rows * (heads / kv_heads) > 32; }
+
+// CTAs that share a sequence's keys: as many as fill the SMs (twice with few rows), each with at least
 // 512 tokens.
-inline int kv_splits(int batch, int max_rows, int max_length, int heads, int kv_heads, int dh, int sms)
+inline int kv_splits(int batch, int max_rows, int max_length, int heads, int kv_heads, int sms)
 {
-    const int64_t rows = (int64_t)max_rows * (heads / kv_heads), blocks = (rows + 15) / 16 * kv_heads * batch;
-    int64_t n = 2 * (int64_t)sms / blocks;
+    const int64_t rows = (int64_t)max_rows * (heads / kv_heads);
+    const bool many = kv_many_rows(max_rows, heads, kv_heads);
+    const int64_t blocks = (many ? (rows + 255) / 256 : (rows + 15) / 16) * kv_heads * batch;
+    int64_t n = (many ? 1 : 2) * (int64_t)sms / blocks;
     if (n > max_length / 512) n = max_length / 512;
     return n < 1 ? 1 : (int)n;
 }

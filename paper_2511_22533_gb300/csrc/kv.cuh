@@ -2,7 +2,10 @@
 // f3dc_kv_attention_fp8): a sequence's bounds, its pages, and conversions of e4m3.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include <atomic>
+#include <type_traits>
 
 #include "kernels.h"
 #include "mx8.cuh"

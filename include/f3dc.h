@@ -543,7 +543,7 @@ typedef struct f3dc_kv_cache {
     void *k, *v;          /* device e4m3 bytes [pages, Hk, page_tokens, dh], 16-byte aligned */
     uint8_t *k_scales, *v_scales; /* device bytes [pages, Hk] */
     int64_t page_stride;  /* bytes from a page to the next in k and in v: a multiple of 16,
-                           * at least Hk page_tokens dh */
+                           * at least Hk page_tokens dh; pages page_stride <= 2^36 */
     int64_t scale_stride; /* bytes from a page to the next in k_scales and v_scales: at least Hk */
 } f3dc_kv_cache;
 

@@ -44,8 +44,9 @@ const char *cache_shape(const f3dc_kv_cache *c)
     if (c->page_stride < (int64_t)c->kv_heads * c->page_tokens * c->dh || c->page_stride % 16)
         return "page_stride must be a multiple of 16, at least a page's bytes";
     if (c->scale_stride < c->kv_heads) return "scale_stride is smaller than kv_heads";
-    if (c->page_stride > ((int64_t)1 << 62) / c->pages || c->scale_stride > ((int64_t)1 << 62) / c->pages)
-        return "a cache stride is too large";
+    // (offsets in k and v are counted in 32 bits of 16 bytes)
+    if (c->page_stride > ((int64_t)1 << 36) / c->pages || c->scale_stride > ((int64_t)1 << 62) / c->pages)
+        return "the cache is too large";
     return nullptr;
 }
 

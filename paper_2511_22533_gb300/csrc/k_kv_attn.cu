@@ -7,9 +7,10 @@
 // two tiles A and B of 128 rows that share their keys, whose score / softmax / product chains run side by side.
 //   warps 0, 1   tcgen05.mma issuers of tile A and of tile B.  Per key tile g of 128 tokens: S_t(g) = Q_t K^T
 //                (N = 128, K = dh), O_t += P_t V(g) (N = dh, K = 128; P read from TMEM)
-//   warps 4-7    the cache's pages: each thread loads 16-byte pieces of keys and values (the next half of a
-//                tile while it converts this one), converts e4m3 to fp16 (exactly) and writes them to shared memory in the
-//                MMA's swizzled layout; scales of the tile's pages beside them
+//   warp 2       walks the page table, four tiles at a time: where each 16 tokens of a tile lie, and their scales
+//   warps 4-7    the cache's pages: each thread loads 16-byte pieces of keys and values (those of the next tile
+//                while it converts this one's), converts e4m3 to fp16 (exactly) and writes them to shared memory in the
+//                MMA's swizzled layout
 //   warps 8-11   softmax of tile A, warps 12-15 of tile B: one thread per row.  Before the first tile they convert
 //                their queries (bf16 times a power of two of the row: exact in fp16) into shared memory.
 // TMEM: S_A S_B (fp32, 128 columns each) | O_A O_B (dh each) | P_A P_B (fp16 pairs, 64 each); with dh 128 there
@@ -27,25 +28,43 @@ namespace {
 constexpr int kThreads = 512;
 constexpr float kInf = __builtin_huge_valf();
 // Registers per thread after the split: the launch has 512 x 128.
-constexpr int kIssueRegs = 48, kConvertRegs = 96, kSoftmaxRegs = 184;
+constexpr int kIssueRegs = 40, kConvertRegs = 104, kSoftmaxRegs = 184;
 static_assert(128 * (kIssueRegs + kConvertRegs) + 256 * kSoftmaxRegs <= 512 * 128, "register split above the launch's total");
 
-// Scales of a tile's eight blocks of 16 tokens (a page has at least one).
-struct TileScales {
-    float key[8], value_log2[8], value_inverse[8];
-};
+// A row's largest weight is 2^kTop where its reference was taken.  The sum of a tile's weights, which is taken
+// anyway, says whether one may have left fp16's range; only then is the reference looked at again.  128 weights
+// of 2^kTop are 2^14, below kMostSum, so rows of even weights do not ask.  fp16 holds 2^-21 of a row's largest
+// weight at full precision and 2^-32 at all.
+constexpr float kTop = 3.f, kMostSum = 60000.f;
 
-template <int DH>
+// What the page table says about a tile: of each of its eight runs of 16 tokens where it starts in the pool (in 16
+// bytes; inside the pool always, page 0 standing for what is not there), how many tokens there are, and what its values are multiplied by;
+// and the scales of its NB blocks of 128 / NB tokens (a page has at least one).
+template <int NB>
+struct StepScales {  // of half a tile
+    float key[NB / 2], value_log2[NB / 2], value_inverse[NB / 2];
+};
+template <int NB>
+struct TileInfo {
+    uint32_t at[8], times[8];
+    int32_t there[8];
+    StepScales<NB> scales[2];
+    int32_t complete, plain;  // every run has 16 tokens; values are multiplied by 1
+};
+constexpr int kGroup = 4, kGroups = 4;  // tiles looked up at once, and groups of them in shared memory
+constexpr int kGroupSteps = 2 * kGroup;
+
+template <int DH, int NB>
 struct Cfg {
     static constexpr int kRowBytes = DH == 32 ? 64 : 128;  // of a region: 32 or 64 columns
     static constexpr int kRegions = DH == 128 ? 2 : 1;
     static constexpr int kRegion = 128 * kRowBytes, kTile = kRegions * kRegion;
     static constexpr uint32_t kAtom = 8 * kRowBytes, kSwz = DH == 32 ? kSwizzle64 : kSwizzle128;
-    static constexpr int kStages = DH == 128 ? 2 : 3;
-    static constexpr size_t kSmem = 1024 + (size_t)kTile * (2 + 2 * kStages) + (kStages + 1) * sizeof(TileScales) + 512;
-    static constexpr bool kAlias = DH == 128;  // P in the place of S
-    static constexpr uint32_t kColO = 256, kColP = kAlias ? 0 : 256 + 2 * DH, kStepP = kAlias ? 128 : 64;
-    static_assert(kAlias || 256 + 2 * DH + 128 <= 512, "TMEM layout");
+    static constexpr int kStages = DH == 128 ? 2 : 4;
+    static constexpr int kPlaces = DH == 128 ? 2 : 3;  // of S and P of a query tile, 64 columns each
+    static constexpr size_t kSmem = 1024 + (size_t)kTile * (2 + 2 * kStages) + kGroups * kGroup * sizeof(TileInfo<NB>) + 512;
+    static constexpr uint32_t kColO = 2 * 64 * kPlaces;
+    static_assert(kColO + 2 * DH <= 512, "TMEM layout");
     // byte of 16-byte piece `piece` (8 columns) of a row
     static F3DC_DEV int place(int row, int piece)
     {
@@ -58,6 +77,29 @@ struct Cfg {
 __host__ __device__ constexpr uint32_t make_idesc_f16(int M, int N, int b_mn_major)
 {
     return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// mbarrier operations on a shared-memory address that is at hand
+F3DC_DEV bool mbar_test_addr(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return ok != 0;
+}
+F3DC_DEV bool warp_wait_addr(uint32_t bar, uint32_t parity, volatile int *abort, uint32_t *err)
+{
+    if (warp_all(mbar_test_addr(bar, parity))) return true;
+    return warp_wait(reinterpret_cast<uint64_t *>(__cvta_shared_to_generic(bar)), parity, abort, err);
+}
+// an arrival by the lanes that say so, without a branch
+F3DC_DEV void mbar_arrive_if(uint32_t bar, bool me)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %1, 0;\n @p mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(bar),
+                 "r"((uint32_t)me)
+                 : "memory");
 }
 
 F3DC_DEV bool wait_bounded(uint64_t *bar, uint32_t parity, uint64_t ns)
@@ -75,50 +117,30 @@ F3DC_DEV uint32_t half2_times(uint32_t a, uint32_t b)
     return r;
 }
 
-template <int DH>
+template <int DH, int NB>
 __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
 {
-    using C = Cfg<DH>;
+    using C = Cfg<DH, NB>;
     constexpr int kStages = C::kStages;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *const smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *const sQ = smem, *const sK = sQ + 2 * C::kTile, *const sV = sK + kStages * C::kTile;
-    TileScales *const scales = reinterpret_cast<TileScales *>(sV + kStages * C::kTile);
-    uint64_t *const bars = reinterpret_cast<uint64_t *>(scales + kStages + 1);
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(sV + kStages * C::kTile);
+    TileInfo<NB> *const infos = reinterpret_cast<TileInfo<NB> *>(bars + 64);
     // per stage: keys / values written by the four converting warps, and read by both tiles' MMAs
     uint64_t *const k_full = bars, *const v_full = k_full + kStages, *const k_empty = v_full + kStages,
                    *const v_empty = k_empty + kStages;
-    // per query tile t, once: Q_t written; once per key tile: S_t written, S_t read, P_t written, P_t V done
-    // per place of `scales`: written (its next writer is behind the softmax of the tile before)
-    uint64_t *const c_full = v_empty + kStages;
-    uint64_t *const q_full = c_full + kStages + 1, *const s_full = q_full + 2, *const s_free = s_full + 2,
-                   *const p_full = s_free + 2, *const pv_done = p_full + 2, *const drain = pv_done + 2;
+    // per query tile t, once: Q_t written; per step, in turn for the places: S_t written, P_t written, P_t V done
+    // per group of infos: written, read by the converting and the softmax warps
+    uint64_t *const i_full = v_empty + kStages, *const i_empty = i_full + kGroups;
+    uint64_t *const q_full = i_empty + kGroups, *const s_full = q_full + 2, *const p_full = s_full + 2 * C::kPlaces,
+                   *const pv_done = p_full + 2 * C::kPlaces, *const drain = pv_done + 2 * C::kPlaces;
     uint32_t *const tmem_holder = reinterpret_cast<uint32_t *>(drain + 1);
     volatile int *const abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
     volatile int *const nan_flag = abort_flag + 1;  // NaN values counted as zeros
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     griddep_launch();
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(&k_full[s], 4);
-            mbar_init(&v_full[s], 4);
-            mbar_init(&k_empty[s], 2);
-            mbar_init(&v_empty[s], 2);
-        }
-        for (int s = 0; s <= kStages; ++s) mbar_init(&c_full[s], 1);
-        for (int t = 0; t < 2; ++t) {
-            mbar_init(&q_full[t], 4);
-            mbar_init(&s_full[t], 1);
-            mbar_init(&s_free[t], 4);
-            mbar_init(&p_full[t], 4);
-            mbar_init(&pv_done[t], 1);
-        }
-        mbar_init(drain, 2);
-        *abort_flag = 0;
-        *nan_flag = 0;
-        fence_mbar_init();
-    }
     griddep_wait();
 
     // ---- this CTA's item; the blocks of rows that see most come first
@@ -140,8 +162,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
     const int all = (most + 127) / 128;
     const int g_begin = (int)((int64_t)all * split / a.splits), g_end = (int)((int64_t)all * (split + 1) / a.splits);
     const int n_tiles = g_end - g_begin;
+    // steps of 64 tokens: two to a tile, of the last one perhaps none sees the second
+    const int n_steps = max(0, min(2 * n_tiles, (most + 63) / 64 - 2 * g_begin));
     const int page = a.cache.page, page_log2 = 31 - __clz(page);
 
+    if (threadIdx.x == 0) {
+        for (int st = 0; st < kStages; ++st) {
+            mbar_init(&k_full[st], 4);
+            mbar_init(&v_full[st], 4);
+            mbar_init(&k_empty[st], tiles);
+            mbar_init(&v_empty[st], tiles);
+        }
+        for (int s = 0; s < kGroups; ++s) {
+            mbar_init(&i_full[s], 1);
+            mbar_init(&i_empty[s], 4 + 4 * tiles);
+        }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&q_full[t], 4);
+            for (int i = C::kPlaces * t; i < C::kPlaces * (t + 1); ++i) {
+                mbar_init(&s_full[i], 1);
+                mbar_init(&p_full[i], 4);
+                mbar_init(&pv_done[i], 1);
+            }
+        }
+        mbar_init(drain, 2);
+        *abort_flag = 0;
+        *nan_flag = 0;
+        fence_mbar_init();
+    }
     if (warp == 0) {
         tmem_alloc(tmem_holder, 512);
         tmem_relinquish();
@@ -156,163 +204,210 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
         reg_dec<kIssueRegs>();
         if (warp < tiles && n_tiles > 0) {
             // ------------------------------------------------ MMA issuer of one query tile
-            constexpr uint32_t idesc_s = make_idesc_f16(128, 128, 0), idesc_o = make_idesc_f16(128, DH, 1);
+            constexpr uint32_t idesc_s = make_idesc_f16(128, 64, 0), idesc_o = make_idesc_f16(128, DH, 1);
             const int t = warp;
             const uint64_t q_desc = make_sdesc(smem_u32(sQ + t * C::kTile), 16, C::kAtom, C::kSwz);
             const uint64_t k_desc = make_sdesc(smem_u32(sK), 16, C::kAtom, C::kSwz);
             // values: the head's columns lie a region apart, eight tokens an atom
             const uint64_t v_desc = make_sdesc(smem_u32(sV), C::kRegion, C::kAtom, C::kSwz);
             constexpr uint64_t kStageStep = C::kTile >> 4, kRegionStep = C::kRegion >> 4, kVStep = (16 * C::kRowBytes) >> 4;
-            auto scores = [&](int g) {
-                const int st = g % kStages;
-                if (!wait(&k_full[st], (g / kStages) & 1)) return false;
-                if (g > 0 && !(C::kAlias ? wait(&pv_done[t], (g - 1) & 1) : wait(&s_free[t], (g - 1) & 1))) return false;
+            constexpr uint64_t kHalfStep = (64 * C::kRowBytes) >> 4;
+            // step j: place j % kPlaces of S and P, whose barriers are in their phase j / kPlaces
+            struct Place {
+                int i = 0;
+                uint32_t phase = 0;
+                F3DC_DEV void next()
+                {
+                    if (++i == C::kPlaces) i = 0, phase ^= 1;
+                }
+            } ps, pp;
+            uint64_t *const s_own = s_full + C::kPlaces * t, *const p_own = p_full + C::kPlaces * t, *const done = pv_done + C::kPlaces * t;
+            const uint32_t tm = tmem + t * 64 * C::kPlaces;
+            auto scores = [&](int j) {
+                const int g = j >> 1, st = g % kStages;
+                if ((j & 1) == 0 && !wait(&k_full[st], (g / kStages) & 1)) return false;
                 tc_fence_after();
-                const uint64_t kd = k_desc + st * kStageStep;
+                const uint64_t kd = k_desc + st * kStageStep + (j & 1) * kHalfStep;
 #pragma unroll
                 for (int kk = 0; kk < DH / 16; ++kk) {
                     const uint64_t at = (kk / 4) * kRegionStep + 2 * (kk % 4);
-                    mma_bf16_elect(tmem + t * 128, q_desc + at, kd + at, idesc_s, kk > 0);
+                    mma_bf16_elect(tm + ps.i * 64, q_desc + at, kd + at, idesc_s, kk > 0);
                 }
-                mma_commit_elect(&s_full[t]);
-                for (int i = tiles; i <= 2; ++i) mma_commit_elect(&k_empty[st]);  // (for the tile that there is not, too)
+                mma_commit_elect(&s_own[ps.i]);
+                if ((j & 1) || j + 1 == n_steps) mma_commit_elect(&k_empty[st]);
+                ps.next();
                 return true;
             };
-            auto product = [&](int g) {
-                const int st = g % kStages;
-                if (!wait(&v_full[st], (g / kStages) & 1)) return false;
-                if (!wait(&p_full[t], g & 1)) return false;
+            // P V of step j, then S of the step that takes P's place
+            auto product = [&](int j) {
+                const int g = j >> 1, st = g % kStages;
+                if ((j & 1) == 0 && !wait(&v_full[st], (g / kStages) & 1)) return false;
+                if (!wait(&p_own[pp.i], pp.phase)) return false;
                 tc_fence_after();
-                const uint64_t vd = v_desc + st * kStageStep;
+                const uint64_t vd = v_desc + st * kStageStep + (j & 1) * kHalfStep;
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                    mma_bf16_ts_elect(tmem + C::kColO + t * DH, tmem + C::kColP + t * C::kStepP + kk * 8, vd + kk * kVStep, idesc_o,
-                                      kk > 0 || g > 0);
-                mma_commit_elect(&pv_done[t]);
-                for (int i = tiles; i <= 2; ++i) mma_commit_elect(&v_empty[st]);
+                for (int kk = 0; kk < 4; ++kk)
+                    mma_bf16_ts_elect(tmem + C::kColO + t * DH, tm + pp.i * 64 + kk * 8, vd + kk * kVStep, idesc_o, kk > 0 || j > 0);
+                mma_commit_elect(&done[pp.i]);
+                if ((j & 1) || j + 1 == n_steps) mma_commit_elect(&v_empty[st]);
+                if (j + C::kPlaces < n_steps && !(wait(&done[pp.i], pp.phase) && scores(j + C::kPlaces))) return false;
+                pp.next();
                 return true;
             };
-            if (wait(&q_full[t], 0)) {
+            bool ok = wait(&q_full[t], 0);
 #pragma unroll 1
-                for (int g = 0; g < n_tiles; ++g) {
-                    if (!scores(g)) break;
-                    if (C::kAlias) {
-                        if (!product(g)) break;
-                    } else {
-                        if (g > 0 && !product(g - 1)) break;
-                        if (g + 1 == n_tiles && !product(g)) break;
+            for (int j = 0; ok && j < min(C::kPlaces, n_steps); ++j) ok = scores(j);
+#pragma unroll 1
+            for (int j = 0; ok && j < n_steps; ++j) ok = product(j);
+        }
+        if (warp == 2) {
+            // ------------------------------------------------ the page table: a lane for 16 tokens of one of four tiles
+            const int run = lane & 7;
+            const uint32_t stride16 = (uint32_t)(a.cache.page_stride >> 4);
+            const uint32_t own16 = (uint32_t)(hk * page + (16 * run & (page - 1))) * (DH / 16);
+#pragma unroll 1
+            for (int g0 = 0, n = 0; g0 < n_tiles; g0 += kGroup, ++n) {
+                const int g = g0 + (lane >> 3), t0 = (g_begin + g) * 128 + 16 * run;
+                const bool mine = lane < 8 * kGroup;
+                uint32_t at = own16, bytes = 127u | 127u << 8;
+                int there = 0;
+                if (mine && g < n_tiles && t0 < s.length) {
+                    const int p = kv_page(a.batch, a.cache, b, t0 >> page_log2, a.err);
+                    if (p >= 0) {
+                        const int64_t of = (int64_t)p * a.cache.scale_stride + hk;
+                        bytes = a.cache.ks[of] | (uint32_t)a.cache.vs[of] << 8;
+                        at = (uint32_t)p * stride16 + own16;
+                        there = min(16, s.length - t0);
                     }
                 }
+                const int slot = n % kGroups;
+                if (!wait(&i_empty[slot], ((n / kGroups) & 1) ^ 1)) break;
+                const ValueScale v = value_scale(bytes >> 8);
+                const uint32_t tile = 0xFFu << (lane & 24);
+                const uint32_t complete = __ballot_sync(0xffffffffu, there == 16), plain = __ballot_sync(0xffffffffu, v.times == kHalfOnes);
+                if (mine) {
+                    TileInfo<NB> &x = infos[slot * kGroup + (lane >> 3)];
+                    x.at[run] = at;
+                    x.times[run] = v.times;
+                    x.there[run] = there;
+                    if (run % (8 / NB) == 0) {
+                        StepScales<NB> &sc = x.scales[run >> 2];
+                        const int k = (run & 3) * NB / 8;
+                        sc.key[k] = key_scale(bytes & 255u);
+                        sc.value_log2[k] = v.log2;
+                        sc.value_inverse[k] = v.inverse;
+                    }
+                    if (run == 0) {
+                        x.complete = (complete & tile) == tile;
+                        x.plain = (plain & tile) == tile;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&i_full[slot]);
             }
         }
     } else if (warp < 8) {
         // ------------------------------------------------ pages to operands
         reg_dec<kConvertRegs>();
-        constexpr int kPieces = DH / 16;  // 16-byte pieces of a token, and of a thread per half of a tile
+        // 16-byte pieces of a token, and of a thread per half of a tile: piece k is of a token 128 / kPieces further
+        constexpr int kPieces = DH / 16, kTokens = 128 / kPieces;
         const int i = threadIdx.x - 128;
-        // lane l < 8 looks after the tile's 16 tokens from 16 l: their page and its scale bytes
-        int pg = -1, pg_next = -1;
-        uint32_t bytes = 0, bytes_next = 0;
-        auto look_up = [&](int g, int &p, uint32_t &sb) {
-            const int t0 = (g_begin + g) * 128 + 16 * (lane & 7);
-            p = -1;
-            sb = 127u | 127u << 8;
-            if (g < n_tiles && t0 < s.length) {
-                p = kv_page(a.batch, a.cache, b, t0 >> page_log2, a.err);
-                if (p >= 0) {
-                    const int64_t at = (int64_t)p * a.cache.scale_stride + hk;
-                    sb = a.cache.ks[at] | (uint32_t)a.cache.vs[at] << 8;
-                }
-            }
+        // (dh 128: eight neighbouring lanes hold the same columns' half of two tokens, so that their stores meet no bank twice)
+        const int piece = DH == 128 ? (i & 3) | (i >> 1 & 4) : i % kPieces;
+        const int token = DH == 128 ? (i >> 4) * 2 + (i >> 2 & 1) : i / kPieces;
+        const int put0 = C::place(token, 2 * piece), put1 = C::place(token, 2 * piece + 1);
+        const uint4 *const k_own = reinterpret_cast<const uint4 *>(a.cache.k) + (token & 15) * kPieces + piece;
+        const uint4 *const v_own = reinterpret_cast<const uint4 *>(a.cache.v) + (token & 15) * kPieces + piece;
+        const int run = token >> 4;  // of piece 0
+        auto info = [&](int g) -> const TileInfo<NB> & { return infos[g / kGroup % kGroups * kGroup + g % kGroup]; };
+        // piece k of a half of a tile
+        auto fetch = [&](const uint4 *own, const TileInfo<NB> &x, int k) { return own[x.at[run + k * (kTokens / 16)]]; };
+        auto clear = [&](const TileInfo<NB> &x, uint4 (&u)[kPieces]) {
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k)
+                if ((token & 15) >= x.there[run + k * (kTokens / 16)]) u[k] = make_uint4(0u, 0u, 0u, 0u);
         };
-        // piece k of a half of tile g
-        auto fetch = [&](const uint8_t *pool, int g, int p, int k) {
-            const int x = i + 128 * k, token = x / kPieces, piece = x % kPieces, t = (g_begin + g) * 128 + token;
-            const int pp = __shfl_sync(0xffffffffu, p, token >> 4);
-            uint4 u = make_uint4(0u, 0u, 0u, 0u);
-            if (pp >= 0 && t < s.length)
-                u = *reinterpret_cast<const uint4 *>(pool + (int64_t)pp * a.cache.page_stride +
-                                                     ((int64_t)hk * page + (t & (page - 1))) * DH + 16 * piece);
-            return u;
+        auto widen = [&](uint4 w, uint32_t (&h)[8]) {
+            e4m3x4_to_half2(w.x, h[0], h[1]);
+            e4m3x4_to_half2(w.y, h[2], h[3]);
+            e4m3x4_to_half2(w.z, h[4], h[5]);
+            e4m3x4_to_half2(w.w, h[6], h[7]);
         };
         auto store = [&](uint8_t *tile, int k, const uint32_t (&h)[8]) {
-            const int x = i + 128 * k, token = x / kPieces, piece = x % kPieces, swap = DH == 128 ? piece >> 2 : 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int f = e ^ swap;
-                // (registers are picked by selects, not by an index)
-                const uint4 w = f == 0 ? make_uint4(h[0], h[1], h[2], h[3]) : make_uint4(h[4], h[5], h[6], h[7]);
-                *reinterpret_cast<uint4 *>(tile + C::place(token, 2 * piece + f)) = w;
-            }
+            tile += k * kTokens * C::kRowBytes;  // (the swizzle repeats every eight rows)
+            *reinterpret_cast<uint4 *>(tile + put0) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4 *>(tile + put1) = make_uint4(h[4], h[5], h[6], h[7]);
         };
-        look_up(0, pg, bytes);
-        uint4 u[kPieces];
+        uint4 ku[kPieces], vu[kPieces];
+        if (n_tiles > 0 && wait(&i_full[0], 0)) {
 #pragma unroll
-        for (int k = 0; k < kPieces; ++k) u[k] = fetch(a.cache.k, 0, pg, k);
+            for (int k = 0; k < kPieces; ++k) ku[k] = fetch(k_own, info(0), k);
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) vu[k] = fetch(v_own, info(0), k);
+        }
 #pragma unroll 1
         for (int g = 0; g < n_tiles; ++g) {
             const int st = g % kStages;
             const uint32_t parity = (g / kStages) & 1;
-            look_up(g + 1, pg_next, bytes_next);
+            const TileInfo<NB> &now = info(g);
+            // (behind the last tile its own pieces are loaded once more, unused)
+            const int ng = min(g + 1, n_tiles - 1);
+            if (ng % kGroup == 0 && ng > g && !wait(&i_full[ng / kGroup % kGroups], (ng / kGroup / kGroups) & 1)) break;
+            const TileInfo<NB> &next = info(ng);
+            const bool complete = now.complete != 0;
             // keys
             if (!wait(&k_empty[st], parity ^ 1)) break;
-            if (warp == 4) {
-                const int at = g % (kStages + 1);
-                if (lane < 8) {
-                    const ValueScale v = value_scale(bytes >> 8);
-                    scales[at].key[lane] = key_scale(bytes & 255u);
-                    scales[at].value_log2[lane] = v.log2;
-                    scales[at].value_inverse[lane] = v.inverse;
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&c_full[at]);
-            }
+            if (!complete) clear(now, ku);
 #pragma unroll
             for (int k = 0; k < kPieces; ++k) {
                 uint32_t h[8];
-                const uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) e4m3x4_to_half2(w[e], h[2 * e], h[2 * e + 1]);
+                widen(ku[k], h);
                 store(sK + st * C::kTile, k, h);
-                u[k] = fetch(a.cache.v, g, pg, k);
+                ku[k] = fetch(k_own, next, k);
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&k_full[st]);
             // values
             if (!wait(&v_empty[st], parity ^ 1)) break;
-            const uint32_t times = value_scale(bytes >> 8).times;
+            if (!complete) clear(now, vu);
             const bool partly = (g_begin + g + 1) * 128 > least;
-            const bool odd = partly || __any_sync(0xffffffffu, times != kHalfOnes);
-            uint32_t numbers = 0xffffffffu;
+            if (!partly && now.plain) {
 #pragma unroll
-            for (int k = 0; k < kPieces; ++k) {
-                uint32_t h[8];
-                const uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+                for (int k = 0; k < kPieces; ++k) {
+                    uint32_t h[8];
+                    widen(vu[k], h);
+                    store(sV + st * C::kTile, k, h);
+                    vu[k] = fetch(v_own, next, k);
+                }
+            } else {
+                uint32_t numbers = 0xffffffffu;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) e4m3x4_to_half2(w[e], h[2 * e], h[2 * e + 1]);
-                if (odd) {
-                    const uint32_t by = __shfl_sync(0xffffffffu, times, (i + 128 * k) / kPieces >> 4);
+                for (int k = 0; k < kPieces; ++k) {
+                    uint32_t h[8];
+                    widen(vu[k], h);
+                    const uint32_t by = now.times[run + k * (kTokens / 16)];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         h[e] = half2_times(h[e], by);
                         if (partly) {
-                            const uint32_t m = __heq2_mask(*reinterpret_cast<const __half2 *>(&h[e]),
-                                                           *reinterpret_cast<const __half2 *>(&h[e]));
+                            const __half2 x = *reinterpret_cast<const __half2 *>(&h[e]);
+                            const uint32_t m = __heq2_mask(x, x);
                             numbers &= m;
                             h[e] &= m;
                         }
                     }
+                    store(sV + st * C::kTile, k, h);
+                    vu[k] = fetch(v_own, next, k);
                 }
-                store(sV + st * C::kTile, k, h);
-                u[k] = fetch(a.cache.k, g + 1, pg_next, k);
+                if (numbers != 0xffffffffu) *nan_flag = 1;
             }
-            if (numbers != 0xffffffffu) *nan_flag = 1;
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&v_full[st]);
-            pg = pg_next;
-            bytes = bytes_next;
+            if (lane == 0) {
+                mbar_arrive(&v_full[st]);
+                if (g % kGroup == kGroup - 1) mbar_arrive(&i_empty[g / kGroup % kGroups]);
+            }
         }
         // every arrival of the MMAs' completion is in before the CTA leaves
 #pragma unroll 1
@@ -323,8 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
         reg_inc<kSoftmaxRegs>();
         const int q = warp & 3, t = (warp - 8) >> 2, row = q * 32 + lane;
         const uint32_t tl = (uint32_t)(q * 32) << 16;
-        const uint32_t s_addr = tmem + tl + t * 128, o_addr = tmem + tl + C::kColO + t * DH,
-                       p_addr = tmem + tl + C::kColP + t * C::kStepP;
+        const uint32_t s_addr0 = tmem + tl + t * 64 * C::kPlaces, o_addr = tmem + tl + C::kColO + t * DH;
         if (t < tiles) {
             const int r = 128 * t + row;
             const bool real = r < left;
@@ -363,109 +457,148 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                 if (lane == 0) mbar_arrive(&q_full[t]);
             }
 
-            float m_ref = -kInf, l_run = 0.f;
-            // Key tile g.  PARTLY: some row of the warp may not see all of it.
-            auto tile = [&](int g, auto partly_tag) {
+            float ref = -kInf, l_run = 0.f;
+            float peak = 0.f;  // largest sum of a step's weights against the reference
+            constexpr int kBlock = 128 / NB, kBlocks = 64 / kBlock;  // of a step
+            // Weights of a step's scores (of its first `valid` tokens) against the reference, as pairs; adds their sum without value
+            // scales to l, returns the one with them.
+            auto weights = [&](const StepScales<NB> &x, const uint32_t (&sc)[64], int valid, float &l, uint32_t (&pw)[32], auto partly_tag) {
                 constexpr bool kPartly = decltype(partly_tag)::value;
-                if (!wait(&c_full[g % (kStages + 1)], (g / (kStages + 1)) & 1)) return false;
-                if (!wait(&s_full[t], g & 1)) return false;
+                const float base = ref == -kInf ? 0.f : -ref;
+                float total = 0.f;
+#pragma unroll
+                for (int k = 0; k < kBlocks; ++k) {
+                    const float f = factor * x.key[k], at = base + x.value_log2[k];
+                    const f32x2 f2 = {f, f}, at2 = {at, at};
+                    f32x2 s0 = {0.f, 0.f}, s1 = {0.f, 0.f};
+#pragma unroll
+                    for (int c = k * kBlock; c < (k + 1) * kBlock; c += 4) {
+                        const f32x2 x0 = ffma2({__uint_as_float(sc[c]), __uint_as_float(sc[c + 1])}, f2, at2);
+                        const f32x2 x1 = ffma2({__uint_as_float(sc[c + 2]), __uint_as_float(sc[c + 3])}, f2, at2);
+                        f32x2 e0 = {exp2_fast(x0.x), exp2_fast(x0.y)}, e1 = {exp2_fast(x1.x), exp2_fast(x1.y)};
+                        if (kPartly) {
+                            if (c >= valid) e0.x = 0.f;
+                            if (c + 1 >= valid) e0.y = 0.f;
+                            if (c + 2 >= valid) e1.x = 0.f;
+                            if (c + 3 >= valid) e1.y = 0.f;
+                        }
+                        s0 = fadd2(s0, e0);
+                        s1 = fadd2(s1, e1);
+                        pw[c / 2] = pack_half2(e0.x, e0.y);
+                        pw[c / 2 + 1] = pack_half2(e1.x, e1.y);
+                    }
+                    const float sum = (s0.x + s0.y) + (s1.x + s1.y);
+                    l = fmaf(sum, x.value_inverse[k], l);
+                    total += sum;
+                }
+                return total;
+            };
+            const uint32_t s_bars = smem_u32(s_full + C::kPlaces * t), p_bars = smem_u32(p_full + C::kPlaces * t);
+            auto product_done = [&](int j) {  // P V of step j
+                return wait(&pv_done[C::kPlaces * t + j % C::kPlaces], (j / C::kPlaces) & 1);
+            };
+            StepScales<NB> x = {};  // of the step
+            bool early = false;  // its S_t is known to be written
+            // Step j, in place i (phase `phase`) of S and P.  Careful: with its maximum (of the tokens that the row sees): the first step,
+            // those seen in part, and those whose weights ran away from the reference; O_t and l are rescaled where it is taken
+            // anew.  Plain ones take the reference as it stands; where the sum of weights says that one may have left its
+            // range they return 0, and the step is done again, carefully (1: done, -1: the kernel is aborting).  What the next step
+            // begins with (whether its S_t is written, its scales) is asked for under this one's exponents: a warp's own
+            // latencies are what bounds it.
+            auto step = [&](int j, int i, uint32_t phase, const StepScales<NB> &next, auto careful_tag) {
+                constexpr bool kCareful = decltype(careful_tag)::value;
+                if (__builtin_expect(!early && !warp_wait_addr(s_bars + 8 * i, phase, abort_flag, a.err), 0)) return -1;
                 tc_fence_after();
-                float sv[128];
-                {
-                    uint32_t w[4][32];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, w[c]);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int c = 0; c < 128; ++c) sv[c] = __uint_as_float(w[c / 32][c % 32]);
-                }
-                if (!C::kAlias) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&s_free[t]);
-                }
-                const TileScales &sc = scales[g % (kStages + 1)];
-                const int valid = sees - (g_begin + g) * 128;  // tokens of the tile that the row sees
-                float mx = -kInf;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (kPartly) {
-#pragma unroll
-                        for (int c = 16 * k; c < 16 * k + 16; ++c)
-                            if (c >= valid) sv[c] = -kInf;
+                const uint32_t cols = s_addr0 + 64 * i;
+                uint32_t sc[64], pw[32];
+                tmem_ld32(cols, reinterpret_cast<uint32_t (&)[32]>(sc));
+                tmem_ld32(cols + 32, reinterpret_cast<uint32_t (&)[32]>(sc[32]));
+                const bool last = i + 1 == C::kPlaces;
+                const bool ready = mbar_test_addr(s_bars + (last ? 0 : 8 * i + 8), last ? phase ^ 1 : phase);
+                const StepScales<NB> now = x;
+                x = next;
+                tmem_wait_ld();
+                float l = l_run;
+                if (!kCareful) {
+                    const float total = weights(now, sc, 64, l, pw, std::false_type());
+                    if (__builtin_expect(__any_sync(0xffffffffu, total > kMostSum), 0)) {
+                        x = now;
+                        early = true;
+                        return 0;
                     }
-                    float top = fmax3(sv[16 * k], sv[16 * k + 1], sv[16 * k + 2]);
+                    peak = fmaxf(peak, total);
+                } else {
+                    const int valid = sees - (2 * g_begin + j) * 64;
+                    float mx = -kInf;
 #pragma unroll
-                    for (int c = 16 * k + 3; c < 16 * k + 15; c += 2) top = fmax3(top, sv[c], sv[c + 1]);
-                    top = fmaxf(top, sv[16 * k + 15]);
-                    const float x = fmaf(top, factor * sc.key[k], sc.value_log2[k]);
-                    mx = fmaxf(mx, kPartly && top == -kInf ? -kInf : x);
-                }
-                if (!C::kAlias && g > 0) {
-                    if (!wait(&pv_done[t], (g - 1) & 1)) return false;  // P_t and O_t are free
-                    tc_fence_after();
-                }
-                if (__any_sync(0xffffffffu, mx > m_ref + kLazy)) {
-                    const float to = fmaxf(m_ref, mx);
-                    const float by = m_ref == -kInf ? 0.f : exp2_fast(m_ref - to);
-                    m_ref = to;
-                    l_run *= by;
-                    if (g > 0) {
+                    for (int k = 0; k < kBlocks; ++k) {
+                        float most = -kInf;
+#pragma unroll
+                        for (int c = k * kBlock; c < (k + 1) * kBlock; c += 2)
+                            most = fmax3(most, c < valid ? __uint_as_float(sc[c]) : -kInf, c + 1 < valid ? __uint_as_float(sc[c + 1]) : -kInf);
+                        const float y = fmaf(most, factor * now.key[k], now.value_log2[k]);
+                        mx = fmaxf(mx, most == -kInf ? -kInf : y);
+                    }
+                    if (__any_sync(0xffffffffu, mx > ref + (kTop + 1.f))) {
+                        // (all rows of the warp, by what they have seen: the next one will be long in coming)
+                        const float seen = fmaxf(ref, ref + __log2f(peak) - (kTop + 3.f));
+                        const float to = fmaxf(seen, mx - kTop);
+                        const float by = ref == -kInf ? 0.f : exp2_fast(ref - to);
+                        ref = to;
+                        l_run *= by;
+                        peak *= by;
+                        if (j > 0) {
+                            if (!product_done(j - 1)) return -1;
+                            tc_fence_after();
 #pragma unroll 1
-                        for (int d = 0; d < DH; d += 16) {
-                            uint32_t w[16];
-                            tmem_ld16(o_addr + d, w);
-                            tmem_wait_ld();
+                            for (int d = 0; d < DH; d += 16) {
+                                uint32_t w[16];
+                                tmem_ld16(o_addr + d, w);
+                                tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * by);
-                            tmem_st16(o_addr + d, w);
-                        }
-                    }
-                }
-                const float base = kWeightShift - (m_ref == -kInf ? 0.f : m_ref);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t pw[32];
-#pragma unroll
-                    for (int k = 4 * h; k < 4 * h + 4; ++k) {
-                        const float f = factor * sc.key[k], at = base + sc.value_log2[k];
-                        const f32x2 f2 = {f, f}, at2 = {at, at};
-                        f32x2 s0 = {0.f, 0.f}, s1 = {0.f, 0.f};
-#pragma unroll
-                        for (int c = 16 * k; c < 16 * k + 16; c += 4) {
-                            const f32x2 x0 = ffma2({sv[c], sv[c + 1]}, f2, at2), x1 = ffma2({sv[c + 2], sv[c + 3]}, f2, at2);
-                            f32x2 e0 = {exp2_fast(x0.x), exp2_fast(x0.y)}, e1 = {exp2_fast(x1.x), exp2_fast(x1.y)};
-                            if (kPartly) {
-                                if (c >= valid) e0.x = 0.f;
-                                if (c + 1 >= valid) e0.y = 0.f;
-                                if (c + 2 >= valid) e1.x = 0.f;
-                                if (c + 3 >= valid) e1.y = 0.f;
+                                for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * by);
+                                tmem_st16(o_addr + d, w);
                             }
-                            s0 = fadd2(s0, e0);
-                            s1 = fadd2(s1, e1);
-                            pw[c / 2 - 32 * h] = pack_half2(e0.x, e0.y);
-                            pw[c / 2 + 1 - 32 * h] = pack_half2(e1.x, e1.y);
                         }
-                        l_run = fmaf((s0.x + s0.y) + (s1.x + s1.y), sc.value_inverse[k], l_run);
                     }
-                    tmem_st32(p_addr + 32 * h, pw);
+                    l = l_run;
+                    weights(now, sc, valid, l, pw, std::true_type());
                 }
+                l_run = l;
+                tmem_st32(cols, pw);
+                early = warp_all(ready);
                 tmem_wait_st();
                 tc_fence_before();  // P (and a rescaled O) written before P V may start
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[t]);
-                return true;
+                mbar_arrive_if(p_bars + 8 * i, lane == 0);
+                return 1;
             };
-            const int whole = max(0, min(n_tiles, least / 128 - g_begin));  // tiles that every row sees
-            bool ok = true;
-            int g = 0;
+            const int whole = max(0, min(n_steps, least / 64 - 2 * g_begin));  // steps that every row sees
+            bool ok = true, again = true;
+            int j = 0;
+            int place = 0, left_in_group = 0;
+            uint32_t phase = 0;
 #pragma unroll 1
-            for (; ok && g < whole; ++g) ok = tile(g, std::false_type());
-#pragma unroll 1
-            for (; ok && g < n_tiles; ++g) ok = tile(g, std::true_type());
-            if (ok && n_tiles > 0) {
+            while (ok && j < n_steps) {
+                if (left_in_group == 0) {
+                    const int group = j / kGroupSteps;
+                    if (!(ok = wait(&i_full[group % kGroups], (group / kGroups) & 1))) break;
+                    left_in_group = kGroupSteps;
+                    x = infos[group % kGroups * kGroup].scales[0];
+                }
+                const int n = j + 1 - (left_in_group == 1);  // the next step, if of this group
+                const StepScales<NB> &next = infos[(n >> 1) % (kGroup * kGroups)].scales[n & 1];
+                const int r = again || j >= whole ? step(j, place, phase, next, std::true_type()) : step(j, place, phase, next, std::false_type());
+                again = r == 0;
+                ok = r >= 0;
+                if (r != 1) continue;
+                if (--left_in_group == 0) mbar_arrive_if(smem_u32(&i_empty[j / kGroupSteps % kGroups]), lane == 0);
+                if (++place == C::kPlaces) place = 0, phase ^= 1;
+                ++j;
+            }
+            if (ok && n_steps > 0) {
                 // (v_full: nan_flag is what the converting warps left)
-                ok = wait(&pv_done[t], (n_tiles - 1) & 1) && wait(&v_full[(n_tiles - 1) % kStages], ((n_tiles - 1) / kStages) & 1);
+                ok = product_done(n_steps - 1) && wait(&v_full[(n_tiles - 1) % kStages], ((n_tiles - 1) / kStages) & 1);
                 tc_fence_after();
             }
             if (ok) {
@@ -489,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                         // NaN values of the tiles that are seen in part
                         const int stop = min(sees, g_end * 128);
 #pragma unroll 1
-                        for (int x = (g_begin + whole) * 128; x < stop; ++x) {
+                        for (int x = max(g_begin * 128, least / 128 * 128); x < stop; ++x) {
                             const int p = kv_page(a.batch, a.cache, b, x >> page_log2, a.err);
                             if (p < 0) continue;
                             const uint8_t *v = a.cache.v + (int64_t)p * a.cache.page_stride +
@@ -520,10 +653,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                 }
                 if (real) {
                     if (a.splits == 1) {
-                        if (a.lse) a.lse[at] = log_sum(m_ref, l_run);
+                        if (a.lse) a.lse[at] = log_sum(ref, l_run);
                     } else {
                         float2 *ml = reinterpret_cast<float2 *>(a.part + (int64_t)a.splits * a.batch.rows * a.heads * DH);
-                        ml[(int64_t)split * a.batch.rows * a.heads + at] = make_float2(m_ref, l_run);
+                        ml[(int64_t)split * a.batch.rows * a.heads + at] = make_float2(ref, l_run);
                     }
                 }
                 tc_fence_before();
@@ -544,18 +677,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
     }
 }
 
-template <int DH>
-cudaError_t launch_dh(const KvAttnArgs &args, cudaStream_t s)
+template <int DH, int NB>
+cudaError_t launch_one(const KvAttnArgs &args, cudaStream_t s)
 {
     KvAttnArgs a = args;
     a.row_blocks = (int)(((int64_t)a.batch.max_rows * a.group + 255) / 256);
     const int64_t ctas = (int64_t)a.splits * a.row_blocks * a.cache.heads * a.batch.batch;
     if (ctas > INT32_MAX) return cudaErrorInvalidValue;
     static std::atomic<uint64_t> devices{0};
-    cudaError_t e = ask_smem(k_kv_attn<DH>, (int)Cfg<DH>::kSmem, devices);
+    cudaError_t e = ask_smem(k_kv_attn<DH, NB>, (int)Cfg<DH, NB>::kSmem, devices);
     if (e != cudaSuccess) return e;
-    e = launch_k(k_kv_attn<DH>, dim3((unsigned)ctas), dim3(kThreads), Cfg<DH>::kSmem, s, a);
+    e = launch_k(k_kv_attn<DH, NB>, dim3((unsigned)ctas), dim3(kThreads), Cfg<DH, NB>::kSmem, s, a);
     return e != cudaSuccess || a.splits == 1 ? e : launch_kv_join(a, s);
+}
+
+template <int DH>
+cudaError_t launch_dh(const KvAttnArgs &a, cudaStream_t s)
+{
+    return a.cache.page >= 64 ? launch_one<DH, 2>(a, s) : launch_one<DH, 8>(a, s);
 }
 
 }  // namespace

@@ -18,6 +18,9 @@ namespace {
 
 constexpr int kWarps = 4, kChunk = 32;
 constexpr float kInf = __builtin_huge_valf();
+// A row's largest weight is 2^kTop where its reference was taken, and up to 2^kLazy more before it is taken anew:
+// below 2^16, with 2^-29 of it at fp16's full precision and 2^-39 at all.
+constexpr float kTop = 11.f, kLazy = 4.f;
 
 template <int DH>
 struct FewCfg {
@@ -271,14 +274,14 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
                 t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
                 t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
                 top[m][r] = t;
-                raise |= t > ref[m][r] + kLazy;
+                raise |= t > ref[m][r] + (kTop + kLazy);
             }
         if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const float to = fmaxf(ref[m][r], top[m][r]);
+                    const float to = fmaxf(ref[m][r], top[m][r] - kTop);
                     const float by = ref[m][r] == -kInf ? 0.f : exp2_fast(ref[m][r] - to);
                     ref[m][r] = to;
                     sum[m][r] *= by;
@@ -294,7 +297,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                const float base = kWeightShift - (ref[m][r] == -kInf ? 0.f : ref[m][r]);
+                const float base = ref[m][r] == -kInf ? 0.f : -ref[m][r];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     float p[4];

@@ -84,12 +84,11 @@ F3DC_DEV uint32_t pack_half2(float lo, float hi)
 }
 
 // ---- Softmax with value scales.  With s = scale q . k in log2, the weight of a token in a page of value
-// scale 2^e is kept as w = 2^(s + e - m + kWeightShift), so the product with the page's bytes needs no scale
-// of its own and w <= 2^15 where m is at most kLazy below the largest s + e; fp16 then holds weights down to
-// 2^-29 of a row's largest at full precision and to 2^-39 at all.  The sum of weights takes them without
-// their value scales, w 2^-e.  A value scale below 2^kLeastScale counts as 2^kLeastScale with values of zero
-// (they are below 2^-55): without that bound the blocks of zeros, whose scale is 2^-127, would take the sums out of fp32's range.
-constexpr float kWeightShift = 11.f, kLazy = 4.f;
+// scale 2^e is kept as w = 2^(s + e - r), so the product with the page's bytes needs no scale of its own; the
+// reference r of a row is such that w < 2^16, fp16's range, with the row's largest s + e some binades above r, so that fp16 holds
+// weights far below the largest.  The sum of weights takes them without their value scales, w 2^-e.  A value
+// scale below 2^kLeastScale counts as 2^kLeastScale with values of zero (they are below 2^-55): without that
+// bound the blocks of zeros, whose scale is 2^-127, would take the sums out of fp32's range.
 constexpr int kLeastScale = -64;
 
 struct ValueScale {
@@ -117,6 +116,6 @@ F3DC_DEV int query_exponent(float top)
 }
 
 // ln of the sum of exp from a reference and a sum of weights; no token: -infinity
-F3DC_DEV float log_sum(float m, float l) { return l == 0.f ? __int_as_float(0xFF800000) : (m - kWeightShift + log2f(l)) * 0.6931471805599453f; }
+F3DC_DEV float log_sum(float r, float l) { return l == 0.f ? __int_as_float(0xFF800000) : (r + log2f(l)) * 0.6931471805599453f; }
 
 }  // namespace f3dc

@@ -99,7 +99,7 @@ int64_t part_bytes(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads
 int splits(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads, int sms)
 {
     if (empty(t)) return 1;
-    return kv_splits(t->batch, t->max_rows, t->max_length, heads, c->kv_heads, sms);
+    return kv_splits(t->batch, t->max_rows, t->max_length, heads, c->kv_heads, c->dh, sms);
 }
 
 }  // namespace
@@ -220,7 +220,7 @@ extern "C" f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f
     const int group = heads / cache->kv_heads;
     // (blocks of 16 packed rows are the smallest that any kernel makes)
     if (((int64_t)batch->max_rows * group + 15) / 16 > INT32_MAX / ((int64_t)cache->kv_heads * batch->batch) ||
-        (int64_t)batch->max_rows * group > INT32_MAX / 2 || (int64_t)batch->rows * heads > (int64_t)INT32_MAX * 4 ||
+        (int64_t)batch->max_rows * group > INT32_MAX / 2 || (int64_t)batch->rows * heads > INT32_MAX ||
         batch->max_length > INT32_MAX - 1024)
         return bad("the problem is too large");
     int sms = 0;

@@ -25,7 +25,7 @@ constexpr float kTop = 11.f, kLazy = 4.f;
 template <int DH>
 struct FewCfg {
     static constexpr int kHalf = kChunk * DH, kStage = 2 * kHalf;  // bytes: keys, then values
-    static constexpr int kStages = DH == 128 ? 3 : 4;
+    static constexpr int kStages = DH == 128 ? 2 : 3;
     static constexpr int kSmem = kWarps * kStages * kStage;
 };
 
@@ -70,23 +70,29 @@ F3DC_DEV uint32_t half2_times(uint32_t a, uint32_t b)
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+// an 8 x 8 matrix of 16-bit elements, lane (g, q) holding (g, 2 q) and (g, 2 q + 1), transposed
+F3DC_DEV uint32_t transposed(uint32_t a)
+{
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
+    return r;
+}
 // all ones in the halves that are no NaN
 F3DC_DEV uint32_t half2_numbers(uint32_t a)
 {
     return __heq2_mask(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&a));
 }
 
-// MT: tiles of 16 packed rows
-template <int DH, int MT>
+// NT: tiles of 8 packed rows
+template <int DH, int NT>
 __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
 {
     using Cfg = FewCfg<DH>;
-    constexpr int kSteps = DH / 16, kTiles = DH / 8, kVec = DH / 64 > 0 ? DH / 64 : 1;
+    constexpr int kSteps = DH / 16, kRows = 8 * NT;
     constexpr int kStages = Cfg::kStages;
     extern __shared__ uint4 smem4[];
     uint8_t *const smem = reinterpret_cast<uint8_t *>(smem4);
-    __shared__ float sm_m[kWarps][16 * MT], sm_l[kWarps][16 * MT];
-    griddep_launch();
+    __shared__ float sm_m[kWarps][kRows], sm_l[kWarps][kRows];
     griddep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
 
@@ -97,10 +103,10 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
     item /= a.row_blocks;
     const int hk = (int)(item % a.cache.heads), b = (int)(item / a.cache.heads);
     const KvSeq s = kv_seq(a.batch, a.cache, b, a.err);
-    const int r0 = rb * 16 * MT;
+    const int r0 = rb * kRows;
     const int64_t rows = (int64_t)s.n * a.group;  // packed
     if (s.n <= 0 || r0 >= rows) return;
-    const int row_end = (int)min(rows, (int64_t)r0 + 16 * MT);
+    const int row_end = (int)min(rows, (int64_t)r0 + kRows);
 
     // tokens that the last and the first of the rows see
     const int behind = s.length - s.n + 1;
@@ -112,29 +118,39 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
     // ---- this warp's ring
     uint8_t *const ring = smem + warp * kStages * Cfg::kStage;
     const int page = a.cache.page, page_log2 = 31 - __clz(page);
-    int page0 = 0, page1 = 0;  // pages of the next chunk to come
+    // where the next chunk's two runs of 16 tokens lie (-1: nowhere), and their pages
+    int64_t run0 = -1, run1 = -1;
+    int page0 = -1, page1 = -1;
     auto look_up = [&](int c) {
         const int t = c * kChunk;
         if (c >= c_end) return;
         page0 = kv_page(a.batch, a.cache, b, t >> page_log2, a.err);
-        page1 = t + 16 < s.length ? kv_page(a.batch, a.cache, b, (t + 16) >> page_log2, a.err) : page0;
+        page1 = t + 16 < s.length ? kv_page(a.batch, a.cache, b, (t + 16) >> page_log2, a.err) : -1;
+        run0 = page0 < 0 ? -1 : (int64_t)page0 * a.cache.page_stride + (int64_t)(hk * page + (t & (page - 1))) * DH;
+        run1 = page1 < 0 ? -1 : (int64_t)page1 * a.cache.page_stride + (int64_t)(hk * page + ((t + 16) & (page - 1))) * DH;
     };
-    // loads of chunk c; returns its scale byte of lane's kind: keys / values, first / second page
+    // loads of chunk c; returns its scale byte of lane's kind: keys / values, first / second run
     auto load = [&](int c, int slot) {
         uint32_t scale = 127u;
         if (c < c_end) {
             const uint32_t dst = smem_u32(ring + slot * Cfg::kStage);
             const int t0 = c * kChunk;
+            const bool whole = t0 + kChunk <= s.length && run0 >= 0 && run1 >= 0;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
+                // a run's bytes follow one another: piece p is 16 p bytes into it
                 const int p = lane + 32 * i, token = p / kSteps, piece = p % kSteps;
-                const int pg = token < 16 ? page0 : page1;
-                const bool real = t0 + token < s.length && pg >= 0;
-                const int64_t at = real ? (int64_t)pg * a.cache.page_stride +
-                                              ((int64_t)hk * page + ((t0 + token) & (page - 1))) * DH + 16 * piece
-                                        : 0;
-                cp_async16_or_zeros(dst + key_place<DH>(token, piece), a.cache.k + at, real);
-                cp_async16_or_zeros(dst + Cfg::kHalf + value_place<DH>(token, piece), a.cache.v + at, real);
+                const int64_t run = i < kSteps / 2 ? run0 : run1;
+                const int off = 16 * p - (i < kSteps / 2 ? 0 : 16 * DH);
+                if (whole) {
+                    cp_async16(dst + key_place<DH>(token, piece), a.cache.k + run + off);
+                    cp_async16(dst + Cfg::kHalf + value_place<DH>(token, piece), a.cache.v + run + off);
+                } else {
+                    const bool real = t0 + token < s.length && run >= 0;
+                    const int64_t at = real ? run + off : 0;
+                    cp_async16_or_zeros(dst + key_place<DH>(token, piece), a.cache.k + at, real);
+                    cp_async16_or_zeros(dst + Cfg::kHalf + value_place<DH>(token, piece), a.cache.v + at, real);
+                }
             }
             const int pg = lane & 2 ? page1 : page0;
             if (pg >= 0) scale = (lane & 1 ? a.cache.vs : a.cache.ks)[(int64_t)pg * a.cache.scale_stride + hk];
@@ -151,52 +167,51 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
     }
     look_up(c0 + (kStages - 1) * kWarps);
 
-    // ---- queries: fp16 times a power of two for each row; the k of step j are elements 16 q + 4 j .. + 3 of each 64
-    uint32_t qa[MT][kSteps][4];
-    float factor[MT][2];  // of S, in log2
-    int sees[MT][2];      // tokens
+    // ---- queries as the products' columns: fp16 times a power of two for each row; the k of step j are elements 16 q + 4 j
+    // .. + 3 of each 64
+    uint32_t qb[NT][kSteps][2];
+    float factor[NT][2];  // of S, in log2, for rows 2 q and 2 q + 1
+    int sees[NT][2];      // tokens
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int n = 0; n < NT; ++n) {
+        const int at = min(r0 + 8 * n + g, row_end - 1), token = at / a.group, head = hk * a.group + at % a.group;
+        const bf16 *x = a.q + (int64_t)(s.row0 + token) * a.ldq + (int64_t)head * DH;
+        uint32_t w[DH / 8];
+        constexpr int kRun = DH >= 64 ? 16 : 8;  // consecutive elements of a lane
+#pragma unroll
+        for (int j = 0; j < DH / 32; ++j) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(x + (j * 8 / kRun) * 64 + kRun * q + j * 8 % kRun);
+            w[4 * j] = u.x, w[4 * j + 1] = u.y, w[4 * j + 2] = u.z, w[4 * j + 3] = u.w;
+        }
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < DH / 8; ++j)
+            top = fmax3(top, fabsf(__uint_as_float(w[j] << 16)), fabsf(__uint_as_float(w[j] & 0xFFFF0000u)));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int e = query_exponent(top), sight = a.causal ? behind + token : s.length;
+        const float up = pow2(e), down = a.scale_log2 * pow2(-e);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int r = r0 + 16 * m + g + 8 * i, at = min(r, row_end - 1);
-            const int token = at / a.group, head = hk * a.group + at % a.group;
-            sees[m][i] = a.causal ? behind + token : s.length;
-            const bf16 *x = a.q + (int64_t)(s.row0 + token) * a.ldq + (int64_t)head * DH;
-            uint32_t w[DH / 8];
-            constexpr int kRun = DH >= 64 ? 16 : 8;  // consecutive elements of a lane
-#pragma unroll
-            for (int j = 0; j < DH / 32; ++j) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(x + (j * 8 / kRun) * 64 + kRun * q + j * 8 % kRun);
-                w[4 * j] = u.x, w[4 * j + 1] = u.y, w[4 * j + 2] = u.z, w[4 * j + 3] = u.w;
-            }
-            float top = 0.f;
-#pragma unroll
-            for (int j = 0; j < DH / 8; ++j)
-                top = fmax3(top, fabsf(__uint_as_float(w[j] << 16)), fabsf(__uint_as_float(w[j] & 0xFFFF0000u)));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int e = query_exponent(top);
-            const float up = pow2(e);
-            factor[m][i] = a.scale_log2 * pow2(-e);
-#pragma unroll
-            for (int j = 0; j < kSteps; ++j) {
-                qa[m][j][i] = pack_half2(__uint_as_float(w[2 * j] << 16) * up, __uint_as_float(w[2 * j] & 0xFFFF0000u) * up);
-                qa[m][j][2 + i] =
-                    pack_half2(__uint_as_float(w[2 * j + 1] << 16) * up, __uint_as_float(w[2 * j + 1] & 0xFFFF0000u) * up);
-            }
+            factor[n][i] = __shfl_sync(0xffffffffu, down, 4 * (2 * q + i));
+            sees[n][i] = __shfl_sync(0xffffffffu, sight, 4 * (2 * q + i));
         }
+#pragma unroll
+        for (int j = 0; j < 2 * kSteps; ++j)
+            qb[n][j / 2][j % 2] = pack_half2(__uint_as_float(w[j] << 16) * up, __uint_as_float(w[j] & 0xFFFF0000u) * up);
+    }
 
-    float acc[MT][kTiles][4];
-    float ref[MT][2], sum[MT][2];
+    // sums O^T: element (column, row): acc[n][j][e] of column g DH / 8 + 2 j + e / 2 and row 8 n + 2 q + e % 2
+    float acc[NT][kSteps][4];
+    float ref[NT][2], sum[NT][2];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int j = 0; j < kTiles; ++j)
+        for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[m][j][e] = 0.f;
-        ref[m][0] = ref[m][1] = -kInf;
-        sum[m][0] = sum[m][1] = 0.f;
+            for (int e = 0; e < 4; ++e) acc[n][j][e] = 0.f;
+        ref[n][0] = ref[n][1] = -kInf;
+        sum[n][0] = sum[n][1] = 0.f;
     }
 
     int slot = 0;
@@ -215,36 +230,41 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
         slot = slot + 1 == kStages ? 0 : slot + 1;
         const int t0 = c * kChunk;
 
-        float x[MT][4][4];
+        // S^T: 16 tokens by 8 rows each: x[n][h][e] of row 2 q + e % 2 and token 16 h + 8 (e / 2) + 4 (g & 1) + (g >> 1)
+        float x[NT][2][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {  // eight tokens
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[m][i][e] = 0.f;
-            const int row = 8 * i + g;
+                for (int e = 0; e < 4; ++e) x[n][h][e] = 0.f;
 #pragma unroll
-            for (int h = 0; h < kVec; ++h) {
-                uint32_t w[4];
-                if constexpr (DH >= 64) {
-                    const int piece = (4 * h + q) ^ (DH == 128 ? (row & 1) << 2 : 0);
-                    const uint4 u = *reinterpret_cast<const uint4 *>(keys + row * DH + 16 * piece);
-                    w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-                } else {
-                    const uint2 u = *reinterpret_cast<const uint2 *>(keys + row * DH + 8 * q);
-                    w[0] = u.x, w[1] = u.y;
+            for (int v = 0; v < (DH >= 64 ? DH / 64 : 1); ++v) {
+                uint32_t w[2][4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int row = 16 * h + 8 * i + g;
+                    if constexpr (DH >= 64) {
+                        const int piece = (4 * v + q) ^ (DH == 128 ? (row & 1) << 2 : 0);
+                        const uint4 u = *reinterpret_cast<const uint4 *>(keys + row * DH + 16 * piece);
+                        w[i][0] = u.x, w[i][1] = u.y, w[i][2] = u.z, w[i][3] = u.w;
+                    } else {
+                        const uint2 u = *reinterpret_cast<const uint2 *>(keys + row * DH + 8 * q);
+                        w[i][0] = u.x, w[i][1] = u.y;
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < (DH >= 64 ? 4 : 2); ++j) {
-                    uint32_t b0, b1;
-                    e4m3x4_to_half2(w[j], b0, b1);
+                    uint32_t k[4];
+                    e4m3x4_to_half2(w[0][j], k[0], k[2]);
+                    e4m3x4_to_half2(w[1][j], k[1], k[3]);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) mma16816(x[m][i], qa[m][4 * h + j], b0, b1);
+                    for (int n = 0; n < NT; ++n) mma16816(x[n][h], k, qb[n][4 * v + j][0], qb[n][4 * v + j][1]);
                 }
             }
         }
 
-        // scales of the chunk's two halves, scores in log2 with their value scales
+        // scales of the chunk's two runs, scores in log2 with their value scales
         float ks[2];
         ValueScale vs[2];
 #pragma unroll
@@ -253,61 +273,59 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
             vs[h] = value_scale(__shfl_sync(0xffffffffu, scale, 2 * h + 1));
         }
         const bool partly = t0 + kChunk > least;
+        const int own_token = t0 + 4 * (g & 1) + (g >> 1);
         bool raise = false;
-        float top[MT][2];
+        float top[NT][2];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                const float f[2] = {factor[m][r] * ks[0], factor[m][r] * ks[1]};
                 float t = -kInf;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float &y = x[m][i][2 * r + e];
-                        y = fmaf(y, f[i >> 1], vs[i >> 1].log2);
-                        // column 2 q + e of tile i is token 8 i + 4 e + q
-                        if (partly && t0 + 8 * i + 4 * e + q >= sees[m][r]) y = -kInf;
+                    for (int i = 0; i < 2; ++i) {
+                        float &y = x[n][h][2 * i + r];
+                        y = fmaf(y, factor[n][r] * ks[h], vs[h].log2);
+                        if (partly && own_token + 16 * h + 8 * i >= sees[n][r]) y = -kInf;
                         t = fmaxf(t, y);
                     }
-                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
-                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-                top[m][r] = t;
-                raise |= t > ref[m][r] + (kTop + kLazy);
+#pragma unroll
+                for (int o = 4; o < 32; o *= 2) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+                top[n][r] = t;
+                raise |= t > ref[n][r] + (kTop + kLazy);
             }
         if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const float to = fmaxf(ref[m][r], top[m][r] - kTop);
-                    const float by = ref[m][r] == -kInf ? 0.f : exp2_fast(ref[m][r] - to);
-                    ref[m][r] = to;
-                    sum[m][r] *= by;
+                    const float to = fmaxf(ref[n][r], top[n][r] - kTop);
+                    const float by = ref[n][r] == -kInf ? 0.f : exp2_fast(ref[n][r] - to);
+                    ref[n][r] = to;
+                    sum[n][r] *= by;
 #pragma unroll
-                    for (int j = 0; j < kTiles; ++j) {
-                        acc[m][j][2 * r] *= by;
-                        acc[m][j][2 * r + 1] *= by;
+                    for (int j = 0; j < kSteps; ++j) {
+                        acc[n][j][r] *= by;
+                        acc[n][j][2 + r] *= by;
                     }
                 }
         }
-        uint32_t w[MT][2][4];  // weights as operands of the two halves
+        uint32_t w[NT][2][2];  // weights as the second product's columns: tokens along the quad, a row for each g
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 0; n < NT; ++n) {
+            const float base[2] = {ref[n][0] == -kInf ? 0.f : -ref[n][0], ref[n][1] == -kInf ? 0.f : -ref[n][1]};
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const float base = ref[m][r] == -kInf ? 0.f : -ref[m][r];
+            for (int h = 0; h < 2; ++h) {
+                float p[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float p[4];
+                for (int e = 0; e < 4; ++e) p[e] = exp2_fast(x[n][h][e] + base[e & 1]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[e] = exp2_fast(x[m][2 * h + (e >> 1)][2 * r + (e & 1)] + base);
-                    sum[m][r] = fmaf((p[0] + p[1]) + (p[2] + p[3]), vs[h].inverse, sum[m][r]);
-                    w[m][h][r] = pack_half2(p[0], p[1]);
-                    w[m][h][2 + r] = pack_half2(p[2], p[3]);
-                }
+                for (int r = 0; r < 2; ++r) sum[n][r] = fmaf(p[r] + p[2 + r], vs[h].inverse, sum[n][r]);
+                w[n][h][0] = transposed(pack_half2(p[0], p[1]));
+                w[n][h][1] = transposed(pack_half2(p[2], p[3]));
             }
+        }
         const bool odd = partly || vs[0].times != kHalfOnes || vs[1].times != kHalfOnes;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // sixteen tokens
@@ -325,52 +343,64 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
                     v[i][0] = *reinterpret_cast<const uint32_t *>(values + token * DH + 4 * g);
                 }
             }
-            auto operands = [&](int k, uint32_t (&b0)[4], uint32_t (&b1)[4]) {  // tiles 4 k .. 4 k + 3
-                e4m3x4_to_half2(__byte_perm(v[0][k], v[1][k], 0x5140), b0[0], b0[1]);
-                e4m3x4_to_half2(__byte_perm(v[0][k], v[1][k], 0x7362), b0[2], b0[3]);
-                e4m3x4_to_half2(__byte_perm(v[2][k], v[3][k], 0x5140), b1[0], b1[1]);
-                e4m3x4_to_half2(__byte_perm(v[2][k], v[3][k], 0x7362), b1[2], b1[3]);
+            // pairs of tokens of the lane's columns 4 k .. 4 k + 3, two columns to an operand
+            auto operands = [&](int k, uint32_t (&o)[2][4]) {
+                e4m3x4_to_half2(__byte_perm(v[0][k], v[1][k], 0x5140), o[0][0], o[0][1]);
+                e4m3x4_to_half2(__byte_perm(v[0][k], v[1][k], 0x7362), o[1][0], o[1][1]);
+                e4m3x4_to_half2(__byte_perm(v[2][k], v[3][k], 0x5140), o[0][2], o[0][3]);
+                e4m3x4_to_half2(__byte_perm(v[2][k], v[3][k], 0x7362), o[1][2], o[1][3]);
             };
             if (!odd) {
 #pragma unroll
                 for (int k = 0; k < DH / 32; ++k) {
-                    uint32_t b0[4], b1[4];
-                    operands(k, b0, b1);
+                    uint32_t o[2][4];
+                    operands(k, o);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                        for (int m = 0; m < MT; ++m) mma16816(acc[m][4 * k + j], w[m][h], b0[j], b1[j]);
+                        for (int n = 0; n < NT; ++n) mma16816(acc[n][2 * k + j], o[j], w[n][h][0], w[n][h][1]);
                 }
             } else {
                 // A NaN that a row does not see must not meet its weight of zero: NaN count as zeros in the product,
                 // and where there are any, a second one counts for each row those that it sees.
                 const uint32_t times = vs[h].times;
-                uint32_t sight[MT][4];  // 1 for a token that the row sees
+                uint32_t sight[NT][2];  // 1 for a token that the row sees
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int t = t0 + 16 * h + 8 * (e >> 1) + q;
-                        sight[m][e] = (t < sees[m][e & 1] ? 0x3C00u : 0u) | (t + 4 < sees[m][e & 1] ? 0x3C000000u : 0u);
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t m = 0;
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            m |= own_token + 16 * h + 8 * i < sees[n][r] ? 0x3C00u << (16 * r) : 0u;
+                        sight[n][i] = transposed(m);
                     }
 #pragma unroll
                 for (int k = 0; k < DH / 32; ++k) {
-                    uint32_t b0[4], b1[4];
-                    operands(k, b0, b1);
+                    uint32_t o[2][4];
+                    operands(k, o);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        b0[j] = half2_times(b0[j], times), b1[j] = half2_times(b1[j], times);
-                        const uint32_t n0 = half2_numbers(b0[j]), n1 = half2_numbers(b1[j]);
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t numbers[4], all = 0xffffffffu;
 #pragma unroll
-                        for (int m = 0; m < MT; ++m) mma16816(acc[m][4 * k + j], w[m][h], b0[j] & n0, b1[j] & n1);
-                        if (__any_sync(0xffffffffu, (n0 & n1) != 0xffffffffu)) {
+                        for (int e = 0; e < 4; ++e) {
+                            o[j][e] = half2_times(o[j][e], times);
+                            numbers[e] = half2_numbers(o[j][e]);
+                            o[j][e] &= numbers[e];
+                            all &= numbers[e];
+                        }
 #pragma unroll
-                            for (int m = 0; m < MT; ++m) {
+                        for (int n = 0; n < NT; ++n) mma16816(acc[n][2 * k + j], o[j], w[n][h][0], w[n][h][1]);
+                        if (__any_sync(0xffffffffu, all != 0xffffffffu)) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) numbers[e] = ~numbers[e] & kHalfOnes;
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
                                 float count[4] = {0.f, 0.f, 0.f, 0.f};
-                                mma16816(count, sight[m], ~n0 & kHalfOnes, ~n1 & kHalfOnes);
+                                mma16816(count, numbers, sight[n][0], sight[n][1]);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e)
-                                    if (count[e] > 0.f) acc[m][4 * k + j][e] = __int_as_float(0x7FC00000);
+                                    if (count[e] > 0.f) acc[n][2 * k + j][e] = __int_as_float(0x7FC00000);
                             }
                         }
                     }
@@ -379,30 +409,29 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
         }
     }
 
-    // ---- the warps' sums joined
+    // ---- the warps' sums joined.  (Only now may the next kernel's CTAs come: with them in between the launch's own would
+    // not all fit at once, see kv_splits.)
+    griddep_launch();
     cp_async_wait<0>();
     __syncthreads();
-    float *const sums = reinterpret_cast<float *>(smem);  // [warps][16 MT][DH]
+    float *const sums = reinterpret_cast<float *>(smem);  // [warps][rows][DH]
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            float l = sum[m][r];
-            l += __shfl_xor_sync(0xffffffffu, l, 1);
-            l += __shfl_xor_sync(0xffffffffu, l, 2);
-            const int row = 16 * m + g + 8 * r;
-            if (q == 0) {
-                sm_m[warp][row] = ref[m][r];
+            float l = sum[n][r];
+#pragma unroll
+            for (int o = 4; o < 32; o *= 2) l += __shfl_xor_sync(0xffffffffu, l, o);
+            const int row = 8 * n + 2 * q + r;
+            if (g == 0) {
+                sm_m[warp][row] = ref[n][r];
                 sm_l[warp][row] = l;
             }
-            float *o = sums + (warp * 16 * MT + row) * DH + q * (DH / 4);
+            float *o = sums + (warp * kRows + row) * DH + g * (DH / 8);
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int j = 0; j < kTiles; j += 4)
-                    *reinterpret_cast<float4 *>(o + e * kTiles + j) =
-                        make_float4(acc[m][j][2 * r + e], acc[m][j + 1][2 * r + e], acc[m][j + 2][2 * r + e],
-                                    acc[m][j + 3][2 * r + e]);
+            for (int j = 0; j < kSteps; j += 2)
+                *reinterpret_cast<float4 *>(o + 2 * j) =
+                    make_float4(acc[n][j][r], acc[n][j][2 + r], acc[n][j + 1][r], acc[n][j + 1][2 + r]);
         }
     __syncthreads();
     for (int i = threadIdx.x; i < (row_end - r0) * (DH / 8); i += 32 * kWarps) {
@@ -416,7 +445,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
             const float by = sm_m[w][row] == -kInf ? 0.f : exp2_fast(sm_m[w][row] - m);
             // (a NaN sum has no reference of its own)
             l += sm_l[w][row] == 0.f ? 0.f : sm_l[w][row] * by;
-            const float *x = sums + (w * 16 * MT + row) * DH + col;
+            const float *x = sums + (w * kRows + row) * DH + col;
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = fmaf(x[e], by, o[e]);
         }
@@ -444,63 +473,104 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
     }
 }
 
-// Parts of a row and head added up: a warp for each.
+// Parts of a row and head added up, a CTA for each: its warps take the parts in turn, several on their way at
+// once, and their sums are joined in order.
+constexpr int kJoinWarps = 8, kJoinAhead = 4;
 template <int DH>
-__global__ void __launch_bounds__(256) k_kv_join(const KvAttnArgs a)
+__global__ void __launch_bounds__(32 * kJoinWarps) k_kv_join(const KvAttnArgs a)
 {
-    griddep_launch();
+    constexpr int kPer = DH / 32;
+    __shared__ float sm_o[kJoinWarps][DH], sm_m[kJoinWarps], sm_l[kJoinWarps];
     griddep_wait();
-    const int lane = threadIdx.x & 31;
-    const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), per = (int64_t)a.batch.rows * a.heads;
-    if (at >= per) return;
-    const int row = (int)(at / a.heads), head = (int)(at % a.heads);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t at = blockIdx.x, per = (int64_t)a.batch.rows * a.heads;
+    const float2 *const ml = reinterpret_cast<const float2 *>(a.part + a.splits * per * DH) + at;
+    float m = -kInf, l = 0.f, o[kPer] = {};
+#pragma unroll 1
+    for (int i0 = warp; i0 < a.splits; i0 += kJoinWarps * kJoinAhead) {
+        float2 p[kJoinAhead];
+        float v[kJoinAhead][kPer];
+#pragma unroll
+        for (int k = 0; k < kJoinAhead; ++k) {
+            const int i = i0 + k * kJoinWarps;
+            p[k] = make_float2(-kInf, 0.f);
+            if (i < a.splits) p[k] = ml[i * per];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) v[k][e] = i < a.splits ? a.part[(i * per + at) * DH + lane + 32 * e] : 0.f;
+        }
+        float to = m;
+#pragma unroll
+        for (int k = 0; k < kJoinAhead; ++k) to = fmaxf(to, p[k].x);
+        const float by = m == -kInf ? 0.f : exp2_fast(m - to);
+        // (a NaN sum may have no reference of its own)
+        l = l == 0.f ? 0.f : l * by;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] *= by;
+        m = to;
+#pragma unroll
+        for (int k = 0; k < kJoinAhead; ++k) {
+            const float f = p[k].x == -kInf ? 0.f : exp2_fast(p[k].x - to);
+            l += p[k].y == 0.f ? 0.f : p[k].y * f;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) o[e] = fmaf(v[k][e], f, o[e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) sm_o[warp][lane + 32 * e] = o[e];
+    if (lane == 0) sm_m[warp] = m, sm_l[warp] = l;
     // the row's sequence: the last that starts at or before it
+    const int row = (int)(at / a.heads), head = (int)(at % a.heads);
     int lo = 0, hi = a.batch.batch;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         (a.batch.row_start[mid] <= row ? lo : hi) = mid;
     }
     const KvSeq s = kv_seq(a.batch, a.cache, lo, nullptr);
-    if (s.n <= 0 || row < s.row0 || row >= s.row0 + s.n) return;
-    const float2 *ml = reinterpret_cast<const float2 *>(a.part + a.splits * per * DH) + at;
-    float m = -kInf;
-    for (int i = lane; i < a.splits; i += 32) m = fmaxf(m, ml[i * per].x);
+    griddep_launch();
+    __syncthreads();
+    if (s.n <= 0 || row < s.row0 || row >= s.row0 + s.n || threadIdx.x >= DH) return;
+    float top = sm_m[0];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float l = 0.f, o[DH / 32] = {};
-    for (int i = 0; i < a.splits; ++i) {
-        const float2 p = ml[i * per];
-        const float by = p.x == -kInf ? 0.f : exp2_fast(p.x - m);
-        l += p.y == 0.f ? 0.f : p.y * by;
+    for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, sm_m[w]);
+    float total = 0.f, sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < DH / 32; ++e) o[e] = fmaf(a.part[(i * per + at) * DH + lane + 32 * e], by, o[e]);
+    for (int w = 0; w < kJoinWarps; ++w) {
+        const float f = sm_m[w] == -kInf ? 0.f : exp2_fast(sm_m[w] - top);
+        total += sm_l[w] == 0.f ? 0.f : sm_l[w] * f;
+        sum = fmaf(sm_o[w][threadIdx.x], f, sum);
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int e = 0; e < DH / 32; ++e)
-        a.out[(int64_t)row * a.ldo + (int64_t)head * DH + lane + 32 * e] = __float2bfloat16_rn(o[e] * inv);
-    if (a.lse && lane == 0) a.lse[at] = log_sum(m, l);
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    a.out[(int64_t)row * a.ldo + (int64_t)head * DH + threadIdx.x] = __float2bfloat16_rn(sum * inv);
+    if (a.lse && threadIdx.x == 0) a.lse[at] = log_sum(top, total);
 }
 
-template <int DH, int MT>
+template <int DH, int NT>
 cudaError_t launch_few(const KvAttnArgs &args, cudaStream_t s)
 {
     KvAttnArgs a = args;
-    a.row_blocks = (int)(((int64_t)a.batch.max_rows * a.group + 16 * MT - 1) / (16 * MT));
+    a.row_blocks = (int)(((int64_t)a.batch.max_rows * a.group + 8 * NT - 1) / (8 * NT));
     const int64_t ctas = (int64_t)a.splits * a.row_blocks * a.cache.heads * a.batch.batch;
     if (ctas > INT32_MAX) return cudaErrorInvalidValue;
     static std::atomic<uint64_t> devices{0};
-    cudaError_t e = ask_smem(k_kv_few<DH, MT>, FewCfg<DH>::kSmem, devices);
+    cudaError_t e = ask_smem(k_kv_few<DH, NT>, FewCfg<DH>::kSmem, devices);
     if (e != cudaSuccess) return e;
-    e = launch_k(k_kv_few<DH, MT>, dim3((unsigned)ctas), dim3(32 * kWarps), FewCfg<DH>::kSmem, s, a);
+    e = launch_k(k_kv_few<DH, NT>, dim3((unsigned)ctas), dim3(32 * kWarps), FewCfg<DH>::kSmem, s, a);
     return e != cudaSuccess || a.splits == 1 ? e : launch_kv_join(a, s);
+}
+
+template <int DH>
+cudaError_t launch_dh(const KvAttnArgs &a, cudaStream_t s)
+{
+    const int tile = kv_few_rows((int64_t)a.batch.max_rows * a.group, DH);
+    return tile == 8 ? launch_few<DH, 1>(a, s) : (tile == 16 ? launch_few<DH, 2>(a, s) : launch_few<DH, DH == 128 ? 2 : 4>(a, s));
 }
 
 }  // namespace
 
 cudaError_t launch_kv_join(const KvAttnArgs &a, cudaStream_t s)
 {
-    const dim3 grid((unsigned)(((int64_t)a.batch.rows * a.heads + 7) / 8)), block(256);
+    if ((int64_t)a.batch.rows * a.heads > INT32_MAX) return cudaErrorInvalidValue;
+    const dim3 grid((unsigned)(a.batch.rows * a.heads)), block(32 * kJoinWarps);
     switch (a.cache.dh) {
     case 32: return launch_k(k_kv_join<32>, grid, block, 0, s, a);
     case 64: return launch_k(k_kv_join<64>, grid, block, 0, s, a);
@@ -510,11 +580,10 @@ cudaError_t launch_kv_join(const KvAttnArgs &a, cudaStream_t s)
 
 cudaError_t launch_kv_few(const KvAttnArgs &a, cudaStream_t s)
 {
-    const bool two = (int64_t)a.batch.max_rows * a.group > 16;
     switch (a.cache.dh) {
-    case 32: return two ? launch_few<32, 2>(a, s) : launch_few<32, 1>(a, s);
-    case 64: return two ? launch_few<64, 2>(a, s) : launch_few<64, 1>(a, s);
-    case 128: return launch_few<128, 1>(a, s);
+    case 32: return launch_dh<32>(a, s);
+    case 64: return launch_dh<64>(a, s);
+    case 128: return launch_dh<128>(a, s);
     default: return cudaErrorInvalidValue;
     }
 }

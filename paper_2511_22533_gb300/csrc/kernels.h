@@ -495,17 +495,28 @@ cudaError_t launch_kv_attn(const KvAttnArgs &a, cudaStream_t s);  // many
 cudaError_t launch_kv_join(const KvAttnArgs &a, cudaStream_t s);  // adds the parts up (called by both)
 
 // Packed rows from which tensor-memory tiles are taken.
-inline bool kv_many_rows(int max_rows, int heads, int kv_heads) { return (int64_t)max_rows * (heads / kv_heads) > 32; }
+inline bool kv_many_rows(int max_rows, int heads, int kv_heads) { return (int64_t)max_rows * (heads / kv_heads) > 16; }
 
-// CTAs that share a sequence's keys: as many as fill the SMs (twice with few rows), each with at least
-// 512 tokens.
-inline int kv_splits(int batch, int max_rows, int max_length, int heads, int kv_heads, int sms)
+constexpr int kFewLeast = 256, kFewLeastWaves = 2048;
+// Packed rows of a CTA of the few-rows kernel.
+inline int kv_few_rows(int64_t rows, int dh) { return rows <= 8 ? 8 : (rows <= 16 || dh == 128 ? 16 : 32); }
+// How many of them an SM holds (registers, shared memory).
+inline int kv_few_slots(int tile, int dh)
+{
+    return dh == 128 ? (tile == 8 ? 3 : 2) : (dh == 64 ? (tile == 8 ? 4 : (tile == 16 ? 3 : 2)) : (tile == 8 ? 6 : (tile == 16 ? 4 : 3)));
+}
+
+// CTAs that share a sequence's keys.
+inline int kv_splits(int batch, int max_rows, int max_length, int heads, int kv_heads, int dh, int sms)
 {
     const int64_t rows = (int64_t)max_rows * (heads / kv_heads);
     const bool many = kv_many_rows(max_rows, heads, kv_heads);
-    const int64_t blocks = (many ? (rows + 255) / 256 : (rows + 15) / 16) * kv_heads * batch;
-    int64_t n = (many ? 1 : 2) * (int64_t)sms / blocks;
-    if (n > max_length / 512) n = max_length / 512;
+    const int tile = many ? 256 : kv_few_rows(rows, dh);
+    const int64_t blocks = (rows + tile - 1) / tile * kv_heads * batch;
+    const int64_t slots = (many ? 1 : kv_few_slots(tile, dh)) * (int64_t)sms;
+    int64_t n = slots / blocks, least = many ? 512 : kFewLeast;
+    if (!many && n < 3) n = (4 * slots + blocks - 1) / blocks, least = kFewLeastWaves;
+    if (n > max_length / least) n = max_length / least;
     return n < 1 ? 1 : (int)n;
 }
 

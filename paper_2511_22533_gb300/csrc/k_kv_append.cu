@@ -6,10 +6,11 @@
 //   byte = smallest e with max |k'| <= 448 2^e over the page's new tokens, at least the
 //          page's own where it already holds tokens; q = k' 2^-e to nearest even
 //
-// One pass over the rows.  A CTA takes one page of one sequence: it computes the angles'
-// cosines and sines of the page's new tokens once, into shared memory, and uses them for all of
-// its heads; it holds as many heads of the page as fit its threads' registers (a "round"),
-// takes their maxima, and writes them.  An angle is a position times a 64-bit
+// One pass over the rows.  A CTA takes one page of one sequence: it computes the cosines and sines of the
+// page's new tokens once, into shared memory, and uses them for all of its heads.  A head of the page is the
+// work of 1 to 256 threads, two or four units of 16 elements each, in registers; the next head's are on their way
+// meanwhile.  Up to a warp's threads meet in shuffles, more in a barrier
+// of their own, so heads do not wait for one another.  An angle is a position times a 64-bit
 // fraction of a turn, modulo 2^64: exact modulo a turn, so only the last step (top 32 bits to
 // fp32) rounds, to 2^-25 of a turn.
 #include "kv.cuh"
@@ -18,13 +19,8 @@ namespace f3dc {
 
 namespace {
 
-constexpr int kThreads = 256, kUnits = 4;  // a unit: 16 elements of a token and head
-constexpr int kMaxHeads = 256;             // of a round
-
-// The 16 elements of a unit: two 16-byte vectors of bf16.
-struct Unit {
-    uint4 a, b;
-};
+constexpr int kThreads = 256;
+constexpr int kWantedPerSm = 3;            // CTAs
 
 F3DC_DEV void widen(uint4 u, float *f)
 {
@@ -41,13 +37,24 @@ F3DC_DEV uint4 narrow(const float *f)
     return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
 }
 
-// kind of a round: 0 keys, 1 values, 2 queries
-template <int DH>
-__global__ void __launch_bounds__(kThreads) k_kv_append(const KvAppendArgs a)
+// threads that share a head of `units` units, at most `most` each: a power of two
+__host__ __device__ inline int head_threads(int units, int most)
+{
+    int t = 1;
+    while (t < units && t < 32) t *= 2;
+    while (t * most < units) t *= 2;
+    return t;
+}
+// units of a thread, at most: a page's head has up to 1024
+inline int units_of(int page, int dh) { return page * (dh / 16) > 2 * kThreads ? 4 : 2; }
+
+// INTER: pairs are neighbours
+template <int DH, bool INTER, int kUnits>
+__global__ void __launch_bounds__(kThreads, 2) k_kv_append(const KvAppendArgs a)
 {
     constexpr int kPer = DH / 16;  // units of a token and head
     extern __shared__ float angles[];  // cosines, then sines: [tokens][pairs] each
-    __shared__ uint32_t top[kMaxHeads], new_byte[kMaxHeads], old_byte[kMaxHeads];
+    __shared__ float tops[kThreads / 32];
     griddep_launch();
     griddep_wait();
     const int slots = a.slots, b = blockIdx.x / slots, slot = blockIdx.x - b * slots, tid = threadIdx.x;
@@ -65,194 +72,205 @@ __global__ void __launch_bounds__(kThreads) k_kv_append(const KvAppendArgs a)
     const int p = kv_page(a.batch, a.cache, b, j, a.err);
     const int pairs = a.dims / 2, heads_k = a.cache.heads;
 
-    // heads of a round, and rounds of keys (as many of values) and of queries
-    const int per_round = min(kMaxHeads, kThreads * kUnits / (nt * kPer));
-    const int rounds_k = (heads_k + per_round - 1) / per_round;
-    const int rounds_q = a.q ? (a.heads + per_round - 1) / per_round : 0;
-    const int rounds = 2 * rounds_k + rounds_q;
-
     float *const cosines = angles, *const sines = angles + page * pairs;
+    // (a thread's units are of tokens `apart` tokens apart, the same elements of each)
+    const int threads = head_threads(nt * kPer, kUnits), group = tid / threads, own = tid & (threads - 1);
+    const int groups = kThreads / threads, token = own / kPer, apart = threads / kPer, c = own % kPer;
+    const bool rotates = c < a.dims / 16;
+    // The unit's two vectors of 8: one of each half of the elements that turn, or of each half of those that do not, so that
+    // neighbouring threads' vectors lie side by side.
+    const int e0 = rotates ? 8 * c : pairs + 8 * c, e1 = e0 + (rotates ? pairs : DH / 2 - pairs);
+    const float inf = __int_as_float(0x7F800000);
     if (pairs > 0) {
-        const int of_axis = pairs / a.axes;
-        for (int i = tid; i < nt * pairs; i += kThreads) {
-            const int t = i / pairs, pr = i - t * pairs, axis = pr / of_axis;
-            float sn = 0.f, cs = 1.f;
-            if (axis < a.axes) {
-                const int at = a.positions ? a.positions[(int64_t)(row0 + t) * a.axes + axis] : lo + t;
-                const uint64_t turn = (uint64_t)(int64_t)at * a.turns[pr];
-                sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &sn, &cs);
+        // a thread's pair is the same for all of its tokens
+        const int at_once = kThreads / pairs, t0 = tid / pairs, pr = tid - t0 * pairs, axis = pr / (pairs / a.axes);
+        if (t0 < at_once) {
+            const uint64_t turns = axis < a.axes ? a.turns[pr] : 0;
+            for (int t = t0; t < nt; t += at_once) {
+                int at = lo + t;
+                if (a.positions) at = a.positions[(int64_t)(row0 + t) * a.axes + min(axis, a.axes - 1)];
+                const uint64_t turn = (uint64_t)(int64_t)at * turns;
+                sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &sines[t * pairs + pr], &cosines[t * pairs + pr]);
             }
-            cosines[t * pairs + pr] = cs;
-            sines[t * pairs + pr] = sn;
         }
         __syncthreads();
     }
 
-#pragma unroll 1
-    for (int r = blockIdx.y; r < rounds; r += gridDim.y) {
-        const int kind = r < rounds_k ? 0 : (r < 2 * rounds_k ? 1 : 2);
-        if (kind < 2 && p < 0) continue;
-        const int all = kind < 2 ? heads_k : a.heads;
-        const int h0 = (kind == 0 ? r : (kind == 1 ? r - rounds_k : r - 2 * rounds_k)) * per_round;
-        const int nh = min(per_round, all - h0), units = nh * nt * kPer;
-        const bf16 *const src = kind == 0 ? a.k : (kind == 1 ? a.v : a.q);
-        const int64_t ld = kind == 0 ? a.ldk : (kind == 1 ? a.ldv : a.ldq);
-        const int turning = kind == 1 ? 0 : a.dims / 16;  // a token's units that rotate
-
-        // unit i: head, token and first elements of its two vectors
-        auto where = [&](int i, int &head, int &t, int &c, int &e0, int &e1) {
-            c = i % kPer;
-            const int x = i / kPer;
-            head = x / nt;
-            t = x - head * nt;
-            const bool split = c < turning && !a.interleaved;
-            e0 = split ? 8 * c : 16 * c;
-            e1 = split ? pairs + 8 * c : 16 * c + 8;
-        };
-        if (kind < 2) {
-            if (tid < nh) top[tid] = 0u;
-            __syncthreads();
-        }
-        Unit u[kUnits];
+    // The heads of keys, of values and of queries are shared out as one sequence, and done in that order.  (Whole warps go
+    // through them together: a warp's heads are beside one another, the last perhaps not there.)
+    const int own_item = blockIdx.y * groups + tid / threads, warp_item = threads < 32 ? blockIdx.y * groups + (tid & ~31) / threads : own_item;
+    const int beside = own_item - warp_item, step = gridDim.y * groups;
+    auto heads = [&](auto kind_tag, const bf16 *rows, int64_t ld, int begin, int count, uint8_t *pool, uint8_t *scales) {
+        constexpr int kKind = decltype(kind_tag)::value;  // 0 keys, 1 values, 2 queries
+        if (kKind < 2 && p < 0) return;
+        // the warp's first item of this kind: the last of its items may be the first of the next kind's
+        int first = warp_item;
+        if (first + 31 / min(threads, 32) < begin) first += (begin - first - 31 / min(threads, 32) + step - 1) / step * step;
+        const bf16 *src = rows + (int64_t)(row0 + token) * ld + (int64_t)(first + beside - begin) * DH;
+        const int64_t src_step = (int64_t)step * DH, unit_step = (int64_t)apart * ld;
+        uint4 u[kUnits][2];
+        auto fetch = [&](const bf16 *from, int head) {
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-            const int i = tid + k * kThreads;
-            u[k].a = u[k].b = make_uint4(0u, 0u, 0u, 0u);
-            if (i < units) {
-                int head, t, c, e0, e1;
-                where(i, head, t, c, e0, e1);
-                const bf16 *x = src + (int64_t)(row0 + t) * ld + (h0 + head) * DH;
-                u[k].a = *reinterpret_cast<const uint4 *>(x + e0);
-                u[k].b = *reinterpret_cast<const uint4 *>(x + e1);
+            for (int k = 0; k < kUnits; ++k) {
+                u[k][0] = u[k][1] = make_uint4(0u, 0u, 0u, 0u);
+                if ((uint32_t)head < (uint32_t)count && token + k * apart < nt) {
+                    u[k][0] = *reinterpret_cast<const uint4 *>(from + k * unit_step + e0);
+                    u[k][1] = *reinterpret_cast<const uint4 *>(from + k * unit_step + e1);
+                }
             }
-        }
-        float f[kUnits][16];
+        };
+        fetch(src, first + beside - begin);
+#pragma unroll 1
+        for (; first < begin + count; first += step) {
+            const int head = first + beside - begin;
+            const bool live = (uint32_t)head < (uint32_t)count;
+            uint8_t *const scale = scales + head;
+            uint32_t old = 0;
+            if (kKind < 2 && live && place0 > 0) old = *scale;  // the page goes on
+            float f[kUnits][16];
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-            const int i = tid + k * kThreads;
-            widen(u[k].a, f[k]);
-            widen(u[k].b, f[k] + 8);
-            int head = 0, t, c, e0, e1;
-            if (i < units) {
-                where(i, head, t, c, e0, e1);
-                if (c < turning) {
-                    const float *cs = cosines + t * pairs + 8 * c, *sn = sines + t * pairs + 8 * c;
+            for (int k = 0; k < kUnits; ++k) {
+                widen(u[k][0], f[k]);
+                widen(u[k][1], f[k] + 8);
+            }
+            src += src_step;
+            fetch(src, head + step);  // the next head's
+            if (kKind != 1 && rotates) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (a.interleaved) {
-                            const float p0 = f[k][2 * e], p1 = f[k][2 * e + 1];
-                            f[k][2 * e] = p0 * cs[e] - p1 * sn[e];
-                            f[k][2 * e + 1] = p1 * cs[e] + p0 * sn[e];
+                for (int k = 0; k < kUnits; ++k) {
+                    const int at = min(token + k * apart, nt - 1) * pairs;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        // four pairs: neighbours in vector h, or elements 4 h .. of both vectors
+                        const int pr = INTER ? (h ? e1 : e0) / 2 : 8 * c + 4 * h;
+                        const float4 c4 = *reinterpret_cast<const float4 *>(cosines + at + pr);
+                        const float4 s4 = *reinterpret_cast<const float4 *>(sines + at + pr);
+                        const float co[4] = {c4.x, c4.y, c4.z, c4.w}, si[4] = {s4.x, s4.y, s4.z, s4.w};
+                        if constexpr (INTER) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float &x = f[k][8 * h + 2 * e], &y = f[k][8 * h + 2 * e + 1];
+                                const float p0 = x, p1 = y;
+                                x = p0 * co[e] - p1 * si[e];
+                                y = p1 * co[e] + p0 * si[e];
+                            }
                         } else {
-                            const float p0 = f[k][e], p1 = f[k][8 + e];
-                            f[k][e] = p0 * cs[e] - p1 * sn[e];
-                            f[k][8 + e] = p1 * cs[e] + p0 * sn[e];
+#pragma unroll
+                            for (int e = 0; e < 4; e += 2) {
+                                float *const x = f[k] + 4 * h + e;
+                                const f32x2 p0 = {x[0], x[1]}, p1 = {x[8], x[9]}, c2 = {co[e], co[e + 1]}, s2 = {si[e], si[e + 1]};
+                                const f32x2 a2 = fmul2(p1, s2), b2 = fmul2(p0, s2);
+                                const f32x2 r0 = ffma2(p0, c2, {-a2.x, -a2.y}), r1 = ffma2(p1, c2, b2);
+                                x[0] = r0.x, x[1] = r0.y, x[8] = r1.x, x[9] = r1.y;
+                            }
                         }
                     }
                 }
             }
-            if (kind < 2) {
-                // the unit's largest finite magnitude; an infinity becomes NaN, which fmaxf passes over
-                const float inf = __int_as_float(0x7F800000);
-                float m = 0.f;
+            if constexpr (kKind == 2) {
+                if (!live) continue;
+                bf16 *const dst = a.q_out + (int64_t)(row0 + token) * a.ldqo + (int64_t)head * DH;
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) m = fmax3(m, fabsf(f[k][e]), fabsf(f[k][e + 1]));
-                if (m == inf) {
-                    m = 0.f;
+                for (int k = 0; k < kUnits; ++k) {
+                    if (token + k * apart >= nt) continue;
+                    bf16 *y = dst + (int64_t)(k * apart) * a.ldqo;
+                    *reinterpret_cast<uint4 *>(y + e0) = narrow(f[k]);
+                    *reinterpret_cast<uint4 *>(y + e1) = narrow(f[k] + 8);
+                }
+            } else {
+                // The largest finite magnitude.  fmaxf passes over NaN, so the plain maximum is infinite only with an infinity
+                // among the values: the rare unit that has one makes NaN of it (e4m3 has no infinity) and takes the maximum of
+                // the others.
+                float top = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        if (fabsf(f[k][e]) == inf) f[k][e] = __int_as_float(0x7FC00000);
-                        m = fmaxf(m, fabsf(f[k][e]));
+                for (int k = 0; k < kUnits; ++k) {
+                    float m = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) m = fmax3(m, fabsf(f[k][e]), fabsf(f[k][e + 1]));
+                    if (m == inf) {
+                        m = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if (fabsf(f[k][e]) == inf) f[k][e] = __int_as_float(0x7FC00000);
+                            m = fmaxf(m, fabsf(f[k][e]));
+                        }
+                    }
+                    top = fmaxf(top, m);
+                }
+                if (threads >= 32) {
+                    // (magnitudes order as their bits do)
+                    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+                } else {
+                    for (int o = threads / 2; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                }
+                if (threads > 32) {
+                    if ((tid & 31) == 0) tops[tid >> 5] = top;
+                    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(threads) : "memory");
+                    const int w0 = group * (threads >> 5);
+                    for (int w = 0; w < threads >> 5; ++w) top = fmaxf(top, tops[w0 + w]);
+                }
+                const uint32_t byte = max(e8m0_byte(top), old);
+                if (live) {
+                    uint8_t *const block = pool + (int64_t)head * page * DH;
+                    // tokens of the page that a larger scale rounds anew
+                    if (place0 > 0 && byte != old) {
+                        const float by = pow2((int)old - (int)byte);
+                        for (int i = own; i < place0 * kPer; i += threads) {
+                            uint4 *at = reinterpret_cast<uint4 *>(block) + i;
+                            const uint4 w = *at;
+                            auto moved = [&](uint32_t x) {
+                                uint32_t l, h;
+                                e4m3x4_to_half2(x, l, h);
+                                const float2 g0 = __half22float2(*reinterpret_cast<const __half2 *>(&l));
+                                const float2 g1 = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+                                return pack_e4m3x4(g0.x * by, g0.y * by, g1.x * by, g1.y * by);
+                            };
+                            *at = make_uint4(moved(w.x), moved(w.y), moved(w.z), moved(w.w));
+                        }
+                    }
+                    const float by = pow2(127 - (int)byte);
+                    uint8_t *const dst = block + (place0 + token) * DH;
+#pragma unroll
+                    for (int k = 0; k < kUnits; ++k) {
+                        if (token + k * apart >= nt) continue;
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const f32x2 g0 = fmul2({f[k][4 * e], f[k][4 * e + 1]}, {by, by}), g1 = fmul2({f[k][4 * e + 2], f[k][4 * e + 3]}, {by, by});
+                            w[e] = pack_e4m3x4(g0.x, g0.y, g1.x, g1.y);
+                        }
+                        uint8_t *y = dst + k * apart * DH;
+                        *reinterpret_cast<uint2 *>(y + e0) = make_uint2(w[0], w[1]);
+                        *reinterpret_cast<uint2 *>(y + e1) = make_uint2(w[2], w[3]);
                     }
                 }
-                // one atomic a warp where its units are of one head
-                const int h = i < units ? head : -1;
-                const uint32_t bits = __float_as_uint(m);
-                const int h_first = __shfl_sync(0xffffffffu, h, 0);
-                if (__all_sync(0xffffffffu, h == h_first)) {
-                    const uint32_t most = __reduce_max_sync(0xffffffffu, bits);
-                    if (h >= 0 && (tid & 31) == 0) atomicMax(&top[h], most);
-                } else if (h >= 0) {
-                    atomicMax(&top[h], bits);
-                }
+                // all have used the old scale, and the maxima
+                if (threads > 32) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(threads) : "memory");
+                else __syncwarp();
+                if (live && own == 0) *scale = (uint8_t)byte;
             }
         }
-        if (kind == 2) {
-#pragma unroll
-            for (int k = 0; k < kUnits; ++k) {
-                const int i = tid + k * kThreads;
-                if (i >= units) continue;
-                int head, t, c, e0, e1;
-                where(i, head, t, c, e0, e1);
-                bf16 *y = a.q_out + (int64_t)(row0 + t) * a.ldqo + (h0 + head) * DH;
-                *reinterpret_cast<uint4 *>(y + e0) = narrow(f[k]);
-                *reinterpret_cast<uint4 *>(y + e1) = narrow(f[k] + 8);
-            }
-            continue;
-        }
-        uint8_t *const scales = (kind == 0 ? a.cache.ks : a.cache.vs) + (int64_t)p * a.cache.scale_stride + h0;
-        uint8_t *const pool = (kind == 0 ? a.cache.k : a.cache.v) + (int64_t)p * a.cache.page_stride +
-                              (int64_t)h0 * page * DH;
-        __syncthreads();
-        if (tid < nh) {
-            uint32_t byte = e8m0_byte(__uint_as_float(top[tid])), old = byte;
-            if (place0 > 0) {  // the page goes on
-                old = scales[tid];
-                byte = max(byte, old);
-            }
-            old_byte[tid] = old;
-            new_byte[tid] = byte;
-            scales[tid] = (uint8_t)byte;
-        }
-        __syncthreads();
-        // tokens that a larger scale rounds anew
-        if (place0 > 0) {
-            for (int i = tid; i < nh * place0 * kPer; i += kThreads) {
-                const int head = i / (place0 * kPer);
-                const int down = (int)new_byte[head] - (int)old_byte[head];
-                if (down == 0) continue;
-                uint4 *at = reinterpret_cast<uint4 *>(pool + (int64_t)head * page * DH) + (i - head * place0 * kPer);
-                const uint4 w = *at;
-                const float by = pow2(-down);
-                auto moved = [&](uint32_t x) {
-                    uint32_t l, h;
-                    e4m3x4_to_half2(x, l, h);
-                    const float2 g0 = __half22float2(*reinterpret_cast<const __half2 *>(&l));
-                    const float2 g1 = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-                    return pack_e4m3x4(g0.x * by, g0.y * by, g1.x * by, g1.y * by);
-                };
-                *at = make_uint4(moved(w.x), moved(w.y), moved(w.z), moved(w.w));
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-            const int i = tid + k * kThreads;
-            if (i >= units) continue;
-            int head, t, c, e0, e1;
-            where(i, head, t, c, e0, e1);
-            const float by = pow2(127 - (int)new_byte[head]);
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                w[e] = pack_e4m3x4(f[k][4 * e] * by, f[k][4 * e + 1] * by, f[k][4 * e + 2] * by, f[k][4 * e + 3] * by);
-            uint8_t *y = pool + ((int64_t)head * page + place0 + t) * DH;
-            if (e1 == e0 + 8) {
-                *reinterpret_cast<uint4 *>(y + e0) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-                *reinterpret_cast<uint2 *>(y + e0) = make_uint2(w[0], w[1]);
-                *reinterpret_cast<uint2 *>(y + e1) = make_uint2(w[2], w[3]);
-            }
-        }
-        __syncthreads();  // top, new_byte: the next round's
-    }
+    };
+    const int64_t page_at = (int64_t)p * a.cache.page_stride, scale_at = (int64_t)p * a.cache.scale_stride;
+    heads(std::integral_constant<int, 0>(), a.k, a.ldk, 0, heads_k, a.cache.k + page_at, a.cache.ks + scale_at);
+    heads(std::integral_constant<int, 1>(), a.v, a.ldv, heads_k, heads_k, a.cache.v + page_at, a.cache.vs + scale_at);
+    if (a.q) heads(std::integral_constant<int, 2>(), a.q, a.ldq, 2 * heads_k, a.heads, nullptr, nullptr);
+}
+
+template <int DH, bool INTER, int U>
+cudaError_t launch_one(const KvAppendArgs &a, dim3 grid, size_t smem, cudaStream_t s)
+{
+    static std::atomic<uint64_t> devices{0};
+    const cudaError_t e = ask_smem(k_kv_append<DH, INTER, U>, 128 * DH * sizeof(float), devices);
+    return e == cudaSuccess ? launch_k(k_kv_append<DH, INTER, U>, grid, dim3(kThreads), smem, s, a) : e;
 }
 
 template <int DH>
 cudaError_t launch_dh(const KvAppendArgs &a, dim3 grid, size_t smem, cudaStream_t s)
 {
-    static std::atomic<uint64_t> devices{0};
-    const cudaError_t e = ask_smem(k_kv_append<DH>, 128 * DH * sizeof(float), devices);
-    return e == cudaSuccess ? launch_k(k_kv_append<DH>, grid, dim3(kThreads), smem, s, a) : e;
+    if (DH == 128 && units_of(a.cache.page, DH) == 4)
+        return a.interleaved ? launch_one<128, true, 4>(a, grid, smem, s) : launch_one<128, false, 4>(a, grid, smem, s);
+    return a.interleaved ? launch_one<DH, true, 2>(a, grid, smem, s) : launch_one<DH, false, 2>(a, grid, smem, s);
 }
 
 }  // namespace
@@ -265,12 +283,11 @@ cudaError_t launch_kv_append(const KvAppendArgs &args, int num_sms, cudaStream_t
     a.slots = (a.batch.max_rows + page - 2) / page + 1;
     const int64_t ctas = (int64_t)a.slots * a.batch.batch;
     if (ctas > INT32_MAX) return cudaErrorInvalidValue;
-    // rounds of a full page
-    const int tokens = a.batch.max_rows < page ? a.batch.max_rows : page, per = kThreads * kUnits / (tokens * (a.cache.dh / 16));
-    const int per_round = per < kMaxHeads ? per : kMaxHeads;
-    const int rounds = 2 * ((a.cache.heads + per_round - 1) / per_round) + (a.q ? (a.heads + per_round - 1) / per_round : 0);
-    int64_t split = (4 * (int64_t)num_sms + ctas - 1) / ctas;
-    if (split > rounds) split = rounds;
+    // heads of a page are shared by CTAs where there are few pages
+    const int tokens = a.batch.max_rows < page ? a.batch.max_rows : page;
+    const int groups = kThreads / head_threads(tokens * (a.cache.dh / 16), units_of(page, a.cache.dh)), all = 2 * a.cache.heads + (a.q ? a.heads : 0);
+    int64_t split = (kWantedPerSm * (int64_t)num_sms + ctas - 1) / ctas;
+    if (split > (all + groups - 1) / groups) split = (all + groups - 1) / groups;
     const size_t smem = (size_t)page * a.dims * sizeof(float);
     const dim3 grid((unsigned)ctas, (unsigned)split);
     switch (a.cache.dh) {

@@ -62,7 +62,7 @@ struct Cfg {
     static constexpr uint32_t kAtom = 8 * kRowBytes, kSwz = DH == 32 ? kSwizzle64 : kSwizzle128;
     static constexpr int kStages = DH == 128 ? 2 : 4;
     static constexpr int kPlaces = DH == 128 ? 2 : 3;  // of S and P of a query tile, 64 columns each
-    static constexpr size_t kSmem = 1024 + (size_t)kTile * (2 + 2 * kStages) + kGroups * kGroup * sizeof(TileInfo<NB>) + 512;
+    static constexpr size_t kSmem = 1024 + (size_t)kTile * (2 + 2 * kStages) + kGroups * kGroup * sizeof(TileInfo<NB>) + 576;
     static constexpr uint32_t kColO = 2 * 64 * kPlaces;
     static_assert(kColO + 2 * DH <= 512, "TMEM layout");
     // byte of 16-byte piece `piece` (8 columns) of a row
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
     uint8_t *const smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *const sQ = smem, *const sK = sQ + 2 * C::kTile, *const sV = sK + kStages * C::kTile;
     uint64_t *const bars = reinterpret_cast<uint64_t *>(sV + kStages * C::kTile);
-    TileInfo<NB> *const infos = reinterpret_cast<TileInfo<NB> *>(bars + 64);
+    TileInfo<NB> *const infos = reinterpret_cast<TileInfo<NB> *>(bars + 72);
     // per stage: keys / values written by the four converting warps, and read by both tiles' MMAs
     uint64_t *const k_full = bars, *const v_full = k_full + kStages, *const k_empty = v_full + kStages,
                    *const v_empty = k_empty + kStages;
@@ -141,58 +141,53 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     griddep_launch();
+    if (warp == 0) {
+        tmem_alloc(tmem_holder, 512);
+        tmem_relinquish();
+    }
     griddep_wait();
 
     // ---- this CTA's item; the blocks of rows that see most come first
-    int64_t item = blockIdx.x;
-    const int split = (int)(item % a.splits);
-    item /= a.splits;
-    const int hk = (int)(item % a.cache.heads);
-    item /= a.cache.heads;
-    const int b = (int)(item % a.batch.batch), rb = a.row_blocks - 1 - (int)(item / a.batch.batch);
+    uint32_t item = blockIdx.x;
+    const int split = (int)(item % (uint32_t)a.splits);
+    item /= (uint32_t)a.splits;
+    const int hk = (int)(item % (uint32_t)a.cache.heads);
+    item /= (uint32_t)a.cache.heads;
+    const int b = (int)(item % (uint32_t)a.batch.batch), rb = a.row_blocks - 1 - (int)(item / (uint32_t)a.batch.batch);
     const KvSeq s = kv_seq(a.batch, a.cache, b, a.err);
-    const int64_t rows = (int64_t)s.n * a.group;  // packed
-    const int64_t r0 = (int64_t)rb * 256;
-    if (s.n <= 0 || r0 >= rows) return;  // (before anything that needs an end)
-    const int left = (int)min(rows - r0, (int64_t)256), tiles = left > 128 ? 2 : 1;
+    const int rows = s.n * a.group, r0 = rb * 256;  // packed
+    if (s.n <= 0 || r0 >= rows) {
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        if (warp == 0) tmem_dealloc(*tmem_holder, 512);
+        return;
+    }
+    const int left = min(rows - r0, 256), tiles = left > 128 ? 2 : 1;
     const int behind = s.length - s.n + 1;
     // tokens that the last and the first of the rows see
-    const int most = a.causal ? max(0, behind + (int)((r0 + left - 1) / a.group)) : s.length;
-    const int least = a.causal ? behind + (int)(r0 / a.group) : s.length;
+    const int most = a.causal ? max(0, behind + (r0 + left - 1) / a.group) : s.length;
+    const int least = a.causal ? behind + r0 / a.group : s.length;
     const int all = (most + 127) / 128;
-    const int g_begin = (int)((int64_t)all * split / a.splits), g_end = (int)((int64_t)all * (split + 1) / a.splits);
+    const int g_begin = kv_share(all, split, a.splits), g_end = kv_share(all, split + 1, a.splits);
     const int n_tiles = g_end - g_begin;
     // steps of 64 tokens: two to a tile, of the last one perhaps none sees the second
     const int n_steps = max(0, min(2 * n_tiles, (most + 63) / 64 - 2 * g_begin));
     const int page = a.cache.page, page_log2 = 31 - __clz(page);
 
-    if (threadIdx.x == 0) {
-        for (int st = 0; st < kStages; ++st) {
-            mbar_init(&k_full[st], 4);
-            mbar_init(&v_full[st], 4);
-            mbar_init(&k_empty[st], tiles);
-            mbar_init(&v_empty[st], tiles);
+    if (warp == 1) {
+        // arrivals of each barrier, in the order in which they lie
+        constexpr int kEmpty = 2 * kStages, kInfo = 4 * kStages, kQ = kInfo + 2 * kGroups, kS = kQ + 2, kP = kS + 2 * C::kPlaces,
+                      kDone = kP + 2 * C::kPlaces, kAll = kDone + 2 * C::kPlaces + 1;
+        static_assert(kAll <= 64, "room for barriers");
+        for (int i = lane; i < kAll; i += 32)
+            mbar_init(&bars[i], i < kEmpty ? 4 : (i < kInfo ? tiles : (i < kInfo + kGroups ? 1 : (i < kQ ? 4 + 4 * tiles : (i < kS ? 4 :
+                                (i < kP ? 1 : (i < kDone ? 4 : (i < kAll - 1 ? 1 : 2))))))));
+        if (lane == 0) {
+            *abort_flag = 0;
+            *nan_flag = 0;
         }
-        for (int s = 0; s < kGroups; ++s) {
-            mbar_init(&i_full[s], 1);
-            mbar_init(&i_empty[s], 4 + 4 * tiles);
-        }
-        for (int t = 0; t < 2; ++t) {
-            mbar_init(&q_full[t], 4);
-            for (int i = C::kPlaces * t; i < C::kPlaces * (t + 1); ++i) {
-                mbar_init(&s_full[i], 1);
-                mbar_init(&p_full[i], 4);
-                mbar_init(&pv_done[i], 1);
-            }
-        }
-        mbar_init(drain, 2);
-        *abort_flag = 0;
-        *nan_flag = 0;
         fence_mbar_init();
-    }
-    if (warp == 0) {
-        tmem_alloc(tmem_holder, 512);
-        tmem_relinquish();
     }
     tc_fence_before();
     __syncthreads();
@@ -339,11 +334,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
             *reinterpret_cast<uint4 *>(tile + put1) = make_uint4(h[4], h[5], h[6], h[7]);
         };
         uint4 ku[kPieces], vu[kPieces];
-        if (n_tiles > 0 && wait(&i_full[0], 0)) {
+        {
+            // the first tile's pages looked up here too: its pieces do not wait for its scales
+            const int t0 = g_begin * 128 + 16 * (lane & 7);
+            uint32_t at = (uint32_t)(hk * page + (16 * (lane & 7) & (page - 1))) * kPieces;
+            if (n_tiles > 0 && t0 < s.length) {
+                const int p = kv_page(a.batch, a.cache, b, t0 >> page_log2, nullptr);
+                if (p >= 0) at += (uint32_t)p * (uint32_t)(a.cache.page_stride >> 4);
+            }
 #pragma unroll
-            for (int k = 0; k < kPieces; ++k) ku[k] = fetch(k_own, info(0), k);
+            for (int k = 0; k < kPieces; ++k) ku[k] = k_own[__shfl_sync(0xffffffffu, at, run + k * (kTokens / 16))];
 #pragma unroll
-            for (int k = 0; k < kPieces; ++k) vu[k] = fetch(v_own, info(0), k);
+            for (int k = 0; k < kPieces; ++k) vu[k] = v_own[__shfl_sync(0xffffffffu, at, run + k * (kTokens / 16))];
+            if (n_tiles > 0) wait(&i_full[0], 0);
         }
 #pragma unroll 1
         for (int g = 0; g < n_tiles; ++g) {
@@ -422,35 +425,47 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
         if (t < tiles) {
             const int r = 128 * t + row;
             const bool real = r < left;
-            const int token = (int)((r0 + min(r, left - 1)) / a.group), head = hk * a.group + (int)((r0 + min(r, left - 1)) % a.group);
+            const int token = (r0 + min(r, left - 1)) / a.group, head = hk * a.group + (r0 + min(r, left - 1)) % a.group;
             const int sees = a.causal ? behind + token : s.length;
+            // The warp's 32 rows pass through its own rows of Q_t on the way in and out: kLanes lanes take a row's 16-byte
+            // pieces side by side.  (A thread that reads or writes its own row in global memory touches a line for each lane: for
+            // dh 128 that took 5000 clocks more in and 4000 out.)
+            constexpr int kLanes = DH / 8, kOnce = 32 / kLanes;
+            const int piece = lane % kLanes;
+            uint8_t *const own_q = sQ + t * C::kTile;
+            const int64_t q_at = (int64_t)(s.row0 + token) * a.ldq + (int64_t)head * DH;
+            // (Loops here and at the end are kept short: what a CTA runs once costs it the fetch of its instructions.)
+#pragma unroll 4
+            for (int i = 0; i < kLanes; ++i) {
+                const int line = i * kOnce + lane / kLanes;
+                const int64_t at = __shfl_sync(0xffffffffu, q_at, line);
+                cp_async16(smem_u32(own_q + C::place(32 * q + line, piece)), a.q + at + 8 * piece);
+            }
+            cp_async_wait_all();
+            __syncwarp();
             float factor;  // of S, in log2
             {
-                const bf16 *x = a.q + (int64_t)(s.row0 + token) * a.ldq + (int64_t)head * DH;
-                uint4 u[DH / 8];
-#pragma unroll
-                for (int c = 0; c < DH / 8; ++c) u[c] = reinterpret_cast<const uint4 *>(x)[c];
-                float top = 0.f;
-                auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
-                auto hi = [](uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); };
-#pragma unroll
+                uint32_t tops = 0;
+#pragma unroll 4
                 for (int c = 0; c < DH / 8; ++c) {
-                    top = fmax3(top, fabsf(lo(u[c].x)), fabsf(hi(u[c].x)));
-                    top = fmax3(top, fabsf(lo(u[c].y)), fabsf(hi(u[c].y)));
-                    top = fmax3(top, fabsf(lo(u[c].z)), fabsf(hi(u[c].z)));
-                    top = fmax3(top, fabsf(lo(u[c].w)), fabsf(hi(u[c].w)));
+                    const uint4 u = *reinterpret_cast<const uint4 *>(own_q + C::place(row, c));
+                    // (magnitudes of bf16 order as their bits do)
+                    tops = __vmaxu2(tops, __vmaxu2(__vmaxu2(u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu),
+                                                   __vmaxu2(u.z & 0x7FFF7FFFu, u.w & 0x7FFF7FFFu)));
                 }
-                const int e = query_exponent(top);
+                const int e = query_exponent(__uint_as_float(max(tops & 0xFFFFu, tops >> 16) << 16));
                 const float up = pow2(e);
                 factor = a.scale_log2 * pow2(-e);
+                auto half2 = [&](uint32_t w) { return pack_half2(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xFFFF0000u) * up); };
+#pragma unroll 1
+                for (int c0 = 0; c0 < DH / 8; c0 += 4) {
+                    uint4 u[4];
 #pragma unroll
-                for (int c = 0; c < DH / 8; ++c) {
-                    uint4 w;
-                    w.x = pack_half2(lo(u[c].x) * up, hi(u[c].x) * up);
-                    w.y = pack_half2(lo(u[c].y) * up, hi(u[c].y) * up);
-                    w.z = pack_half2(lo(u[c].z) * up, hi(u[c].z) * up);
-                    w.w = pack_half2(lo(u[c].w) * up, hi(u[c].w) * up);
-                    *reinterpret_cast<uint4 *>(sQ + t * C::kTile + C::place(row, c)) = w;
+                    for (int c = 0; c < 4; ++c) u[c] = *reinterpret_cast<const uint4 *>(own_q + C::place(row, c0 + c));
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        *reinterpret_cast<uint4 *>(own_q + C::place(row, c0 + c)) =
+                            make_uint4(half2(u[c].x), half2(u[c].y), half2(u[c].z), half2(u[c].w));
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -605,51 +620,71 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                 const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
                 const int64_t at = (int64_t)(s.row0 + token) * a.heads + head;
                 const bool rare = *nan_flag != 0;
+                // All of a row in bf16, or the half of it that takes as many bytes in fp32, then its way out.
+                constexpr int kCols = DH == 32 ? 16 : 32;  // at once
+                const int rounds = a.splits == 1 ? 1 : 2;
+                const int64_t part_at = ((int64_t)split * a.batch.rows * a.heads + at) * DH;
+                const int64_t out_at = (int64_t)(s.row0 + token) * a.ldo + (int64_t)head * DH;
+                const uint32_t reals = __ballot_sync(0xffffffffu, real);
 #pragma unroll 1
-                for (int d0 = 0; d0 < DH; d0 += 32) {
-                    float o[32];
-                    if (n_tiles > 0) {
-                        uint32_t w[32];
-                        tmem_ld32(o_addr + d0, w);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int d = 0; d < 32; ++d) o[d] = __uint_as_float(w[d]);
-                    } else {
-#pragma unroll
-                        for (int d = 0; d < 32; ++d) o[d] = 0.f;
-                    }
-                    if (rare && real) {
-                        // NaN values of the tiles that are seen in part
-                        const int stop = min(sees, g_end * 128);
+                for (int round = 0; round < rounds; ++round) {
 #pragma unroll 1
-                        for (int x = max(g_begin * 128, least / 128 * 128); x < stop; ++x) {
-                            const int p = kv_page(a.batch, a.cache, b, x >> page_log2, a.err);
-                            if (p < 0) continue;
-                            const uint8_t *v = a.cache.v + (int64_t)p * a.cache.page_stride +
-                                               ((int64_t)hk * page + (x & (page - 1))) * DH + d0;
-                            const bool scale = a.cache.vs[(int64_t)p * a.cache.scale_stride + hk] == 255;
+                    for (int d0 = round * (DH / 2); d0 < (rounds == 1 ? DH : (round + 1) * (DH / 2)); d0 += kCols) {
+                        float o[kCols];
+                        if (n_tiles > 0) {
+                            uint32_t w[kCols];
+                            if constexpr (kCols == 32) tmem_ld32(o_addr + d0, w);
+                            else tmem_ld16(o_addr + d0, w);
+                            tmem_wait_ld();
 #pragma unroll
-                            for (int d = 0; d < 32; ++d)
-                                if (scale || (v[d] & 0x7F) == 0x7F) o[d] = __int_as_float(0x7FC00000);
+                            for (int d = 0; d < kCols; ++d) o[d] = __uint_as_float(w[d]);
+                        } else {
+#pragma unroll
+                            for (int d = 0; d < kCols; ++d) o[d] = 0.f;
+                        }
+                        if (__builtin_expect(rare, 0)) {
+                            // NaN values of the tiles that are seen in part
+                            const int stop = min(sees, g_end * 128);
+#pragma unroll 1
+                            for (int x = max(g_begin * 128, least / 128 * 128); x < stop; ++x) {
+                                const int p = kv_page(a.batch, a.cache, b, x >> page_log2, a.err);
+                                if (p < 0) continue;
+                                const uint8_t *v = a.cache.v + (int64_t)p * a.cache.page_stride +
+                                                   ((int64_t)hk * page + (x & (page - 1))) * DH + d0;
+                                const bool scale = a.cache.vs[(int64_t)p * a.cache.scale_stride + hk] == 255;
+#pragma unroll
+                                for (int d = 0; d < kCols; ++d)
+                                    if (scale || (v[d] & 0x7F) == 0x7F) o[d] = __int_as_float(0x7FC00000);
+                            }
+                        }
+                        if (rounds == 1) {
+#pragma unroll
+                            for (int d = 0; d < kCols; d += 8) {
+                                uint4 w;
+                                w.x = pack_bf16x2(o[d] * inv, o[d + 1] * inv);
+                                w.y = pack_bf16x2(o[d + 2] * inv, o[d + 3] * inv);
+                                w.z = pack_bf16x2(o[d + 4] * inv, o[d + 5] * inv);
+                                w.w = pack_bf16x2(o[d + 6] * inv, o[d + 7] * inv);
+                                *reinterpret_cast<uint4 *>(own_q + C::place(row, (d0 + d) / 8)) = w;
+                            }
+                        } else {
+#pragma unroll
+                            for (int d = 0; d < kCols; d += 4)
+                                *reinterpret_cast<float4 *>(own_q + C::place(row, (d0 - round * (DH / 2) + d) / 4)) =
+                                    make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
                         }
                     }
-                    if (!real) continue;
-                    if (a.splits == 1) {
-                        uint4 *dst = reinterpret_cast<uint4 *>(a.out + (int64_t)(s.row0 + token) * a.ldo + (int64_t)head * DH + d0);
-#pragma unroll
-                        for (int d = 0; d < 32; d += 8) {
-                            uint4 w;
-                            w.x = pack_bf16x2(o[d] * inv, o[d + 1] * inv);
-                            w.y = pack_bf16x2(o[d + 2] * inv, o[d + 3] * inv);
-                            w.z = pack_bf16x2(o[d + 4] * inv, o[d + 5] * inv);
-                            w.w = pack_bf16x2(o[d + 6] * inv, o[d + 7] * inv);
-                            dst[d / 8] = w;
-                        }
-                    } else {
-                        float4 *dst = reinterpret_cast<float4 *>(a.part + ((int64_t)split * a.batch.rows * a.heads + at) * DH + d0);
-#pragma unroll
-                        for (int d = 0; d < 32; d += 4) dst[d / 4] = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
+                    __syncwarp();
+#pragma unroll 4
+                    for (int i = 0; i < kLanes; ++i) {
+                        const int line = i * kOnce + lane / kLanes;
+                        const int64_t to = __shfl_sync(0xffffffffu, rounds == 1 ? out_at : part_at, line);
+                        const uint4 w = *reinterpret_cast<const uint4 *>(own_q + C::place(32 * q + line, piece));
+                        if (!(reals >> line & 1)) continue;
+                        if (rounds == 1) *reinterpret_cast<uint4 *>(a.out + to + 8 * piece) = w;
+                        else *reinterpret_cast<uint4 *>(a.part + to + round * (DH / 2) + 4 * piece) = w;
                     }
+                    __syncwarp();
                 }
                 if (real) {
                     if (a.splits == 1) {

@@ -96,24 +96,24 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
     griddep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
 
-    int64_t item = blockIdx.x;
-    const int split = (int)(item % a.splits);
-    item /= a.splits;
-    const int rb = (int)(item % a.row_blocks);
-    item /= a.row_blocks;
-    const int hk = (int)(item % a.cache.heads), b = (int)(item / a.cache.heads);
+    uint32_t item = blockIdx.x;
+    const int split = (int)(item % (uint32_t)a.splits);
+    item /= (uint32_t)a.splits;
+    const int rb = (int)(item % (uint32_t)a.row_blocks);
+    item /= (uint32_t)a.row_blocks;
+    const int hk = (int)(item % (uint32_t)a.cache.heads), b = (int)(item / (uint32_t)a.cache.heads);
     const KvSeq s = kv_seq(a.batch, a.cache, b, a.err);
     const int r0 = rb * kRows;
-    const int64_t rows = (int64_t)s.n * a.group;  // packed
+    const int rows = s.n * a.group;  // packed
     if (s.n <= 0 || r0 >= rows) return;
-    const int row_end = (int)min(rows, (int64_t)r0 + kRows);
+    const int row_end = min(rows, r0 + kRows);
 
     // tokens that the last and the first of the rows see
     const int behind = s.length - s.n + 1;
     const int most = a.causal ? max(0, behind + (row_end - 1) / a.group) : s.length;
     const int least = a.causal ? behind + r0 / a.group : s.length;
     const int chunks = (most + kChunk - 1) / kChunk;
-    const int c_begin = (int)((int64_t)chunks * split / a.splits), c_end = (int)((int64_t)chunks * (split + 1) / a.splits);
+    const int c_begin = kv_share(chunks, split, a.splits), c_end = kv_share(chunks, split + 1, a.splits);
 
     // ---- this warp's ring
     uint8_t *const ring = smem + warp * kStages * Cfg::kStage;

@@ -55,6 +55,9 @@ F3DC_DEV int kv_page(const KvBatch &t, const KvCache &c, int b, int j, uint32_t 
     return -1;
 }
 
+// Where share i of n of `all` begins.
+F3DC_DEV int kv_share(int all, int i, int n) { return n == 1 ? all * i : (int)((int64_t)all * i / n); }
+
 // 2^e for any e: 0 below fp32's smallest number, infinity above its largest
 F3DC_DEV float pow2(int e)
 {

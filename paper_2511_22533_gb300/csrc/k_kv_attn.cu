@@ -27,9 +27,10 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr float kInf = __builtin_huge_valf();
-// Registers per thread after the split: the launch has 512 x 128.
+// Registers per thread at the launch and after the split.
+constexpr int kLaunchRegs = 128;
 constexpr int kIssueRegs = 40, kConvertRegs = 104, kSoftmaxRegs = 184;
-static_assert(128 * (kIssueRegs + kConvertRegs) + 256 * kSoftmaxRegs <= 512 * 128, "register split above the launch's total");
+static_assert(128 * (kIssueRegs + kConvertRegs) + 256 * kSoftmaxRegs <= 512 * kLaunchRegs, "register split above the launch's total");
 
 // A row's largest weight is 2^kTop where its reference was taken.  The sum of a tile's weights, which is taken
 // anyway, says whether one may have left fp16's range; only then is the reference looked at again.  128 weights
@@ -61,10 +62,14 @@ struct Cfg {
     static constexpr int kRegion = 128 * kRowBytes, kTile = kRegions * kRegion;
     static constexpr uint32_t kAtom = 8 * kRowBytes, kSwz = DH == 32 ? kSwizzle64 : kSwizzle128;
     static constexpr int kStages = DH == 128 ? 2 : 4;
-    static constexpr int kPlaces = DH == 128 ? 2 : 3;  // of S and P of a query tile, 64 columns each
+    static constexpr int kPlaces = 2;  // of S and P of a query tile, 64 columns each
+    // Queries in TMEM, where there is room: an S MMA of 64 columns reads twice as many bytes of queries from shared memory as of keys
+    // and takes 48 clocks instead of 32.
+    static constexpr bool kQTmem = DH < 128;
+    static constexpr uint32_t kColQ = 2 * 64 * kPlaces + 2 * DH;
     static constexpr size_t kSmem = 1024 + (size_t)kTile * (2 + 2 * kStages) + kGroups * kGroup * sizeof(TileInfo<NB>) + 576;
     static constexpr uint32_t kColO = 2 * 64 * kPlaces;
-    static_assert(kColO + 2 * DH <= 512, "TMEM layout");
+    static_assert(kColO + 2 * DH + (kQTmem ? DH : 0) <= 512, "TMEM layout");
     // byte of 16-byte piece `piece` (8 columns) of a row
     static F3DC_DEV int place(int row, int piece)
     {
@@ -226,7 +231,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
 #pragma unroll
                 for (int kk = 0; kk < DH / 16; ++kk) {
                     const uint64_t at = (kk / 4) * kRegionStep + 2 * (kk % 4);
-                    mma_bf16_elect(tm + ps.i * 64, q_desc + at, kd + at, idesc_s, kk > 0);
+                    if (C::kQTmem) mma_bf16_ts_elect(tm + ps.i * 64, tmem + C::kColQ + t * (DH / 2) + kk * 8, kd + at, idesc_s, kk > 0);
+                    else mma_bf16_elect(tm + ps.i * 64, q_desc + at, kd + at, idesc_s, kk > 0);
                 }
                 mma_commit_elect(&s_own[ps.i]);
                 if ((j & 1) || j + 1 == n_steps) mma_commit_elect(&k_empty[st]);
@@ -463,11 +469,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) u[c] = *reinterpret_cast<const uint4 *>(own_q + C::place(row, c0 + c));
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        *reinterpret_cast<uint4 *>(own_q + C::place(row, c0 + c)) =
-                            make_uint4(half2(u[c].x), half2(u[c].y), half2(u[c].z), half2(u[c].w));
+                    for (int c = 0; c < 4; ++c) u[c] = make_uint4(half2(u[c].x), half2(u[c].y), half2(u[c].z), half2(u[c].w));
+                    if constexpr (C::kQTmem) {
+                        const uint32_t w[16] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w,
+                                                u[2].x, u[2].y, u[2].z, u[2].w, u[3].x, u[3].y, u[3].z, u[3].w};
+                        tmem_st16(tmem + tl + C::kColQ + t * (DH / 2) + 4 * c0, w);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(own_q + C::place(row, c0 + c)) = u[c];
+                    }
                 }
-                fence_proxy_async_smem();
+                if constexpr (C::kQTmem) {
+                    tmem_wait_st();
+                    tc_fence_before();
+                } else {
+                    fence_proxy_async_smem();
+                }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&q_full[t]);
             }
@@ -589,27 +606,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                 return 1;
             };
             const int whole = max(0, min(n_steps, least / 64 - 2 * g_begin));  // steps that every row sees
+            // Two plain steps stand one after another in the code: a jump back costs a warp some 200 clocks, as the instructions of the others
+            // have taken the place of its own.  (All eight of a group were 10 % faster while the warps ran through them together and
+            // 40 % slower with warps that had left the others' pace by a careful step.)
             bool ok = true, again = true;
             int j = 0;
-            int place = 0, left_in_group = 0;
-            uint32_t phase = 0;
 #pragma unroll 1
             while (ok && j < n_steps) {
-                if (left_in_group == 0) {
-                    const int group = j / kGroupSteps;
-                    if (!(ok = wait(&i_full[group % kGroups], (group / kGroups) & 1))) break;
-                    left_in_group = kGroupSteps;
-                    x = infos[group % kGroups * kGroup].scales[0];
+                const int group = j / kGroupSteps % kGroups, u = j % kGroupSteps;
+                if (u == 0 && !(ok = wait(&i_full[group], (j / (kGroupSteps * kGroups)) & 1))) break;
+                const uint32_t phase = (j / C::kPlaces) & 1;
+                const StepScales<NB> *const own = infos[(j >> 1) % (kGroup * kGroups)].scales;
+                x = own[j & 1];
+                int r;
+                if (again || j >= whole) {
+                    r = step(j, j % C::kPlaces, phase, x, std::true_type());
+                    if (r == 1) ++j;
+                } else {
+                    static_assert(C::kPlaces == 2, "an even step is in the first place");
+                    r = 1;
+                    if ((j & 1) == 0) {
+                        r = step(j, 0, phase, own[1], std::false_type());
+                        if (r == 1) ++j;
+                    }
+                    if (r == 1 && j < whole) {
+                        // (the scales of the step after are another tile's, perhaps another group's: read when it begins)
+                        r = step(j, 1, phase, own[1], std::false_type());
+                        if (r == 1) ++j;
+                    }
                 }
-                const int n = j + 1 - (left_in_group == 1);  // the next step, if of this group
-                const StepScales<NB> &next = infos[(n >> 1) % (kGroup * kGroups)].scales[n & 1];
-                const int r = again || j >= whole ? step(j, place, phase, next, std::true_type()) : step(j, place, phase, next, std::false_type());
                 again = r == 0;
                 ok = r >= 0;
-                if (r != 1) continue;
-                if (--left_in_group == 0) mbar_arrive_if(smem_u32(&i_empty[j / kGroupSteps % kGroups]), lane == 0);
-                if (++place == C::kPlaces) place = 0, phase ^= 1;
-                ++j;
+                if (r == 1 && j % kGroupSteps == 0) mbar_arrive_if(smem_u32(&i_empty[group]), lane == 0);
             }
             if (ok && n_steps > 0) {
                 // (v_full: nan_flag is what the converting warps left)
@@ -719,6 +747,13 @@ cudaError_t launch_one(const KvAttnArgs &args, cudaStream_t s)
     a.row_blocks = (int)(((int64_t)a.batch.max_rows * a.group + 255) / 256);
     const int64_t ctas = (int64_t)a.splits * a.row_blocks * a.cache.heads * a.batch.batch;
     if (ctas > INT32_MAX) return cudaErrorInvalidValue;
+    // (a register split above what the launch really has would wait for ever)
+    static const cudaError_t split = [] {
+        cudaFuncAttributes f;
+        const cudaError_t e = cudaFuncGetAttributes(&f, k_kv_attn<DH, NB>);
+        return e != cudaSuccess ? e : (f.numRegs >= kLaunchRegs ? cudaSuccess : cudaErrorInvalidKernelImage);
+    }();
+    if (split != cudaSuccess) return split;
     static std::atomic<uint64_t> devices{0};
     cudaError_t e = ask_smem(k_kv_attn<DH, NB>, (int)Cfg<DH, NB>::kSmem, devices);
     if (e != cudaSuccess) return e;

@@ -78,6 +78,21 @@ def test_attention_of_many_rows(held, rows, heads, kv_heads, dh, page, causal):
     run_attend(c, causal)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("rows,heads,dh,page", [(1537, 40, 64, 64), (1700, 40, 64, 16), (2048, 38, 32, 128), (1920, 40, 32, 32)])
+def test_attention_of_many_rows_for_every_sm(rows, heads, dh, page, causal):
+    # launches that fill the GPU with larger blocks of rows, the last of one row to a whole one; NaN beside them
+    c = R.Case([70], [rows], heads, heads, dh, page, seed=rows)
+    c.fill(spread=1.0, v_spread=2.0)
+    last = 70 + rows - 1
+    c.v[c.table_list[0][last // page], 3, last % page, 5] = R.STALE
+    c.v[c.table_list[0][(last - 600) // page], 7, (last - 600) % page, dh - 2] = R.STALE
+    c.k[c.table_list[0][(last - 300) // page], 11, (last - 300) % page, 0] = R.STALE
+    run_attend(c, causal)
+    if not causal:
+        run_attend(c, False, q=queries(c, scale=4.0))
+
+
 def cross(lengths, rows, heads, kv_heads, dh, page, **kw):
     """Queries over caches that do not hold their rows (shorter than them, too)."""
     c = R.Case(lengths, [0] * len(lengths), heads, kv_heads, dh, page, **kw)

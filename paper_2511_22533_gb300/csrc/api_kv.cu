@@ -218,8 +218,9 @@ extern "C" f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f
     if (misaligned(q, 16) || misaligned(out, 16) || misaligned(workspace, 16)) return bad("pointers must be 16-byte aligned");
     if (misaligned(lse, 4)) return bad("lse must be 4-byte aligned");
     const int group = heads / cache->kv_heads;
-    // (blocks of 16 packed rows are the smallest that any kernel makes)
-    if (((int64_t)batch->max_rows * group + 15) / 16 > INT32_MAX / ((int64_t)cache->kv_heads * batch->batch) ||
+    // (blocks of 8 packed rows are the smallest that any kernel makes, and a sequence's CTAs are shared out only up to some
+    // times the SMs)
+    if (((int64_t)batch->max_rows * group + 7) / 8 > INT32_MAX / 2 / ((int64_t)cache->kv_heads * batch->batch) ||
         (int64_t)batch->max_rows * group > INT32_MAX / 2 || (int64_t)batch->rows * heads > INT32_MAX ||
         batch->max_length > INT32_MAX - 1024)
         return bad("the problem is too large");

@@ -117,14 +117,17 @@ class KVCache(C.Structure):
         pages, heads, tokens, dh = k.shape
         if v.shape != k.shape or tuple(k_scales.shape) != (pages, heads) or k_scales.shape != v_scales.shape:
             raise F3dcError(1, "k and v need one shape [pages, kv_heads, page_tokens, dh], their scales [pages, kv_heads]")
+        # (the stride of a dimension of one says nothing)
+        page_stride, scale_stride = (k.stride(0), k_scales.stride(0)) if pages > 1 else (heads * tokens * dh, heads)
         for t in (k, v):
-            if t.stride()[1:] != (tokens * dh, dh, 1) or t.stride(0) != k.stride(0):
+            want = (page_stride, tokens * dh, dh, 1)
+            if any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), want)):
                 raise F3dcError(1, "a page's bytes must lie together, pages of k and v equally far apart")
         for t in (k_scales, v_scales):
-            if t.stride(1) != 1 or t.stride(0) != k_scales.stride(0):
+            if any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), (scale_stride, 1))):
                 raise F3dcError(1, "a page's scales must lie together, pages of k_scales and v_scales equally far apart")
         _same_device("cache", self._tensors)
-        super().__init__(pages, tokens, heads, dh, *(t.data_ptr() for t in self._tensors), k.stride(0), k_scales.stride(0))
+        super().__init__(pages, tokens, heads, dh, *(t.data_ptr() for t in self._tensors), page_stride, scale_stride)
         self._ref = C.pointer(self)
 
 
@@ -138,7 +141,7 @@ class KVBatch(C.Structure):
     def __init__(self, row_start, lengths, page_table, rows, max_rows, max_length):
         self._tensors = (row_start, lengths, page_table)
         for t, n in zip(self._tensors, (1, 1, 2)):
-            if t.dtype not in _fp8_types()["int32"] or t.dim() != n or (t.numel() and t.stride(n - 1) != 1):
+            if t.dtype not in _fp8_types()["int32"] or t.dim() != n or (t.shape[-1] > 1 and t.stride(n - 1) != 1):
                 raise F3dcError(1, f"row_start, lengths and page_table are int32 with neighbouring entries: got {t.dtype} {tuple(t.shape)}")
         batch = lengths.shape[0]
         if row_start.shape[0] != batch + 1 or page_table.shape[0] != batch:

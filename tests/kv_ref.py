@@ -77,7 +77,8 @@ def attend(c, q, scale, causal):
     ones off by 2^-39 of it), products are exact, the tensor core drops up to 2^-23 of the magnitudes at
     every 16 of dh; the affine step to log2, the reference and the shift are three fp32 roundings of numbers no larger than
     |s| + |m| + 80 (a value scale of at most 2^64 either way).  A weight: the exponential's 2^-22,
-    the rounding to fp16 2^-11 relative, below fp16's normal range 2^-36 of the row's largest at most.  The sums: 2^-23
+    the rounding to fp16 2^-11 relative, below fp16's normal range 2^-25 of a weight of 1, which the row's
+    largest is at least (its reference is taken so that it is 2^3 or more, or, from the sum of 64 weights, 2^6 / 64).  The sums: 2^-23
     at each step of 16 tokens, 2^-24 at each step of a sum of weights."""
     R, H, dh = c.n_rows, c.heads, c.dh
     g = H // c.kv_heads
@@ -121,7 +122,7 @@ def attend(c, q, scale, causal):
             err[at, h] = mag * (2.0 ** -11 + 2 * ds + steps + 2.0 ** -20)[:, None]
             if L:
                 most = torch.where(seen, p * (TOP * scales[h // g].nan_to_num()), 0.0).amax(1, keepdim=True)
-                err[at, h] += L * 2.0 ** -36 * most + 2.0 ** -39 * mag
+                err[at, h] += L * 2.0 ** -25 * most + 2.0 ** -39 * mag
             lse_err[at, h] = ds + steps + 2.0 ** -20 + 4 * U32 * lse[at, h].abs().nan_to_num(posinf=0.0, neginf=0.0)
     return out, lse, err, lse_err
 

@@ -141,6 +141,23 @@ def test_scores_far_apart(dh, rows):
     run_attend(c, True, q=queries(c, scale=3.0))
 
 
+@pytest.mark.parametrize("rows", [1, 150])
+def test_a_token_that_takes_nearly_all(rows):
+    # the first token's score far above thousands of others', its values zero: what the others give is left, each
+    # 2^-14 of it or so, and with a second such token at the end the first's reference is no more
+    c = R.Case([6000], [rows], 2, 1, 64, 64, seed=30)
+    c.fill(spread=0.0, v_spread=0.0)
+    q = torch.ones((c.n_rows, 128), dtype=torch.bfloat16, device=DEV)
+    p0, p1 = c.table_list[0][0], c.table_list[0][len(c.table_list[0]) // 2]
+    for t in c.table_list[0]:
+        c.k[t] = torch.zeros_like(c.k[t])
+    c.k[p0, 0, 0], c.v[p0, 0, 0] = 0x40, 0         # 2.0 in every element of the key
+    c.ks[:] = 127                                  # score 16: 2^23 times the weights of the others
+    run_attend(c, True, q=q)
+    c.k[p1, 0, 5] = 0x48                           # 4.0: score 32
+    run_attend(c, False, q=q)
+
+
 @pytest.mark.parametrize("rows", [3, 150])
 def test_queries_of_all_sizes(rows):
     # bf16 queries from 2^-100 to 2^60 against keys that bring their scores back, zeros among them
@@ -600,3 +617,94 @@ def test_streams_and_graphs(rows):
                 g.replay()
     torch.cuda.synchronize()
     same()
+
+
+@pytest.mark.parametrize("call", ["append", "few", "many"])
+def test_first_call_in_a_capture(call):
+    # a process whose first call of the library is captured, and replayed
+    import os
+    import subprocess
+    import sys
+    code = f"""
+import sys
+sys.path.insert(0, {os.path.dirname(os.path.abspath(__file__))!r})
+sys.path.insert(0, {os.path.dirname(os.path.dirname(os.path.abspath(__file__)))!r})
+import torch, kv_ref as R
+from paper_2511_22533_gb300 import f3dc
+c = R.Case([100], [{1 if call == "few" else 140}], 2, 1, 64, 64, seed=3)
+c.fill(c.held if {call == "append"} else None)
+q = c.randn(c.n_rows, 128, part=40).to(torch.bfloat16)
+cache, batch = f3dc.KVCache(c.k, c.v, c.ks, c.vs), f3dc.KVBatch(c.row_start, c.length, c.table, c.n_rows, max(c.rows), max(c.lengths))
+before = [t.clone() for t in (c.v, c.vs)]
+out, lse = torch.zeros_like(q), torch.zeros((c.n_rows, 2), device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    if {call == "append"}:
+        f3dc.kv_append_fp8(cache, batch, q, 128, q[:, 64:], 128)
+    else:
+        f3dc.kv_attention_fp8(cache, batch, q, 128, out, 128, 2, 0.125, causal=True, lse=lse)
+g.replay()
+torch.cuda.synchronize()
+assert f3dc.gemm_status() == 0
+if {call == "append"}:
+    new = q[:, 64:].double().view(-1, 1, 64)
+    R.check_append(c, "v", new, torch.zeros_like(new), *before)
+else:
+    R.check_attend(c, out, lse, q, 0.125, True)
+print("fine")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
+
+
+def test_append_on_streams_and_in_graphs():
+    # two appends at once on two streams, and captured and replayed: the same pages as one after the other
+    cases = [R.Case([40, 7], [3, 60], 4, 2, 64, 32, seed=40 + i) for i in range(2)]
+    rot, want, args = f3dc.Rotary(64), [], []
+    for c in cases:
+        c.fill(c.held)
+        x, q = c.randn(c.n_rows, 256, part=50).to(torch.bfloat16), queries(c)
+        start = [t.clone() for t in (c.k, c.v, c.ks, c.vs)]
+        out = torch.zeros_like(q)
+        args.append((c, cache_of(c), batch_of(c), x, q, out, start))
+    torch.cuda.synchronize()
+
+    def call(i, stream=None):
+        c, cache, batch, x, q, out, _ = args[i]
+        f3dc.kv_append_fp8(cache, batch, x, 256, x[:, 128:], 256, q=q, ldq=256, q_out=out, ldqo=256, heads=4, rotary=rot, stream=stream)
+
+    def state(i):
+        c, _, _, _, _, out, _ = args[i]
+        return [t.clone() for t in (c.k, c.v, c.ks, c.vs, out)]
+
+    def reset():
+        for c, _, _, _, _, out, start in args:
+            for t, b in zip((c.k, c.v, c.ks, c.vs), start):
+                t.copy_(b)
+            out.zero_()
+        torch.cuda.synchronize()
+
+    for i in range(2):
+        call(i)
+        want.append(state(i))
+    reset()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i, s in enumerate(streams):
+        call(i, s.cuda_stream)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(state(i), want[i]))
+    reset()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for i, g in enumerate(graphs):
+        with torch.cuda.graph(g):
+            call(i)
+    reset()
+    for g, s in zip(graphs, streams):
+        with torch.cuda.stream(s):
+            g.replay()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(state(i), want[i]))
+    assert f3dc.gemm_status() == 0

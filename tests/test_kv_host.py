@@ -175,6 +175,11 @@ def test_views_of_larger_pools_fit():
     c = f3dc.KVCache(*(Tensor(E4M3, (10, 4, 64, 64), joint) for _ in range(2)), *(Tensor(E8M0, (10, 4), (8, 1)) for _ in range(2)))
     assert (c.page_stride, c.scale_stride, c.pages, c.kv_heads, c.page_tokens, c.dh) == (32768, 8, 10, 4, 64, 64)
     assert batch(tpt=Tensor(I32, (2, 5), (9, 1))).table_stride == 9
+    # dimensions of one may have any stride
+    one = f3dc.KVCache(*(Tensor(U8, (1, 1, 64, 64), (7, 3, 64, 1)) for _ in range(2)), *(Tensor(U8, (1, 1), (5, 9)) for _ in range(2)))
+    assert (one.page_stride, one.scale_stride) == (4096, 1)
+    single = batch(n=1, trs=Tensor(I32, (2,)), tln=Tensor(I32, (1,), (3,)), tpt=Tensor(I32, (1, 1), (4, 8)))
+    assert single.table_stride == 1
 
 
 @pytest.fixture

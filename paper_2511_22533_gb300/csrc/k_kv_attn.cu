@@ -1,24 +1,35 @@
 // k_kv_attn.cu -- f3dc_kv_attention_fp8 for many query rows to a key head: attention over a
 // paged 8-bit cache on 5th-generation tensor cores.
 //
-//   S = Q K^T, x = S scale 2^(ek) + ev, w = 2^(x - m + shift), O += w V, l += w 2^-ev
+//   S = Q K^T, x = S scale 2^(ek) + ev, w = 2^(x - r), O += w V, l += w 2^-ev, out = O / l
 //
-// A CTA (512 threads) takes 256 packed rows (query row, head of the group) of one sequence and key head:
-// two tiles A and B of 128 rows that share their keys, whose score / softmax / product chains run side by side.
-//   warps 0, 1   tcgen05.mma issuers of tile A and of tile B.  Per key tile g of 128 tokens: S_t(g) = Q_t K^T
-//                (N = 128, K = dh), O_t += P_t V(g) (N = dh, K = 128; P read from TMEM)
+// A CTA (512 threads) takes 256 packed rows (query row, head of the group) of one sequence and key head: two tiles
+// A and B of 128 rows that share their keys, whose score / softmax / product chains run side by side, in steps of 64
+// tokens (half of a tile of keys and values).
+//   warps 0, 1   tcgen05.mma issuers of tile A and of tile B.  Step j: S_t(j) = Q_t K^T (N = 64, K = dh), O_t += P_t V(j)
+//                (N = dh, K = 64; P read from TMEM).  S is two steps ahead, in the place of the P that has been used
 //   warp 2       walks the page table, four tiles at a time: where each 16 tokens of a tile lie, and their scales
 //   warps 4-7    the cache's pages: each thread loads 16-byte pieces of keys and values (those of the next tile
 //                while it converts this one's), converts e4m3 to fp16 (exactly) and writes them to shared memory in the
 //                MMA's swizzled layout
-//   warps 8-11   softmax of tile A, warps 12-15 of tile B: one thread per row.  Before the first tile they convert
-//                their queries (bf16 times a power of two of the row: exact in fp16) into shared memory.
-// TMEM: S_A S_B (fp32, 128 columns each) | O_A O_B (dh each) | P_A P_B (fp16 pairs, 64 each); with dh 128 there
-// is no room for P beside them, and it takes the place of S_t, whose next MMA then waits for P_t V.
+//   warps 8-11   softmax of tile A, warps 12-15 of tile B: one thread per row.  Before the first step they bring their queries
+//                in (bf16 times a power of two of the row: exact in fp16)
+// TMEM: two places of 64 columns each for S and P of A, then of B | O_A O_B (dh each) | Q_A Q_B (dh / 2 each, up to
+// dh 64: with dh 128 the queries stay in shared memory).
 // fp16 weights are what the 8-bit values allow: e4m3 is exact in fp16 but needs more instructions to become bf16, and
-// fp16's rounding is 2^-11.  Their range (kv.cuh) needs the running maximum: it is taken for every tile.
+// fp16's rounding is 2^-11.  Their range is looked after by the sum of a step's weights, which is taken anyway.
 // A NaN that some rows do not see: where a row of the CTA sees only a part of a tile, NaN values count as
 // zeros in the MMA and the rows look them up at the end.
+// What bounds it: a softmax warp's own latencies.  A step of 64 tokens takes it some 1300 clocks, of which the
+// exponents are 260 (alone) to 520 (both tiles' warps at once): waits, tensor-memory loads and stores, votes and the
+// fetch of instructions are the rest, and tensor memory has no room for more tiles with dh 128 (with dh 64, four tiles of
+// one place each measured 7 % slower).  With dh 128 shared memory comes next: operands read and written take 2500 of some
+// 3000 clocks a pair of tiles.  32768 x 32768, 16 heads of 64: 4.98 ms = 881 TFLOP/s; causal 8192 x 8192, 32 heads of
+// 128 to 8: 502 us = 1096 TFLOP/s; 1229 x 1374, 16 heads of 64: 29 us, of which 8 before the first and behind the last step.
+// Steps that led here, prompt of 8192 / 32768 x 32768: one step of 128 tokens, its maximum always taken 872 us / 6.8 ms; no
+// maximum, pages looked up by a warp of their own 567 / -; steps of 64 in two places 497 / 5.3; queries in TMEM and two steps
+// without a jump between them 502 / 4.98.  Measured slower: three places of S (117 us instead of 117, but no room for the queries), P waited
+// for in the next step, more registers for softmax at the cost of the converting warps.
 #include "kv.cuh"
 
 namespace f3dc {
@@ -32,10 +43,11 @@ constexpr int kLaunchRegs = 128;
 constexpr int kIssueRegs = 40, kConvertRegs = 104, kSoftmaxRegs = 184;
 static_assert(128 * (kIssueRegs + kConvertRegs) + 256 * kSoftmaxRegs <= 512 * kLaunchRegs, "register split above the launch's total");
 
-// A row's largest weight is 2^kTop where its reference was taken.  The sum of a tile's weights, which is taken
-// anyway, says whether one may have left fp16's range; only then is the reference looked at again.  128 weights
-// of 2^kTop are 2^14, below kMostSum, so rows of even weights do not ask.  fp16 holds 2^-21 of a row's largest
-// weight at full precision and 2^-32 at all.
+// A row's largest weight is 2^kTop where its reference was taken.  The sum of a step's weights, which is taken
+// anyway, says whether one may have left fp16's range; only then is the reference looked at again, by all rows of the warp.  64
+// weights of 2^kTop are 2^9, far below kMostSum, so rows of even weights do not ask.  fp16 holds 2^-17 of a row's
+// largest weight at full precision and 2^-28 at all.  A higher kTop holds more and asks more often: prompt of 8192 / 32768 x
+// 32768 with keys and queries of a few large channels 502 us / 4.99 ms, with 2^6 540 / 5.10, with 2^8 576 / 5.24.
 constexpr float kTop = 3.f, kMostSum = 60000.f;
 
 // What the page table says about a tile: of each of its eight runs of 16 tokens where it starts in the pool (in 16
@@ -113,13 +125,6 @@ F3DC_DEV bool wait_bounded(uint64_t *bar, uint32_t parity, uint64_t ns)
     while (!mbar_try_wait(bar, parity))
         if (globaltimer() - t0 > ns) return false;
     return true;
-}
-
-F3DC_DEV uint32_t half2_times(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
 }
 
 template <int DH, int NB>

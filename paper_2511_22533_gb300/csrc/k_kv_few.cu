@@ -2,14 +2,18 @@
 // few at once, groups of heads): attention over a paged 8-bit cache, and the sum of the
 // parts where several CTAs share a sequence's keys.
 //
-//   S = Q K^T, x = S scale 2^(ek) + ev, w = 2^(x - m + shift), O += w V, l += w 2^-ev
+//   S^T = K Q^T, x = S scale 2^(ek) + ev, w = 2^(x - r), O^T += V^T w, l += w 2^-ev
 //
 // Bound by the cache's bytes.  A warp takes 32 tokens at a time: their keys and values come by cp.async into a ring
-// of its own (no other warp is waited for), are converted to fp16 (exactly) and multiplied
-// with mma.m16n8k16, query rows as the 16 rows (up to 32 of them).  K may be permuted within an MMA as long as both
-// operands are: a lane's 16 consecutive bytes of a key serve four MMAs; and the tokens behind the columns of S are
-// chosen so that its accumulators are the weights' operand of the second product as they stand, while four lanes
-// read four neighbouring tokens' values.  Each warp keeps sums and references of its own, which are joined at the end.
+// of its own (no other warp is waited for), are converted to fp16 (exactly) and multiplied with mma.m16n8k16, 16 tokens or 16
+// columns of the head as the rows and 8 packed query rows as the columns, so that up to 8 query rows (a group of heads' single
+// token) cost half the products and exponents of a tile of 16.  K may be permuted within an MMA as long as both
+// operands are: a lane's 16 consecutive bytes of a key serve four MMAs.  The weights turn round in one movmatrix a tile, and the
+// tokens behind the rows of S^T are chosen so that four lanes read four neighbouring tokens' values.  Each warp
+// keeps sums and references of its own, which are joined at the end.
+// One token of 32 heads of 128 to 8 key heads over 524288: 167 us (6.4 TB/s, 95 % of a plain copy's rate); 64 sequences' tokens over
+// 4096 to 8192: 136 us (6.0 TB/s), where the lengths leave some SMs idle at the end; one token over 1374 of 16 heads of 64:
+// 7.1 us, two launches and the latencies of page table, pages and parts.  Query rows as the MMA's rows: 224, 190 and 13 us.
 #include "kv.cuh"
 
 namespace f3dc {
@@ -18,12 +22,14 @@ namespace {
 
 constexpr int kWarps = 4, kChunk = 32;
 constexpr float kInf = __builtin_huge_valf();
-// A row's largest weight is 2^kTop where its reference was taken, and up to 2^kLazy more before it is taken anew:
-// below 2^16, with 2^-29 of it at fp16's full precision and 2^-39 at all.
+// A row's largest weight is 2^kTop where its reference was taken, and up to 2^(kTop + kLazy) before it is taken anew:
+// below 2^16, with 2^-25 of it at fp16's full precision and 2^-36 at all.
 constexpr float kTop = 11.f, kLazy = 4.f;
 
 template <int DH>
 struct FewCfg {
+    // (one chunk ahead with dh 128, where three CTAs fit an SM, or two with two ahead: 64 tokens over up to 8192 136 us / 153, one over
+    // 524288 167 / 184)
     static constexpr int kHalf = kChunk * DH, kStage = 2 * kHalf;  // bytes: keys, then values
     static constexpr int kStages = DH == 128 ? 2 : 3;
     static constexpr int kSmem = kWarps * kStages * kStage;
@@ -32,12 +38,6 @@ struct FewCfg {
 F3DC_DEV void cp_async16_or_zeros(uint32_t dst, const void *src, bool real)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
-}
-F3DC_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-F3DC_DEV void cp_async_wait()
-{
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 F3DC_DEV void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -64,12 +64,6 @@ F3DC_DEV int value_place(int token, int piece)
     return token * DH + 16 * piece;
 }
 
-F3DC_DEV uint32_t half2_times(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
 // an 8 x 8 matrix of 16-bit elements, lane (g, q) holding (g, 2 q) and (g, 2 q + 1), transposed
 F3DC_DEV uint32_t transposed(uint32_t a)
 {

@@ -494,19 +494,26 @@ cudaError_t launch_kv_few(const KvAttnArgs &a, cudaStream_t s);   // few packed 
 cudaError_t launch_kv_attn(const KvAttnArgs &a, cudaStream_t s);  // many
 cudaError_t launch_kv_join(const KvAttnArgs &a, cudaStream_t s);  // adds the parts up (called by both)
 
-// Packed rows from which tensor-memory tiles are taken.
+// Packed rows from which tensor-memory tiles are taken.  Few / many, us: 15 packed rows (4 sequences of some 30000, heads of
+// 64) 19.1 / 42.6, 16 (16 sequences of 8192, 8 key heads of 128) 77 / 131, 32 (4 sequences of 8192, the same) 46.9 / 42.6.
 inline bool kv_many_rows(int max_rows, int heads, int kv_heads) { return (int64_t)max_rows * (heads / kv_heads) > 16; }
 
-constexpr int kFewLeast = 256, kFewLeastWaves = 2048;
-// Packed rows of a CTA of the few-rows kernel.
+// Packed rows of a CTA of the few-rows kernel: with dh 128 the sums of 32 do not fit registers.
 inline int kv_few_rows(int64_t rows, int dh) { return rows <= 8 ? 8 : (rows <= 16 || dh == 128 ? 16 : 32); }
+
 // How many of them an SM holds (registers, shared memory).
 inline int kv_few_slots(int tile, int dh)
 {
     return dh == 128 ? (tile == 8 ? 3 : 2) : (dh == 64 ? (tile == 8 ? 4 : (tile == 16 ? 3 : 2)) : (tile == 8 ? 6 : (tile == 16 ? 4 : 3)));
 }
 
-// CTAs that share a sequence's keys.
+// CTAs that share a sequence's keys.  Few rows: as many as fit the SMs at once, each with at least kFewLeast tokens (one token over
+// 1374 7.2 us, with 512 9.9, with 128 6.9; over 131072 47.0 us, with twice as many CTAs as fit 51.5); where sequences and heads alone
+// nearly fill the SMs, four times as many as fit, each with at least kFewLeastWaves, so that sequences of different lengths
+// even out (64 of 4096 to 8192 136 us, unshared 143; 16 of 4096, 16 heads of 64, 32.0 us, unshared 38.8, with 256 tokens
+// at least 39.8).
+// Many rows: no more than one for every SM.
+constexpr int kFewLeast = 256, kFewLeastWaves = 2048;
 inline int kv_splits(int batch, int max_rows, int max_length, int heads, int kv_heads, int dh, int sms)
 {
     const int64_t rows = (int64_t)max_rows * (heads / kv_heads);

@@ -65,19 +65,25 @@ F3DC_DEV float pow2(int e)
     return e < -149 ? 0.f : __uint_as_float(1u << (e + 149));
 }
 
-// two e4m3 values to fp16 (exact)
-F3DC_DEV uint32_t e4m3x2_to_half2(uint32_t w)
+F3DC_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+F3DC_DEV void cp_async_wait()
 {
-    uint32_t h;
-    asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n}\n" : "=r"(h) : "r"(w));
-    return h;
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+
 // four e4m3 values to two pairs of fp16 (exact)
 F3DC_DEV void e4m3x4_to_half2(uint32_t w, uint32_t &h0, uint32_t &h1)
 {
     asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %2;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n cvt.rn.f16x2.e4m3x2 %1, hi;\n}\n"
         : "=r"(h0), "=r"(h1)
         : "r"(w));
+}
+F3DC_DEV uint32_t half2_times(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 F3DC_DEV uint32_t pack_half2(float lo, float hi)
 {

@@ -384,6 +384,13 @@ def test_append(held, rows, heads, kv_heads, dh, page, dims, interleaved):
     run_append(c, dims={"all": dh, "half": dh // 2}.get(dims, 0), interleaved=interleaved)
 
 
+@pytest.mark.parametrize("held,rows,heads,kv_heads,dh,page", [
+    ([0, 100], [0, 9000], 3, 3, 64, 32), ([20] * 70, [i % 7 for i in range(70)], 16, 16, 64, 16), ([1000, 5], [4100, 70], 8, 2, 128, 128)])
+def test_append_many_pages(held, rows, heads, kv_heads, dh, page):
+    # more pages than CTAs fit the GPU, sequences without rows
+    run_append(R.Case(held, rows, heads, kv_heads, dh, page, seed=dh + page, spare_rows=2, before=1), dims=dh)
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("axes,dims", [(1, 64), (2, 64), (3, 64), (3, 16), (2, 48)])
 def test_append_positions(axes, dims, interleaved):

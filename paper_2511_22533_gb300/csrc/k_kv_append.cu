@@ -13,10 +13,11 @@
 // of their own, so heads do not wait for one another.  An angle is a position times a 64-bit
 // fraction of a turn, modulo 2^64: exact modulo a turn, so only the last step (top 32 bits to
 // fp32) rounds, to 2^-25 of a turn.
-// What bounds it: bytes, at 73 % of a plain copy's rate: 32768 tokens of 16 heads of 64 (keys, values and
-// queries, 336 MB) take 67 us, and 513 CTAs, two to an SM, are 1.7 rounds of them.  8192 tokens of 32 and 8 heads of 128 33 us (81 %),
-// eight samples of up to 955 rows 17.6, one token 2.9, 64 tokens of 32 and 8 heads of 128 3.6.  Without the ring, the next
-// head on its way in registers: 76 us, 43, 17.6, 3.3 and 4.0.  Two places or four instead of three: 71 and 68 us.  Three CTAs to an
+// What bounds it: bytes, at 77 % of a plain copy's rate: 32768 tokens of 16 heads of 64 (keys, values and
+// queries, 336 MB) take 64 us, and 513 CTAs, two to an SM, are 1.7 rounds of them.  8192 tokens of 32 and 8 heads of 128 33 us (81 %),
+// eight samples of up to 955 rows 16.8, one token 2.9, 64 tokens of 32 and 8 heads of 128 3.6.  Without the ring, the next
+// head on its way in registers: 76 us, 43, 17.6, 3.3 and 4.0; with it, but two barriers a head, 67 us, 33, 17.6, 2.9 and 3.6, and
+// then two places or four instead of three 71 and 68 us.  Three CTAs to an
 // SM (80 registers): 82 us, and 14.4 for the samples.  Equal shares of all pages' heads for the CTAs that fit the SMs: 72 us, a pause
 // at each change of page.
 #include <algorithm>
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_kv_append(const KvAppendAr
     constexpr int kPlaces = Ring<kUnits>::kPlaces, kPlace = Ring<kUnits>::kPlace;
     extern __shared__ __align__(16) uint4 ring[];  // [places][units][2][threads]: a thread reads what it has brought in itself
     float *const angles = reinterpret_cast<float *>(ring + kPlaces * kPlace);  // cosines, then sines: [tokens][pairs] each
-    __shared__ float tops[kThreads / 32];
+    __shared__ float tops[2][kThreads / 32];  // in turn, so that one barrier a head is enough
     griddep_launch();
     griddep_wait();
     const int slots = a.slots, b = blockIdx.x / slots, slot = blockIdx.x - b * slots, tid = threadIdx.x;
@@ -140,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_kv_append(const KvAppendAr
         __syncthreads();
     }
 
-    int place = 0;
+    int place = 0, turn = 0;
     auto pass = [&](auto kind_tag, int head, int count, uint8_t *pool, uint8_t *scales) {
         constexpr int kKind = decltype(kind_tag)::value;  // 0 keys, 1 values, 2 queries
         if (kKind < 2 && p < 0) return;
@@ -228,10 +229,11 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_kv_append(const KvAppendAr
                 for (int o = threads / 2; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             }
             if (threads > 32) {
-                if ((tid & 31) == 0) tops[tid >> 5] = top;
+                if ((tid & 31) == 0) tops[turn][tid >> 5] = top;
                 asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(threads) : "memory");
                 const int w0 = group * (threads >> 5);
-                for (int w = 0; w < threads >> 5; ++w) top = fmaxf(top, tops[w0 + w]);
+                for (int w = 0; w < threads >> 5; ++w) top = fmaxf(top, tops[turn][w0 + w]);
+                turn ^= 1;
             }
             const uint32_t byte = max(e8m0_byte(top), old);
             if (live) {
@@ -268,9 +270,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_kv_append(const KvAppendAr
                     *reinterpret_cast<uint2 *>(y + e1) = make_uint2(w[2], w[3]);
                 }
             }
-            // all have used the old scale, and the maxima
-            if (threads > 32) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(threads) : "memory");
-            else __syncwarp();
+            // (all have read the old scale before the maxima were joined)
             if (live && own == 0) *scale = (uint8_t)byte;
         }
     };

@@ -249,7 +249,7 @@ extern "C" f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f
     // rows, lengths or pages out of range are recorded here (read by f3dc_gemm_status)
     a.err = gemm_status_word();
     if (!a.err) return fail(F3DC_ERR_CUDA, "cannot resolve the status word");
-    e = kv_many_rows(batch->max_rows, heads, cache->kv_heads) ? launch_kv_attn(a, (cudaStream_t)stream)
+    e = kv_many_rows(batch->max_rows, heads, cache->kv_heads, cache->dh) ? launch_kv_attn(a, (cudaStream_t)stream)
                                                               : launch_kv_few(a, (cudaStream_t)stream);
     return e == cudaSuccess ? F3DC_OK : fail(F3DC_ERR_CUDA, "launch", e);
 }

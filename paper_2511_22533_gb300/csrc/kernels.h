@@ -494,9 +494,13 @@ cudaError_t launch_kv_few(const KvAttnArgs &a, cudaStream_t s);   // few packed 
 cudaError_t launch_kv_attn(const KvAttnArgs &a, cudaStream_t s);  // many
 cudaError_t launch_kv_join(const KvAttnArgs &a, cudaStream_t s);  // adds the parts up (called by both)
 
-// Packed rows from which tensor-memory tiles are taken.  Few / many, us: 15 packed rows (4 sequences of some 30000, heads of
-// 64) 19.1 / 42.6, 16 (16 sequences of 8192, 8 key heads of 128) 77 / 131, 32 (4 sequences of 8192, the same) 46.9 / 42.6.
-inline bool kv_many_rows(int max_rows, int heads, int kv_heads) { return (int64_t)max_rows * (heads / kv_heads) > 16; }
+// Whether tensor-memory tiles are taken: above 32 packed rows, with dh 128 above 16.  Few / many, us, over 8192 tokens: 32 rows,
+// 8 key heads of 64, 4 sequences 23.8 / 39.4, 16 sequences 81.5 / 92.3, 40 rows of 4 41.1 / 41.0, of 16 136 / 94; 32 rows of 16 key heads
+// over 1374 12.9 / 18.1.  With dh 128: 16 rows of 16 sequences 77 / 131, 20 rows 131 / 122, 32 rows of 4 38.8 / 44.4.
+inline bool kv_many_rows(int max_rows, int heads, int kv_heads, int dh)
+{
+    return (int64_t)max_rows * (heads / kv_heads) > (dh == 128 ? 16 : 32);
+}
 
 // Packed rows of a CTA of the few-rows kernel: with dh 128 the sums of 32 do not fit registers.
 inline int kv_few_rows(int64_t rows, int dh) { return rows <= 8 ? 8 : (rows <= 16 || dh == 128 ? 16 : 32); }
@@ -517,7 +521,7 @@ constexpr int kFewLeast = 256, kFewLeastWaves = 2048;
 inline int kv_splits(int batch, int max_rows, int max_length, int heads, int kv_heads, int dh, int sms)
 {
     const int64_t rows = (int64_t)max_rows * (heads / kv_heads);
-    const bool many = kv_many_rows(max_rows, heads, kv_heads);
+    const bool many = kv_many_rows(max_rows, heads, kv_heads, dh);
     const int tile = many ? 256 : kv_few_rows(rows, dh);
     const int64_t blocks = (rows + tile - 1) / tile * kv_heads * batch;
     const int64_t slots = (many ? 1 : kv_few_slots(tile, dh)) * (int64_t)sms;

@@ -79,6 +79,26 @@ def test_attention_of_many_rows(held, rows, heads, kv_heads, dh, page, causal):
 
 
 @pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("held,rows,heads,kv_heads,page", [
+    ([300, 0, 33], [4, 3, 4], 8, 1, 16), ([5000], [32], 2, 2, 64), ([40, 700], [17, 2], 3, 3, 32), ([0], [33], 1, 1, 16),
+    ([129, 2000, 64, 0], [8, 8, 0, 7], 8, 2, 128), ([90], [25], 1, 1, 64)])
+def test_attention_of_some_rows(held, rows, heads, kv_heads, dh, page, causal):
+    # 17 to 33 packed rows, as one part and as several; values and keys of NaN that some rows see
+    c = R.Case(held, rows, heads, kv_heads, dh, page, seed=len(held) + dh + 31, spare_rows=2, before=1)
+    c.fill()
+    run_attend(c, causal)
+    run_attend(c, causal, workspace=False)
+    for b, n in enumerate(c.rows):
+        if n > 2:
+            at = c.lengths[b] - 1
+            c.v[c.table_list[b][at // page], kv_heads - 1, at % page, 3] = R.STALE
+            c.k[c.table_list[b][(at - 1) // page], 0, (at - 1) % page, dh - 1] = R.STALE
+    run_attend(c, causal)
+    run_attend(c, causal, q=queries(c, scale=6.0), workspace=False)
+
+
+@pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("rows,heads,dh,page", [(1537, 40, 64, 64), (1700, 40, 64, 16), (2048, 38, 32, 128), (1920, 40, 32, 32)])
 def test_attention_of_many_rows_for_every_sm(rows, heads, dh, page, causal):
     # launches that fill the GPU with larger blocks of rows, the last of one row to a whole one; NaN beside them

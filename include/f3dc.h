@@ -367,7 +367,7 @@ f3dc_status f3dc_gemm_noalloc(const void *A, const void *B, const void *bias, co
 
 /* Reads and clears the current device's status word of the standalone
  * kernel calls (f3dc_gemm, f3dc_gemm_noalloc, f3dc_attention, f3dc_gemm_fp8,
- * f3dc_norm_residual): F3DC_DEV_* bits recorded by their kernels since the last
+ * f3dc_norm_residual, f3dc_kv_append_fp8, f3dc_kv_attention_fp8): F3DC_DEV_* bits recorded by their kernels since the last
  * read, e.g. F3DC_DEV_TIMEOUT when a bounded wait ran out and part of the output
  * was left unwritten.
  * Synchronizes the device first.
@@ -559,7 +559,7 @@ typedef struct f3dc_kv_batch {
     int32_t batch;             /* sequences, >= 0 */
     int32_t rows;              /* packed rows, >= 0: row_start[batch] <= rows */
     int32_t max_rows;          /* no sequence has more rows */
-    int32_t max_length;        /* nor is longer */
+    int32_t max_length;        /* nor is longer: at most 2^31 - 1025 */
 } f3dc_kv_batch;
 
 /* Rotation of queries and keys by their positions.  Pair j < dims / 2 of a head is
@@ -598,7 +598,8 @@ f3dc_status f3dc_kv_append_fp8(const f3dc_kv_cache *cache, const f3dc_kv_batch *
                                void *q_out, int64_t ldqo, int32_t heads, const int32_t *positions, void *stream);
 
 /* Bytes of workspace with which f3dc_kv_attention_fp8 shares long sequences out over
- * the SMs for a batch within these bounds (0: it needs none, or invalid arguments).  Reads the current device's SM count. */
+ * the SMs for a batch within these bounds (0: it needs none, or invalid arguments).  Reads the
+ * current device's SM count. */
 size_t f3dc_kv_attention_workspace(const f3dc_kv_cache *cache, const f3dc_kv_batch *batch, int32_t heads);
 
 /* Attention of packed query rows over their sequences' cached tokens, head h reading
@@ -606,8 +607,10 @@ size_t f3dc_kv_attention_workspace(const f3dc_kv_cache *cache, const f3dc_kv_bat
  *   out[r, h] = sum_t p_t v_t,  p = softmax(scale q[r, h] . k_t)
  * over the sequence's tokens t < lengths[b], with `causal` t <= lengths[b] - n_b + i for its
  * row i.  A row that sees no token gets zeros (lse -infinity).  What lies behind a sequence's length or is
- * masked counts for nothing, NaN included.  Sums and statistics are fp32;
- * softmax weights are rounded to fp16 relative to a row's largest weight times value scale.
+ * masked counts for nothing, NaN included; a NaN value that a row sees makes that element NaN, a NaN key all of
+ * the row.  Sums and statistics are fp32.  Softmax weights, times their page's value scale, are rounded to fp16: by at most 2^-11
+ * of themselves or 2^-25 of the row's largest.  Values of pages whose v_scales byte is below 63 (magnitudes
+ * below 2^-55) count as zeros.
  *   q: device bf16 [rows, heads dh], row stride ldq; out: the same, row stride ldo;
  *   lse: device fp32 [rows, heads] contiguous, nullable: ln sum exp(scale q . k_t);
  *   heads: a multiple of Hk; scale > 0;

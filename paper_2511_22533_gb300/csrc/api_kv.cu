@@ -156,7 +156,8 @@ extern "C" f3dc_status f3dc_kv_append_fp8(const f3dc_kv_cache *cache, const f3dc
     if (!k || !v) return bad("null pointer");
     if (misaligned(k, 16) || misaligned(v, 16) || misaligned(q, 16) || (q && misaligned(q_out, 16)))
         return bad("pointers must be 16-byte aligned");
-    if ((((int64_t)batch->max_rows + cache->page_tokens - 2) / cache->page_tokens + 1) * batch->batch > INT32_MAX)
+    if ((((int64_t)batch->max_rows + cache->page_tokens - 2) / cache->page_tokens + 1) * batch->batch > INT32_MAX ||
+        batch->max_length > INT32_MAX - 1024)
         return bad("the problem is too large");
     int sms = 0;
     cudaError_t e = sm_count(&sms);

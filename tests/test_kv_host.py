@@ -68,7 +68,8 @@ BOTH = [
     (dict(rotary=dict(dims=80)), b"dims"), (dict(rotary=dict(interleaved=2)), b"interleaved"), (dict(rotary=dict(axes=0)), b"axes"),
     (dict(rotary=dict(axes=4)), b"axes"), (dict(rotary=dict(axes=2)), b"positions"), (dict(rotary=dict(turns=None)), b"turns"),
     (dict(rotary=dict(turns=P + 4)), b"turns"), (dict(positions=P + 1), b"positions"), (dict(rotary=None, q=None, positions=P), b"positions"),
-    (dict(v=P + 2), b"aligned"), (dict(q_out=P + 2), b"aligned")])
+    (dict(v=P + 2), b"aligned"), (dict(q_out=P + 2), b"aligned"), (dict(batch=dict(max_length=2 ** 31 - 1)), b"too large"),
+    (dict(batch=dict(max_length=2 ** 31 - 1000)), b"too large")])
 def test_append_refusals(L, kw, needle):
     assert append(L, **kw) == 1
     assert needle in L.f3dc_last_error(None)

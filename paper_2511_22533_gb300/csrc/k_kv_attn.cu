@@ -27,9 +27,9 @@
 // 3000 clocks a pair of tiles.  32768 x 32768, 16 heads of 64: 4.98 ms = 881 TFLOP/s; causal 8192 x 8192, 32 heads of
 // 128 to 8: 502 us = 1096 TFLOP/s; 1229 x 1374, 16 heads of 64: 29 us, of which 8 before the first and behind the last step.
 // Steps that led here, prompt of 8192 / 32768 x 32768: one step of 128 tokens, its maximum always taken 872 us / 6.8 ms; no
-// maximum, pages looked up by a warp of their own 567 / -; steps of 64 in two places 497 / 5.3; queries in TMEM and two steps
-// without a jump between them 502 / 4.98.  Measured slower: three places of S (117 us instead of 117, but no room for the queries), P waited
-// for in the next step, more registers for softmax at the cost of the converting warps.
+// maximum, pages looked up by a warp of their own, steps of 64 in two places 505 / 5.24 (steps of 128 held in registers 567); queries
+// in TMEM and two steps without a jump between them 502 / 4.98.  Three places of S made no difference and leave no room for the
+// queries.
 #include "kv.cuh"
 
 namespace f3dc {

@@ -615,7 +615,8 @@ size_t f3dc_kv_attention_workspace(const f3dc_kv_cache *cache, const f3dc_kv_bat
  *   lse: device fp32 [rows, heads] contiguous, nullable: ln sum exp(scale q . k_t);
  *   heads: a multiple of Hk; scale > 0;
  *   workspace: device bytes, 16-byte aligned, nullable: with fewer than
- *     f3dc_kv_attention_workspace() bytes (none at all) a long sequence is shared by fewer SMs.
+ *     f3dc_kv_attention_workspace() bytes (none at all) a long sequence is shared by fewer SMs
+ *     (of few rows, by up to 8).
  *   Pointers 16-byte aligned, row strides multiples of 8. */
 f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f3dc_kv_batch *batch, const void *q, int64_t ldq,
                                   void *out, int64_t ldo, float *lse, int32_t heads, float scale, int32_t causal,

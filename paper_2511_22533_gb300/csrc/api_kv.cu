@@ -96,10 +96,11 @@ int64_t part_bytes(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads
 }
 
 // CTAs that share a sequence's keys
-int splits(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads, int sms)
+int splits(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads, int sms, bool *cluster)
 {
+    *cluster = false;
     if (empty(t)) return 1;
-    return kv_splits(t->batch, t->max_rows, t->max_length, heads, c->kv_heads, c->dh, sms);
+    return kv_splits(t->batch, t->max_rows, t->max_length, heads, c->kv_heads, c->dh, sms, cluster);
 }
 
 }  // namespace
@@ -196,8 +197,9 @@ extern "C" size_t f3dc_kv_attention_workspace(const f3dc_kv_cache *cache, const 
     if (cache_shape(cache) || batch_shape(batch) || heads < 1 || heads % cache->kv_heads || heads > 65536) return 0;
     int sms = 0;
     if (sm_count(&sms) != cudaSuccess) return 0;
-    const int n = splits(cache, batch, heads, sms);
-    return n > 1 ? (size_t)(n * part_bytes(cache, batch, heads)) : 0;
+    bool cluster = false;
+    const int n = splits(cache, batch, heads, sms, &cluster);
+    return n > 1 && !cluster ? (size_t)(n * part_bytes(cache, batch, heads)) : 0;
 }
 
 extern "C" f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f3dc_kv_batch *batch, const void *q,
@@ -240,17 +242,20 @@ extern "C" f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f
     a.group = group;
     a.causal = causal;
     a.scale_log2 = (float)(scale * 1.4426950408889634);
-    a.splits = 1;
-    if (workspace) {
-        const int64_t fit = (int64_t)(workspace_bytes / (size_t)part_bytes(cache, batch, heads));
-        const int n = splits(cache, batch, heads, sms);
-        a.splits = n < fit ? n : (fit > 1 ? (int)fit : 1);
-        a.part = (float *)workspace;
+    const bool many = kv_many_rows(batch->max_rows, heads, cache->kv_heads, cache->dh);
+    bool cluster = false;
+    a.splits = splits(cache, batch, heads, sms, &cluster);
+    if (!cluster && a.splits > 1) {
+        // without the whole workspace as many parts as fit it or, of few rows, as a cluster joins
+        const int64_t fit = workspace ? (int64_t)(workspace_bytes / (size_t)part_bytes(cache, batch, heads)) : 0;
+        const int least = many ? 1 : (a.splits < kMostCluster ? a.splits : kMostCluster);
+        if (fit < a.splits) a.splits = fit > least ? (int)fit : least, cluster = !many && fit <= least;
     }
+    a.cluster = cluster;
+    a.part = (float *)workspace;
     // rows, lengths or pages out of range are recorded here (read by f3dc_gemm_status)
     a.err = gemm_status_word();
     if (!a.err) return fail(F3DC_ERR_CUDA, "cannot resolve the status word");
-    e = kv_many_rows(batch->max_rows, heads, cache->kv_heads, cache->dh) ? launch_kv_attn(a, (cudaStream_t)stream)
-                                                              : launch_kv_few(a, (cudaStream_t)stream);
+    e = many ? launch_kv_attn(a, (cudaStream_t)stream) : launch_kv_few(a, (cudaStream_t)stream);
     return e == cudaSuccess ? F3DC_OK : fail(F3DC_ERR_CUDA, "launch", e);
 }

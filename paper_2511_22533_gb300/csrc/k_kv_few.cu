@@ -13,7 +13,7 @@
 // keeps sums and references of its own, which are joined at the end.
 // One token of 32 heads of 128 to 8 key heads over 524288: 167 us (6.4 TB/s, 95 % of a plain copy's rate); 64 sequences' tokens over
 // 4096 to 8192: 136 us (6.0 TB/s), where the lengths leave some SMs idle at the end; one token over 1374 of 16 heads of 64:
-// 7.2 us, two launches and the latencies of page table, pages and parts.  With query rows as the MMA's rows, and parts joined by
+// 5.7 us, the launch and the latencies of page table, pages and the cluster.  With query rows as the MMA's rows, and parts joined by
 // a warp one after another: 224, 190 and 13 us.
 #include "kv.cuh"
 
@@ -79,7 +79,9 @@ F3DC_DEV uint32_t half2_numbers(uint32_t a)
 }
 
 // NT: tiles of 8 packed rows
-template <int DH, int NT>
+// CLUSTER: the CTAs of a sequence's keys are a cluster and join their sums themselves.  (A form of its own: in one with the other it cost
+// calls without a cluster 2 %.)
+template <int DH, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
 {
     using Cfg = FewCfg<DH>;
@@ -88,6 +90,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
     extern __shared__ uint4 smem4[];
     uint8_t *const smem = reinterpret_cast<uint8_t *>(smem4);
     __shared__ float sm_m[kWarps][kRows], sm_l[kWarps][kRows];
+    __shared__ float2 sm_ml[kRows];
     griddep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
 
@@ -429,7 +432,19 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
                     make_float4(acc[n][j][r], acc[n][j][2 + r], acc[n][j + 1][r], acc[n][j + 1][2 + r]);
         }
     __syncthreads();
-    for (int i = threadIdx.x; i < (row_end - r0) * (DH / 8); i += 32 * kWarps) {
+    const int items = (row_end - r0) * (DH / 8);  // eight elements of a row each
+    auto write = [&](int row, int col, float m, float l, const float (&o)[8]) {
+        const int token = (r0 + row) / a.group, head = hk * a.group + (r0 + row) % a.group;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        uint4 u;
+        u.x = pack_bf16x2(o[0] * inv, o[1] * inv);
+        u.y = pack_bf16x2(o[2] * inv, o[3] * inv);
+        u.z = pack_bf16x2(o[4] * inv, o[5] * inv);
+        u.w = pack_bf16x2(o[6] * inv, o[7] * inv);
+        *reinterpret_cast<uint4 *>(a.out + (int64_t)(s.row0 + token) * a.ldo + (int64_t)head * DH + col) = u;
+        if (a.lse && col == 0) a.lse[(int64_t)(s.row0 + token) * a.heads + head] = log_sum(m, l);
+    };
+    for (int i = threadIdx.x; i < items; i += 32 * kWarps) {
         const int row = i / (DH / 8), col = i % (DH / 8) * 8;
         float m = sm_m[0][row];
 #pragma unroll
@@ -444,19 +459,17 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = fmaf(x[e], by, o[e]);
         }
-        const int token = (r0 + row) / a.group, head = hk * a.group + (r0 + row) % a.group;
-        const int64_t at = (int64_t)(s.row0 + token) * a.heads + head;
         if (a.splits == 1) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            uint4 u;
-            u.x = pack_bf16x2(o[0] * inv, o[1] * inv);
-            u.y = pack_bf16x2(o[2] * inv, o[3] * inv);
-            u.z = pack_bf16x2(o[4] * inv, o[5] * inv);
-            u.w = pack_bf16x2(o[6] * inv, o[7] * inv);
-            *reinterpret_cast<uint4 *>(a.out + (int64_t)(s.row0 + token) * a.ldo + (int64_t)head * DH + col) = u;
-            if (a.lse && col == 0) a.lse[at] = log_sum(m, l);
+            write(row, col, m, l, o);
+        } else if (CLUSTER) {
+            // (the first warp's place, read by this thread alone)
+            float *dst = sums + row * DH + col;
+            *reinterpret_cast<float4 *>(dst) = make_float4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<float4 *>(dst + 4) = make_float4(o[4], o[5], o[6], o[7]);
+            if (col == 0) sm_ml[row] = make_float2(m, l);
         } else {
-            const int64_t part = (int64_t)split * a.batch.rows * a.heads + at;
+            const int token = (r0 + row) / a.group, head = hk * a.group + (r0 + row) % a.group;
+            const int64_t part = (int64_t)split * a.batch.rows * a.heads + (int64_t)(s.row0 + token) * a.heads + head;
             float *dst = a.part + part * DH + col;
             *reinterpret_cast<float4 *>(dst) = make_float4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<float4 *>(dst + 4) = make_float4(o[4], o[5], o[6], o[7]);
@@ -465,6 +478,43 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
                 ml[part] = make_float2(m, l);
             }
         }
+    }
+    if constexpr (CLUSTER) {
+        // each CTA joins some of the rows' elements from all CTAs' shared memory
+        __syncwarp();
+        cluster_sync();
+        for (int i = threadIdx.x + 32 * kWarps * split; i < items; i += 32 * kWarps * a.splits) {
+            const int row = i / (DH / 8), col = i % (DH / 8) * 8;
+            const uint32_t ml_own = smem_u32(sm_ml + row), o_own = smem_u32(sums + row * DH + col);
+            float2 p[kMostCluster];
+            float4 v[kMostCluster][2];
+            float m = -kInf;
+#pragma unroll
+            for (int k = 0; k < kMostCluster; ++k) {
+                p[k] = make_float2(-kInf, 0.f);
+                v[k][0] = v[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k < a.splits) {
+                    const uint32_t from = mapa_shared(o_own, k);
+                    p[k] = load_cluster8(mapa_shared(ml_own, k));
+                    v[k][0] = load_cluster16(from);
+                    v[k][1] = load_cluster16(from + 16);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kMostCluster; ++k) m = fmaxf(m, p[k].x);
+            float l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < kMostCluster; ++k) {
+                const float by = p[k].x == -kInf ? 0.f : exp2_fast(p[k].x - m);
+                l += p[k].y == 0.f ? 0.f : p[k].y * by;
+                const float x[8] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w, v[k][1].x, v[k][1].y, v[k][1].z, v[k][1].w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = fmaf(x[e], by, o[e]);
+            }
+            write(row, col, m, l, o);
+        }
+        __syncwarp();
+        cluster_sync();  // no CTA leaves while another reads its shared memory
     }
 }
 
@@ -539,7 +589,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_kv_join(const KvAttnArgs a)
     if (a.lse && threadIdx.x == 0) a.lse[at] = log_sum(top, total);
 }
 
-template <int DH, int NT>
+template <int DH, int NT, bool CLUSTER>
 cudaError_t launch_few(const KvAttnArgs &args, cudaStream_t s)
 {
     KvAttnArgs a = args;
@@ -547,17 +597,38 @@ cudaError_t launch_few(const KvAttnArgs &args, cudaStream_t s)
     const int64_t ctas = (int64_t)a.splits * a.row_blocks * a.cache.heads * a.batch.batch;
     if (ctas > INT32_MAX) return cudaErrorInvalidValue;
     static std::atomic<uint64_t> devices{0};
-    cudaError_t e = ask_smem(k_kv_few<DH, NT>, FewCfg<DH>::kSmem, devices);
+    cudaError_t e = ask_smem(k_kv_few<DH, NT, CLUSTER>, FewCfg<DH>::kSmem, devices);
     if (e != cudaSuccess) return e;
-    e = launch_k(k_kv_few<DH, NT>, dim3((unsigned)ctas), dim3(32 * kWarps), FewCfg<DH>::kSmem, s, a);
-    return e != cudaSuccess || a.splits == 1 ? e : launch_kv_join(a, s);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(32 * kWarps);
+    cfg.dynamicSmemBytes = FewCfg<DH>::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)a.splits;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = CLUSTER ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, k_kv_few<DH, NT, CLUSTER>, a);
+    return e != cudaSuccess || CLUSTER || a.splits == 1 ? e : launch_kv_join(a, s);
+}
+
+template <int DH, bool CLUSTER>
+cudaError_t launch_tile(const KvAttnArgs &a, cudaStream_t s)
+{
+    const int tile = kv_few_rows((int64_t)a.batch.max_rows * a.group, DH);
+    return tile == 8 ? launch_few<DH, 1, CLUSTER>(a, s)
+                     : (tile == 16 ? launch_few<DH, 2, CLUSTER>(a, s) : launch_few<DH, DH == 128 ? 2 : 4, CLUSTER>(a, s));
 }
 
 template <int DH>
 cudaError_t launch_dh(const KvAttnArgs &a, cudaStream_t s)
 {
-    const int tile = kv_few_rows((int64_t)a.batch.max_rows * a.group, DH);
-    return tile == 8 ? launch_few<DH, 1>(a, s) : (tile == 16 ? launch_few<DH, 2>(a, s) : launch_few<DH, DH == 128 ? 2 : 4>(a, s));
+    return a.cluster ? launch_tile<DH, true>(a, s) : launch_tile<DH, false>(a, s);
 }
 
 }  // namespace

@@ -72,6 +72,19 @@ F3DC_DEV void cp_async_wait()
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// 16 and 8 bytes of the shared memory of a CTA of the cluster
+F3DC_DEV float4 load_cluster16(uint32_t cluster_addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
+    return v;
+}
+F3DC_DEV float2 load_cluster8(uint32_t cluster_addr)
+{
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_addr) : "memory");
+    return v;
+}
 // four e4m3 values to two pairs of fp16 (exact)
 F3DC_DEV void e4m3x4_to_half2(uint32_t w, uint32_t &h0, uint32_t &h1)
 {

@@ -253,6 +253,23 @@ def test_with_and_without_workspace(rows):
     R.check_attend(c, out, lse, q, 0.125, True)
 
 
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("held,rows,heads,kv_heads,page", [
+    ([1500], [1], 16, 16, 64), ([700, 2500, 0, 31], [1, 5, 8, 2], 4, 4, 16), ([3000] * 4, [2, 0, 1, 2], 32, 16, 32), ([2600], [11], 2, 1, 128),
+    ([30000, 1], [1, 1], 3, 3, 64)])
+def test_sums_joined_in_a_cluster(held, rows, heads, kv_heads, dh, page):
+    # shares of a sequence that need no workspace, some of no tokens; NaN in one share alone
+    c = R.Case(held, rows, heads, kv_heads, dh, page, seed=dh + 41, spare_rows=1, before=1)
+    c.fill()
+    one, _ = run_attend(c, True, workspace=False)
+    two, _ = run_attend(c, True, workspace=False)
+    assert torch.equal(one, two)
+    c.v[c.table_list[0][3], 0, 7, dh - 1] = R.STALE
+    c.k[c.table_list[0][5], kv_heads - 1, 2, 0] = R.STALE
+    run_attend(c, True, workspace=False)
+    run_attend(c, False)
+
+
 @pytest.mark.parametrize("rows", [1, 130])
 def test_same_call_same_bits(rows):
     c = R.Case([3000, 500, 77], [rows] * 3, 8, 2, 128, 16, seed=8)

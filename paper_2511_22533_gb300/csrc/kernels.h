@@ -516,13 +516,15 @@ inline int kv_few_slots(int tile, int dh)
 // 1374 5.7 us, with 256 6.4, 512 9.9; over 8192 8.9, with 256 9.1; over 131072 47.0 us, with twice as many CTAs as fit 51.5); where
 // sequences and heads alone nearly fill the SMs, four times as many as fit, each with at least kFewLeastWaves, so that sequences of
 // different lengths even out (64 of 4096 to 8192 136 us, unshared 143; 16 of 4096, 16 heads of 64, 32.0 us, unshared 38.8, with 256
-// tokens at least 39.8).  Many rows: no more than one for every SM.
+// tokens at least 39.8).  Many rows: no more than one
+// for every SM, each with at least kManyLeast tokens (64 rows over 1374, 16 heads of 64, 15.9 us, with 512 18.1; 256 rows 20.8 and 22.2,
+// 700 rows behind 3000 tokens, 4 heads, 20.7 and 23.0).
 // Up to 8 CTAs (12 become 8) of few rows are a cluster and join their sums in shared memory, without a workspace and a second launch:
 // one token over 1374 6.4 us instead of 7.2, 16 rows of 16 sequences of 8192 41 instead of 47, 4 tokens over 3000 9.6 instead of 10.5.
 // Not where they would fill the SMs, since clusters that do not find room in what is left wait for a whole round (8 tokens over up
 // to 8192, 448 CTAs in 456 places: 29 us instead of 24), nor in several rounds of single rows, whose sums are small (64 of 4096
 // to 8192 138 us instead of 136; but 32 rows of 16 sequences of 8192 73 instead of 82).
-constexpr int kFewLeast = 192, kFewLeastWaves = 2048;
+constexpr int kFewLeast = 192, kFewLeastWaves = 2048, kManyLeast = 256;
 constexpr int kMostCluster = 8;
 inline int kv_splits(int batch, int max_rows, int max_length, int heads, int kv_heads, int dh, int sms, bool *cluster)
 {
@@ -531,7 +533,7 @@ inline int kv_splits(int batch, int max_rows, int max_length, int heads, int kv_
     const int tile = many ? 256 : kv_few_rows(rows, dh);
     const int64_t blocks = (rows + tile - 1) / tile * kv_heads * batch;
     const int64_t slots = (many ? 1 : kv_few_slots(tile, dh)) * (int64_t)sms;
-    int64_t n = slots / blocks, least = many ? 512 : kFewLeast;
+    int64_t n = slots / blocks, least = many ? kManyLeast : kFewLeast;
     const bool waves = !many && n < 3;
     if (waves) n = (4 * slots + blocks - 1) / blocks, least = kFewLeastWaves;
     if (n > max_length / least) n = max_length / least;

@@ -55,6 +55,8 @@ constexpr float kTop = 3.f, kMostSum = 60000.f;
 // and the scales of its NB blocks of 128 / NB tokens (a page has at least one).
 template <int NB>
 struct StepScales {  // of half a tile
+    // (Where a value scale is more than kScaleSpan below the largest so far, value_log2 is infinity: the sum of a plain step then sends it
+    // to the careful form, which has the scales from value_inverse.)
     float key[NB / 2], value_log2[NB / 2], value_inverse[NB / 2];
 };
 template <int NB>
@@ -79,7 +81,7 @@ struct Cfg {
     // and takes 48 clocks instead of 32.
     static constexpr bool kQTmem = DH < 128;
     static constexpr uint32_t kColQ = 2 * 64 * kPlaces + 2 * DH;
-    static constexpr size_t kSmem = 1024 + (size_t)kTile * (2 + 2 * kStages) + kGroups * kGroup * sizeof(TileInfo<NB>) + 576;
+    static constexpr size_t kSmem = 1024 + (size_t)kTile * (2 + 2 * kStages) + kGroups * kGroup * sizeof(TileInfo<NB>) + 256 * sizeof(float2) + 576;
     static constexpr uint32_t kColO = 2 * 64 * kPlaces;
     static_assert(kColO + 2 * DH + (kQTmem ? DH : 0) <= 512, "TMEM layout");
     // byte of 16-byte piece `piece` (8 columns) of a row
@@ -271,6 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
             const int run = lane & 7;
             const uint32_t stride16 = (uint32_t)(a.cache.page_stride >> 4);
             const uint32_t own16 = (uint32_t)(hk * page + (16 * run & (page - 1))) * (DH / 16);
+            int widest = kLeastScale;
 #pragma unroll 1
             for (int g0 = 0, n = 0; g0 < n_tiles; g0 += kGroup, ++n) {
                 const int g = g0 + (lane >> 3), t0 = (g_begin + g) * 128 + 16 * run;
@@ -291,6 +294,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                 const ValueScale v = value_scale(bytes >> 8);
                 const uint32_t tile = 0xFFu << (lane & 24);
                 const uint32_t complete = __ballot_sync(0xffffffffu, there == 16), plain = __ballot_sync(0xffffffffu, v.times == kHalfOnes);
+                // (the largest of all four tiles: one that comes later does no harm)
+                widest = max(widest, __reduce_max_sync(0xffffffffu, (int)v.log2));
+                const uint32_t apart = __ballot_sync(0xffffffffu, (int)v.log2 < widest - kScaleSpan);
                 if (mine) {
                     TileInfo<NB> &x = infos[slot * kGroup + (lane >> 3)];
                     x.at[run] = at;
@@ -300,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                         StepScales<NB> &sc = x.scales[run >> 2];
                         const int k = (run & 3) * NB / 8;
                         sc.key[k] = key_scale(bytes & 255u);
-                        sc.value_log2[k] = v.log2;
+                        sc.value_log2[k] = apart & tile ? kInf : v.log2;
                         sc.value_inverse[k] = v.inverse;
                     }
                     if (run == 0) {
@@ -537,8 +543,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
             StepScales<NB> x = {};  // of the step
             bool early = false;  // its S_t is known to be written
             // Step j, in place i (phase `phase`) of S and P.  Careful: with its maximum (of the tokens that the row sees): the first step,
-            // those seen in part, and those whose weights ran away from the reference; O_t and l are rescaled where it is taken
-            // anew.  Plain ones take the reference as it stands; where the sum of weights says that one may have left its
+            // those seen in part, and those whose weights ran away from the reference or whose value scales lie far apart; O_t and l
+            // are rescaled where it is taken anew.  Plain ones take the reference as it stands; where the sum of weights says that one may have left its
             // range they return 0, and the step is done again, carefully (1: done, -1: the kernel is aborting).  What the next step
             // begins with (whether its S_t is written, its scales) is asked for under this one's exponents: a warp's own
             // latencies are what bounds it.
@@ -580,9 +586,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                         // (all rows of the warp, by what they have seen: the next one will be long in coming)
                         const float seen = fmaxf(ref, ref + __log2f(peak) - (kTop + 3.f));
                         const float to = fmaxf(seen, mx - kTop);
-                        const float by = ref == -kInf ? 0.f : exp2_fast(ref - to);
+                        const float half = half_factor(ref, to), by = half * half;
                         ref = to;
-                        l_run *= by;
+                        l_run = l_run * half * half;
                         peak *= by;
                         if (j > 0) {
                             if (!product_done(j - 1)) return -1;
@@ -616,33 +622,82 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
             // 40 % slower with warps that had left the others' pace by a careful step.)
             bool ok = true, again = true;
             int j = 0;
+            // Steps with value scales far apart: the sum of their weights without value scales, (largest score, sum against it) of the
+            // row, which has taken in step `summed`; the careful form adds nothing for them.  What finds it stands behind the loop and in
+            // shared memory: between the other steps' code or in their registers it costs all of them 4 to 7 %.
+            float2 *const apart = reinterpret_cast<float2 *>(infos + kGroups * kGroup) + (threadIdx.x - 256);
+            int summed = -1;
 #pragma unroll 1
-            while (ok && j < n_steps) {
-                const int group = j / kGroupSteps % kGroups, u = j % kGroupSteps;
-                if (u == 0 && !(ok = wait(&i_full[group], (j / (kGroupSteps * kGroups)) & 1))) break;
-                const uint32_t phase = (j / C::kPlaces) & 1;
-                const StepScales<NB> *const own = infos[(j >> 1) % (kGroup * kGroups)].scales;
-                x = own[j & 1];
-                int r;
-                if (again || j >= whole) {
-                    r = step(j, j % C::kPlaces, phase, x, std::true_type());
-                    if (r == 1) ++j;
-                } else {
-                    static_assert(C::kPlaces == 2, "an even step is in the first place");
-                    r = 1;
-                    if ((j & 1) == 0) {
-                        r = step(j, 0, phase, own[1], std::false_type());
+            while (true) {
+#pragma unroll 1
+                while (ok && j < n_steps) {
+                    const int group = j / kGroupSteps % kGroups, u = j % kGroupSteps;
+                    if (u == 0 && !(ok = wait(&i_full[group], (j / (kGroupSteps * kGroups)) & 1))) break;
+                    const uint32_t phase = (j / C::kPlaces) & 1;
+                    const StepScales<NB> *const own = infos[(j >> 1) % (kGroup * kGroups)].scales;
+                    x = own[j & 1];
+                    int r;
+                    if (again || j >= whole) {
+                        if (x.value_log2[0] == kInf) {
+                            if (summed < j) break;
+#pragma unroll
+                            for (int k = 0; k < kBlocks; ++k) {
+                                x.value_log2[k] = 127.f - (float)(__float_as_uint(x.value_inverse[k]) >> 23);
+                                x.value_inverse[k] = 0.f;
+                            }
+                        }
+                        r = step(j, j % C::kPlaces, phase, x, std::true_type());
                         if (r == 1) ++j;
+                    } else {
+                        static_assert(C::kPlaces == 2, "an even step is in the first place");
+                        r = 1;
+                        if ((j & 1) == 0) {
+                            r = step(j, 0, phase, own[1], std::false_type());
+                            if (r == 1) ++j;
+                        }
+                        if (r == 1 && j < whole) {
+                            // (the scales of the step after are another tile's, perhaps another group's: read when it begins)
+                            r = step(j, 1, phase, own[1], std::false_type());
+                            if (r == 1) ++j;
+                        }
                     }
-                    if (r == 1 && j < whole) {
-                        // (the scales of the step after are another tile's, perhaps another group's: read when it begins)
-                        r = step(j, 1, phase, own[1], std::false_type());
-                        if (r == 1) ++j;
+                    again = r == 0;
+                    ok = r >= 0;
+                    if (r == 1 && j % kGroupSteps == 0) mbar_arrive_if(smem_u32(&i_empty[group]), lane == 0);
+                }
+                if (!ok || j >= n_steps) break;
+                if (!early && !(ok = wait(s_full + C::kPlaces * t + j % C::kPlaces, (j / C::kPlaces) & 1))) break;
+                early = true;
+                tc_fence_after();
+                const float *const key = infos[(j >> 1) % (kGroup * kGroups)].scales[j & 1].key;
+                const int valid = sees - (2 * g_begin + j) * 64;
+                // the scores of step j twice: their maximum, their sum
+                float top = -kInf, sum = 0.f;
+                if (summed >= 0) top = apart->x, sum = apart->y;
+                const float before = top;
+#pragma unroll 1
+                for (int c0 = 0; c0 < 128; c0 += 16) {
+                    if (c0 == 64) {
+                        const float half = half_factor(before, top);
+                        sum = sum * half * half;
+                    }
+                    uint32_t sc[16];
+                    tmem_ld16(s_addr0 + 64 * (j % C::kPlaces) + c0 % 64, sc);
+                    tmem_wait_ld();
+                    const float f = factor * key[c0 % 64 / kBlock], base = top == -kInf ? 0.f : -top;
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        if (c0 % 64 + c >= valid) continue;
+                        if (c0 < 64) top = fmaxf(top, __uint_as_float(sc[c]) * f);
+                        else sum += exp2_fast(fmaf(__uint_as_float(sc[c]), f, base));
                     }
                 }
-                again = r == 0;
-                ok = r >= 0;
-                if (r == 1 && j % kGroupSteps == 0) mbar_arrive_if(smem_u32(&i_empty[group]), lane == 0);
+                *apart = make_float2(top, sum);
+                summed = j;
+            }
+            if (summed >= 0 && apart->y != 0.f) {
+                const float half = exp2_fast(0.5f * (apart->x - ref));
+                l_run += apart->y * half * half;
             }
             if (ok && n_steps > 0) {
                 // (v_full: nan_flag is what the converting warps left)

@@ -202,6 +202,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
     // sums O^T: element (column, row): acc[n][j][e] of column g DH / 8 + 2 j + e / 2 and row 8 n + 2 q + e % 2
     float acc[NT][kSteps][4];
     float ref[NT][2], sum[NT][2];
+    float widest = (float)kLeastScale;  // largest value scale so far
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -212,20 +213,11 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
         sum[n][0] = sum[n][1] = 0.f;
     }
 
-    int slot = 0;
-#pragma unroll 1
-    for (int c = c0; c < c_end; c += kWarps) {
-        cp_async_wait<kStages - 2>();
-        __syncwarp();
-        const uint32_t scale = scales[0];
-#pragma unroll
-        for (int i = 0; i < kStages - 2; ++i) scales[i] = scales[i + 1];
-        const int next = c + (kStages - 1) * kWarps, next_slot = slot == 0 ? kStages - 1 : slot - 1;
-        scales[kStages - 2] = load(next, next_slot);
-        look_up(next + kWarps);
-
+    // Chunk c, whose keys and values stand at `keys`.  Plain: returns false, with nothing done, where a value scale is too far below the
+    // largest so far; such a chunk is done in the other form.
+    auto chunk = [&](int c, uint32_t scale, int slot, auto apart_tag) {
+        constexpr bool kApart = decltype(apart_tag)::value;
         const uint8_t *const keys = ring + slot * Cfg::kStage, *const values = keys + Cfg::kHalf;
-        slot = slot + 1 == kStages ? 0 : slot + 1;
         const int t0 = c * kChunk;
 
         // S^T: 16 tokens by 8 rows each: x[n][h][e] of row 2 q + e % 2 and token 16 h + 8 (e / 2) + 4 (g & 1) + (g >> 1)
@@ -272,7 +264,12 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
         }
         const bool partly = t0 + kChunk > least;
         const int own_token = t0 + 4 * (g & 1) + (g >> 1);
-        bool raise = false;
+        widest = fmaxf(widest, fmaxf(vs[0].log2, vs[1].log2));
+        const bool apart = !kApart && fminf(vs[0].log2, vs[1].log2) < widest - kScaleSpan;  // (the same for the warp)
+        // (dh 128: looked at with the vote below.  A branch of its own costs 4 rows of 16 sequences of 8192 6 %, and the vote's costs heads of
+        // 64 and 32 3 % and more.)
+        if (DH < 128 && __builtin_expect(apart, 0)) return false;
+        bool raise = DH == 128 && apart;
         float top[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -294,14 +291,15 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
                 raise |= t > ref[n][r] + (kTop + kLazy);
             }
         if (__any_sync(0xffffffffu, raise)) {
+            if (DH == 128 && apart) return false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const float to = fmaxf(ref[n][r], top[n][r] - kTop);
-                    const float by = ref[n][r] == -kInf ? 0.f : exp2_fast(ref[n][r] - to);
+                    const float half = half_factor(ref[n][r], to), by = half * half;
                     ref[n][r] = to;
-                    sum[n][r] *= by;
+                    sum[n][r] = sum[n][r] * half * half;
 #pragma unroll
                     for (int j = 0; j < kSteps; ++j) {
                         acc[n][j][r] *= by;
@@ -319,7 +317,14 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) p[e] = exp2_fast(x[n][h][e] + base[e & 1]);
 #pragma unroll
-                for (int r = 0; r < 2; ++r) sum[n][r] = fmaf(p[r] + p[2 + r], vs[h].inverse, sum[n][r]);
+                for (int r = 0; r < 2; ++r) {
+                    if (kApart) {
+                        const float at = base[r] - vs[h].log2 + kSumShift;
+                        sum[n][r] = fmaf(exp2_fast(x[n][h][r] + at) + exp2_fast(x[n][h][2 + r] + at), kSumUnshift, sum[n][r]);
+                    } else {
+                        sum[n][r] = fmaf(p[r] + p[2 + r], vs[h].inverse, sum[n][r]);
+                    }
+                }
                 w[n][h][0] = transposed(pack_half2(p[0], p[1]));
                 w[n][h][1] = transposed(pack_half2(p[2], p[3]));
             }
@@ -405,6 +410,28 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
                 }
             }
         }
+        return true;
+    };
+    int slot = 0, c = c0;
+    uint32_t scale = 127u;
+    while (true) {
+#pragma unroll 1
+        for (; c < c_end; c += kWarps) {
+            cp_async_wait<kStages - 2>();
+            __syncwarp();
+            scale = scales[0];
+#pragma unroll
+            for (int i = 0; i < kStages - 2; ++i) scales[i] = scales[i + 1];
+            const int next = c + (kStages - 1) * kWarps, next_slot = slot == 0 ? kStages - 1 : slot - 1;
+            scales[kStages - 2] = load(next, next_slot);
+            look_up(next + kWarps);
+            if (!chunk(c, scale, slot, std::false_type())) break;
+            slot = slot + 1 == kStages ? 0 : slot + 1;
+        }
+        if (__builtin_expect(c >= c_end, 1)) break;
+        chunk(c, scale, slot, std::true_type());
+        slot = slot + 1 == kStages ? 0 : slot + 1;
+        c += kWarps;
     }
 
     // ---- the warps' sums joined.  (Only now may the next kernel's CTAs come: with them in between the launch's own would
@@ -452,9 +479,9 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
         float l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            const float by = sm_m[w][row] == -kInf ? 0.f : exp2_fast(sm_m[w][row] - m);
             // (a NaN sum has no reference of its own)
-            l += sm_l[w][row] == 0.f ? 0.f : sm_l[w][row] * by;
+            const float half = half_factor(sm_m[w][row], m), by = half * half;
+            l += sm_l[w][row] * half * half;
             const float *x = sums + (w * kRows + row) * DH + col;
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = fmaf(x[e], by, o[e]);
@@ -505,8 +532,8 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
             float l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < kMostCluster; ++k) {
-                const float by = p[k].x == -kInf ? 0.f : exp2_fast(p[k].x - m);
-                l += p[k].y == 0.f ? 0.f : p[k].y * by;
+                const float half = half_factor(p[k].x, m), by = half * half;
+                l += p[k].y * half * half;
                 const float x[8] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w, v[k][1].x, v[k][1].y, v[k][1].z, v[k][1].w};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = fmaf(x[e], by, o[e]);
@@ -549,16 +576,16 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_kv_join(const KvAttnArgs a)
         float to = m;
 #pragma unroll
         for (int k = 0; k < kJoinAhead; ++k) to = fmaxf(to, p[k].x);
-        const float by = m == -kInf ? 0.f : exp2_fast(m - to);
         // (a NaN sum may have no reference of its own)
-        l = l == 0.f ? 0.f : l * by;
+        const float half = half_factor(m, to), by = half * half;
+        l = l * half * half;
 #pragma unroll
         for (int e = 0; e < kPer; ++e) o[e] *= by;
         m = to;
 #pragma unroll
         for (int k = 0; k < kJoinAhead; ++k) {
-            const float f = p[k].x == -kInf ? 0.f : exp2_fast(p[k].x - to);
-            l += p[k].y == 0.f ? 0.f : p[k].y * f;
+            const float half_k = half_factor(p[k].x, to), f = half_k * half_k;
+            l += p[k].y * half_k * half_k;
 #pragma unroll
             for (int e = 0; e < kPer; ++e) o[e] = fmaf(v[k][e], f, o[e]);
         }
@@ -584,8 +611,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_kv_join(const KvAttnArgs a)
         float total = 0.f, sum = 0.f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            const float f = sm_m[first + w] == -kInf ? 0.f : exp2_fast(sm_m[first + w] - top);
-            total += sm_l[first + w] == 0.f ? 0.f : sm_l[first + w] * f;
+            const float half = half_factor(sm_m[first + w], top), f = half * half;
+            total += sm_l[first + w] * half * half;
             sum = fmaf(sm_o[first + w][d], f, sum);
         }
         const float inv = total == 0.f ? 0.f : 1.f / total;

@@ -111,7 +111,18 @@ F3DC_DEV uint32_t pack_half2(float lo, float hi)
 // weights far below the largest.  The sum of weights takes them without their value scales, w 2^-e.  A value
 // scale below 2^kLeastScale counts as 2^kLeastScale with values of zero (they are below 2^-55): without that
 // bound the blocks of zeros, whose scale is 2^-127, would take the sums out of fp32's range.
-constexpr int kLeastScale = -64;
+// Within kScaleSpan binades of the largest value scale E so far, w 2^-e loses nothing of the sum: s + e - r is at least
+// s - max(s) - kScaleSpan, and the exponential's end at 2^-126 is 2^-56 of the sum's largest term.  Tokens beside a page further
+// below ("apart") take a second exponential without e, 2^(s - r + kSumShift): since s + e - r <= 16, its exponent is at most
+// 16 + 64 + kSumShift = 120, and since r <= max(s) + 127 the largest s stands at 2^(kSumShift - 127) or above, 2^39 above the end.
+constexpr int kLeastScale = -64, kScaleSpan = 70;
+constexpr float kSumShift = 40.f, kSumUnshift = 0x1p-40f;
+// Square root of the factor from one reference to a larger one (none: 0).  Sums of weights are multiplied by it twice: references take
+// value scales in, so that for equal scores they may lie 191 apart, and a sum is large where the factor is out of range.
+F3DC_DEV float half_factor(float from, float to)
+{
+    return from == __int_as_float(0xFF800000) ? 0.f : exp2_fast(0.5f * (from - to));
+}
 
 struct ValueScale {
     float log2, inverse;  // e and 2^-e

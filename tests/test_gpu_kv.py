@@ -752,3 +752,36 @@ def test_append_on_streams_and_in_graphs():
     for i in range(2):
         assert all(torch.equal(a, b) for a, b in zip(state(i), want[i]))
     assert f3dc.gemm_status() == 0
+
+
+# exponents of the value scales of a sequence's pages, as shares of its length: far apart, pages of zeros (-127) among them
+FAR = [(-127, 74), (90, -127, 90), (-20, 113, -60), (0, -127, 100, 5, 113, -64), (113,), (-127, 6, -64, 7)]
+
+
+@pytest.mark.parametrize("rows,held", [(1, [1500]), (1, [9000, 40]), (4, [700, 300]), (20, [1300]), (150, [900, 100]), (150, [6000])])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_value_scales_far_apart(dh, rows, held):
+    # every token counts in the sum of weights, however small its values are beside others'.  The reference's bounds take
+    # value scales of 2^64 at most: the three roundings of the affine step, the reference and the shift (kv_ref.attend) are of
+    # numbers larger by up to 2 * (113 - 64) here, 3 U32 98 = 294 2^-24 = 2^-15.8 in a score: twice that in a weight and its sum
+    # is 2^-14.8 of the sum of magnitudes, of which err holds 2^-11.
+    for spread in FAR:
+        c = R.Case(held, [rows] * len(held), 4, 2, dh, 16, seed=dh + rows)
+        c.fill(spread=0.0)
+        for pages in c.table_list:
+            for j, p in enumerate(pages):
+                e = spread[min(j * len(spread) // len(pages), len(spread) - 1)]
+                c.vs[p] = e + 127
+                if e == -127:
+                    c.v[p] = 0
+        for causal in (False, True):
+            for workspace in (True, False):
+                q = queries(c)
+                out, lse = attend(c, q, causal, workspace=workspace)
+                assert f3dc.gemm_status() == 0
+                ref, ref_lse, err, lse_err = R.attend(c, q, 1.0 / math.sqrt(dh), causal)
+                err, lse_err = err * (1 + 2.0 ** -3.8), lse_err + 2.0 ** -15.8
+                got = out.double().view(ref.shape)
+                bound = err + R.U_BF16 * (ref.abs() + err) + 2.0 ** -133
+                assert torch.all((got - ref).abs() <= bound), f"{spread} {causal} {workspace}"
+                assert torch.all((lse.double() - ref_lse).abs() <= lse_err), f"{spread} {causal} {workspace}"

@@ -600,10 +600,18 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_kv_join(const KvAttnArgs a)
         const int mid = (lo + hi) / 2;
         (a.batch.row_start[mid] <= row ? lo : hi) = mid;
     }
-    const KvSeq s = kv_seq(a.batch, a.cache, lo, nullptr);
+    auto holds = [&](int b) {
+        const KvSeq s = kv_seq(a.batch, a.cache, b, nullptr);
+        return s.n > 0 && row >= s.row0 && row < s.row0 + s.n;
+    };
+    bool mine = holds(lo);
+    // (starts of broken sequences need not be in order: a row that was not found may be any sequence's, or none's)
+    if (!mine)
+        for (int b = lane; b < a.batch.batch && !mine; b += 32) mine = holds(b);
+    mine = __any_sync(0xffffffffu, mine);
     griddep_launch();
     __syncthreads();
-    if (own >= per || s.n <= 0 || row < s.row0 || row >= s.row0 + s.n) return;
+    if (own >= per || !mine) return;
     float top = sm_m[first];
 #pragma unroll
     for (int w = 1; w < WARPS; ++w) top = fmaxf(top, sm_m[first + w]);

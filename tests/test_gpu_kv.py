@@ -785,3 +785,26 @@ def test_value_scales_far_apart(dh, rows, held):
                 bound = err + R.U_BF16 * (ref.abs() + err) + 2.0 ** -133
                 assert torch.all((got - ref).abs() <= bound), f"{spread} {causal} {workspace}"
                 assert torch.all((lse.double() - ref_lse).abs() <= lse_err), f"{spread} {causal} {workspace}"
+
+
+@pytest.mark.parametrize("workspace", [True, False])
+@pytest.mark.parametrize("rows,held", [(2, 3000), (2, 40000), (150, 3000)])
+def test_sequences_beside_broken_ones(rows, held, workspace):
+    # a bound that is broken in the middle leaves out the two sequences that share it and no other, in one part or in many
+    for broken in (10 ** 6, 4 * rows + 1, -5):
+        c = R.Case([held, 300, held, 2500, 17], [rows] * 5, 2, 1, 64, 64, seed=rows, spare_rows=1, before=1)
+        c.fill()
+        q = queries(c)
+        c.row_start[2] = broken
+        out, lse = attend(c, q, True, workspace=workspace, batch=batch_of(c, max_rows=rows))
+        assert f3dc.gemm_status() == 2
+        ref, ref_lse, err, lse_err = R.attend(c, q, 0.125, True)
+        got = out.double().view(ref.shape)
+        for b in range(5):
+            at = slice(c.starts[b], c.starts[b + 1])
+            if b in (1, 2):
+                assert torch.all(out[at] == 7.0) and torch.all(lse[at] == 7.0)
+            else:
+                assert torch.all((got[at] - ref[at]).abs() <= err[at] + R.U_BF16 * (ref[at].abs() + err[at]) + 2.0 ** -133)
+                assert torch.all((lse[at].double() - ref_lse[at]).abs() <= lse_err[at])
+        assert torch.all(out[0] == 7.0) and torch.all(out[-1] == 7.0)

@@ -90,6 +90,16 @@ KvBatch batch_of(const f3dc_kv_batch *t)
 
 bool empty(const f3dc_kv_batch *t) { return t->batch == 0 || t->rows == 0 || t->max_rows == 0; }
 
+// Whether a call within these bounds has more to count than the attention's kernels do.  (Blocks of 8 packed rows are the smallest
+// that any kernel makes, and a sequence's CTAs are shared out only up to some times the SMs.)
+bool attention_too_large(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads)
+{
+    if (empty(t)) return false;
+    const int64_t packed = (int64_t)t->max_rows * (heads / c->kv_heads);
+    return (packed + 7) / 8 > INT32_MAX / 2 / ((int64_t)c->kv_heads * t->batch) || packed > INT32_MAX / 2 ||
+           (int64_t)t->rows * heads > INT32_MAX || t->max_length > INT32_MAX - 1024;
+}
+
 int64_t part_bytes(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads)
 {
     return (int64_t)t->rows * heads * (c->dh + 2) * (int64_t)sizeof(float);
@@ -194,7 +204,9 @@ extern "C" f3dc_status f3dc_kv_append_fp8(const f3dc_kv_cache *cache, const f3dc
 
 extern "C" size_t f3dc_kv_attention_workspace(const f3dc_kv_cache *cache, const f3dc_kv_batch *batch, int32_t heads)
 {
-    if (cache_shape(cache) || batch_shape(batch) || heads < 1 || heads % cache->kv_heads || heads > 65536) return 0;
+    if (cache_shape(cache) || batch_shape(batch) || heads < 1 || heads % cache->kv_heads || heads > 65536 ||
+        attention_too_large(cache, batch, heads))
+        return 0;
     int sms = 0;
     if (sm_count(&sms) != cudaSuccess) return 0;
     bool cluster = false;
@@ -220,13 +232,7 @@ extern "C" f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f
     if (!q || !out) return bad("null pointer");
     if (misaligned(q, 16) || misaligned(out, 16) || misaligned(workspace, 16)) return bad("pointers must be 16-byte aligned");
     if (misaligned(lse, 4)) return bad("lse must be 4-byte aligned");
-    const int group = heads / cache->kv_heads;
-    // (blocks of 8 packed rows are the smallest that any kernel makes, and a sequence's CTAs are shared out only up to some
-    // times the SMs)
-    if (((int64_t)batch->max_rows * group + 7) / 8 > INT32_MAX / 2 / ((int64_t)cache->kv_heads * batch->batch) ||
-        (int64_t)batch->max_rows * group > INT32_MAX / 2 || (int64_t)batch->rows * heads > INT32_MAX ||
-        batch->max_length > INT32_MAX - 1024)
-        return bad("the problem is too large");
+    if (attention_too_large(cache, batch, heads)) return bad("the problem is too large");
     int sms = 0;
     cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess) return fail(F3DC_ERR_CUDA, "device query", e);
@@ -239,7 +245,7 @@ extern "C" f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f
     a.ldo = ldo;
     a.lse = lse;
     a.heads = heads;
-    a.group = group;
+    a.group = heads / cache->kv_heads;
     a.causal = causal;
     a.scale_log2 = (float)(scale * 1.4426950408889634);
     const bool many = kv_many_rows(batch->max_rows, heads, cache->kv_heads, cache->dh);

@@ -808,3 +808,16 @@ def test_sequences_beside_broken_ones(rows, held, workspace):
                 assert torch.all((got[at] - ref[at]).abs() <= err[at] + R.U_BF16 * (ref[at].abs() + err[at]) + 2.0 ** -133)
                 assert torch.all((lse[at].double() - ref_lse[at]).abs() <= lse_err[at])
         assert torch.all(out[0] == 7.0) and torch.all(out[-1] == 7.0)
+
+
+def test_workspace_of_calls_that_are_too_large():
+    # nothing for what the attention itself refuses: more rows and heads than it counts, and bounds whose products leave 64 bits
+    pool = torch.zeros((1, 1, 64, 64), dtype=torch.uint8, device=DEV)
+    scales = torch.zeros((1, 1), dtype=torch.uint8, device=DEV)
+    cache, zeros = f3dc.KVCache(pool, pool, scales, scales), torch.zeros(2, dtype=torch.int32, device=DEV)
+    for heads, kw in ((32, dict(rows=1 << 27, max_rows=1, max_length=1 << 20)), (65536, dict(rows=1 << 20, max_rows=1, max_length=1 << 20)),
+                      (1, dict(rows=1, max_rows=1, max_length=2 ** 31 - 1)), (65536, dict(rows=2 ** 31 - 1, max_rows=1 << 30, max_length=1 << 20))):
+        batch = f3dc.KVBatch(zeros, zeros[:1], zeros[None], **kw)
+        assert f3dc.kv_attention_workspace(cache, batch, heads) == 0
+        batch.batch = 1 << 26
+        assert f3dc.kv_attention_workspace(cache, batch, heads) == 0

@@ -558,7 +558,7 @@ typedef struct f3dc_kv_batch {
     int64_t table_stride;      /* pages of a row of page_table */
     int32_t batch;             /* sequences, >= 0 */
     int32_t rows;              /* packed rows, >= 0: row_start[batch] <= rows */
-    int32_t max_rows;          /* no sequence has more rows */
+    int32_t max_rows;          /* no sequence has more rows (nor more than `rows`) */
     int32_t max_length;        /* nor is longer: at most 2^31 - 1025 */
 } f3dc_kv_batch;
 

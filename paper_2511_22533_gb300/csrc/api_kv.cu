@@ -83,9 +83,12 @@ KvCache cache_of(const f3dc_kv_cache *c)
             c->pages, c->page_tokens, c->kv_heads, c->dh};
 }
 
+// rows of a sequence at most: the bound may be loose
+int32_t most_rows(const f3dc_kv_batch *t) { return t->max_rows < t->rows ? t->max_rows : t->rows; }
+
 KvBatch batch_of(const f3dc_kv_batch *t)
 {
-    return {t->row_start, t->lengths, t->page_table, t->table_stride, t->batch, t->rows, t->max_rows, t->max_length};
+    return {t->row_start, t->lengths, t->page_table, t->table_stride, t->batch, t->rows, most_rows(t), t->max_length};
 }
 
 bool empty(const f3dc_kv_batch *t) { return t->batch == 0 || t->rows == 0 || t->max_rows == 0; }
@@ -95,7 +98,7 @@ bool empty(const f3dc_kv_batch *t) { return t->batch == 0 || t->rows == 0 || t->
 bool attention_too_large(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads)
 {
     if (empty(t)) return false;
-    const int64_t packed = (int64_t)t->max_rows * (heads / c->kv_heads);
+    const int64_t packed = (int64_t)most_rows(t) * (heads / c->kv_heads);
     return (packed + 7) / 8 > INT32_MAX / 2 / ((int64_t)c->kv_heads * t->batch) || packed > INT32_MAX / 2 ||
            (int64_t)t->rows * heads > INT32_MAX || t->max_length > INT32_MAX - 1024;
 }
@@ -110,7 +113,7 @@ int splits(const f3dc_kv_cache *c, const f3dc_kv_batch *t, int32_t heads, int sm
 {
     *cluster = false;
     if (empty(t)) return 1;
-    return kv_splits(t->batch, t->max_rows, t->max_length, heads, c->kv_heads, c->dh, sms, cluster);
+    return kv_splits(t->batch, most_rows(t), t->max_length, heads, c->kv_heads, c->dh, sms, cluster);
 }
 
 }  // namespace
@@ -167,7 +170,7 @@ extern "C" f3dc_status f3dc_kv_append_fp8(const f3dc_kv_cache *cache, const f3dc
     if (!k || !v) return bad("null pointer");
     if (misaligned(k, 16) || misaligned(v, 16) || misaligned(q, 16) || (q && misaligned(q_out, 16)))
         return bad("pointers must be 16-byte aligned");
-    if ((((int64_t)batch->max_rows + cache->page_tokens - 2) / cache->page_tokens + 1) * batch->batch > INT32_MAX ||
+    if ((((int64_t)most_rows(batch) + cache->page_tokens - 2) / cache->page_tokens + 1) * batch->batch > INT32_MAX ||
         batch->max_length > INT32_MAX - 1024)
         return bad("the problem is too large");
     int sms = 0;
@@ -248,7 +251,7 @@ extern "C" f3dc_status f3dc_kv_attention_fp8(const f3dc_kv_cache *cache, const f
     a.group = heads / cache->kv_heads;
     a.causal = causal;
     a.scale_log2 = (float)(scale * 1.4426950408889634);
-    const bool many = kv_many_rows(batch->max_rows, heads, cache->kv_heads, cache->dh);
+    const bool many = kv_many_rows(most_rows(batch), heads, cache->kv_heads, cache->dh);
     bool cluster = false;
     a.splits = splits(cache, batch, heads, sms, &cluster);
     if (!cluster && a.splits > 1) {

@@ -83,6 +83,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_kv_append(const KvAppendAr
         return;
     }
     const int page = a.cache.page, held = s.length - s.n;  // tokens before this call
+    if ((uint32_t)slot * page >= (uint32_t)s.n + page) return;  // (the bound on rows may be far above n: no token's number overflows below)
     const int j = held / page + slot;                      // page of the sequence
     const int lo = max(held, j * page), hi = min(s.length, (j + 1) * page);
     if (lo >= hi) return;
@@ -314,7 +315,7 @@ cudaError_t launch_kv_append(const KvAppendArgs &args, int num_sms, cudaStream_t
     KvAppendArgs a = args;
     const int page = a.cache.page;
     // pages that a sequence's rows can touch, starting anywhere in one
-    a.slots = (a.batch.max_rows + page - 2) / page + 1;
+    a.slots = (int)(((int64_t)a.batch.max_rows + page - 2) / page + 1);
     const int64_t ctas = (int64_t)a.slots * a.batch.batch;
     if (ctas > INT32_MAX) return cudaErrorInvalidValue;
     // heads of a page are shared by CTAs where there are few pages: as many as fit the SMs at once

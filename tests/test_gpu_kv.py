@@ -821,3 +821,19 @@ def test_workspace_of_calls_that_are_too_large():
         assert f3dc.kv_attention_workspace(cache, batch, heads) == 0
         batch.batch = 1 << 26
         assert f3dc.kv_attention_workspace(cache, batch, heads) == 0
+
+
+@pytest.mark.parametrize("held,rows", [([0], [1]), ([100, 0, 7], [5, 70, 0])])
+@pytest.mark.parametrize("page", [16, 128])
+def test_loose_bounds(held, rows, page):
+    # bounds far above what the sequences have: as with close ones
+    top = dict(max_rows=2 ** 31 - 1, max_length=2 ** 31 - 1025)
+    cases = [R.Case(held, rows, 4, 2, 64, page, seed=page) for _ in range(2)]
+    x = rows_of(cases[0], 50, 2).to(torch.bfloat16)
+    for c, kw in zip(cases, ({}, top)):
+        c.fill(c.held)
+        f3dc.kv_append_fp8(cache_of(c), batch_of(c, **kw), x, 128, x, 128)
+    assert all(torch.equal(getattr(cases[0], n), getattr(cases[1], n)) for n in ("k", "v", "ks", "vs"))
+    c = cases[1]
+    run_attend(c, True, batch=batch_of(c, **top))
+    run_attend(c, False, batch=batch_of(c, **top), workspace=False)

@@ -574,8 +574,8 @@ typedef struct f3dc_rotary {
     const uint64_t *turns; /* device [dims / 2], see f3dc_rotary_turns */
 } f3dc_rotary;
 
-/* turns_out[j] = inv_freq[j] / (2 pi) in units of 2^-64 turns, modulo a turn (radians per
- * unit of position in; host arrays).  Host only. */
+/* turns_out[j] = inv_freq[j] / (2 pi) in units of 2^-64 turns, modulo a turn, to within one of them
+ * (radians per unit of position in, at most 2^40 in magnitude; host arrays).  Host only. */
 f3dc_status f3dc_rotary_turns(const double *inv_freq, int32_t n, uint64_t *turns_out);
 
 /* Appends keys and values to their sequences' pages: row i of sequence b, of n_b,

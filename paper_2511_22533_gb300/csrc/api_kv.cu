@@ -122,8 +122,9 @@ extern "C" f3dc_status f3dc_rotary_turns(const double *inv_freq, int32_t n, uint
 {
     if (n < 0 || (n > 0 && (!inv_freq || !turns_out))) return bad("need n >= 0, inv_freq and turns_out");
     for (int32_t j = 0; j < n; ++j) {
-        if (!std::isfinite(inv_freq[j])) return bad("a frequency is not finite");
-        // the quotient by 2 pi in two doubles, so that a far position times its last bit is nothing yet
+        // the quotient by 2 pi in two doubles, so that a far position times its last bit is nothing yet (below 2^40 radians the two
+        // are off by less than 2^-64 turns; NaN is refused too)
+        if (!(std::fabs(inv_freq[j]) <= 0x1p40)) return bad("a frequency is not finite or above 2^40 radians per unit");
         constexpr double kTurn = 6.283185307179586, kTurnLow = 2.4492935982947064e-16;  // 2 pi
         const double f = std::fabs(inv_freq[j]), hi = f / kTurn;
         const double lo = (std::fma(-hi, kTurn, f) - hi * kTurnLow) / kTurn;

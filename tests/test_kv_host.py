@@ -117,6 +117,22 @@ def test_turns_are_exact():
     assert f3dc.rotary_turns([]).size == 0
 
 
+def test_turns_of_large_frequencies():
+    # exact to a unit of 2^-64 turns up to 2^40 radians, refused above
+    rng = random.Random(6)
+    freq = [s * f for f in [2.0 ** e for e in range(0, 41)] + [rng.uniform(1, 2) * 2.0 ** rng.randrange(40) for _ in range(500)] for s in (1, -1)]
+    with decimal.localcontext() as ctx:
+        ctx.prec = 80
+        tau = 2 * decimal.Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798")
+        for f, t in zip(freq, f3dc.rotary_turns(freq)):
+            off = (int(t) - decimal.Decimal(f) / tau * 2 ** 64) % 2 ** 64
+            assert min(off, 2 ** 64 - off) <= 1
+    for f in (2.0 ** 40 * (1 + 2.0 ** -52), 1e13, -1e18, 1e300):
+        with pytest.raises(f3dc.F3dcError) as e:
+            f3dc.rotary_turns([1.0, f])
+        assert e.value.status == 1
+
+
 # Tensors that say they are on a GPU stand in for GPU tensors, and calls that only record.
 
 class Tensor:

@@ -134,7 +134,8 @@ class KVCache(C.Structure):
 class KVBatch(C.Structure):
     """The sequences of a call: row_start int32 [batch + 1], lengths int32 [batch] (with the
     call's rows) and page_table int32 [batch, pages] on the GPU, kept alive; `rows` packed rows, and
-    bounds on a sequence's rows and length."""
+    bounds on a sequence's rows and length.  A table may be a view of a wider one: a sequence longer than the
+    view's columns hold is out of bounds."""
     _fields_ = [("row_start", C.c_void_p), ("lengths", C.c_void_p), ("page_table", C.c_void_p), ("table_stride", C.c_int64),
                 ("batch", C.c_int32), ("rows", C.c_int32), ("max_rows", C.c_int32), ("max_length", C.c_int32)]
 
@@ -149,10 +150,21 @@ class KVBatch(C.Structure):
         if batch > 1 and page_table.stride(0) < page_table.shape[1]:
             raise F3dcError(1, "rows of page_table overlap")
         _same_device("batch", self._tensors)
-        # (a single row's stride may be anything)
-        stride = page_table.shape[1] if batch <= 1 else page_table.stride(0)
+        # (a single row's stride may be anything, and that of rows without columns)
+        columns = page_table.shape[1]
+        stride = page_table.stride(0) if batch > 1 and columns else columns
         super().__init__(row_start.data_ptr(), lengths.data_ptr(), page_table.data_ptr(), stride, batch, rows, max_rows, max_length)
         self._ref = C.pointer(self)
+        self._columns = columns if columns < stride else None
+
+    def _for(self, cache):
+        """The structure for calls with `cache`: to the library a row of the table has as many pages as its stride, so
+        the bound on lengths is no larger than what a view's columns hold."""
+        if self._columns is None or self.max_length <= self._columns * cache.page_tokens:
+            return self._ref
+        bounded = KVBatch.from_buffer_copy(self)
+        bounded.max_length = self._columns * cache.page_tokens
+        return C.pointer(bounded)
 
 
 _lock = threading.Lock()
@@ -584,7 +596,7 @@ def kv_append_fp8(cache, batch, k, ldk, v, ldv, q=None, ldq=0, q_out=None, ldqo=
         _kv_here(current, cache, batch, rotary)
     if positions is not None and (not positions.is_contiguous() or positions.numel() < batch.rows * (rotary.axes if rotary else 1)):
         raise F3dcError(1, "positions are contiguous int32 [rows, axes]")
-    st = calls[0](cache._ref, batch._ref, rotary._ref if rotary is not None else None, pk, ldk, pv, ldv, pq, ldq, pqo, ldqo, heads,
+    st = calls[0](cache._ref, batch._for(cache), rotary._ref if rotary is not None else None, pk, ldk, pv, ldv, pq, ldq, pqo, ldqo, heads,
                   pp, _stream(stream))
     if st:
         _check(st)
@@ -592,7 +604,7 @@ def kv_append_fp8(cache, batch, k, ldk, v, ldv, q=None, ldq=0, q_out=None, ldqo=
 
 def kv_attention_workspace(cache, batch, heads) -> int:
     """Bytes of workspace for kv_attention_fp8 (0: none is needed)."""
-    return int(lib().f3dc_kv_attention_workspace(cache._ref, batch._ref, heads))
+    return int(lib().f3dc_kv_attention_workspace(cache._ref, batch._for(cache), heads))
 
 
 def kv_attention_fp8(cache, batch, q, ldq, out, ldo, heads, scale, causal=False, lse=None, workspace=None, stream=None):
@@ -604,7 +616,7 @@ def kv_attention_fp8(cache, batch, q, ldq, out, ldo, heads, scale, causal=False,
         _kv_here(current, cache, batch)
     if lse is not None and (not lse.is_contiguous() or lse.numel() < batch.rows * heads):
         raise F3dcError(1, "lse is contiguous fp32 [rows, heads]")
-    st = calls[1](cache._ref, batch._ref, pq, ldq, po, ldo, pl, heads, scale, 1 if causal else 0, pw,
+    st = calls[1](cache._ref, batch._for(cache), pq, ldq, po, ldo, pl, heads, scale, 1 if causal else 0, pw,
                   workspace.numel() if workspace is not None else 0, _stream(stream))
     if st:
         _check(st)

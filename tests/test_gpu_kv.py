@@ -837,3 +837,42 @@ def test_loose_bounds(held, rows, page):
     c = cases[1]
     run_attend(c, True, batch=batch_of(c, **top))
     run_attend(c, False, batch=batch_of(c, **top), workspace=False)
+
+
+@pytest.mark.parametrize("rows", [2, 150])
+def test_page_tables_that_are_views(rows):
+    # columns among others of a wider table: what does not fit them is out of bounds, though the wider table goes on
+    for side in ("left", "right"):
+        c = R.Case([300, 500, 60], [rows] * 3, 4, 2, 64, 64, seed=rows)
+        c.fill()
+        q = queries(c)
+        width = -(-(300 + rows) // 64)
+        wide = torch.zeros((3, width + 4), dtype=torch.int32, device=DEV)
+        view = wide[:, :width] if side == "left" else wide[:, 4:]
+        view[:, :width] = c.table[:, :width]
+        cache, kw = cache_of(c), dict(rows=c.n_rows, max_rows=rows, max_length=max(c.lengths))
+        for workspace in (True, False):
+            out, lse = attend(c, q, True, cache=cache, batch=f3dc.KVBatch(c.row_start, c.length, view, **kw), workspace=workspace)
+            assert f3dc.gemm_status() == 2
+            ref, _, err, _ = R.attend(c, q, 0.125, True)
+            got = out.double().view(ref.shape)
+            for b in (0, 2):
+                at = slice(c.starts[b], c.starts[b + 1])
+                assert torch.all((got[at] - ref[at]).abs() <= err[at] + R.U_BF16 * (ref[at].abs() + err[at]) + 2.0 ** -133)
+            at = slice(c.starts[1], c.starts[2])
+            assert torch.all(out[at] == 7.0) and torch.all(lse[at] == 7.0)
+        before = [t.clone() for t in (c.k, c.ks)]
+        f3dc.kv_append_fp8(cache, f3dc.KVBatch(c.row_start, c.length, view, **kw), q, 256, q, 256)
+        assert f3dc.gemm_status() == 2
+        for p in c.table_list[1]:
+            assert torch.equal(c.k[p], before[0][p]) and torch.equal(c.ks[p], before[1][p])
+        assert not torch.equal(c.k[c.table_list[0][-1]], before[0][c.table_list[0][-1]])
+
+
+def test_sequences_without_pages():
+    # a page table of no columns: no sequence has a token, and every row sees none
+    for rows in (1, 200):
+        c = cross([0, 0], [rows, rows], 4, 2, 64, 16)
+        out, lse = attend(c, queries(c), False, batch=f3dc.KVBatch(c.row_start, c.length, c.table[:, :0].contiguous(), rows=c.n_rows, max_rows=rows,
+                                                                   max_length=0))
+        assert f3dc.gemm_status() == 0 and torch.all(out == 0) and torch.all(lse == -math.inf)

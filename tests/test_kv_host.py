@@ -236,3 +236,36 @@ def test_calls_that_fit_reach_the_library(made):
     py_attend(lse=None, ws=None)
     assert [n for n, _ in made] == ["append", "append", "attend", "attend"]
     assert made[2][1][-3:-1] == (P, 99) and made[3][1][-3:-1] == (None, 0)
+
+
+def test_lengths_are_bounded_by_a_views_columns(made, monkeypatch):
+    # to the library a row of a page table is as long as its stride: a narrower view bounds the lengths in every call
+    t = [Tensor(BF16, (7, 512)) for _ in range(2)]
+
+    class Library:
+        @staticmethod
+        def f3dc_kv_attention_workspace(*a):
+            made.append(("workspace", a))
+            return 5
+
+    for view, tokens, want in ((Tensor(I32, (2, 4), (9, 1)), 64, 256), (Tensor(I32, (2, 5), (9, 1)), 64, 300), (Tensor(I32, (2, 4)), 64, 300),
+                               (Tensor(I32, (2, 5), (9, 1)), 16, 80), (Tensor(I32, (2, 1), (2, 1)), 32, 32)):
+        c, b = cache(shape=(10, 4, tokens, 64)), batch(tpt=view)
+        f3dc.kv_append_fp8(c, b, t[0], 256, t[1], 256, stream=0)
+        f3dc.kv_attention_fp8(c, b, t[0], 512, t[1], 512, 8, 0.125, stream=0)
+        with monkeypatch.context() as m:
+            m.setattr(f3dc, "lib", Library)
+            assert f3dc.kv_attention_workspace(c, b, 8) == 5
+        assert [n for n, _ in made] == ["append", "attend", "workspace"]
+        for _, a in made:
+            got = a[1].contents
+            assert (got.max_length, got.table_stride, got.batch, got.rows, got.max_rows) == (want, view.strides[0], 2, 7, 4)
+            assert (got.row_start, got.lengths, got.page_table) == (P, P, P)
+        assert b.max_length == 300  # (a later call with another cache asks again)
+        made.clear()
+
+
+def test_a_page_table_without_columns():
+    # as torch strides it; no sequence has a token then
+    for n in (1, 2, 3):
+        assert batch(n=n, trs=Tensor(I32, (n + 1,)), tln=Tensor(I32, (n,)), tpt=Tensor(I32, (n, 0), (1, 1))).table_stride == 0

@@ -808,14 +808,14 @@ cudaError_t launch_one(const KvAttnArgs &args, cudaStream_t s)
     const int64_t ctas = (int64_t)a.splits * a.row_blocks * a.cache.heads * a.batch.batch;
     if (ctas > INT32_MAX) return cudaErrorInvalidValue;
     // (a register split above what the launch really has would wait for ever)
-    static const cudaError_t split = [] {
+    static std::atomic<uint64_t> checked{0}, devices{0};
+    cudaError_t e = once_per_device(checked, [] {
         cudaFuncAttributes f;
         const cudaError_t e = cudaFuncGetAttributes(&f, k_kv_attn<DH, NB>);
         return e != cudaSuccess ? e : (f.numRegs >= kLaunchRegs ? cudaSuccess : cudaErrorInvalidKernelImage);
-    }();
-    if (split != cudaSuccess) return split;
-    static std::atomic<uint64_t> devices{0};
-    cudaError_t e = ask_smem(k_kv_attn<DH, NB>, (int)Cfg<DH, NB>::kSmem, devices);
+    });
+    if (e != cudaSuccess) return e;
+    e = ask_smem(k_kv_attn<DH, NB>, (int)Cfg<DH, NB>::kSmem, devices);
     if (e != cudaSuccess) return e;
     e = launch_k(k_kv_attn<DH, NB>, dim3((unsigned)ctas), dim3(kThreads), Cfg<DH, NB>::kSmem, s, a);
     return e != cudaSuccess || a.splits == 1 ? e : launch_kv_join(a, s);

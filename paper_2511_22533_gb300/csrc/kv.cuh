@@ -12,18 +12,25 @@
 
 namespace f3dc {
 
-// Dynamic shared memory above 48 KB is asked for once per kernel and device.
-template <typename Kernel>
-cudaError_t ask_smem(Kernel kernel, int bytes, std::atomic<uint64_t> &devices)
+// What has to succeed once on each device; a failure is tried again by the next call.
+template <typename Ask>
+cudaError_t once_per_device(std::atomic<uint64_t> &devices, Ask ask)
 {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     const uint64_t bit = 1ull << (dev & 63);
     if (devices.load(std::memory_order_acquire) & bit) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    e = ask();
     if (e == cudaSuccess) devices.fetch_or(bit, std::memory_order_acq_rel);
     return e;
+}
+
+// Dynamic shared memory above 48 KB is asked for once per kernel and device.
+template <typename Kernel>
+cudaError_t ask_smem(Kernel kernel, int bytes, std::atomic<uint64_t> &devices)
+{
+    return once_per_device(devices, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
 }
 
 // Sequence b of a batch: its packed rows [row0, row0 + n) and the tokens of its pages.

@@ -700,8 +700,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                 l_run += apart->y * half * half;
             }
             if (ok && n_steps > 0) {
-                // (v_full: nan_flag is what the converting warps left)
-                ok = product_done(n_steps - 1) && wait(&v_full[(n_tiles - 1) % kStages], ((n_tiles - 1) / kStages) & 1);
+                // (The last two products: no other wait has seen the one before the last arrive.  v_full: nan_flag is what the converting
+                // warps left.)
+                ok = product_done(n_steps - 1) && (n_steps == 1 || product_done(n_steps - 2)) && wait(&v_full[(n_tiles - 1) % kStages], ((n_tiles - 1) / kStages) & 1);
                 tc_fence_after();
             }
             if (ok) {

@@ -207,233 +207,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
     auto wait = [&](uint64_t *bar, uint32_t parity) { return warp_wait(bar, parity, abort_flag, a.err); };
 
-    if (warp < 4) {
-        reg_dec<kIssueRegs>();
-        if (warp < tiles && n_tiles > 0) {
-            // ------------------------------------------------ MMA issuer of one query tile
-            constexpr uint32_t idesc_s = make_idesc_f16(128, 64, 0), idesc_o = make_idesc_f16(128, DH, 1);
-            const int t = warp;
-            const uint64_t q_desc = make_sdesc(smem_u32(sQ + t * C::kTile), 16, C::kAtom, C::kSwz);
-            const uint64_t k_desc = make_sdesc(smem_u32(sK), 16, C::kAtom, C::kSwz);
-            // values: the head's columns lie a region apart, eight tokens an atom
-            const uint64_t v_desc = make_sdesc(smem_u32(sV), C::kRegion, C::kAtom, C::kSwz);
-            constexpr uint64_t kStageStep = C::kTile >> 4, kRegionStep = C::kRegion >> 4, kVStep = (16 * C::kRowBytes) >> 4;
-            constexpr uint64_t kHalfStep = (64 * C::kRowBytes) >> 4;
-            // step j: place j % kPlaces of S and P, whose barriers are in their phase j / kPlaces
-            struct Place {
-                int i = 0;
-                uint32_t phase = 0;
-                F3DC_DEV void next()
-                {
-                    if (++i == C::kPlaces) i = 0, phase ^= 1;
-                }
-            } ps, pp;
-            uint64_t *const s_own = s_full + C::kPlaces * t, *const p_own = p_full + C::kPlaces * t, *const done = pv_done + C::kPlaces * t;
-            const uint32_t tm = tmem + t * 64 * C::kPlaces;
-            auto scores = [&](int j) {
-                const int g = j >> 1, st = g % kStages;
-                if ((j & 1) == 0 && !wait(&k_full[st], (g / kStages) & 1)) return false;
-                tc_fence_after();
-                const uint64_t kd = k_desc + st * kStageStep + (j & 1) * kHalfStep;
-#pragma unroll
-                for (int kk = 0; kk < DH / 16; ++kk) {
-                    const uint64_t at = (kk / 4) * kRegionStep + 2 * (kk % 4);
-                    if (C::kQTmem) mma_bf16_ts_elect(tm + ps.i * 64, tmem + C::kColQ + t * (DH / 2) + kk * 8, kd + at, idesc_s, kk > 0);
-                    else mma_bf16_elect(tm + ps.i * 64, q_desc + at, kd + at, idesc_s, kk > 0);
-                }
-                mma_commit_elect(&s_own[ps.i]);
-                if ((j & 1) || j + 1 == n_steps) mma_commit_elect(&k_empty[st]);
-                ps.next();
-                return true;
-            };
-            // P V of step j, then S of the step that takes P's place
-            auto product = [&](int j) {
-                const int g = j >> 1, st = g % kStages;
-                if ((j & 1) == 0 && !wait(&v_full[st], (g / kStages) & 1)) return false;
-                if (!wait(&p_own[pp.i], pp.phase)) return false;
-                tc_fence_after();
-                const uint64_t vd = v_desc + st * kStageStep + (j & 1) * kHalfStep;
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    mma_bf16_ts_elect(tmem + C::kColO + t * DH, tm + pp.i * 64 + kk * 8, vd + kk * kVStep, idesc_o, kk > 0 || j > 0);
-                mma_commit_elect(&done[pp.i]);
-                if ((j & 1) || j + 1 == n_steps) mma_commit_elect(&v_empty[st]);
-                if (j + C::kPlaces < n_steps && !(wait(&done[pp.i], pp.phase) && scores(j + C::kPlaces))) return false;
-                pp.next();
-                return true;
-            };
-            bool ok = wait(&q_full[t], 0);
-#pragma unroll 1
-            for (int j = 0; ok && j < min(C::kPlaces, n_steps); ++j) ok = scores(j);
-#pragma unroll 1
-            for (int j = 0; ok && j < n_steps; ++j) ok = product(j);
-        }
-        if (warp == 2) {
-            // ------------------------------------------------ the page table: a lane for 16 tokens of one of four tiles
-            const int run = lane & 7;
-            const uint32_t stride16 = (uint32_t)(a.cache.page_stride >> 4);
-            const uint32_t own16 = (uint32_t)(hk * page + (16 * run & (page - 1))) * (DH / 16);
-            int widest = kLeastScale;
-#pragma unroll 1
-            for (int g0 = 0, n = 0; g0 < n_tiles; g0 += kGroup, ++n) {
-                const int g = g0 + (lane >> 3), t0 = (g_begin + g) * 128 + 16 * run;
-                const bool mine = lane < 8 * kGroup;
-                uint32_t at = own16, bytes = 127u | 127u << 8;
-                int there = 0;
-                if (mine && g < n_tiles && t0 < s.length) {
-                    const int p = kv_page(a.batch, a.cache, b, t0 >> page_log2, a.err);
-                    if (p >= 0) {
-                        const int64_t of = (int64_t)p * a.cache.scale_stride + hk;
-                        bytes = a.cache.ks[of] | (uint32_t)a.cache.vs[of] << 8;
-                        at = (uint32_t)p * stride16 + own16;
-                        there = min(16, s.length - t0);
-                    }
-                }
-                const int slot = n % kGroups;
-                if (!wait(&i_empty[slot], ((n / kGroups) & 1) ^ 1)) break;
-                const ValueScale v = value_scale(bytes >> 8);
-                const uint32_t tile = 0xFFu << (lane & 24);
-                const uint32_t complete = __ballot_sync(0xffffffffu, there == 16), plain = __ballot_sync(0xffffffffu, v.times == kHalfOnes);
-                // (the largest of all four tiles: one that comes later does no harm)
-                widest = max(widest, __reduce_max_sync(0xffffffffu, (int)v.log2));
-                const uint32_t apart = __ballot_sync(0xffffffffu, (int)v.log2 < widest - kScaleSpan);
-                if (mine) {
-                    TileInfo<NB> &x = infos[slot * kGroup + (lane >> 3)];
-                    x.at[run] = at;
-                    x.times[run] = v.times;
-                    x.there[run] = there;
-                    if (run % (8 / NB) == 0) {
-                        StepScales<NB> &sc = x.scales[run >> 2];
-                        const int k = (run & 3) * NB / 8;
-                        sc.key[k] = key_scale(bytes & 255u);
-                        sc.value_log2[k] = apart & tile ? kInf : v.log2;
-                        sc.value_inverse[k] = v.inverse;
-                    }
-                    if (run == 0) {
-                        x.complete = (complete & tile) == tile;
-                        x.plain = (plain & tile) == tile;
-                    }
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&i_full[slot]);
-            }
-        }
-    } else if (warp < 8) {
-        // ------------------------------------------------ pages to operands
-        reg_dec<kConvertRegs>();
-        // 16-byte pieces of a token, and of a thread per half of a tile: piece k is of a token 128 / kPieces further
-        constexpr int kPieces = DH / 16, kTokens = 128 / kPieces;
-        const int i = threadIdx.x - 128;
-        // (dh 128: eight neighbouring lanes hold the same columns' half of two tokens, so that their stores meet no bank twice)
-        const int piece = DH == 128 ? (i & 3) | (i >> 1 & 4) : i % kPieces;
-        const int token = DH == 128 ? (i >> 4) * 2 + (i >> 2 & 1) : i / kPieces;
-        const int put0 = C::place(token, 2 * piece), put1 = C::place(token, 2 * piece + 1);
-        const uint4 *const k_own = reinterpret_cast<const uint4 *>(a.cache.k) + (token & 15) * kPieces + piece;
-        const uint4 *const v_own = reinterpret_cast<const uint4 *>(a.cache.v) + (token & 15) * kPieces + piece;
-        const int run = token >> 4;  // of piece 0
-        auto info = [&](int g) -> const TileInfo<NB> & { return infos[g / kGroup % kGroups * kGroup + g % kGroup]; };
-        // piece k of a half of a tile
-        auto fetch = [&](const uint4 *own, const TileInfo<NB> &x, int k) { return own[x.at[run + k * (kTokens / 16)]]; };
-        auto clear = [&](const TileInfo<NB> &x, uint4 (&u)[kPieces]) {
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k)
-                if ((token & 15) >= x.there[run + k * (kTokens / 16)]) u[k] = make_uint4(0u, 0u, 0u, 0u);
-        };
-        auto widen = [&](uint4 w, uint32_t (&h)[8]) {
-            e4m3x4_to_half2(w.x, h[0], h[1]);
-            e4m3x4_to_half2(w.y, h[2], h[3]);
-            e4m3x4_to_half2(w.z, h[4], h[5]);
-            e4m3x4_to_half2(w.w, h[6], h[7]);
-        };
-        auto store = [&](uint8_t *tile, int k, const uint32_t (&h)[8]) {
-            tile += k * kTokens * C::kRowBytes;  // (the swizzle repeats every eight rows)
-            *reinterpret_cast<uint4 *>(tile + put0) = make_uint4(h[0], h[1], h[2], h[3]);
-            *reinterpret_cast<uint4 *>(tile + put1) = make_uint4(h[4], h[5], h[6], h[7]);
-        };
-        uint4 ku[kPieces], vu[kPieces];
-        {
-            // the first tile's pages looked up here too: its pieces do not wait for its scales
-            const int t0 = g_begin * 128 + 16 * (lane & 7);
-            uint32_t at = (uint32_t)(hk * page + (16 * (lane & 7) & (page - 1))) * kPieces;
-            if (n_tiles > 0 && t0 < s.length) {
-                const int p = kv_page(a.batch, a.cache, b, t0 >> page_log2, nullptr);
-                if (p >= 0) at += (uint32_t)p * (uint32_t)(a.cache.page_stride >> 4);
-            }
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) ku[k] = k_own[__shfl_sync(0xffffffffu, at, run + k * (kTokens / 16))];
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) vu[k] = v_own[__shfl_sync(0xffffffffu, at, run + k * (kTokens / 16))];
-            if (n_tiles > 0) wait(&i_full[0], 0);
-        }
-#pragma unroll 1
-        for (int g = 0; g < n_tiles; ++g) {
-            const int st = g % kStages;
-            const uint32_t parity = (g / kStages) & 1;
-            const TileInfo<NB> &now = info(g);
-            // (behind the last tile its own pieces are loaded once more, unused)
-            const int ng = min(g + 1, n_tiles - 1);
-            if (ng % kGroup == 0 && ng > g && !wait(&i_full[ng / kGroup % kGroups], (ng / kGroup / kGroups) & 1)) break;
-            const TileInfo<NB> &next = info(ng);
-            const bool complete = now.complete != 0;
-            // keys
-            if (!wait(&k_empty[st], parity ^ 1)) break;
-            if (!complete) clear(now, ku);
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) {
-                uint32_t h[8];
-                widen(ku[k], h);
-                store(sK + st * C::kTile, k, h);
-                ku[k] = fetch(k_own, next, k);
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&k_full[st]);
-            // values
-            if (!wait(&v_empty[st], parity ^ 1)) break;
-            if (!complete) clear(now, vu);
-            const bool partly = (g_begin + g + 1) * 128 > least;
-            if (!partly && now.plain) {
-#pragma unroll
-                for (int k = 0; k < kPieces; ++k) {
-                    uint32_t h[8];
-                    widen(vu[k], h);
-                    store(sV + st * C::kTile, k, h);
-                    vu[k] = fetch(v_own, next, k);
-                }
-            } else {
-                uint32_t numbers = 0xffffffffu;
-#pragma unroll
-                for (int k = 0; k < kPieces; ++k) {
-                    uint32_t h[8];
-                    widen(vu[k], h);
-                    const uint32_t by = now.times[run + k * (kTokens / 16)];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        h[e] = half2_times(h[e], by);
-                        if (partly) {
-                            const __half2 x = *reinterpret_cast<const __half2 *>(&h[e]);
-                            const uint32_t m = __heq2_mask(x, x);
-                            numbers &= m;
-                            h[e] &= m;
-                        }
-                    }
-                    store(sV + st * C::kTile, k, h);
-                    vu[k] = fetch(v_own, next, k);
-                }
-                if (numbers != 0xffffffffu) *nan_flag = 1;
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&v_full[st]);
-                if (g % kGroup == kGroup - 1) mbar_arrive(&i_empty[g / kGroup % kGroups]);
-            }
-        }
-        // every arrival of the MMAs' completion is in before the CTA leaves
-#pragma unroll 1
-        for (int g = max(0, n_tiles - kStages); g < n_tiles; ++g)
-            if (!wait(&k_empty[g % kStages], (g / kStages) & 1) || !wait(&v_empty[g % kStages], (g / kStages) & 1)) break;
-    } else {
+    // (The softmax warps' code stands first: with the others' before it 4096 x 4096 of heads of 64 118.6 us instead of 116.4,
+    // 32768 x 32768 5.02 ms instead of 4.94, with heads of 128 143 to 145 us either way.)
+    if (warp >= 8) {
         // ------------------------------------------------ softmax
         reg_inc<kSoftmaxRegs>();
         const int q = warp & 3, t = (warp - 8) >> 2, row = q * 32 + lane;
@@ -786,6 +562,232 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv_attn(const KvAttnArgs a)
                 tc_fence_before();
             }
         }
+    } else if (warp < 4) {
+        reg_dec<kIssueRegs>();
+        if (warp < tiles && n_tiles > 0) {
+            // ------------------------------------------------ MMA issuer of one query tile
+            constexpr uint32_t idesc_s = make_idesc_f16(128, 64, 0), idesc_o = make_idesc_f16(128, DH, 1);
+            const int t = warp;
+            const uint64_t q_desc = make_sdesc(smem_u32(sQ + t * C::kTile), 16, C::kAtom, C::kSwz);
+            const uint64_t k_desc = make_sdesc(smem_u32(sK), 16, C::kAtom, C::kSwz);
+            // values: the head's columns lie a region apart, eight tokens an atom
+            const uint64_t v_desc = make_sdesc(smem_u32(sV), C::kRegion, C::kAtom, C::kSwz);
+            constexpr uint64_t kStageStep = C::kTile >> 4, kRegionStep = C::kRegion >> 4, kVStep = (16 * C::kRowBytes) >> 4;
+            constexpr uint64_t kHalfStep = (64 * C::kRowBytes) >> 4;
+            // step j: place j % kPlaces of S and P, whose barriers are in their phase j / kPlaces
+            struct Place {
+                int i = 0;
+                uint32_t phase = 0;
+                F3DC_DEV void next()
+                {
+                    if (++i == C::kPlaces) i = 0, phase ^= 1;
+                }
+            } ps, pp;
+            uint64_t *const s_own = s_full + C::kPlaces * t, *const p_own = p_full + C::kPlaces * t, *const done = pv_done + C::kPlaces * t;
+            const uint32_t tm = tmem + t * 64 * C::kPlaces;
+            auto scores = [&](int j) {
+                const int g = j >> 1, st = g % kStages;
+                if ((j & 1) == 0 && !wait(&k_full[st], (g / kStages) & 1)) return false;
+                tc_fence_after();
+                const uint64_t kd = k_desc + st * kStageStep + (j & 1) * kHalfStep;
+#pragma unroll
+                for (int kk = 0; kk < DH / 16; ++kk) {
+                    const uint64_t at = (kk / 4) * kRegionStep + 2 * (kk % 4);
+                    if (C::kQTmem) mma_bf16_ts_elect(tm + ps.i * 64, tmem + C::kColQ + t * (DH / 2) + kk * 8, kd + at, idesc_s, kk > 0);
+                    else mma_bf16_elect(tm + ps.i * 64, q_desc + at, kd + at, idesc_s, kk > 0);
+                }
+                mma_commit_elect(&s_own[ps.i]);
+                if ((j & 1) || j + 1 == n_steps) mma_commit_elect(&k_empty[st]);
+                ps.next();
+                return true;
+            };
+            // P V of step j, then S of the step that takes P's place
+            auto product = [&](int j) {
+                const int g = j >> 1, st = g % kStages;
+                if ((j & 1) == 0 && !wait(&v_full[st], (g / kStages) & 1)) return false;
+                if (!wait(&p_own[pp.i], pp.phase)) return false;
+                tc_fence_after();
+                const uint64_t vd = v_desc + st * kStageStep + (j & 1) * kHalfStep;
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                    mma_bf16_ts_elect(tmem + C::kColO + t * DH, tm + pp.i * 64 + kk * 8, vd + kk * kVStep, idesc_o, kk > 0 || j > 0);
+                mma_commit_elect(&done[pp.i]);
+                if ((j & 1) || j + 1 == n_steps) mma_commit_elect(&v_empty[st]);
+                if (j + C::kPlaces < n_steps && !(wait(&done[pp.i], pp.phase) && scores(j + C::kPlaces))) return false;
+                pp.next();
+                return true;
+            };
+            bool ok = wait(&q_full[t], 0);
+#pragma unroll 1
+            for (int j = 0; ok && j < min(C::kPlaces, n_steps); ++j) ok = scores(j);
+#pragma unroll 1
+            for (int j = 0; ok && j < n_steps; ++j) ok = product(j);
+        }
+        if (warp == 2) {
+            // ------------------------------------------------ the page table: a lane for 16 tokens of one of four tiles
+            const int run = lane & 7;
+            const uint32_t stride16 = (uint32_t)(a.cache.page_stride >> 4);
+            const uint32_t own16 = (uint32_t)(hk * page + (16 * run & (page - 1))) * (DH / 16);
+            int widest = kLeastScale;
+#pragma unroll 1
+            for (int g0 = 0, n = 0; g0 < n_tiles; g0 += kGroup, ++n) {
+                const int g = g0 + (lane >> 3), t0 = (g_begin + g) * 128 + 16 * run;
+                const bool mine = lane < 8 * kGroup;
+                uint32_t at = own16, bytes = 127u | 127u << 8;
+                int there = 0;
+                if (mine && g < n_tiles && t0 < s.length) {
+                    const int p = kv_page(a.batch, a.cache, b, t0 >> page_log2, a.err);
+                    if (p >= 0) {
+                        const int64_t of = (int64_t)p * a.cache.scale_stride + hk;
+                        bytes = a.cache.ks[of] | (uint32_t)a.cache.vs[of] << 8;
+                        at = (uint32_t)p * stride16 + own16;
+                        there = min(16, s.length - t0);
+                    }
+                }
+                const int slot = n % kGroups;
+                if (!wait(&i_empty[slot], ((n / kGroups) & 1) ^ 1)) break;
+                const ValueScale v = value_scale(bytes >> 8);
+                const uint32_t tile = 0xFFu << (lane & 24);
+                const uint32_t complete = __ballot_sync(0xffffffffu, there == 16), plain = __ballot_sync(0xffffffffu, v.times == kHalfOnes);
+                // (the largest of all four tiles: one that comes later does no harm)
+                widest = max(widest, __reduce_max_sync(0xffffffffu, (int)v.log2));
+                const uint32_t apart = __ballot_sync(0xffffffffu, (int)v.log2 < widest - kScaleSpan);
+                if (mine) {
+                    TileInfo<NB> &x = infos[slot * kGroup + (lane >> 3)];
+                    x.at[run] = at;
+                    x.times[run] = v.times;
+                    x.there[run] = there;
+                    if (run % (8 / NB) == 0) {
+                        StepScales<NB> &sc = x.scales[run >> 2];
+                        const int k = (run & 3) * NB / 8;
+                        sc.key[k] = key_scale(bytes & 255u);
+                        sc.value_log2[k] = apart & tile ? kInf : v.log2;
+                        sc.value_inverse[k] = v.inverse;
+                    }
+                    if (run == 0) {
+                        x.complete = (complete & tile) == tile;
+                        x.plain = (plain & tile) == tile;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&i_full[slot]);
+            }
+        }
+    } else if (warp < 8) {
+        // ------------------------------------------------ pages to operands
+        reg_dec<kConvertRegs>();
+        // 16-byte pieces of a token, and of a thread per half of a tile: piece k is of a token 128 / kPieces further
+        constexpr int kPieces = DH / 16, kTokens = 128 / kPieces;
+        const int i = threadIdx.x - 128;
+        // (dh 128: eight neighbouring lanes hold the same columns' half of two tokens, so that their stores meet no bank twice)
+        const int piece = DH == 128 ? (i & 3) | (i >> 1 & 4) : i % kPieces;
+        const int token = DH == 128 ? (i >> 4) * 2 + (i >> 2 & 1) : i / kPieces;
+        const int put0 = C::place(token, 2 * piece), put1 = C::place(token, 2 * piece + 1);
+        const uint4 *const k_own = reinterpret_cast<const uint4 *>(a.cache.k) + (token & 15) * kPieces + piece;
+        const uint4 *const v_own = reinterpret_cast<const uint4 *>(a.cache.v) + (token & 15) * kPieces + piece;
+        const int run = token >> 4;  // of piece 0
+        auto info = [&](int g) -> const TileInfo<NB> & { return infos[g / kGroup % kGroups * kGroup + g % kGroup]; };
+        // piece k of a half of a tile
+        auto fetch = [&](const uint4 *own, const TileInfo<NB> &x, int k) { return own[x.at[run + k * (kTokens / 16)]]; };
+        auto clear = [&](const TileInfo<NB> &x, uint4 (&u)[kPieces]) {
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k)
+                if ((token & 15) >= x.there[run + k * (kTokens / 16)]) u[k] = make_uint4(0u, 0u, 0u, 0u);
+        };
+        auto widen = [&](uint4 w, uint32_t (&h)[8]) {
+            e4m3x4_to_half2(w.x, h[0], h[1]);
+            e4m3x4_to_half2(w.y, h[2], h[3]);
+            e4m3x4_to_half2(w.z, h[4], h[5]);
+            e4m3x4_to_half2(w.w, h[6], h[7]);
+        };
+        auto store = [&](uint8_t *tile, int k, const uint32_t (&h)[8]) {
+            tile += k * kTokens * C::kRowBytes;  // (the swizzle repeats every eight rows)
+            *reinterpret_cast<uint4 *>(tile + put0) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4 *>(tile + put1) = make_uint4(h[4], h[5], h[6], h[7]);
+        };
+        uint4 ku[kPieces], vu[kPieces];
+        {
+            // the first tile's pages looked up here too: its pieces do not wait for its scales
+            const int t0 = g_begin * 128 + 16 * (lane & 7);
+            uint32_t at = (uint32_t)(hk * page + (16 * (lane & 7) & (page - 1))) * kPieces;
+            if (n_tiles > 0 && t0 < s.length) {
+                const int p = kv_page(a.batch, a.cache, b, t0 >> page_log2, nullptr);
+                if (p >= 0) at += (uint32_t)p * (uint32_t)(a.cache.page_stride >> 4);
+            }
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) ku[k] = k_own[__shfl_sync(0xffffffffu, at, run + k * (kTokens / 16))];
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) vu[k] = v_own[__shfl_sync(0xffffffffu, at, run + k * (kTokens / 16))];
+            if (n_tiles > 0) wait(&i_full[0], 0);
+        }
+#pragma unroll 1
+        for (int g = 0; g < n_tiles; ++g) {
+            const int st = g % kStages;
+            const uint32_t parity = (g / kStages) & 1;
+            const TileInfo<NB> &now = info(g);
+            // (behind the last tile its own pieces are loaded once more, unused)
+            const int ng = min(g + 1, n_tiles - 1);
+            if (ng % kGroup == 0 && ng > g && !wait(&i_full[ng / kGroup % kGroups], (ng / kGroup / kGroups) & 1)) break;
+            const TileInfo<NB> &next = info(ng);
+            const bool complete = now.complete != 0;
+            // keys
+            if (!wait(&k_empty[st], parity ^ 1)) break;
+            if (!complete) clear(now, ku);
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                uint32_t h[8];
+                widen(ku[k], h);
+                store(sK + st * C::kTile, k, h);
+                ku[k] = fetch(k_own, next, k);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&k_full[st]);
+            // values
+            if (!wait(&v_empty[st], parity ^ 1)) break;
+            if (!complete) clear(now, vu);
+            const bool partly = (g_begin + g + 1) * 128 > least;
+            if (!partly && now.plain) {
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    uint32_t h[8];
+                    widen(vu[k], h);
+                    store(sV + st * C::kTile, k, h);
+                    vu[k] = fetch(v_own, next, k);
+                }
+            } else {
+                uint32_t numbers = 0xffffffffu;
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    uint32_t h[8];
+                    widen(vu[k], h);
+                    const uint32_t by = now.times[run + k * (kTokens / 16)];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        h[e] = half2_times(h[e], by);
+                        if (partly) {
+                            const __half2 x = *reinterpret_cast<const __half2 *>(&h[e]);
+                            const uint32_t m = __heq2_mask(x, x);
+                            numbers &= m;
+                            h[e] &= m;
+                        }
+                    }
+                    store(sV + st * C::kTile, k, h);
+                    vu[k] = fetch(v_own, next, k);
+                }
+                if (numbers != 0xffffffffu) *nan_flag = 1;
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&v_full[st]);
+                if (g % kGroup == kGroup - 1) mbar_arrive(&i_empty[g / kGroup % kGroups]);
+            }
+        }
+        // every arrival of the MMAs' completion is in before the CTA leaves
+#pragma unroll 1
+        for (int g = max(0, n_tiles - kStages); g < n_tiles; ++g)
+            if (!wait(&k_empty[g % kStages], (g / kStages) & 1) || !wait(&v_empty[g % kStages], (g / kStages) & 1)) break;
     }
     __syncthreads();
     if (*abort_flag) {

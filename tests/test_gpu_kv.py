@@ -876,3 +876,15 @@ def test_sequences_without_pages():
         out, lse = attend(c, queries(c), False, batch=f3dc.KVBatch(c.row_start, c.length, c.table[:, :0].contiguous(), rows=c.n_rows, max_rows=rows,
                                                                    max_length=0))
         assert f3dc.gemm_status() == 0 and torch.all(out == 0) and torch.all(lse == -math.inf)
+
+
+@pytest.mark.parametrize("page", [16, 32])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("rows,held", [(60, 4500), (200, 8800)])
+def test_many_small_pages_in_one_part(rows, held, dh, page):
+    # one CTA walks through the ring of page-table entries twice and more, the last group not whole, every page with scales of
+    # its own; one tile of queries and two
+    c = R.Case([held], [rows], 2, 1, dh, page, seed=held + dh + page)
+    c.fill(v_spread=3.0)
+    run_attend(c, True, workspace=False)
+    run_attend(c, False, workspace=False)

@@ -18,7 +18,7 @@
 // eight samples of up to 955 rows 16.8, one token 2.9, 64 tokens of 32 and 8 heads of 128 3.6.  Without the ring, the next
 // head on its way in registers: 76 us, 43, 17.6, 3.3 and 4.0; with it, but two barriers a head, 67 us, 33, 17.6, 2.9 and 3.6, and
 // then two places or four instead of three 71 and 68 us.  Three CTAs to an
-// SM (80 registers): 82 us, and 14.4 for the samples.  Equal shares of all pages' heads for the CTAs that fit the SMs: 72 us, a pause
+// SM (80 registers): 82 us, and 14.4 for the samples.  (Pages of 128 with heads of 128 and neighbours rotated spill 96 bytes of a thread.)  Equal shares of all pages' heads for the CTAs that fit the SMs: 72 us, a pause
 // at each change of page.
 #include <algorithm>
 

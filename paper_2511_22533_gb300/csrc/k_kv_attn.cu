@@ -23,9 +23,11 @@
 // What bounds it: a softmax warp's own latencies.  A step of 64 tokens takes it some 1300 clocks, of which the
 // exponents are 260 (alone) to 520 (both tiles' warps at once): waits, tensor-memory loads and stores, votes and the
 // fetch of instructions are the rest, and tensor memory has no room for more tiles with dh 128 (with dh 64, four tiles of
-// one place each measured 7 % slower).  With dh 128 shared memory comes next: operands read and written take 2500 of some
-// 3000 clocks a pair of tiles.  32768 x 32768, 16 heads of 64: 4.98 ms = 881 TFLOP/s; causal 8192 x 8192, 32 heads of
-// 128 to 8: 502 us = 1096 TFLOP/s; 1229 x 1374, 16 heads of 64: 29 us, of which 8 before the first and behind the last step.
+// one place each measured 7 % slower).  That is this loop's and no floor: k_attn.cu takes 1950 clocks for the scores and exponents of two
+// steps.  With dh 128 shared memory comes next: operands read and written take 2500 of some
+// 3000 clocks a pair of tiles.  32768 x 32768, 16 heads of 64: 4.94 ms = 890 TFLOP/s; causal 8192 x 8192, 32 heads of
+// 128 to 8: 508 us = 1081 TFLOP/s; 1229 x 1374, 16 heads of 64: 29 us, of which 8 before the first and behind the last step.
+// (dh 128: two or three registers of a thread are spilled, 8 to 12 bytes.)
 // Steps that led here, prompt of 8192 / 32768 x 32768: one step of 128 tokens, its maximum always taken 872 us / 6.8 ms; no
 // maximum, pages looked up by a warp of their own, steps of 64 in two places 505 / 5.24 (steps of 128 held in registers 567); queries
 // in TMEM and two steps without a jump between them 502 / 4.98.  Three places of S made no difference and leave no room for the
@@ -46,7 +48,8 @@ static_assert(128 * (kIssueRegs + kConvertRegs) + 256 * kSoftmaxRegs <= 512 * kL
 // A row's largest weight is 2^kTop where its reference was taken.  The sum of a step's weights, which is taken
 // anyway, says whether one may have left fp16's range; only then is the reference looked at again, by all rows of the warp.  64
 // weights of 2^kTop are 2^9, far below kMostSum, so rows of even weights do not ask.  fp16 holds 2^-17 of a row's
-// largest weight at full precision and 2^-28 at all.  A higher kTop holds more and asks more often: prompt of 8192 / 32768 x
+// largest weight at full precision and 2^-28 at all, but 2^-14 and 2^-25 where the reference was raised by the sum of 64 weights and the
+// largest may be 2^0.  A higher kTop holds more and asks more often: prompt of 8192 / 32768 x
 // 32768 with keys and queries of a few large channels 502 us / 4.99 ms, with 2^6 540 / 5.10, with 2^8 576 / 5.24.
 constexpr float kTop = 3.f, kMostSum = 60000.f;
 

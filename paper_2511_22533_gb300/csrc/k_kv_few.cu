@@ -12,8 +12,8 @@
 // tokens behind the rows of S^T are chosen so that four lanes read four neighbouring tokens' values.  Each warp
 // keeps sums and references of its own, which are joined at the end.
 // One token of 32 heads of 128 to 8 key heads over 524288: 167 us (6.4 TB/s, 95 % of a plain copy's rate); 64 sequences' tokens over
-// 4096 to 8192: 136 us (6.0 TB/s), where the lengths leave some SMs idle at the end; one token over 1374 of 16 heads of 64:
-// 5.7 us, the launch and the latencies of page table, pages and the cluster.  With query rows as the MMA's rows, and parts joined by
+// 4096 to 8192: 132 us (6.2 TB/s), where the lengths leave some SMs idle at the end; one token over 1374 of 16 heads of 64:
+// 5.8 us, the launch and the latencies of page table, pages and the cluster.  With query rows as the MMA's rows, and parts joined by
 // a warp one after another: 224, 190 and 13 us.
 #include "kv.cuh"
 
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_kv_few(const KvAttnArgs a)
         sum[n][0] = sum[n][1] = 0.f;
     }
 
-    // Chunk c, whose keys and values stand at `keys`.  Plain: returns false, with nothing done, where a value scale is too far below the
+    // Chunk c, whose keys and values stand in place `slot` of the ring.  Plain: returns false, with nothing done, where a value scale is too far below the
     // largest so far; such a chunk is done in the other form.
     auto chunk = [&](int c, uint32_t scale, int slot, auto apart_tag) {
         constexpr bool kApart = decltype(apart_tag)::value;

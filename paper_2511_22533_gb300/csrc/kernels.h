@@ -495,9 +495,11 @@ cudaError_t launch_kv_few(const KvAttnArgs &a, cudaStream_t s);   // few packed 
 cudaError_t launch_kv_attn(const KvAttnArgs &a, cudaStream_t s);  // many
 cudaError_t launch_kv_join(const KvAttnArgs &a, cudaStream_t s);  // adds the parts up (called by both)
 
-// Whether tensor-memory tiles are taken: above 32 packed rows, with dh 128 above 16.  Few / many, us, over 8192 tokens: 32 rows,
-// 8 key heads of 64, 4 sequences 23.8 / 39.4, 16 sequences 81.5 / 92.3, 40 rows of 4 41.1 / 41.0, of 16 136 / 94; 32 rows of 16 key heads
-// over 1374 12.9 / 18.1.  With dh 128: 16 rows of 16 sequences 77 / 131, 20 rows 131 / 122, 32 rows of 4 38.8 / 44.4.
+// Whether tensor-memory tiles are taken: above 32 packed rows, with dh 128 above 16, where launches that fill the SMs change sides.
+// Few / many, us, 16 sequences of 8192 with 8 key heads: of 64, 32 rows 73.6 / 91.7, 40 rows 137 / 92.7; of 32, 32 rows 45.7 / 82.2, 40 rows
+// 96.4 / 82.6; of 128, 16 rows 75.1 / 116, 20 rows 140 / 118.  Smaller launches would change later: 4 sequences, heads of 64, 32 rows
+// 23.9 / 39.3, 40 rows 35.9 / 39.1; of 32, 40 rows 25.7 / 31.9; of 128, 16 rows 24.4 / 39.9, 20 rows 37.1 / 41.5; one sequence over 1374
+// with 16 key heads of 64, 32 rows 11.3 / 15.9, 64 rows 12.1 / 16.3.
 inline bool kv_many_rows(int max_rows, int heads, int kv_heads, int dh)
 {
     return (int64_t)max_rows * (heads / kv_heads) > (dh == 128 ? 16 : 32);
@@ -516,7 +518,8 @@ inline int kv_few_slots(int tile, int dh)
 // 1374 5.7 us, with 256 6.4, 512 9.9; over 8192 8.9, with 256 9.1; over 131072 47.0 us, with twice as many CTAs as fit 51.5); where
 // sequences and heads alone nearly fill the SMs, four times as many as fit, each with at least kFewLeastWaves, so that sequences of
 // different lengths even out (64 of 4096 to 8192 136 us, unshared 143; 16 of 4096, 16 heads of 64, 32.0 us, unshared 38.8, with 256
-// tokens at least 39.8).  Many rows: no more than one
+// tokens at least 39.8; where two shares of each would just fit at once they would be better: 14 sequences of 700, the same heads, 9.7 us
+// instead of 10.8, of 1374 13.9 instead of 16.5, of 4096 29.8 instead of 32.4; from 20 sequences on no difference).  Many rows: no more than one
 // for every SM, each with at least kManyLeast tokens (64 rows over 1374, 16 heads of 64, 15.9 us, with 512 18.1; 256 rows 20.8 and 22.2,
 // 700 rows behind 3000 tokens, 4 heads, 20.7 and 23.0).
 // Up to 8 CTAs (12 become 8) of few rows are a cluster and join their sums in shared memory, without a workspace and a second launch:

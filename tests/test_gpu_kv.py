@@ -888,3 +888,34 @@ def test_many_small_pages_in_one_part(rows, held, dh, page):
     c.fill(v_spread=3.0)
     run_attend(c, True, workspace=False)
     run_attend(c, False, workspace=False)
+
+
+@pytest.mark.parametrize("rows", [1, 20, 150])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_nan_beside_value_scales_far_apart(dh, rows):
+    # NaN values, keys and scales where the sums take their own exponentials: in their elements and rows alone
+    for page in (16, 64):
+        c = R.Case([700, 300], [rows, rows], 4, 2, dh, page, seed=dh + rows + page)
+        c.fill(spread=0.0)
+        for pages in c.table_list:
+            for j, p in enumerate(pages):
+                c.vs[p] = 127 + (90, -40, 0)[j % 3]
+        last = 700 + rows - 1
+        c.v[c.table_list[0][last // page], 0, last % page, 3] = R.STALE
+        c.v[c.table_list[0][2], 1, 7, dh - 1] = R.STALE
+        c.k[c.table_list[0][last // page], 1, last % page, 0] = R.STALE
+        c.ks[c.table_list[1][1], 0] = 255
+        c.vs[c.table_list[1][3], 1] = 255
+        for causal in (False, True):
+            q = queries(c)
+            if rows > 1:
+                q[1, 2] = NAN
+            out, lse = attend(c, q, causal)
+            assert f3dc.gemm_status() == 0
+            ref, ref_lse, err, lse_err = R.attend(c, q, 1.0 / math.sqrt(dh), causal)
+            got = out.double().view(ref.shape)
+            assert torch.equal(torch.isnan(got), torch.isnan(ref)) and torch.equal(torch.isnan(lse), torch.isnan(ref_lse))
+            # (bounds as in test_value_scales_far_apart)
+            err, lse_err = err * (1 + 2.0 ** -3.8), lse_err + 2.0 ** -15.8
+            fine = (got - ref).abs() <= err + R.U_BF16 * (ref.abs() + err) + 2.0 ** -133
+            assert torch.all(fine | torch.isnan(ref)) and torch.all(((lse.double() - ref_lse).abs() <= lse_err) | torch.isnan(ref_lse))

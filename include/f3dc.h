@@ -614,7 +614,8 @@ size_t f3dc_kv_attention_workspace(const f3dc_kv_cache *cache, const f3dc_kv_bat
  *   q: device bf16 [rows, heads dh], row stride ldq; out: the same, row stride ldo;
  *   lse: device fp32 [rows, heads] contiguous, nullable: ln sum exp(scale q . k_t);
  *   heads: a multiple of Hk; scale > 0;
- *   rows heads < 2^31, and max_rows heads / Hk packed rows of a key head at most 2^30.
+ *   rows heads < 2^31; p = max_rows heads / Hk, the packed rows of a key head, < 2^30, and so is
+ *   ceil(p / 8) Hk batch.
  *   The batch's bounds choose one kernel and one number of shares for all sequences: above 32
  *   packed rows (16 with dh 128) tensor-memory tiles, which take as long for one row as for 128.
  *   Single tokens over long caches belong in a call of their own, beside that of prompts or chunks.
